@@ -329,6 +329,137 @@ int32_t tr_jacobi_generate(const trj_model_desc* desc, const trj_weights* weight
                            int32_t* h_tokens, int32_t* h_n_tokens, int32_t* h_accept_hist,
                            int32_t* h_n_steps, void* stream);
 
+/* ---- Serving from a paged 8-bit cache ------------------------------------------------
+ * A cache of half the size for batches whose lengths only the device knows: pages of
+ * TRJ_KV_BLOCK slots that any sequence may own, found through a table; K and V in 8 bits
+ * (e4m3: sign, 4 bits of exponent, 3 of mantissa, largest value 448) with one scale for
+ * the K and one for the V of a page and head.  kv_block_tables hands the pages out,
+ * tree_attention_q8 reads them, kv_append_q8 writes what has been committed; the rows of
+ * the tree under verification stay in 16 bits with the caller until they are accepted, so
+ * rejected drafts never touch the cache and nothing is compacted.  tree_logits turns raw
+ * logits into those that sampling rules ask for, at every node.
+ *
+ * One layer of the cache: K and V codes [n_kv_heads][n_blocks][32 * head_dim] bytes, scales
+ * [n_kv_heads][n_blocks] fp32; value = code * scale.  A scale is a power of two (of another
+ * number the fraction is ignored), so that products with it are exact.  Inside a page, row
+ * r (slot % 32) and column c lie at byte
+ *   K: ((c/32 * 2 + c%32/16) * 32 + r) * 16 + c%16
+ *   V: ((c/32 * 2 + r/4%2) * 32 + c%32) * 16 + r/16 * 8 + r/8%2 * 4 + r%4
+ * block_table[B][max_blocks]: position p of sequence s is slot p % 32 of page
+ * block_table[s][p / 32].  Entries behind a sequence's length are not read.
+ *
+ * Rows (q_rows, k_rows, v_rows): [T][heads][head_dim] in `dtype` with *_stride elements from
+ * row to row (a part of a wider row, as a common projection of q, k and v leaves it),
+ * k already rotated; addresses are multiples of 16 bytes and strides of 8 elements, else
+ * TRJ_ERR_BAD_SHAPE.  dtype is TRJ_BF16 (the 32-bit mode keeps its 32-bit pool:
+ * TRJ_ERR_BAD_DTYPE), head_dim 64 or 128.  At most TRJ_SERVE_MAX_SEQS sequences per call.
+ *
+ * node_off need not cover all T rows, and a sequence may have no rows; rows that no sequence
+ * owns are left as they were in every output.  What the device finds wrong with a
+ * sequence sets status_dev[s] = 1 (else 0) and is stated at each call. */
+#define TRJ_SERVE_MAX_SEQS 4096
+
+/* Pages follow lengths.  Sequence s is to hold want = ceil((prefix_len[s] + N_s) / 32) pages,
+ * N_s = node_off[s+1] - node_off[s]; it holds held[s] now.
+ *  - More than it wants: its last pages go back, in order, on top of the stack free_list[0 ..
+ *    free_count) (sequences in index order).
+ *  - Fewer: then pages are taken from the top, sequence by sequence, and written to the table
+ *    behind those it holds.  Where the pages do not last for sequence s and all before it,
+ *    it gets none: status_dev[s] = 1, it keeps what it holds, and so does every sequence behind it
+ *    that wants more.
+ * held_out[B], free_count_out[1]: the new counts; row_slot[T]: the slot of every row (page
+ * number * 32 + position % 32), -1 for rows of sequences with status 1.
+ * Also status 1, and unchanged: negative or descending sizes, more than max_blocks pages wanted
+ * or held, rows outside [0, T).  A free_count outside [0, n_blocks] counts as 0.
+ * free_list has n_blocks entries, the number of pages there are; what would be stacked beyond them
+ * (pages held twice) is dropped.  Page numbers are copied, not judged.  Nothing that a call reads is
+ * overwritten, so that it may be repeated: the counts come in pairs of buffers that must not
+ * overlap (TRJ_ERR_BAD_SHAPE where they are the same), table entries below held and the stack
+ * below free_count stay.  T = 0: row_slot may be NULL. */
+int32_t kv_block_tables(int32_t* block_table, int32_t max_blocks, const int32_t* held,
+                        const int32_t* prefix_len, const int32_t* node_off, int32_t B, int32_t T,
+                        int32_t* free_list, int32_t n_blocks, const int32_t* free_count,
+                        int32_t* held_out, int32_t* free_count_out, int32_t* row_slot,
+                        int32_t* status_dev, void* stream);
+
+/* Quantises rows into the cache, all layers in one call.  path == NULL: all N_s rows of a
+ * sequence, of any number, go to positions prefix_len[s] + j.  Else the accepted path of
+ * accept_path: row path[s][j] (path has TRJ_N_MAX columns) for j = 0..accept_len[s].
+ * The scale of a page is the smallest power of two (from 2^-100 on) with which its largest
+ * value fits; a page that holds earlier rows keeps at least theirs, and where it has to grow
+ * the earlier codes are rounded to it (exact down to the type's subnormal values).  Codes
+ * round to nearest, ties to even.  A value that is not finite is stored as NaN and has no part
+ * in the scale.  Slots of a page behind the last row keep their bytes.
+ * new_len[s] = prefix_len[s] + rows stored.  Repeating a call changes nothing.
+ * Pools: n_layers of the layout above, one behind the other; rows of layer l start
+ * l * row_layer_stride elements behind layer 0's (a multiple of 8).
+ * Nothing is stored, new_len = prefix_len and status 1: accept_len[s] < 0 or >= N_s, a path
+ * entry outside [0, N_s), N_s > TRJ_N_MAX with a path, rows outside [0, T), a negative size, more than
+ * max_blocks pages, a page number outside [0, n_blocks).  Two sequences (or two entries
+ * of one) must not name the same page where rows are stored: the result is undefined. */
+int32_t kv_append_q8(void* k_pool, void* v_pool, float* k_scale, float* v_scale, const void* k_rows,
+                     const void* v_rows, int32_t row_stride, size_t row_layer_stride,
+                     const int32_t* path, const int32_t* accept_len, const int32_t* node_off,
+                     const int32_t* block_table, int32_t max_blocks, const int32_t* prefix_len,
+                     int32_t B, int32_t T, int32_t n_layers, int32_t n_kv_heads, int32_t head_dim,
+                     int32_t n_blocks, int32_t dtype, int32_t* new_len, int32_t* status_dev,
+                     void* stream);
+
+/* Bytes of device scratch for tree_attention_q8 with these sizes. */
+int32_t tree_attention_q8_workspace_bytes(int32_t B, int32_t T, int32_t n_heads, int32_t n_kv_heads,
+                                          int32_t head_dim, int32_t max_prefix, size_t* h_bytes);
+
+/* tree_attention for one layer of the paged cache: row i of sequence s sees the
+ * prefix_len[s] positions of the cache and the rows of its own ancestors and itself in k_rows,
+ * v_rows (which the cache need not hold).  A sequence of one row is plain decoding, a chain of rows a
+ * causal pass.  out: [T][n_heads][head_dim].  A key that a row does not see has no part in it
+ * whatever it holds, infinities and NaN included; a row that sees a value that is not finite
+ * gets what the sums give.  max_prefix: host upper bound of prefix_len[s].
+ * Rows of zeros and status 1: malformed tree (as trj_tree_mask), more than TRJ_N_MAX rows,
+ * prefix_len[s] outside [0, max_prefix] or beyond max_blocks pages; nothing and status 1: rows outside [0, T).
+ * NaN in all rows and status 1: a page number outside [0, n_blocks).
+ * Calls that overlap in time need workspaces of their own; nothing in one needs clearing. */
+int32_t tree_attention_q8(const void* q_rows, int32_t q_stride, const void* k_pool, const void* v_pool,
+                          const float* k_scale, const float* v_scale, const void* k_rows,
+                          const void* v_rows, int32_t row_stride, const int32_t* parent,
+                          const int32_t* node_off, const int32_t* block_table, int32_t max_blocks,
+                          const int32_t* prefix_len, int32_t B, int32_t T, int32_t n_heads,
+                          int32_t n_kv_heads, int32_t head_dim, int32_t n_blocks, int32_t max_prefix,
+                          int32_t dtype, float scale, void* workspace, size_t ws_bytes, void* out,
+                          int32_t* status_dev, void* stream);
+
+/* Bytes of device scratch for tree_logits with these sizes. */
+int32_t tree_logits_workspace_bytes(int32_t B, int32_t T, int32_t V, size_t* h_bytes);
+
+/* Logits of every tree node after penalties, biases and a mask, and the greedy prediction from
+ * them: what accept_path (with logits NULL) then takes, so that a verified tree equals
+ * token-by-token decoding under the same rules.  The text before the prediction at node i is the
+ * committed tokens ctx[ctx_off[s] .. ctx_off[s+1]) (the root's token is the last of them, as in
+ * trj_fill_tree) and the drafts tok on the path from the root, exclusive, to i.  For token v with count n
+ * among the generated ones (ctx from ctx_off[s] + gen_start[s] on, and the drafts):
+ *   x = logit;  if v occurs anywhere in the text: x = x > 0 ? x / repetition : x * repetition
+ *   x = x - frequency * n;  x = x - (n > 0 ? presence : 0);  x = x + bias(v)
+ *   x = -infinity unless the row's mask allows v
+ * each step rounded to fp32.  penalties[B][3] = repetition, frequency, presence.  Biases of
+ * sequence s: entries bias_off[s] .. bias_off[s+1] of bias_tok, bias_val; of a token named more than
+ * once the last entry counts.  allowed: bit v%32 of allowed[t][v/32], rows of ceil(V/32) words.  Token
+ * ids outside [0, V) are passed over in ctx, tok and bias_tok.
+ * Parts may be left out: ctx NULL (with ctx_off, gen_start): the drafts are the only text; penalties
+ * NULL: none, ctx and tok are not looked at; bias_off NULL; allowed NULL.  n_ctx, n_bias: how many tokens
+ * ctx, and entries bias_tok and bias_val, hold.
+ * logits_out: [T][V], may be logits itself, NULL if only predictions are wanted; argmax_out[T], may
+ * be NULL (not both): the lowest index of the largest value among the allowed tokens, NaN below all
+ * numbers (of nothing but NaN the first), -1 if the mask allows none, which no draft
+ * matches.  Malformed trees and offsets (descending, or outside their array): status 1, the sequence's
+ * rows are left as they were. */
+int32_t tree_logits(const float* logits, const int32_t* tok, const int32_t* parent,
+                    const int32_t* node_off, int32_t B, int32_t T, int32_t V, const int32_t* ctx,
+                    int32_t n_ctx, const int32_t* ctx_off, const int32_t* gen_start,
+                    const float* penalties, const int32_t* bias_tok, const float* bias_val,
+                    int32_t n_bias, const int32_t* bias_off,
+                    const uint32_t* allowed, float* logits_out, int32_t* argmax_out, void* workspace,
+                    size_t ws_bytes, int32_t* status_dev, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -101,6 +101,13 @@ _SIGS = {
     "tr_jacobi_generate": (_i32, [C.POINTER(ModelDesc), C.POINTER(Weights), _vp, _vp, _sz, _i32,
                                   _ip, _i32, C.POINTER(DecodeConfig), _vp, _sz, _ip, _ip, _ip, _ip,
                                   _vp]),
+    "kv_block_tables": (_i32, [_vp, _i32] + [_vp] * 3 + [_i32] * 2 + [_vp, _i32] + [_vp] * 6),
+    "kv_append_q8": (_i32, [_vp] * 6 + [_i32, _sz] + [_vp] * 4 + [_i32, _vp] + [_i32] * 7 + [_vp] * 3),
+    "tree_attention_q8_workspace_bytes": (_i32, [_i32] * 6 + [C.POINTER(_sz)]),
+    "tree_attention_q8": (_i32, [_vp, _i32] + [_vp] * 6 + [_i32] + [_vp] * 3 + [_i32, _vp] + [_i32] * 8 +
+                          [_f, _vp, _sz] + [_vp] * 3),
+    "tree_logits_workspace_bytes": (_i32, [_i32] * 3 + [C.POINTER(_sz)]),
+    "tree_logits": (_i32, [_vp] * 4 + [_i32] * 3 + [_vp, _i32] + [_vp] * 5 + [_i32] + [_vp] * 5 + [_sz] + [_vp] * 2),
 }
 
 
@@ -328,6 +335,98 @@ def tr_verify_step_template(desc: ModelDesc, weights: Weights, k_pool, v_pool, k
         workspace.numel() * workspace.element_size(), _ptr(logits), _ptr(argmax_out),
         _ptr(accept_len), _ptr(best_node), _ptr(path), _ptr(bonus_tok), _ptr(new_len),
         _ptr(status_dev), _stream()))
+
+
+# ------------------------------------------------------------------ paged 8-bit cache
+def _rows(t: torch.Tensor):
+    """Pointer, row stride and layer stride of rows [(layers,) T, heads, head_dim], which may be parts of
+    wider rows."""
+    if not t.is_cuda:
+        raise ValueError("device tensor expected")
+    st, sh = t.stride(), t.shape
+    if st[-1] != 1 or (sh[-2] > 1 and st[-2] != sh[-1]):
+        raise ValueError("the heads of a row must be contiguous")
+    width = sh[-2] * sh[-1]
+    row = st[-3] if sh[-3] > 1 else width
+    return t.data_ptr(), row, (st[0] if len(sh) == 4 and sh[0] > 1 else row * sh[-3])
+
+
+def kv_block_tables(block_table, held, prefix_len, node_off, T, free_list, free_count, held_out, free_count_out,
+                    row_slot, status_dev):
+    B, max_blocks = block_table.shape
+    _check("kv_block_tables", lib().kv_block_tables(
+        _ptr(block_table), max_blocks, _ptr(held), _ptr(prefix_len), _ptr(node_off), B, T, _ptr(free_list),
+        free_list.shape[0], _ptr(free_count), _ptr(held_out), _ptr(free_count_out), _ptr(row_slot),
+        _ptr(status_dev), _stream()))
+
+
+def kv_append_q8(k_pool, v_pool, k_scale, v_scale, k_rows, v_rows, path, accept_len, node_off, block_table,
+                 prefix_len, new_len, status_dev):
+    """Pools [n_layers, n_kv_heads, n_blocks, 32 * head_dim] (one layer: without the first), scales without
+    the last, rows [n_layers, T, n_kv_heads, head_dim]."""
+    B, max_blocks = block_table.shape
+    n_kv_heads, n_blocks = k_scale.shape[-2:]
+    kp, stride, layer_stride = _rows(k_rows)
+    vp, v_stride, v_layer_stride = _rows(v_rows)
+    if k_rows.shape != v_rows.shape or (stride, layer_stride) != (v_stride, v_layer_stride) or k_rows.dtype != v_rows.dtype:
+        raise ValueError("k_rows and v_rows are laid out alike")
+    n_layers = k_rows.shape[0] if k_rows.dim() == 4 else 1
+    T, heads, head_dim = k_rows.shape[-3:]
+    if heads != n_kv_heads or k_pool.numel() != n_layers * n_kv_heads * n_blocks * KV_BLOCK * head_dim or \
+            v_pool.numel() != k_pool.numel() or v_scale.shape != k_scale.shape:
+        raise ValueError("pools, scales and rows are not of the same layers, heads and pages")
+    _check("kv_append_q8", lib().kv_append_q8(
+        _ptr(k_pool), _ptr(v_pool), _ptr(k_scale), _ptr(v_scale), kp, vp, stride, layer_stride, _ptr(path),
+        _ptr(accept_len), _ptr(node_off), _ptr(block_table), max_blocks, _ptr(prefix_len), B, T, n_layers, n_kv_heads,
+        head_dim, n_blocks, dtype_code(k_rows.dtype), _ptr(new_len), _ptr(status_dev), _stream()))
+
+
+def tree_attention_q8_workspace_bytes(B, T, n_heads, n_kv_heads, head_dim, max_prefix) -> int:
+    n = _sz(0)
+    _check("tree_attention_q8_workspace_bytes", lib().tree_attention_q8_workspace_bytes(
+        B, T, n_heads, n_kv_heads, head_dim, max_prefix, C.byref(n)))
+    return int(n.value)
+
+
+def tree_attention_q8(q_rows, k_pool, v_pool, k_scale, v_scale, k_rows, v_rows, parent, node_off, block_table,
+                      prefix_len, max_prefix, scale, workspace, out, status_dev):
+    """One layer: pools [n_kv_heads, n_blocks, 32 * head_dim], scales [n_kv_heads, n_blocks], rows [T, heads,
+    head_dim], block_table [B, max_blocks]."""
+    B, max_blocks = block_table.shape
+    n_kv_heads, n_blocks = k_scale.shape
+    T, n_heads, head_dim = q_rows.shape
+    qp, q_stride, _ = _rows(q_rows)
+    kp, stride, _ = _rows(k_rows)
+    vp, v_stride, _ = _rows(v_rows)
+    if k_rows.shape != (T, n_kv_heads, head_dim) or v_rows.shape != k_rows.shape or stride != v_stride or \
+            k_rows.dtype != q_rows.dtype or v_rows.dtype != q_rows.dtype or out.dtype != q_rows.dtype:
+        raise ValueError("k_rows and v_rows are laid out alike, of q_rows' type and the pool's heads")
+    if k_pool.numel() != n_kv_heads * n_blocks * KV_BLOCK * head_dim or v_pool.numel() != k_pool.numel() or \
+            v_scale.shape != k_scale.shape or out.shape != q_rows.shape:
+        raise ValueError("pools, scales, rows and out are not of the same heads and pages")
+    _check("tree_attention_q8", lib().tree_attention_q8(
+        qp, q_stride, _ptr(k_pool), _ptr(v_pool), _ptr(k_scale), _ptr(v_scale), kp, vp, stride, _ptr(parent),
+        _ptr(node_off), _ptr(block_table), max_blocks, _ptr(prefix_len), B, T, n_heads, n_kv_heads, head_dim, n_blocks,
+        max_prefix, dtype_code(q_rows.dtype), scale, _ptr(workspace), workspace.numel() * workspace.element_size(),
+        _ptr(out), _ptr(status_dev), _stream()))
+
+
+def tree_logits_workspace_bytes(B: int, T: int, V: int) -> int:
+    n = _sz(0)
+    _check("tree_logits_workspace_bytes", lib().tree_logits_workspace_bytes(B, T, V, C.byref(n)))
+    return int(n.value)
+
+
+def tree_logits(logits, tok, parent, node_off, ctx, ctx_off, gen_start, penalties, bias_tok, bias_val, bias_off,
+                allowed, logits_out, argmax_out, workspace, status_dev):
+    T, V = logits.shape
+    B = node_off.shape[0] - 1
+    _check("tree_logits", lib().tree_logits(
+        _ptr(logits), _ptr(tok), _ptr(parent), _ptr(node_off), B, T, V, _ptr(ctx), 0 if ctx is None else ctx.numel(),
+        _ptr(ctx_off), _ptr(gen_start),
+        _ptr(penalties), _ptr(bias_tok), _ptr(bias_val),
+        0 if bias_val is None else min(bias_tok.numel(), bias_val.numel()), _ptr(bias_off), _ptr(allowed), _ptr(logits_out),
+        _ptr(argmax_out), _ptr(workspace), workspace.numel() * workspace.element_size(), _ptr(status_dev), _stream()))
 
 
 # ------------------------------------------------------------------ decoding loop

@@ -284,4 +284,27 @@ int check_model(const trj_model_desc* m);
 // beyond that blocks of 4
 inline int padded_rows(int T) { return T <= 96 ? (T <= 32 ? 32 : (T + 31) / 32 * 32) : (T + 127) / 128 * 128; }
 
+// kv_q8.hip, attn_q8.hip, logits.hip: serving from the paged 8-bit cache (arguments as in trjacobi.h)
+int launch_block_tables(int32_t* block_table, int max_blocks, const int32_t* held, const int32_t* prefix_len,
+                        const int32_t* node_off, int B, int T, int32_t* free_list, int n_blocks,
+                        const int32_t* free_count, int32_t* held_out, int32_t* free_count_out, int32_t* row_slot,
+                        int32_t* status, hipStream_t st);
+int launch_kv_append_q8(void* k_pool, void* v_pool, float* k_scale, float* v_scale, const void* k_rows,
+                        const void* v_rows, int row_stride, size_t row_layer_stride, const int32_t* path,
+                        const int32_t* accept_len, const int32_t* node_off, const int32_t* block_table, int max_blocks,
+                        const int32_t* prefix_len, int B, int T, int n_layers, int n_kv_heads, int head_dim,
+                        int n_blocks, int32_t* new_len, int32_t* status, hipStream_t st);
+size_t attn_q8_ws_floats(int B, int T, int group, int n_kv_heads, int head_dim, int max_prefix);
+int launch_tree_attn_q8(const uint16_t* q, int q_stride, const void* k_pool, const void* v_pool, const float* k_scale,
+                        const float* v_scale, const uint16_t* k_rows, const uint16_t* v_rows, int row_stride,
+                        const int32_t* parent, const int32_t* node_off, const int32_t* block_table, int max_blocks,
+                        const int32_t* prefix_len, int B, int T, int n_heads, int n_kv_heads, int head_dim,
+                        int n_blocks, int max_prefix, float scale, float* ws, uint16_t* out, int32_t* status,
+                        hipStream_t st);
+size_t tree_logits_ws_bytes(int T, int V);
+int launch_tree_logits(const float* x, const int32_t* tok, const int32_t* parent, const int32_t* node_off, int B, int T,
+                       int V, const int32_t* ctx, int n_ctx, const int32_t* ctx_off, const int32_t* gen_start, const float* pen,
+                       const int32_t* bias_tok, const float* bias_val, int n_bias, const int32_t* bias_off, const uint32_t* allowed,
+                       float* out, int32_t* argmax, uint64_t* cand, int32_t* status, hipStream_t st);
+
 }  // namespace trj

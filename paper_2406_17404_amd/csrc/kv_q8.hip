@@ -1,0 +1,318 @@
+// Pages that follow lengths, and the append that quantises rows into the paged 8-bit cache.
+#include "kernels.h"
+#include "q8.h"
+
+namespace trj {
+
+// ------------------------------------------------------------------ block tables and row slots
+// Integer work on a few KiB, bound by one launch and its chain of dependent loads.  Every
+// workgroup scans all sequences by itself (20 bytes each, from L2) rather than wait for a first
+// launch to do it, then the workgroups share out table entries, released pages and rows.
+// Nothing that one of them reads is written by another: pages taken by this call that this
+// call released are read from the table row they leave, not from the stack.
+constexpr int TABLES_THREADS = 256;
+struct SeqPages {  // of one sequence
+  int held, want, bad;
+};
+__device__ inline SeqPages seq_pages(const int32_t* held, const int32_t* prefix_len, const int32_t* node_off, int T,
+                                     int max_blocks, int s) {
+  const int h = held[s], L = prefix_len[s], r0 = node_off[s], r1 = node_off[s + 1];
+  const long want = ((long)L + (r1 - (long)r0) + TRJ_KV_BLOCK - 1) / TRJ_KV_BLOCK;
+  const bool bad = h < 0 || h > max_blocks || L < 0 || r0 < 0 || r1 < r0 || r1 > T || want > max_blocks;
+  return bad ? SeqPages{h, h, 1} : SeqPages{h, (int)want, 0};
+}
+
+__global__ __launch_bounds__(TABLES_THREADS) void block_tables_kernel(
+    int32_t* block_table, int max_blocks, const int32_t* held, const int32_t* prefix_len, const int32_t* node_off,
+    int B, int T, int32_t* free_list, int n_blocks, const int32_t* free_count, int32_t* held_out,
+    int32_t* free_count_out, int32_t* row_slot, int32_t* status) {
+  // per sequence: pages needed and released by those before it; two further words close the lists
+  extern __shared__ int smem[];
+  int* need_at = smem;
+  int* give_at = smem + B + 1;
+  __shared__ int part[2][TABLES_THREADS / 64];
+  __shared__ int mono;
+  const int tid = threadIdx.x, lane = tid & 63, wv = tid >> 6;
+  if (tid == 0) mono = 1;
+  int base_need = 0, base_give = 0;
+  for (int s0 = 0; s0 < B; s0 += TABLES_THREADS) {
+    const int s = s0 + tid;
+    SeqPages p{0, 0, 0};
+    if (s < B) p = seq_pages(held, prefix_len, node_off, T, max_blocks, s);
+    const int need = max(p.want - p.held, 0), give = max(p.held - p.want, 0);
+    const int a = wave_scan(need), b = wave_scan(give);
+    __syncthreads();
+    if (lane == 63) part[0][wv] = a, part[1][wv] = b;
+    if (s < B && node_off[s + 1] < node_off[s]) mono = 0;
+    __syncthreads();
+    int before_need = base_need, before_give = base_give;
+#pragma unroll
+    for (int w = 0; w < TABLES_THREADS / 64; ++w) {
+      if (w < wv) before_need += part[0][w], before_give += part[1][w];
+      base_need += part[0][w];
+      base_give += part[1][w];
+    }
+    if (s < B) {
+      need_at[s] = before_need + a - need;
+      give_at[s] = before_give + b - give;
+    }
+  }
+  if (tid == 0) need_at[B] = base_need, give_at[B] = base_give;
+  __syncthreads();
+
+  int have0 = free_count[0];
+  if (have0 < 0 || have0 > n_blocks) have0 = 0;
+  const int have = (int)min((long)have0 + base_give, (long)n_blocks);
+  // the sequence whose list entry is x: last s with at[s] <= x among those with entries
+  auto owner = [&](const int* at, int x) {
+    int lo = 0, hi = B;  // at[lo] <= x < at[hi]
+    while (hi - lo > 1) {
+      const int mid = (lo + hi) >> 1;
+      if (at[mid] <= x) lo = mid;
+      else hi = mid;
+    }
+    return lo;
+  };
+  auto stacked = [&](int i) {  // the page at place i of the stack once the released ones lie on it
+    if (i < have0) return free_list[i];
+    const int s = owner(give_at, i - have0);
+    const SeqPages p = seq_pages(held, prefix_len, node_off, T, max_blocks, s);
+    return block_table[(size_t)s * max_blocks + p.want + (i - have0 - give_at[s])];
+  };
+  auto served = [&](int s, const SeqPages& p) { return !p.bad && (p.want <= p.held || need_at[s + 1] <= have); };
+  const int first = blockIdx.x * TABLES_THREADS + tid, step = gridDim.x * TABLES_THREADS;
+  const int needed = base_need, given = have - have0;
+  // pages taken: entry x of the list belongs to its sequence if all of that sequence's entries are there
+  for (int x = first; x < min(needed, have); x += step) {
+    const int s = owner(need_at, x);
+    if (need_at[s + 1] > have) continue;
+    block_table[(size_t)s * max_blocks + held[s] + (x - need_at[s])] = stacked(have - 1 - x);
+  }
+  for (int x = first; x < given; x += step) free_list[have0 + x] = stacked(have0 + x);
+  for (int t = first; t < T; t += step) {
+    int s = -1;
+    if (mono) {  // last s with node_off[s] <= t
+      int lo = -1, hi = B;
+      while (hi - lo > 1) {
+        const int mid = (lo + hi) >> 1;
+        if (node_off[mid] <= t) lo = mid;
+        else hi = mid;
+      }
+      s = lo;
+    } else {  // some range is malformed: the last sequence that has the row and is not
+      for (int k = 0; k < B; ++k)
+        if (node_off[k] <= t && t < node_off[k + 1] && served(k, seq_pages(held, prefix_len, node_off, T, max_blocks, k))) s = k;
+    }
+    int slot = -1;
+    if (s >= 0 && t < node_off[s + 1]) {
+      const SeqPages p = seq_pages(held, prefix_len, node_off, T, max_blocks, s);
+      if (served(s, p)) {
+        const int pos = prefix_len[s] + t - node_off[s], j = pos / TRJ_KV_BLOCK;
+        const int page = j < p.held ? block_table[(size_t)s * max_blocks + j] : stacked(have - 1 - (need_at[s] + j - p.held));
+        slot = (int)((unsigned)page * TRJ_KV_BLOCK + pos % TRJ_KV_BLOCK);
+      }
+    }
+    row_slot[t] = slot;
+  }
+  for (int s = first; s < B; s += step) {
+    const SeqPages p = seq_pages(held, prefix_len, node_off, T, max_blocks, s);
+    held_out[s] = served(s, p) ? p.want : p.held;
+    status[s] = !served(s, p);
+  }
+  if (first == 0) {
+    int taken = needed;  // the sequences up to the first without room
+    if (needed > have) {
+      const int s = owner(need_at, have);
+      taken = need_at[s];
+    }
+    free_count_out[0] = have - taken;
+  }
+}
+
+int launch_block_tables(int32_t* block_table, int max_blocks, const int32_t* held, const int32_t* prefix_len,
+                        const int32_t* node_off, int B, int T, int32_t* free_list, int n_blocks,
+                        const int32_t* free_count, int32_t* held_out, int32_t* free_count_out, int32_t* row_slot,
+                        int32_t* status, hipStream_t st) {
+  const long most = (long)B * min(max_blocks, 8) + T;
+  const int wgs = (int)min(256l, (most + TABLES_THREADS - 1) / TABLES_THREADS);
+  block_tables_kernel<<<max(wgs, 1), TABLES_THREADS, (2 * (size_t)B + 2) * sizeof(int), st>>>(
+      block_table, max_blocks, held, prefix_len, node_off, B, T, free_list, n_blocks, free_count, held_out,
+      free_count_out, row_slot, status);
+  return check_launch();
+}
+
+// ------------------------------------------------------------------ append
+// A workgroup quantises one page of one head, K or V: 32 x DH values, 16 of a row per thread.
+//   top = max |x| over the page's new rows;  2^k with top <= 448 * 2^k;  code = e4m3(x * 2^-k)
+// With a power of two the products are exact, so a page whose scale grows is requantised by
+// multiplying its codes with the (power of two) ratio.
+// Bound by memory for prompts (2 bytes read, 1 written per value) and by latency for a few rows: count,
+// table entry, rows, maximum over the workgroup, codes.
+struct AppendArgs {
+  uint8_t* pool[2];
+  float* scale[2];
+  const uint16_t* rows[2];
+  int row_stride;
+  size_t row_layer_stride;
+  const int32_t *path, *accept_len, *node_off, *block_table, *prefix_len;
+  int max_blocks, B, T, n_kv_heads, n_blocks;
+  int32_t *new_len, *status;
+};
+// rows to store of sequence s; -1: the sequence is refused
+__device__ inline int append_rows(const AppendArgs& a, int s) {
+  const int L = a.prefix_len[s], r0 = a.node_off[s], r1 = a.node_off[s + 1];
+  if (L < 0 || r0 < 0 || r1 < r0 || r1 > a.T) return -1;
+  const int n = r1 - r0;
+  int m = n;
+  if (a.path) {
+    const int acc = a.accept_len[s];
+    if (n > TRJ_N_MAX || acc < 0 || acc >= n) return -1;
+    m = acc + 1;
+  }
+  return (long)L + m > (long)a.max_blocks * TRJ_KV_BLOCK ? -1 : m;
+}
+__device__ inline int pages_touched(int L, int m) {
+  return m <= 0 ? 0 : (L + m - 1) / TRJ_KV_BLOCK - L / TRJ_KV_BLOCK + 1;
+}
+// whether the pages that m rows go to exist and the path's entries are nodes (one wavefront, uniform)
+__device__ inline bool append_valid(const AppendArgs& a, int s, int L, int m) {
+  const int lane = threadIdx.x & 63;
+  bool bad = false;
+  const int p0 = L / TRJ_KV_BLOCK, p1 = p0 + pages_touched(L, m);
+  for (int p = p0 + lane; p < p1; p += 64) bad = bad || (unsigned)a.block_table[(size_t)s * a.max_blocks + p] >= (unsigned)a.n_blocks;
+  if (a.path) {
+    const int n = a.node_off[s + 1] - a.node_off[s];
+    for (int j = lane; j < m; j += 64) bad = bad || (unsigned)a.path[(size_t)s * TRJ_N_MAX + j] >= (unsigned)n;
+  }
+  return __ballot(bad) == 0;
+}
+
+template <int DH>
+__global__ __launch_bounds__(2 * DH) void kv_append_kernel(AppendArgs a) {
+  constexpr int THREADS = 2 * DH, WAVES = THREADS / 64, CH = DH / 16;
+  __shared__ __align__(16) uint8_t tile[32 * DH];
+  __shared__ uint32_t tops[WAVES];
+  const int tid = threadIdx.x, lane = tid & 63, wv = tid >> 6;
+  const int head = blockIdx.y, layer = blockIdx.z >> 1, which = blockIdx.z & 1;
+
+  if (blockIdx.y == 0 && blockIdx.z == 0) {  // the verdicts
+    for (int s = blockIdx.x * WAVES + wv; s < a.B; s += gridDim.x * WAVES) {
+      const int m = append_rows(a, s);
+      const bool ok = m >= 0 && append_valid(a, s, a.prefix_len[s], m);
+      if (lane == 0) {
+        a.new_len[s] = a.prefix_len[s] + (ok ? m : 0);
+        a.status[s] = !ok;
+      }
+    }
+  }
+  for (int x = blockIdx.x;; x += gridDim.x) {
+    int s, nth;
+    if (!find_seq(x, a.B, [&](int q) { return pages_touched(a.prefix_len[q], append_rows(a, q)); }, s, nth)) return;
+    const int L = a.prefix_len[s], m = append_rows(a, s), r0 = a.node_off[s];
+    if (!append_valid(a, s, L, m)) continue;  // uniform over the workgroup
+    const int pg = L / TRJ_KV_BLOCK + nth, page = a.block_table[(size_t)s * a.max_blocks + pg];
+    const int old_rows = max(0, min(32, L - pg * 32)), end = min(32, L + m - pg * 32);  // new: [old_rows, end)
+
+    // 16 values of row r
+    const int r = tid / CH, c0 = (tid % CH) * 16;
+    const bool mine = r >= old_rows && r < end;
+    u32x4 raw[2] = {{0, 0, 0, 0}, {0, 0, 0, 0}};
+    if (mine) {
+      const int j = pg * 32 + r - L;
+      const int row = r0 + (a.path ? a.path[(size_t)s * TRJ_N_MAX + j] : j);
+      const u32x4* src = reinterpret_cast<const u32x4*>(a.rows[which] + layer * a.row_layer_stride + (size_t)row * a.row_stride +
+                                                        (size_t)head * DH + c0);
+      raw[0] = src[0];
+      raw[1] = src[1];
+    }
+    uint32_t top = 0;  // bits of the largest finite magnitude
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const uint32_t w = raw[i >> 2][i & 3], lo = (w << 16) & 0x7fffffffu, hi = w & 0x7fff0000u;
+      top = max(top, max(lo < 0x7f800000u ? lo : 0u, hi < 0x7f800000u ? hi : 0u));
+    }
+    for (int o = 32; o > 0; o >>= 1) top = max(top, (uint32_t)__shfl_xor((int)top, o));
+    if (lane == 0) tops[wv] = top;
+    __syncthreads();
+#pragma unroll
+    for (int w = 0; w < WAVES; ++w) top = max(top, tops[w]);
+    const size_t plane = ((size_t)layer * a.n_kv_heads + head) * a.n_blocks + page;
+    float* const scale = a.scale[which] + plane;
+    int e = q8_exp(top), e_old = 0;
+    if (old_rows > 0) {
+      e_old = q8_exp_of(*scale);
+      e = max(e, e_old);
+    }
+    const float inv = q8_pow2(-e);
+    u32x4 codes;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      uint32_t c[2];
+#pragma unroll
+      for (int k = 0; k < 2; ++k) {
+        const uint32_t w = raw[i >> 1][(i & 1) * 2 + k];
+        c[k] = q8_codes(__uint_as_float(w << 16) * inv, __uint_as_float(w & 0xffff0000u) * inv);
+      }
+      codes[i] = c[0] | c[1] << 16;
+    }
+    // through LDS into the page's order
+    if (which == 0) {
+      *reinterpret_cast<u32x4*>(tile + q8_k_off(r, c0)) = codes;
+    } else {
+#pragma unroll
+      for (int i = 0; i < 16; ++i) tile[q8_v_off(r, c0 + i)] = (uint8_t)(codes[i >> 2] >> (8 * (i & 3)));
+    }
+    __syncthreads();  // every thread has read the old scale as well
+    if (tid == 0) *scale = q8_pow2(e);
+    u32x4* const dst = reinterpret_cast<u32x4*>(a.pool[which] + plane * 32 * DH) + tid;
+    const bool grew = old_rows > 0 && e > e_old;
+    const float ratio = grew ? q8_pow2(max(e_old - e, -126)) : 1.f;
+    const u32x4 fresh = reinterpret_cast<const u32x4*>(tile)[tid];
+    // byte i of dword d of this thread's 16: row
+    const bool whole = old_rows == 0 && end == 32;
+    u32x4 old = {0, 0, 0, 0};
+    const int kr = tid & 31;  // K: all 16 bytes belong to one row
+    const bool k_new = kr >= old_rows && kr < end;
+    if (which == 0 ? (grew && kr < old_rows) : !whole) old = *dst;
+    u32x4 put;
+#pragma unroll
+    for (int d = 0; d < 4; ++d) {
+      uint32_t kept = old[d];
+      if (grew) {
+        const f32x2 p = __builtin_amdgcn_cvt_pk_f32_fp8((int)kept, false), q = __builtin_amdgcn_cvt_pk_f32_fp8((int)kept, true);
+        kept = q8_codes(p[0] * ratio, p[1] * ratio) | q8_codes(q[0] * ratio, q[1] * ratio) << 16;
+      }
+      if (which == 0) {
+        put[d] = k_new ? fresh[d] : kept;
+      } else {
+        uint32_t is_new = 0, is_old = 0;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const int row = 8 * d + 4 * ((tid >> 5) & 1) + i;
+          if (row < old_rows) is_old |= 0xffu << (8 * i);
+          else if (row < end) is_new |= 0xffu << (8 * i);
+        }
+        put[d] = (fresh[d] & is_new) | (kept & is_old) | (old[d] & ~(is_new | is_old));
+      }
+    }
+    if (which == 0 ? (k_new || (grew && kr < old_rows)) : true) *dst = put;
+    __syncthreads();  // the tile is free again
+  }
+}
+
+int launch_kv_append_q8(void* k_pool, void* v_pool, float* k_scale, float* v_scale, const void* k_rows, const void* v_rows,
+                        int row_stride, size_t row_layer_stride, const int32_t* path, const int32_t* accept_len,
+                        const int32_t* node_off, const int32_t* block_table, int max_blocks, const int32_t* prefix_len,
+                        int B, int T, int n_layers, int n_kv_heads, int head_dim, int n_blocks, int32_t* new_len,
+                        int32_t* status, hipStream_t st) {
+  const AppendArgs a{{(uint8_t*)k_pool, (uint8_t*)v_pool}, {k_scale, v_scale}, {(const uint16_t*)k_rows, (const uint16_t*)v_rows},
+                     row_stride, row_layer_stride, path, accept_len, node_off, block_table, prefix_len, max_blocks, B, T,
+                     n_kv_heads, n_blocks, new_len, status};
+  // all rows: a sequence touches at most two pages more than its rows fill; a path mostly one or two
+  const dim3 grid(path ? 2 * B : T / TRJ_KV_BLOCK + 2 * B, n_kv_heads, 2 * n_layers);
+  if (head_dim == 128) kv_append_kernel<128><<<grid, 256, 0, st>>>(a);
+  else kv_append_kernel<64><<<grid, 128, 0, st>>>(a);
+  return check_launch();
+}
+
+}  // namespace trj

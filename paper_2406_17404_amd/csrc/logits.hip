@@ -1,0 +1,259 @@
+// Logits of tree nodes after penalties, biases and masks, with the greedy prediction.
+//
+// One pass over [T][V] fp32.  A workgroup owns SLICE tokens of the vocabulary, four per thread, for some
+// rows of one sequence.  What all rows of the sequence share (how often a token occurs in the committed text,
+// its bias) it works out once: it scans the text, counts the tokens of its slice in LDS (integers, so the
+// order of the atomics does not matter), and every thread keeps the counts of its four tokens in
+// registers.  Per row remain the drafts above the node, of which few fall into a slice.
+// Every step is rounded by itself (no fused multiply-add), so that a prediction does not depend on
+// how the compiler joins them.
+#include <algorithm>
+
+#include "kernels.h"
+#include "q8.h"
+#include "tree_anc.h"
+
+namespace trj {
+
+constexpr int LG_THREADS = 256, LG_SLICE = 4 * LG_THREADS;
+typedef float f32x4_any __attribute__((ext_vector_type(4), aligned(4)));  // rows of odd length start anywhere
+
+struct LogitsArgs {
+  const float* x;
+  const int32_t *tok, *parent, *node_off;
+  int B, T, V;
+  const int32_t *ctx, *ctx_off, *gen_start;
+  int n_ctx, n_bias;
+  const float* pen;
+  const int32_t* bias_tok;
+  const float* bias_val;
+  const int32_t* bias_off;
+  const uint32_t* allowed;
+  float* out;
+  int32_t* argmax;
+  uint64_t* cand;  // [T][slices] if there are several
+  int32_t* status;
+  int rows;  // per workgroup
+};
+
+// larger value first, then lower index; 0: no token.  NaN is below all numbers, the zeros are equal
+__device__ inline uint64_t pick_key(float x, int i) {
+  const uint32_t u = __float_as_uint(x + 0.f);
+  const uint32_t ord = x != x ? 0u : (u >> 31 ? ~u : u | 0x80000000u);
+  return (uint64_t)ord << 32 | (uint32_t)~i;
+}
+__device__ inline uint64_t wave_max(uint64_t k) {
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) {
+    const uint64_t u = (uint64_t)(uint32_t)__shfl_xor((int)(k >> 32), o) << 32 | (uint32_t)__shfl_xor((int)k, o);
+    k = u > k ? u : k;
+  }
+  return k;
+}
+__device__ inline int picked(uint64_t key) { return key == 0 ? -1 : (int)~(uint32_t)key; }
+
+// rows of sequence s, -1: malformed offsets
+__device__ inline int logits_rows(const LogitsArgs& a, int s) {
+  const int r0 = a.node_off[s], r1 = a.node_off[s + 1];
+  bool bad = r0 < 0 || r1 < r0 || r1 > a.T || r1 - r0 > TRJ_N_MAX;
+  if (a.ctx && a.pen) bad = bad || a.ctx_off[s] < 0 || a.ctx_off[s + 1] < a.ctx_off[s] || a.ctx_off[s + 1] > a.n_ctx;
+  if (a.bias_off) bad = bad || a.bias_off[s] < 0 || a.bias_off[s + 1] < a.bias_off[s] || a.bias_off[s + 1] > a.n_bias;
+  return bad ? -1 : r1 - r0;
+}
+
+__global__ __launch_bounds__(LG_THREADS) void tree_logits_kernel(LogitsArgs a) {
+  __shared__ int seen_n[LG_SLICE], made_n[LG_SLICE], bias_at[LG_SLICE];
+  __shared__ uint32_t above[TRJ_N_MAX][4];  // drafts of this slice on the path to a node
+  __shared__ int draft[TRJ_N_MAX];          // a draft's place in the slice
+  __shared__ uint64_t best[TRJ_N_MAX][LG_THREADS / 64];
+  const int tid = threadIdx.x, lane = tid & 63, wv = tid >> 6;
+  const int v0 = blockIdx.x * LG_SLICE, mine = v0 + 4 * tid;
+  const int words = (a.V + 31) >> 5;
+
+  if (blockIdx.x == 0 && blockIdx.y == 0) {  // sequences without rows
+    for (int s = tid; s < a.B; s += LG_THREADS) {
+      const int n = logits_rows(a, s);
+      if (n <= 0) a.status[s] = n < 0;
+    }
+  }
+  for (int y = blockIdx.y;; y += gridDim.y) {
+    int s, nth;
+    if (!find_seq(y, a.B, [&](int q) { return max(0, (logits_rows(a, q) + a.rows - 1) / a.rows); }, s, nth)) return;
+    const int r0 = a.node_off[s], n = a.node_off[s + 1] - r0;
+    const TreeParents par = load_parents(a.parent, r0, n);
+    const bool ok = tree_valid(par, n);
+    if (blockIdx.x == 0 && nth == 0 && tid == 0) a.status[s] = !ok;
+    if (!ok) continue;  // uniform over the workgroup
+    const int i0 = nth * a.rows, i1 = min(n, i0 + a.rows);
+
+    int seen[4] = {0, 0, 0, 0}, made[4] = {0, 0, 0, 0};
+    float bias[4] = {0.f, 0.f, 0.f, 0.f}, rep = 1.f, freq = 0.f, pres = 0.f;
+    if (a.pen || a.bias_off) {
+      for (int k = tid; k < LG_SLICE; k += LG_THREADS) seen_n[k] = made_n[k] = bias_at[k] = 0;
+      __syncthreads();
+      if (a.pen) {
+        rep = a.pen[3 * s], freq = a.pen[3 * s + 1], pres = a.pen[3 * s + 2];
+        if (a.ctx) {
+          const int c0 = a.ctx_off[s], c1 = a.ctx_off[s + 1], g0 = a.gen_start[s];
+          for (int k = c0 + tid; k < c1; k += LG_THREADS) {
+            const int v = a.ctx[k] - v0;
+            if (a.ctx[k] >= 0 && (unsigned)v < (unsigned)LG_SLICE) {
+              atomicAdd(&seen_n[v], 1);
+              if (k - c0 >= g0) atomicAdd(&made_n[v], 1);
+            }
+          }
+        }
+        if (wv == 0) {  // the drafts of this slice, and where they lie above a node
+          uint32_t in[4];
+#pragma unroll
+          for (int h = 0; h < 2; ++h) {
+            const int i = lane + 64 * h;
+            const int t = i > 0 && i < n ? a.tok[r0 + i] : -1, v = t - v0;
+            const bool here = t >= 0 && t < a.V && (unsigned)v < (unsigned)LG_SLICE;
+            draft[i] = v;
+            const uint64_t b = __ballot(here);
+            in[2 * h] = (uint32_t)b;
+            in[2 * h + 1] = (uint32_t)(b >> 32);
+          }
+          const TreeBits bits = tree_bits(par, n);
+#pragma unroll
+          for (int h = 0; h < 2; ++h)
+#pragma unroll
+            for (int k = 0; k < 4; ++k) above[lane + 64 * h][k] = (uint32_t)bits.w[k][h] & in[k];
+        }
+      }
+      if (a.bias_off) {
+        const int c0 = a.bias_off[s], c1 = a.bias_off[s + 1];
+        for (int k = c0 + tid; k < c1; k += LG_THREADS) {
+          const int v = a.bias_tok[k] - v0;
+          if (a.bias_tok[k] >= 0 && (unsigned)v < (unsigned)LG_SLICE) atomicMax(&bias_at[v], k - c0 + 1);
+        }
+      }
+      __syncthreads();
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        seen[e] = seen_n[4 * tid + e];
+        made[e] = made_n[4 * tid + e];
+        const int at = bias_at[4 * tid + e];
+        if (at > 0) bias[e] = a.bias_val[a.bias_off[s] + at - 1];
+      }
+    }
+
+    for (int i = i0; i < i1; ++i) {
+      const size_t t = r0 + i;
+      const float* src = a.x + t * a.V + mine;
+      float x[4];
+      if (mine + 4 <= a.V) {
+        const f32x4_any v = *reinterpret_cast<const f32x4_any*>(src);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) x[e] = v[e];
+      } else {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) x[e] = mine + e < a.V ? src[e] : 0.f;
+      }
+      uint32_t may = mine < a.V ? 15u : 0u;
+      if (a.allowed && mine < a.V) may = a.allowed[t * words + (mine >> 5)] >> (mine & 31);
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        if (mine + e >= a.V) may &= ~(1u << e);
+      if (a.pen) {
+#pragma clang fp contract(off)
+        int n_seen[4], n_made[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) n_seen[e] = seen[e], n_made[e] = made[e];
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+          for (uint32_t b = above[i][k]; b; b &= b - 1) {
+            const int v = draft[32 * k + __builtin_ctz(b)];
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+              if (v == 4 * tid + e) ++n_seen[e], ++n_made[e];
+          }
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          if (n_seen[e]) x[e] = x[e] > 0.f ? x[e] / rep : x[e] * rep;
+          const float f = freq * (float)n_made[e];
+          x[e] = x[e] - f;
+          x[e] = x[e] - (n_made[e] ? pres : 0.f);
+        }
+      }
+      uint64_t top = 0;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        if (a.bias_off) x[e] = x[e] + bias[e];
+        const bool yes = (may >> e) & 1;
+        if (!yes) x[e] = -INFINITY;
+        const uint64_t k = yes ? pick_key(x[e], mine + e) : 0;
+        top = k > top ? k : top;
+      }
+      if (a.out) {
+        float* dst = a.out + t * a.V + mine;
+        if (mine + 4 <= a.V) {
+          *reinterpret_cast<f32x4_any*>(dst) = f32x4_any{x[0], x[1], x[2], x[3]};
+        } else {
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+            if (mine + e < a.V) dst[e] = x[e];
+        }
+      }
+      if (a.argmax) {
+        top = wave_max(top);
+        if (lane == 0) best[i - i0][wv] = top;
+      }
+    }
+    __syncthreads();
+    if (a.argmax)
+      for (int i = tid; i < i1 - i0; i += LG_THREADS) {
+        uint64_t k = best[i][0];
+#pragma unroll
+        for (int w = 1; w < LG_THREADS / 64; ++w) k = best[i][w] > k ? best[i][w] : k;
+        const size_t t = r0 + i0 + i;
+        if (gridDim.x == 1) a.argmax[t] = picked(k);
+        else a.cand[t * gridDim.x + blockIdx.x] = k;
+      }
+    __syncthreads();
+  }
+}
+
+// The best of a row's candidates, a wavefront per row.
+__global__ __launch_bounds__(256) void logits_pick_kernel(LogitsArgs a, int slices) {
+  const int lane = threadIdx.x & 63, w = blockIdx.x * 4 + (threadIdx.x >> 6);
+  int s, i;
+  if (!find_seq(w, a.B, [&](int q) { return max(0, logits_rows(a, q)); }, s, i)) return;
+  const int r0 = a.node_off[s], n = a.node_off[s + 1] - r0;
+  if (!tree_valid(load_parents(a.parent, r0, n), n)) return;
+  uint64_t k = 0;
+  for (int c = lane; c < slices; c += 64) {
+    const uint64_t u = a.cand[(size_t)(r0 + i) * slices + c];
+    k = u > k ? u : k;
+  }
+  k = wave_max(k);
+  if (lane == 0) a.argmax[r0 + i] = picked(k);
+}
+
+static int logits_slices(int V) { return (V + LG_SLICE - 1) / LG_SLICE; }
+size_t tree_logits_ws_bytes(int T, int V) {
+  const int n = logits_slices(V);
+  return n > 1 ? (size_t)T * n * sizeof(uint64_t) : 0;
+}
+
+int launch_tree_logits(const float* x, const int32_t* tok, const int32_t* parent, const int32_t* node_off, int B, int T, int V,
+                       const int32_t* ctx, int n_ctx, const int32_t* ctx_off, const int32_t* gen_start, const float* pen,
+                       const int32_t* bias_tok, const float* bias_val, int n_bias, const int32_t* bias_off, const uint32_t* allowed,
+                       float* out, int32_t* argmax, uint64_t* cand, int32_t* status, hipStream_t st) {
+  const int slices = logits_slices(V);
+  // rows per workgroup: enough workgroups to fill the chip, few scans of the text
+  int rows = 8;
+  while (rows < 64 && (long)slices * T / rows > 4096) rows *= 2;
+  while (rows > 1 && (long)slices * T / rows < 512) rows /= 2;
+  const LogitsArgs a{x, tok, parent, node_off, B, T, V, ctx, ctx_off, gen_start, n_ctx, n_bias, pen, bias_tok, bias_val, bias_off, allowed,
+                     out, argmax, cand, status, rows};
+  const dim3 grid(slices, std::min((long)T / rows + B, 65535l));
+  tree_logits_kernel<<<grid, LG_THREADS, 0, st>>>(a);
+  int rc = check_launch();
+  if (rc != TRJ_OK || !argmax || slices == 1) return rc;
+  logits_pick_kernel<<<(T + 3) / 4, 256, 0, st>>>(a, slices);
+  return check_launch();
+}
+
+}  // namespace trj
