@@ -350,7 +350,7 @@ int32_t tr_jacobi_generate(const trj_model_desc* desc, const trj_weights* weight
  *
  * Rows (q_rows, k_rows, v_rows): [T][heads][head_dim] in `dtype` with *_stride elements from
  * row to row (a part of a wider row, as a common projection of q, k and v leaves it),
- * k already rotated; addresses are multiples of 16 bytes and strides of 8 elements, else
+ * k already rotated; addresses are multiples of 16 bytes, strides of 8 elements up to 2^24, else
  * TRJ_ERR_BAD_SHAPE.  dtype is TRJ_BF16 (the 32-bit mode keeps its 32-bit pool:
  * TRJ_ERR_BAD_DTYPE), head_dim 64 or 128.  At most TRJ_SERVE_MAX_SEQS sequences per call.
  *

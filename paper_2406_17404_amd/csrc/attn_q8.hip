@@ -19,6 +19,7 @@
 // How the keys are split is decided on the device, where the lengths are: every workgroup scans the
 // sequences (64 per round), works out the same plan and finds its own part of it.
 #include <algorithm>
+#include <type_traits>
 
 #include "kernels.h"
 #include "q8.h"
@@ -41,51 +42,96 @@ struct Q8Args {
   int32_t* status;
 };
 
-// what a sequence has to do; nodes < 0: nothing but the verdict
+// What a sequence has to do, one per lane (MANY: of the 64 from s0 on).
 struct Q8Seq {
-  int r0, nodes, L, cached, blocks;
+  int r0, nodes, L, blocks;  // L < 0: refused, its rows read as zeros (one block of work); blocks 0: nothing to do
+  __device__ inline int cached() const { return (L + 31) >> 5; }
 };
 __device__ inline Q8Seq q8_seq(const Q8Args& a, int s) {
+  Q8Seq q{0, 0, 0, 0};
+  if (s >= a.B) return q;
   const int r0 = a.node_off[s], r1 = a.node_off[s + 1], L = a.prefix_len[s];
-  Q8Seq q{r0, r1 - r0, L, 0, 0};
-  if (r0 < 0 || r1 < r0 || r1 > a.T) q.nodes = -1;
+  q.r0 = r0;
+  q.L = L;
+  q.nodes = r0 < 0 || r1 < r0 || r1 > a.T ? -1 : r1 - r0;
+  if (q.nodes <= 0) return q;
   const bool fits = L >= 0 && L <= a.max_prefix && (L + 31) / 32 <= a.max_blocks && q.nodes <= TRJ_N_MAX;
-  if (q.nodes > 0 && fits) {
-    q.cached = (L + 31) / 32;
-    q.blocks = q.cached + (q.nodes + 31) / 32;
-  } else if (q.nodes > 0) {
-    q.L = -1;  // rows of zeros: one block of work
-    q.blocks = 1;
-  }
+  if (!fits) q.L = -1;
+  q.blocks = fits ? q.cached() + (q.nodes + 31) / 32 : 1;
   return q;
 }
-// The plan: a split has `chunk` blocks at most, of one sequence evenly many.
-struct Q8Plan {
-  int chunk;
+__device__ inline int q8_groups(const Q8Args& a, const Q8Seq& q, int tile_queries) {  // query groups
+  return q.blocks == 0 ? 0 : q.L < 0 ? 1 : (q.nodes * a.group + tile_queries - 1) / tile_queries;
+}
+template <class T>
+__device__ inline T lane_value(T v, int lane) { return (T)__builtin_amdgcn_readlane((int)v, lane); }
+
+// The plan, the same on every wavefront of every workgroup: a split has `chunk` blocks at most, of one
+// sequence evenly many.  Sequences come longest first (up to 64 of them; index order beyond), so that what
+// starts last is short.
+struct Q8Work {  // of an item
+  Q8Seq seq;
+  int s, nth, splits, part0;  // nth item of sequence s; its first partial
 };
-template <int NTW>
-__device__ inline int q8_groups(const Q8Args& a, const Q8Seq& q) {  // query groups
-  const int n = min(q.nodes, q.L < 0 ? 1 : TRJ_N_MAX);
-  return n <= 0 ? 0 : (n * a.group + 32 * NTW - 1) / (32 * NTW);
-}
-template <int NTW>
-__device__ inline Q8Plan q8_plan(const Q8Args& a) {
-  long work = 0;
-  for (int s0 = 0; s0 < a.B; s0 += 64) {
-    const int s = s0 + (int)(threadIdx.x & 63);
-    long w = 0;
-    if (s < a.B) {
-      const Q8Seq q = q8_seq(a, s);
-      w = (long)q8_groups<NTW>(a, q) * a.n_kv_heads * q.blocks;
-    }
+template <bool MANY, int QUERIES>
+struct Q8Plan {
+  const Q8Args& a;
+  Q8Seq mine;   // sequence `id` (sorted)
+  int id, chunk;
+
+  __device__ inline explicit Q8Plan(const Q8Args& args) : a(args) {
+    const int lane = threadIdx.x & 63;
+    long work = 0;
+    for (int s0 = 0; s0 < (MANY ? a.B : 1); s0 += 64) {
+      mine = q8_seq(a, s0 + lane);
+      long w = (long)q8_groups(a, mine, QUERIES) * mine.blocks;
 #pragma unroll
-    for (int o = 32; o > 0; o >>= 1) w += __shfl_xor(w, o);
-    work += w;
+      for (int o = 32; o > 0; o >>= 1) w += __shfl_xor(w, o);
+      work += w;
+    }
+    work *= a.n_kv_heads;
+    chunk = __builtin_amdgcn_readfirstlane((int)max((work + a.target - 1) / a.target, (long)a.min_blocks));
+    id = lane;
+    if (!MANY && a.B > 1) {  // longest first
+      int rank = 0;
+      for (int t = 0; t < a.B; ++t) {
+        const int b = lane_value(mine.blocks, t);
+        rank += b > mine.blocks || (b == mine.blocks && t < lane);
+      }
+      rank = lane < a.B ? rank : lane;
+      auto to = [&](int v) { return __builtin_amdgcn_ds_permute(rank << 2, v); };
+      mine = Q8Seq{to(mine.r0), to(mine.nodes), to(mine.L), to(mine.blocks)};
+      id = to(lane);
+    }
   }
-  const long c = (work + a.target - 1) / a.target;
-  return Q8Plan{(int)max(c, (long)a.min_blocks)};
-}
-__device__ inline int q8_splits(const Q8Plan& p, const Q8Seq& q) { return (q.blocks + p.chunk - 1) / p.chunk; }
+  __device__ inline int splits(const Q8Seq& q) const { return (q.blocks + chunk - 1) / chunk; }
+  // item x of all, of which every (sequence, query group, K/V head) counts its splits, or, TILES > 0, once per
+  // tile where there are several splits
+  template <int TILES>
+  __device__ inline bool find(int x, Q8Work& w) {
+    const int lane = threadIdx.x & 63;
+    int base = 0, parts = 0;
+    for (int s0 = 0; s0 < (MANY ? a.B : 1); s0 += 64) {
+      if (MANY) mine = q8_seq(a, s0 + lane), id = s0 + lane;
+      const int k = splits(mine), g = q8_groups(a, mine, QUERIES) * a.n_kv_heads;
+      const int n = TILES == 0 ? g * k : k > 1 ? g * TILES : 0;
+      const int upto = base + wave_scan(n), pupto = parts + wave_scan(k > 1 ? g * k : 0);
+      const uint64_t here = __ballot(x < upto);
+      if (here) {
+        const int l = __builtin_ctzll(here);
+        w.seq = Q8Seq{lane_value(mine.r0, l), lane_value(mine.nodes, l), lane_value(mine.L, l), lane_value(mine.blocks, l)};
+        w.s = lane_value(id, l);
+        w.nth = x - (lane_value(upto, l) - lane_value(n, l));
+        w.splits = lane_value(k, l);
+        w.part0 = lane_value(pupto, l) - (w.splits > 1 ? lane_value(g, l) * w.splits : 0);
+        return true;
+      }
+      base = lane_value(upto, 63);
+      parts = lane_value(pupto, 63);
+    }
+    return false;
+  }
+};
 
 __device__ inline uint32_t bf16_pair(uint32_t codes, float scale, bool hi) {
   return hi ? __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(codes, scale, true))
@@ -96,22 +142,32 @@ __device__ inline bf16x8 operand(uint32_t a, uint32_t b, float scale) {  // 8 co
   return __builtin_bit_cast(bf16x8, v);
 }
 
-// Running softmax of one tile of 32 queries, a query per lane and its partner lane + 32: scores of 32
-// keys in, -infinity where not visible; bf16 weights out (the B operand of the second product).
+// Running softmax of one tile of 32 queries, a query per lane and its partner lane + 32: products of
+// 32 keys in (times f: log2 scores), -infinity where not visible; bf16 weights out (the B operand of the
+// second product).  Weights are relative to a reference, the largest score when it was last
+// set; it is set again once a score exceeds it by more than SLACK, so weights are at most 2^SLACK, which
+// costs nothing (they are floating-point numbers) and spares most of the rescaling of the sums:
+// with the running maximum itself some query of a tile moves it in nearly every block.
+constexpr float SLACK = 8.f;
 struct Softmax {
   float m = -INFINITY, l = 0.f;
-  __device__ inline float take(const float (&s)[16], u32x4 (&pk)[2]) {  // the factor of the sums so far
+  __device__ __forceinline__ float take(const f32x16& s, float f, u32x4 (&pk)[2]) {  // the factor of the sums so far
+#pragma clang fp contract(off)
     float mx = s[0];
 #pragma unroll
     for (int v = 1; v < 16; ++v) mx = fmaxf(mx, s[v]);
-    mx = fmaxf(mx, __shfl_xor(mx, 32));
-    const float top = fmaxf(m, mx);
+    const auto both = __builtin_amdgcn_permlane32_swap(__float_as_uint(mx), __float_as_uint(mx), false, false);
+    mx = fmaxf(__uint_as_float(both[0]), __uint_as_float(both[1])) * f;
+    const float top = mx > m + SLACK || m == -INFINITY ? fmaxf(m, mx) : m;
     const float ref = top == -INFINITY ? 0.f : top;  // nothing visible yet: weights 2^-inf = 0
     const float alpha = __builtin_amdgcn_exp2f(m - ref);
     float p[16], sum = 0.f;
+    // product and difference rounded one by one: fused, the rounding of the reference's own product would
+    // stay in the exponent, 1 and more for scores beyond 2^24
 #pragma unroll
     for (int v = 0; v < 16; ++v) {
-      p[v] = __builtin_amdgcn_exp2f(s[v] - ref);
+      const float x = s[v] * f;
+      p[v] = __builtin_amdgcn_exp2f(x - ref);
       sum += p[v];
     }
     l = l * alpha + sum;
@@ -133,361 +189,514 @@ __device__ inline void q8_rescale(f32x16 (&o)[MTV], float alpha) {
     for (int v = 0; v < 16; ++v) o[mt][v] *= alpha;
 }
 
+// Scheduling of what stands in front of it: after every matrix product N vector instructions.
+template <int PRODUCTS, int N>
+__device__ __forceinline__ void interleave() {
+#pragma unroll
+  for (int i = 0; i < PRODUCTS; ++i) {
+    __builtin_amdgcn_sched_group_barrier(0x8, 1, 0);
+    __builtin_amdgcn_sched_group_barrier(0x2, N, 0);
+  }
+}
+
 // An infinity or NaN among the tree's V rows: times the weight 0 of a row that does not see it it
-// would be NaN.  Such values are taken out of the operand and added to the rows that do see
-// them.  key: of the block's 32; value: V(key, c) as bits.
-template <int MTV, class F, class G>
-__device__ __forceinline__ void q8_add_odd_values(f32x16 (&o)[MTV], const u32x4 (&pk)[2], int keys, F visible, G value) {
+// would be NaN.  Such values are left out of the operand and added here to the rows that do see
+// them.  rows: V row of the block's first key, this K/V head.
+template <int NT, int MTV>
+__device__ __forceinline__ void q8_add_odd_values(f32x16 (&o)[NT][MTV], const u32x4 (&pk)[NT][2], const uint32_t (&sees)[NT],
+                                                  const uint16_t* rows, int stride, int keys) {
   const int lane = threadIdx.x & 63, hh = lane >> 5;
 #pragma unroll 1
   for (int key = 0; key < keys; ++key) {
-    const int v = (key >> 3) * 4 + (key & 3);  // the register that holds its weight, on half (key >> 2) & 1
-    uint32_t word = 0;
+    const int v = (key >> 3) * 4 + (key & 3);  // the register with its weight, on half (key >> 2) & 1
+    const uint16_t* p = rows + (size_t)key * stride + 4 * hh;
+    float w[NT];
 #pragma unroll
-    for (int i = 0; i < 8; ++i)
-      if (i == v >> 1) word = pk[i >> 2][i & 3];
-    word = (uint32_t)__shfl((int)word, (lane & 31) + 32 * ((key >> 2) & 1));
-    const float w = bf2f((uint16_t)(v & 1 ? word >> 16 : word));
-    if (!visible(key)) continue;
+    for (int t = 0; t < NT; ++t) {
+      uint32_t word = 0;
+#pragma unroll
+      for (int i = 0; i < 8; ++i)
+        if (i == v >> 1) word = pk[t][i >> 2][i & 3];
+      word = (uint32_t)__shfl((int)word, (lane & 31) + 32 * ((key >> 2) & 1));
+      w[t] = bf2f((uint16_t)(v & 1 ? word >> 16 : word));
+    }
 #pragma unroll
     for (int mt = 0; mt < MTV; ++mt)
 #pragma unroll
-      for (int r = 0; r < 16; ++r) {
-        const uint16_t x = value(key, 32 * mt + 8 * (r >> 2) + 4 * hh + (r & 3));
-        if ((x & 0x7f80) == 0x7f80) o[mt][r] += w * bf2f(x);
-      }
+      for (int g = 0; g < 4; ++g)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const uint16_t x = p[32 * mt + 8 * g + i];
+          if ((x & 0x7f80) != 0x7f80) continue;
+#pragma unroll
+          for (int t = 0; t < NT; ++t)
+            if ((sees[t] >> key) & 1) o[t][mt][4 * g + i] += w[t] * bf2f(x);
+        }
   }
 }
 
-template <int DH, int NTW, int KS>
-__global__ __launch_bounds__(KS* NTW * 64, 2) void tree_attn_q8_kernel(Q8Args a) {
-  constexpr int MTV = DH / 32, OW = MTV * 16 * 64;
-  extern __shared__ __align__(16) uint8_t smem[];  // parts handed over
-  __shared__ float sm_m[KS * NTW][32], sm_l[KS * NTW][32];
+// A stream's ring in LDS is its wavefront's own: loads go there without registers (1 KiB each, in
+// order), nobody else reads it and nobody waits.  Slot of 32 keys: K pieces, then V pieces.
+// No branch that the compiler sees: it would copy the accumulators around it.
+// all loads have landed but those of `later` further blocks (P each, up to 3 of them) and EXTRA; MOST, if
+// later is 4
+template <int P, int EXTRA, int MOST>
+__device__ __forceinline__ void wait_blocks(int blocks) {
+  const int later = __builtin_amdgcn_readfirstlane(blocks);
+  asm volatile(
+      "s_cmp_lt_u32 %0, 1\n\ts_cbranch_scc1 1f\n\t"
+      "s_cmp_lt_u32 %0, 2\n\ts_cbranch_scc1 2f\n\t"
+      "s_cmp_lt_u32 %0, 3\n\ts_cbranch_scc1 3f\n\t"
+      "s_cmp_lt_u32 %0, 4\n\ts_cbranch_scc1 4f\n\t"
+      "s_waitcnt vmcnt(%5)\n\ts_branch 5f\n"
+      "1:\n\ts_waitcnt vmcnt(%1)\n\ts_branch 5f\n"
+      "2:\n\ts_waitcnt vmcnt(%2)\n\ts_branch 5f\n"
+      "3:\n\ts_waitcnt vmcnt(%3)\n\ts_branch 5f\n"
+      "4:\n\ts_waitcnt vmcnt(%4)\n"
+      "5:" ::"s"(later), "n"(EXTRA), "n"(P + EXTRA), "n"(2 * P + EXTRA), "n"(3 * P + EXTRA), "n"(MOST) : "memory", "scc");
+}
+#pragma clang diagnostic push
+#pragma clang diagnostic ignored "-Winline-asm"
+// P pieces of 1 KiB from base (uniform) to LDS at `lds` (uniform) if `yes`
+template <int P>
+__device__ __forceinline__ void request(const void* base, uint32_t lane16, uint32_t lds, int if_yes) {
+  static_assert(P == 2 || P == 4, "");
+  const int yes = __builtin_amdgcn_readfirstlane(if_yes);
+  // what was read from these slots is in registers
+  // (no instruction offsets: these loads add them to the LDS address as well)
+  if constexpr (P == 4)
+    asm volatile(
+        "s_waitcnt lgkmcnt(0)\n\ts_cmp_eq_u32 %3, 0\n\ts_cbranch_scc1 1f\n\t"
+        "s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1\n\t"
+        "s_add_u32 m0, %2, 0x400\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %4, %1\n\t"
+        "s_add_u32 m0, %2, 0x800\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %5, %1\n\t"
+        "s_add_u32 m0, %2, 0xc00\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %6, %1\n"
+        "1:" ::"v"(lane16), "s"(base), "s"(lds), "s"(yes), "v"(lane16 + 1024), "v"(lane16 + 2048), "v"(lane16 + 3072)
+        : "memory", "m0", "scc");
+  else
+    asm volatile(
+        "s_waitcnt lgkmcnt(0)\n\ts_cmp_eq_u32 %3, 0\n\ts_cbranch_scc1 1f\n\t"
+        "s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1\n\t"
+        "s_add_u32 m0, %2, 0x400\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %4, %1\n"
+        "1:" ::"v"(lane16), "s"(base), "s"(lds), "s"(yes), "v"(lane16 + 1024) : "memory", "m0", "scc");
+}
+#pragma clang diagnostic pop
+
+// rings; in the same place what the streams hand over at the end
+template <int DH, int NT, int KS, int D>
+constexpr size_t q8_lds() {
+  const size_t ring = (size_t)KS * D * 64 * DH, merge = (size_t)(DH / 32) * (KS - 1) * 4096;
+  return ring > merge ? ring : merge;
+}
+
+// KS key streams of one wavefront each, which takes NT tiles of 32 queries
+template <int DH, int NT, int KS, int D, bool MANY>
+__global__ __launch_bounds__(KS * 64, KS / 4) void tree_attn_q8_kernel(Q8Args a) {
+  constexpr int MTV = DH / 32, OW = MTV * 16 * 64, P = MTV, SLOT = 64 * DH, QUERIES = 32 * NT;
+  constexpr int TILE = 64 * DH, CH = DH / 8;
+  static_assert(D >= 2 && KS >= TRJ_N_MAX / 32 && NT <= 2, "a stream's ring takes a block of the tree's rows");
+  extern __shared__ __align__(16) uint8_t smem[];  // rings, then parts handed over
+  __shared__ float sm_m[KS][NT][32], sm_l[KS][NT][32];
   const int tid = threadIdx.x, lane = tid & 63, n32 = lane & 31, hh = lane >> 5;
-  const int wv = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int nt = wv % NTW, ks = wv / NTW;
-  const Q8Plan plan = q8_plan<NTW>(a);
-  if (blockIdx.x == 0)  // sequences without work
-    for (int s = tid; s < a.B; s += KS * NTW * 64) {
-      const Q8Seq q = q8_seq(a, s);
-      if (q8_groups<NTW>(a, q) == 0) a.status[s] = q.nodes < 0;
-    }
-  auto item = [&](int x) -> bool {  // false: behind the last one
-  // item -> (sequence, query group, split, K/V head), K/V head fastest: the groups that read the same
-  // blocks are a multiple of the heads apart, which is mostly one die (XCD)
-  int s, nth;
-  if (!find_seq(x, a.B, [&](int y) {
-        const Q8Seq q = q8_seq(a, y);
-        return q8_groups<NTW>(a, q) * a.n_kv_heads * q8_splits(plan, q);
-      }, s, nth)) return false;
-  const Q8Seq seq = q8_seq(a, s);
-  const int splits = q8_splits(plan, seq);
-  const int head = nth % a.n_kv_heads, sp = nth / a.n_kv_heads % splits, qg = nth / a.n_kv_heads / splits;
-  const int nq = seq.nodes * a.group, n = seq.nodes;
-  const int row_len = a.n_kv_heads * a.group * DH;  // of out
-  auto zero_rows = [&](int i0, int i1) {  // nodes i0.. of the sequence, this K/V head's part
-    const size_t w = (size_t)a.group * DH / 4;
-    const u32x2 z = {0, 0};
-    for (size_t i = tid; i < (i1 - i0) * w; i += KS * NTW * 64)
-      *reinterpret_cast<u32x2*>(a.out + (size_t)(seq.r0 + i0 + i / w) * row_len + head * a.group * DH + i % w * 4) = z;
-  };
-  const bool first = sp == 0 && qg == 0;
-  if (seq.L < 0) {
-    zero_rows(0, n);
-    if (first && head == 0 && tid == 0) a.status[s] = 1;
-    return true;
-  }
-  const TreeParents par = load_parents(a.parent, seq.r0, n);
-  if (!tree_valid(par, n)) {  // the same in every wavefront
-    if (first) zero_rows(0, n);
-    if (first && head == 0 && tid == 0) a.status[s] = 1;
-    return true;
-  }
-  const int32_t* table = a.block_table + (size_t)s * a.max_blocks;
-  if (first && head == 0) {  // the verdict on the sequence's pages
-    bool bad = false;
-    for (int j = tid; j < seq.cached; j += KS * NTW * 64) bad = bad || (unsigned)table[j] >= (unsigned)a.n_blocks;
-    bad = __syncthreads_or(bad);
-    if (tid == 0) a.status[s] = bad;
-  }
-  const int per = (seq.blocks + splits - 1) / splits;
-  const int b0 = sp * per, b1 = min(seq.blocks, b0 + per);
+  const int ks = __builtin_amdgcn_readfirstlane(tid >> 6);
 
-  // this lane's query
-  const int qi = (qg * NTW + nt) * 32 + n32, qc = min(qi, nq - 1);
-  const int node = qc / a.group, qhead = head * a.group + qc % a.group;
-  const bool live = (qg * NTW + nt) * 32 < nq;
-  bf16x8 qreg[2 * MTV];  // step 2j + i: columns 32j + 16hh + 8i ..
-  {
-    const uint16_t* qp = a.q + (size_t)(seq.r0 + node) * a.q_stride + (size_t)qhead * DH + hh * 16;
-#pragma unroll
-    for (int j = 0; j < MTV; ++j) {
-      qreg[2 * j] = *reinterpret_cast<const bf16x8*>(qp + 32 * j);
-      qreg[2 * j + 1] = *reinterpret_cast<const bf16x8*>(qp + 32 * j + 8);
-    }
+  Q8Plan<MANY, QUERIES> plan(a);
+  if (blockIdx.x == 0) {  // sequences without work
+    if (!MANY && ks == 0 && lane < a.B && plan.mine.blocks == 0) a.status[plan.id] = plan.mine.nodes < 0;
+    if (MANY)
+      for (int s = tid; s < a.B; s += KS * 64) {
+        const Q8Seq q = q8_seq(a, s);
+        if (q.blocks == 0) a.status[s] = q.nodes < 0;
+      }
   }
-  f32x16 o[MTV];
-#pragma unroll
-  for (int mt = 0; mt < MTV; ++mt)
-#pragma unroll
-    for (int v = 0; v < 16; ++v) o[mt][v] = 0.f;
-  Softmax sm;
+  for (int x = blockIdx.x;; x += gridDim.x) {
+    Q8Work w;
+    if (!plan.template find<0>(x, w)) return;
+    const Q8Seq seq = w.seq;
+    const int splits = w.splits, n = seq.nodes, nq = n * a.group;
+    const int head = w.nth % a.n_kv_heads, sp = w.nth / a.n_kv_heads % splits, qg = w.nth / a.n_kv_heads / splits;
+    const int row_len = a.n_kv_heads * a.group * DH;  // of out
+    const bool first = sp == 0 && qg == 0;
+    const TreeParents par = load_parents(a.parent, seq.r0, seq.L < 0 ? 0 : n);
+    if (seq.L < 0 || !tree_valid(par, n)) {  // the same in every wavefront
+      if (first) {  // rows of zeros, this K/V head's part
+        const size_t width = (size_t)a.group * DH / 4;
+        const u32x2 z = {0, 0};
+        for (size_t i = tid; i < n * width; i += KS * 64)
+          *reinterpret_cast<u32x2*>(a.out + (size_t)(seq.r0 + i / width) * row_len + head * a.group * DH + i % width * 4) = z;
+        if (head == 0 && tid == 0) a.status[w.s] = 1;
+      }
+      continue;
+    }
+    const int32_t* table = a.block_table + (size_t)w.s * a.max_blocks;
+    const int cached = seq.cached();
+    const int per = (seq.blocks + splits - 1) / splits, b0 = sp * per, b1 = min(seq.blocks, b0 + per);
 
-  // ---- cached blocks b0 + ks, b0 + ks + KS, ..
-  const int cend = min(b1, seq.cached);
-  const int mine = live && b0 + ks < cend ? (cend - b0 - ks + KS - 1) / KS : 0;
-  const size_t plane = (size_t)head * a.n_blocks;
-  int ids = 0;           // page, K and V scale of block i of this stream, i % 64 == lane
-  float ksc = 0.f, vsc = 0.f;
-  auto look_up = [&](int i0) {
-    const int i = i0 + lane;
-    if (i < mine) {
-      ids = table[b0 + ks + i * KS];
+    // ---- cached blocks b0 + ks, b0 + ks + KS, ..: page, K and V scale of block i in lane i % 64
+    const int cend = min(b1, cached);
+    const int mine = b0 + ks < cend ? (cend - b0 - ks + KS - 1) / KS : 0;
+    const size_t plane = (size_t)head * a.n_blocks;
+    int ids = 0;
+    float ksc = 1.f, vsc = 1.f;
+    auto look_up = [&](int i0) {
+      const int i = i0 + lane;
+      ids = i < mine ? table[b0 + ks + i * KS] : 0;
       const bool ok = (unsigned)ids < (unsigned)a.n_blocks;
       ids = ok ? ids : 0;
-      ksc = a.k_scale[plane + ids] ;
+      ksc = ok ? a.k_scale[plane + ids] : NAN;  // a page that is not there makes its rows NaN
       vsc = a.v_scale[plane + ids];
-      if (!ok) ksc = NAN;
+    };
+    if (mine > 0) look_up(0);
+    // queries: tile t, column n32; step 2j + i of the product: columns 32j + 16hh + 8i ..
+    int node[NT], qhead[NT];
+    bool live[NT];
+    bf16x8 qreg[NT][2 * MTV];
+#pragma unroll
+    for (int t = 0; t < NT; ++t) {
+      const int qi = (qg * NT + t) * 32 + n32, qc = min(qi, nq - 1);
+      node[t] = qc / a.group;
+      qhead[t] = head * a.group + qc % a.group;
+      live[t] = qi < nq;
+      const uint16_t* qp = a.q + (size_t)(seq.r0 + node[t]) * a.q_stride + (size_t)qhead[t] * DH + hh * 16;
+#pragma unroll
+      for (int j = 0; j < 2 * MTV; ++j) qreg[t][j] = *reinterpret_cast<const bf16x8*>(qp + 32 * (j >> 1) + 8 * (j & 1));
     }
-  };
-  u32x4 kreg[MTV], vreg[MTV];
-  auto load = [&](u32x4 (&r)[MTV], const uint8_t* pool, int i) {
-    const size_t page = (uint32_t)__builtin_amdgcn_readlane(ids, i & 63);
-    const u32x4* p = reinterpret_cast<const u32x4*>(pool + (plane + page) * 32 * DH) + lane;
+    f32x16 o[NT][MTV];
+    Softmax sm[NT];
 #pragma unroll
-    for (int j = 0; j < MTV; ++j) r[j] = p[j * 64];
-  };
-  if (mine > 0) {
-    look_up(0);
-    load(kreg, a.k_pool, 0);
-    load(vreg, a.v_pool, 0);
-  }
-  for (int i = 0; i < mine; ++i) {
-    const float kscale = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(ksc), i & 63));
-    const float vscale = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(vsc), i & 63));
-    if (((i + 1) & 63) == 0) look_up(i + 1);
-    const int key0 = (b0 + ks + i * KS) * 32, rest = seq.L - key0;
-    f32x16 sacc;
-#pragma unroll
-    for (int v = 0; v < 16; ++v) sacc[v] = 0.f;
-#pragma unroll
-    for (int j = 0; j < MTV; ++j) {
-      sacc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(operand(kreg[j][0], kreg[j][1], kscale), qreg[2 * j], sacc, 0, 0, 0);
-      sacc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(operand(kreg[j][2], kreg[j][3], kscale), qreg[2 * j + 1], sacc, 0, 0, 0);
-    }
-    if (i + 1 < mine) load(kreg, a.k_pool, i + 1);
-    float sc[16];
-    const float f = kscale == kscale ? a.scale_log2e : NAN;  // a page that is not there
-#pragma unroll
-    for (int v = 0; v < 16; ++v) sc[v] = sacc[v] * f;
-    if (rest < 32) {
-#pragma unroll
-      for (int v = 0; v < 16; ++v)
-        if (8 * (v >> 2) + 4 * hh + (v & 3) >= rest) sc[v] = -INFINITY;
-      // slots past the end may hold anything: their weights are 0, their values have to be numbers
-#pragma unroll
-      for (int d = 0; d < 4; ++d) {
-        const int keep = min(max(rest - 8 * d - 4 * hh, 0), 4);
-        const uint32_t mask = keep == 4 ? 0xffffffffu : (1u << (8 * keep)) - 1u;
-#pragma unroll
-        for (int mt = 0; mt < MTV; ++mt) vreg[mt][d] &= mask;
-      }
-    }
-    u32x4 pk[2];
-    q8_rescale<MTV>(o, sm.take(sc, pk));
-#pragma unroll
-    for (int mt = 0; mt < MTV; ++mt) {
-      o[mt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(operand(vreg[mt][0], vreg[mt][1], vscale), __builtin_bit_cast(bf16x8, pk[0]), o[mt], 0, 0, 0);
-      o[mt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(operand(vreg[mt][2], vreg[mt][3], vscale), __builtin_bit_cast(bf16x8, pk[1]), o[mt], 0, 0, 0);
-    }
-    if (i + 1 < mine) load(vreg, a.v_pool, i + 1);
-  }
-
-  // ---- the tree's own rows
-  int tb = max(b0, seq.cached);
-  tb += (ks - (tb - b0) % KS + KS) % KS;  // this stream's first
-  if (live && tb < b1) {
-    const TreeBits bits = tree_bits(par, n);
-    uint32_t anc[4];
-#pragma unroll
-    for (int k = 0; k < 4; ++k) {
-      const uint32_t w = (uint32_t)from_node(bits.w[k], node);
-      anc[k] = qi < nq ? w : 0u;
-    }
-    for (; tb < b1; tb += KS) {
-      const int key0 = (tb - seq.cached) * 32;  // node
-      const uint32_t sees = key0 == 0 ? anc[0] : key0 == 32 ? anc[1] : key0 == 64 ? anc[2] : anc[3];
-      const size_t at = (size_t)head * DH;
-      f32x16 sacc;
-#pragma unroll
-      for (int v = 0; v < 16; ++v) sacc[v] = 0.f;
-      {
-        const uint16_t* kp = a.k_rows + (size_t)(seq.r0 + min(key0 + n32, n - 1)) * a.row_stride + at + hh * 16;
-#pragma unroll
-        for (int j = 0; j < MTV; ++j) {
-          sacc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(*reinterpret_cast<const bf16x8*>(kp + 32 * j), qreg[2 * j], sacc, 0, 0, 0);
-          sacc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(*reinterpret_cast<const bf16x8*>(kp + 32 * j + 8), qreg[2 * j + 1], sacc, 0, 0, 0);
-        }
-      }
-      float sc[16];
-#pragma unroll
-      for (int v = 0; v < 16; ++v)
-        sc[v] = (sees >> (8 * (v >> 2) + 4 * hh + (v & 3))) & 1 ? sacc[v] * a.scale_log2e : -INFINITY;
-      u32x4 pk[2];
-      q8_rescale<MTV>(o, sm.take(sc, pk));
-      auto value = [&](int key, int c) -> uint16_t {
-        return key0 + key < n ? a.v_rows[(size_t)(seq.r0 + key0 + key) * a.row_stride + at + c] : (uint16_t)0;
-      };
-      bool odd = false;
+    for (int t = 0; t < NT; ++t)
 #pragma unroll
       for (int mt = 0; mt < MTV; ++mt)
 #pragma unroll
-        for (int kg = 0; kg < 2; ++kg) {
-          u32x4 v;
-#pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            const int key = 16 * kg + 8 * (e >> 1) + 4 * hh + 2 * (e & 1);
-            uint32_t lo = value(key, 32 * mt + n32), hi = value(key + 1, 32 * mt + n32);
-            if ((lo & 0x7f80u) == 0x7f80u) odd = true, lo = 0;
-            if ((hi & 0x7f80u) == 0x7f80u) odd = true, hi = 0;
-            v[e] = lo | hi << 16;
-          }
-          o[mt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, v), __builtin_bit_cast(bf16x8, pk[kg]), o[mt], 0, 0, 0);
-        }
-      if (__ballot(odd))
-        q8_add_odd_values<MTV>(o, pk, min(32, n - key0), [&](int key) { return ((sees >> key) & 1) != 0; }, value);
-    }
-  }
+        for (int v = 0; v < 16; ++v) o[t][mt][v] = 0.f;
 
-  // ---- merge the key streams of every query tile in a fixed order: stream mt % KS owns part mt
-  const float lt = sm.l + __shfl_xor(sm.l, 32);
-  if (hh == 0) {
-    sm_m[wv][n32] = sm.m;
-    sm_l[wv][n32] = lt;
-  }
-  __syncthreads();
-  float* red = reinterpret_cast<float*>(smem);
-  float mg = -INFINITY;
+    const uint32_t ring = __builtin_amdgcn_readfirstlane((uint32_t)(size_t)(__attribute__((address_space(3))) uint8_t*)smem + ks * D * SLOT);
+    const u32x4* const ring_r = reinterpret_cast<const u32x4*>(smem + (size_t)ks * D * SLOT) + lane;
+    auto ask = [&](const uint8_t* pool, int i, int part, int yes) {  // block i of this stream, K (0) or V (1)
+      const size_t page = (uint32_t)__builtin_amdgcn_readlane(ids, i & 63);
+      request<P>(pool + (plane + page) * 32 * DH, lane * 16, ring + (i % D) * SLOT + part * (SLOT / 2), yes);
+    };
+    u32x4 kraw[P];  // codes of the next K
+    auto read_k = [&](int i) {
 #pragma unroll
-  for (int k = 0; k < KS; ++k) mg = fmaxf(mg, sm_m[nt + NTW * k][n32]);
-  const float ref = mg == -INFINITY ? 0.f : mg;
-  float lg = 0.f;
+      for (int j = 0; j < P; ++j) kraw[j] = ring_r[(i % D) * (SLOT / 16) + j * 64];
+    };
+    auto values = [&](int t, const bf16x8 (&vop)[2 * MTV], const u32x4 (&pk)[2]) {
 #pragma unroll
-  for (int k = 0; k < KS; ++k) lg += sm_l[nt + NTW * k][n32] * __builtin_amdgcn_exp2f(sm_m[nt + NTW * k][n32] - ref);
-  const float mine_f = __builtin_amdgcn_exp2f(sm.m - ref);
+      for (int mt = 0; mt < MTV; ++mt)
 #pragma unroll
-  for (int mt = 0; mt < MTV; ++mt)
+        for (int kg = 0; kg < 2; ++kg)
+          o[t][mt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vop[2 * mt + kg], __builtin_bit_cast(bf16x8, pk[kg]), o[t][mt], 0, 0, 0);
+    };
+    // Block i of those up to c1; its K is in kraw, its V and up to D - 1 blocks are on the way.  LAST: `rest` of its
+    // 32 keys exist.  With two tiles the products of one run while the softmax of the other does.
+    auto block = [&](int i, int c1, auto last_c, int rest) {
+      constexpr bool LAST = decltype(last_c)::value;
+      const float kscale = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(ksc), i & 63));
+      const float vscale = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(vsc), i & 63));
+      const float f = kscale == kscale ? a.scale_log2e : NAN;  // a page that is not there
+      const int later = min(D - 1, c1 - 1 - i);
+      const bool more = i + D < c1;
+      bf16x8 kop[2 * MTV], vop[2 * MTV];
 #pragma unroll
-    for (int v = 0; v < 16; ++v) o[mt][v] *= mine_f;
-  constexpr int PART = 16 * 64;
+      for (int j = 0; j < 2 * MTV; ++j) kop[j] = operand(kraw[j >> 1][2 * (j & 1)], kraw[j >> 1][2 * (j & 1) + 1], kscale);
+      f32x16 sacc[NT];
+      auto scores = [&](int t) {
 #pragma unroll
-  for (int mt = 0; mt < MTV; ++mt) {
-    const int owner = mt % KS;
-    if (ks != owner) {
-      float* dst = red + (((nt * MTV + mt) * (KS - 1)) + (ks < owner ? ks : ks - 1)) * PART + lane;
+        for (int v = 0; v < 16; ++v) sacc[t][v] = 0.f;
 #pragma unroll
-      for (int v = 0; v < 16; ++v) dst[v * 64] = o[mt][v];
-    }
-  }
-  __syncthreads();
-  if (!live) return true;
-  size_t part = 0;
-  if (splits > 1) {  // place among the partials: those of the split sequences before, then this one's in item order
-    int before = 0;
-    for (int s0 = 0; s0 < s; s0 += 64) {
-      int c = 0;
-      if (s0 + lane < s) {
-        const Q8Seq q = q8_seq(a, s0 + lane);
-        const int k = q8_splits(plan, q);
-        c = k > 1 ? q8_groups<NTW>(a, q) * a.n_kv_heads * k : 0;
-      }
-      before += __shfl(wave_scan(c), 63);
-    }
-    part = (size_t)(before + nth) * NTW + nt;
-    if (before + nth >= a.max_parts) return true;  // more work than T rows can be: ranges that overlap
-    if (ks == 0 && hh == 0) {
-      a.pm[part * 32 + n32] = mg;
-      a.pl[part * 32 + n32] = lg;
-    }
-  }
-  const float inv = 1.0f / lg;
+        for (int j = 0; j < 2 * MTV; ++j) sacc[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kop[j], qreg[t][j], sacc[t], 0, 0, 0);
+      };
+      auto hide = [&](int t) {
+        if (LAST)
 #pragma unroll
-  for (int mt = 0; mt < MTV; ++mt) {
-    if (ks != mt % KS) continue;
-    const float* src = red + ((nt * MTV + mt) * (KS - 1)) * PART + lane;
+          for (int v = 0; v < 16; ++v)
+            if (8 * (v >> 2) + 4 * hh + (v & 3) >= rest) sacc[t][v] = -INFINITY;
+      };
+      ask(a.k_pool, i + D, 0, more);
+      scores(0);
+      // V: behind it the later blocks and, if asked for, K of block i + D
+      wait_blocks<2 * P, 0, 2 * P * (D - 1) + P>(more ? 4 : later);
+      u32x4 vraw[P];
 #pragma unroll
-    for (int k = 0; k < KS - 1; ++k)
+      for (int j = 0; j < P; ++j) vraw[j] = ring_r[(i % D) * (SLOT / 16) + (P + j) * 64];
+      u32x4 pk[NT][2];
+      float alpha[NT];
+      if constexpr (NT == 2) scores(1);
+      hide(0);
+      alpha[0] = sm[0].take(sacc[0], f, pk[0]);
+      if (LAST) {
+        // slots past the end may hold anything: their weights are 0, their values have to be numbers
 #pragma unroll
-      for (int v = 0; v < 16; ++v) o[mt][v] += src[(k * 16 + v) * 64];
-    if (splits == 1) {
-      if (qi < nq) {
-        uint16_t* dst = a.out + (size_t)(seq.r0 + node) * row_len + (size_t)qhead * DH + 32 * mt + 4 * hh;
+        for (int d = 0; d < 4; ++d) {
+          const int keep = min(max(rest - 8 * d - 4 * hh, 0), 4);
+          const uint32_t mask = keep == 4 ? 0xffffffffu : (1u << (8 * keep)) - 1u;
 #pragma unroll
-        for (int g = 0; g < 4; ++g) {
-          const u32x2 v = {pack2bf(o[mt][4 * g] * inv, o[mt][4 * g + 1] * inv), pack2bf(o[mt][4 * g + 2] * inv, o[mt][4 * g + 3] * inv)};
-          *reinterpret_cast<u32x2*>(dst + 8 * g) = v;
+          for (int j = 0; j < P; ++j) vraw[j][d] &= mask;
         }
       }
-    } else {
-      float* img = a.po + part * OW + mt * PART + lane;
 #pragma unroll
-      for (int v = 0; v < 16; ++v) img[v * 64] = o[mt][v];
+      for (int j = 0; j < 2 * MTV; ++j) vop[j] = operand(vraw[j >> 1][2 * (j & 1)], vraw[j >> 1][2 * (j & 1) + 1], vscale);
+      if constexpr (NT == 2) interleave<8, 10>();
+      ask(a.v_pool, i + D, 1, more);
+      q8_rescale<MTV>(o[0], alpha[0]);
+      if constexpr (NT == 2) {
+        values(0, vop, pk[0]);
+        hide(1);
+        alpha[1] = sm[1].take(sacc[1], f, pk[1]);
+        interleave<2 * MTV, 10>();
+        q8_rescale<MTV>(o[1], alpha[1]);
+      }
+      // K of the next block (behind the last one: whatever is there)
+      wait_blocks<2 * P, P, 2 * P * (D - 1) + P>(more ? 4 : max(later - 1, 0));
+      read_k(i + 1);
+      values(NT - 1, vop, pk[NT - 1]);
+    };
+    auto fill = [&](int c0, int c1) {
+#pragma unroll
+      for (int i = 0; i < D; ++i) {
+        ask(a.k_pool, c0 + i, 0, c0 + i < c1);
+        ask(a.v_pool, c0 + i, 1, c0 + i < c1);
+      }
+    };
+    // ---- the tree's own rows first: they need no table, and the cached blocks come meanwhile.  Everybody puts
+    // them into the order of the operands, each block into the ring of the stream that takes it, which asks for
+    // its cached blocks later.
+    const int t0 = max(b0, cached), tree = max(0, b1 - t0);  // blocks
+    const int tb = (ks - (t0 - b0) % KS + KS) % KS;          // this stream's of them
+    if (tb >= tree) fill(0, min(mine, 64));
+    bool odd = false;
+    for (int u = tid; u < tree * 16 * CH; u += KS * 64) {  // two rows, 8 columns
+      const int b = u / (16 * CH), r = u / CH % 16 * 2, c = u % CH, key = (t0 + b - cached) * 32 + r;
+      const size_t lo = (size_t)(seq.r0 + min(key, n - 1)) * a.row_stride + (size_t)head * DH + 8 * c;
+      const size_t hi = (size_t)(seq.r0 + min(key + 1, n - 1)) * a.row_stride + (size_t)head * DH + 8 * c;
+      const u32x4 k0 = *reinterpret_cast<const u32x4*>(a.k_rows + lo), k1 = *reinterpret_cast<const u32x4*>(a.k_rows + hi);
+      const u32x4 v0 = *reinterpret_cast<const u32x4*>(a.v_rows + lo), v1 = *reinterpret_cast<const u32x4*>(a.v_rows + hi);
+      uint8_t* const kt = smem + (size_t)((t0 - b0 + b) % KS) * D * SLOT;
+      u32x4* const kd = reinterpret_cast<u32x4*>(kt + ((c >> 2) * 2 + (c & 1)) * 1024 + ((c >> 1) & 1) * 512 + r * 16);
+      kd[0] = k0;
+      kd[1] = k1;
+      uint32_t* const vd = reinterpret_cast<uint32_t*>(kt + TILE + (c >> 2) * 2048 + (r >> 4) * 1024 + ((r >> 2) & 1) * 512 +
+                                                       (c & 3) * 128 + ((r >> 3) & 1) * 8 + (r & 3) * 2);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        uint32_t x = i & 1 ? v0[i >> 1] >> 16 : v0[i >> 1] & 0xffffu, y = i & 1 ? v1[i >> 1] & 0xffff0000u : v1[i >> 1] << 16;
+        if ((x & 0x7f80u) == 0x7f80u) odd = true, x = 0;
+        if ((y & 0x7f800000u) == 0x7f800000u) odd = true, y = 0;
+        vd[4 * i] = x | y;
+      }
     }
+    bool any_odd = false;
+    if (tree > 0) any_odd = __syncthreads_or(odd);
+    if (tb < tree) {
+      {
+        const TreeBits bits = tree_bits(par, n);
+        const int key0 = (t0 + tb - cached) * 32;
+        uint32_t sees[NT];
+#pragma unroll
+        for (int t = 0; t < NT; ++t) {
+          const int lo = from_node(key0 < 64 ? (key0 ? bits.w[1] : bits.w[0]) : (key0 == 64 ? bits.w[2] : bits.w[3]), node[t]);
+          sees[t] = live[t] ? (uint32_t)lo : 0u;
+        }
+        const u32x4* const kt = reinterpret_cast<const u32x4*>(smem + (size_t)ks * D * SLOT) + lane;
+        f32x16 sacc[NT];
+#pragma unroll
+        for (int t = 0; t < NT; ++t)
+#pragma unroll
+          for (int v = 0; v < 16; ++v) sacc[t][v] = 0.f;
+#pragma unroll
+        for (int j = 0; j < 2 * MTV; ++j) {
+          const bf16x8 kop = __builtin_bit_cast(bf16x8, kt[j * 64]);
+#pragma unroll
+          for (int t = 0; t < NT; ++t) sacc[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kop, qreg[t][j], sacc[t], 0, 0, 0);
+        }
+        u32x4 pk[NT][2];
+#pragma unroll
+        for (int t = 0; t < NT; ++t) {
+#pragma unroll
+          for (int v = 0; v < 16; ++v)
+            if (!((sees[t] >> (8 * (v >> 2) + 4 * hh + (v & 3))) & 1)) sacc[t][v] = -INFINITY;
+          q8_rescale<MTV>(o[t], sm[t].take(sacc[t], a.scale_log2e, pk[t]));
+        }
+#pragma unroll
+        for (int mt = 0; mt < MTV; ++mt)
+#pragma unroll
+          for (int kg = 0; kg < 2; ++kg) {
+            const bf16x8 vop = __builtin_bit_cast(bf16x8, kt[TILE / 16 + (mt * 2 + kg) * 64]);
+#pragma unroll
+            for (int t = 0; t < NT; ++t)
+              o[t][mt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vop, __builtin_bit_cast(bf16x8, pk[t][kg]), o[t][mt], 0, 0, 0);
+          }
+        if (any_odd)
+          q8_add_odd_values(o, pk, sees, a.v_rows + (size_t)(seq.r0 + key0) * a.row_stride + (size_t)head * DH, a.row_stride,
+                            min(32, n - key0));
+      }
+      fill(0, min(mine, 64));
+    }
+
+    // ---- the cached blocks
+    for (int c0 = 0; c0 < mine; c0 += 64) {
+      const int c1 = min(mine, c0 + 64);
+      if (c0 > 0) {
+        look_up(c0);
+        fill(c0, c1);
+      }
+      const int rest = seq.L - (b0 + ks + (c1 - 1) * KS) * 32;
+      const int whole = rest < 32 ? c1 - 1 : c1;
+      wait_blocks<2 * P, P, 0>(min(D - 1, c1 - 1 - c0));
+      read_k(c0);
+      for (int i = c0; i < whole; ++i) block(i, c1, std::false_type{}, 32);
+      if (whole < c1) block(whole, c1, std::true_type{}, rest);
+    }
+    if (first && head == 0) {  // the verdict on the sequence's pages
+      bool bad = false;
+      for (int j = tid; j < cached; j += KS * 64) bad = bad || (unsigned)table[j] >= (unsigned)a.n_blocks;
+      bad = __syncthreads_or(bad);
+      if (tid == 0) a.status[w.s] = bad;
+    }
+
+    // ---- merge the key streams of every query tile in a fixed order: stream mt (second tile: mt + KS / 2)
+    // owns part mt
+#pragma unroll
+    for (int t = 0; t < NT; ++t) {
+      const float l = sm[t].l + __shfl_xor(sm[t].l, 32);
+      if (hh == 0) {
+        sm_m[ks][t][n32] = sm[t].m;
+        sm_l[ks][t][n32] = l;
+      }
+    }
+    __syncthreads();  // the rings are free, too
+    float* const red = reinterpret_cast<float*>(smem);
+    constexpr int PART = 16 * 64;
+#pragma unroll
+    for (int t = 0; t < NT; ++t) {  // tile by tile: all at once do not fit LDS
+      if (t > 0) __syncthreads();
+      float mg = -INFINITY, lg = 0.f;
+#pragma unroll
+      for (int k = 0; k < KS; ++k) mg = fmaxf(mg, sm_m[k][t][n32]);
+      const float ref = mg == -INFINITY ? 0.f : mg;
+#pragma unroll
+      for (int k = 0; k < KS; ++k) lg += sm_l[k][t][n32] * __builtin_amdgcn_exp2f(sm_m[k][t][n32] - ref);
+      const float f = __builtin_amdgcn_exp2f(sm[t].m - ref);
+#pragma unroll
+      for (int mt = 0; mt < MTV; ++mt) {
+#pragma unroll
+        for (int v = 0; v < 16; ++v) o[t][mt][v] *= f;
+        const int owner = (mt + t * (KS / 2)) % KS;
+        if (ks != owner) {
+          float* dst = red + ((mt * (KS - 1)) + (ks < owner ? ks : ks - 1)) * PART + lane;
+#pragma unroll
+          for (int v = 0; v < 16; ++v) dst[v * 64] = o[t][mt][v];
+        }
+      }
+      __syncthreads();
+      if ((qg * NT + t) * 32 >= nq) continue;
+      const int part = w.part0 + w.nth;
+      if (splits > 1 && part >= a.max_parts) continue;  // more work than T rows can be: ranges that overlap
+      const size_t tile = (size_t)part * NT + t;
+      if (splits > 1 && ks == 0 && hh == 0) {
+        a.pm[tile * 32 + n32] = mg;
+        a.pl[tile * 32 + n32] = lg;
+      }
+      const float inv = 1.0f / lg;
+#pragma unroll
+      for (int mt = 0; mt < MTV; ++mt) {
+        if (ks != (mt + t * (KS / 2)) % KS) continue;
+        const float* src = red + (mt * (KS - 1)) * PART + lane;
+#pragma unroll
+        for (int k = 0; k < KS - 1; ++k)
+#pragma unroll
+          for (int v = 0; v < 16; ++v) o[t][mt][v] += src[(k * 16 + v) * 64];
+        if (splits == 1) {
+          if (live[t]) {
+            uint16_t* dst = a.out + (size_t)(seq.r0 + node[t]) * row_len + (size_t)qhead[t] * DH + 32 * mt + 4 * hh;
+#pragma unroll
+            for (int g = 0; g < 4; ++g) {
+              const u32x2 v = {pack2bf(o[t][mt][4 * g] * inv, o[t][mt][4 * g + 1] * inv),
+                               pack2bf(o[t][mt][4 * g + 2] * inv, o[t][mt][4 * g + 3] * inv)};
+              *reinterpret_cast<u32x2*>(dst + 8 * g) = v;
+            }
+          }
+        } else {
+          float* img = a.po + tile * OW + mt * PART + lane;
+#pragma unroll
+          for (int v = 0; v < 16; ++v) img[v * 64] = o[t][mt][v];
+        }
+      }
+    }
+    __syncthreads();  // LDS is free again
   }
-  return true;
-  };
-  for (int x = blockIdx.x; item(x); x += gridDim.x) __syncthreads();  // LDS is free again
 }
 
 // Merges the partials of a (sequence, query tile, K/V head) in split order, one 32-column part of the
-// rows per workgroup: thread (lane, g) owns the accumulator registers 4g .. 4g+3 that lane held.
-template <int DH, int NTW>
-__global__ __launch_bounds__(256) void attn_q8_combine_kernel(Q8Args a) {
-  constexpr int MTV = DH / 32, PART = 16 * 64;
-  const int tid = threadIdx.x, lane = tid & 63, n32 = lane & 31, hh = lane >> 5, g = tid >> 6;
-  const Q8Plan plan = q8_plan<NTW>(a);
-  auto count = [&](int x) {
-    const Q8Seq q = q8_seq(a, x);
-    const int k = q8_splits(plan, q);
-    return k > 1 ? q8_groups<NTW>(a, q) * a.n_kv_heads * k : 0;
-  };
-  for (int x = blockIdx.x / MTV;; x += gridDim.x / MTV) {  // tiles, in the order of the partials
+// rows per workgroup.  Thread (lane, g, h) adds the accumulator registers 4g .. 4g+3 that lane held, over
+// every fourth split from h on; the four sums are added through LDS.  All loads of a batch are asked
+// for together (clamped, never predicated): one after the other 32 splits took 35 us.
+template <int DH, int NT, bool MANY>
+__global__ __launch_bounds__(1024) void attn_q8_combine_kernel(Q8Args a) {
+  constexpr int MTV = DH / 32, PART = 16 * 64, BATCH = 4;
+  __shared__ float sm_m[32][33], sm_l[4][32];
+  __shared__ f32x4 sm_o[3][256];
+  const int tid = threadIdx.x, lane = tid & 63, n32 = lane & 31, hh = lane >> 5, g = (tid >> 6) & 3, h = tid >> 8;
+  Q8Plan<MANY, 32 * NT> plan(a);
+  for (int x = blockIdx.x / MTV;; x += gridDim.x / MTV) {  // tiles
     const int mt = blockIdx.x % MTV;
-    int s, nth, base = 0;
-    if (!find_seq(x, a.B, [&](int y) {
-          const Q8Seq q = q8_seq(a, y);
-          return q8_splits(plan, q) > 1 ? q8_groups<NTW>(a, q) * a.n_kv_heads * NTW : 0;
-        }, s, nth)) return;
-    for (int s0 = 0; s0 < s; s0 += 64) base += __shfl(wave_scan(s0 + lane < s ? count(s0 + lane) : 0), 63);
-    const Q8Seq seq = q8_seq(a, s);
-    const int splits = q8_splits(plan, seq);
-    const int nt = nth % NTW, head = nth / NTW % a.n_kv_heads, qg = nth / NTW / a.n_kv_heads;
-    const int nq = seq.nodes * a.group, qi = (qg * NTW + nt) * 32 + n32;
-    if ((qg * NTW + nt) * 32 >= nq) continue;
-    if (!tree_valid(load_parents(a.parent, seq.r0, seq.nodes), seq.nodes)) continue;  // zeros are there already
-    if (base + (qg + 1) * splits * a.n_kv_heads > a.max_parts) continue;  // see there
-    auto at = [&](int sp) { return (size_t)(base + (qg * splits + sp) * a.n_kv_heads + head) * NTW + nt; };
+    Q8Work w;
+    if (!plan.template find<NT>(x, w)) return;
+    const Q8Seq seq = w.seq;
+    const int splits = w.splits, nt = w.nth % NT, head = w.nth / NT % a.n_kv_heads, qg = w.nth / NT / a.n_kv_heads;
+    const int nq = seq.nodes * a.group, qi = (qg * NT + nt) * 32 + n32;
+    if ((qg * NT + nt) * 32 >= nq) continue;
+    if (w.part0 + (qg + 1) * splits * a.n_kv_heads > a.max_parts) continue;  // see there
+    const bool valid = tree_valid(load_parents(a.parent, seq.r0, seq.nodes), seq.nodes);  // uniform
+    auto at = [&](int sp) { return (size_t)(w.part0 + (qg * splits + sp) * a.n_kv_heads + head) * NT + nt; };
+    // largest maximum: thread (row of 32 splits, query)
     float m = -INFINITY;
-    for (int sp = 0; sp < splits; ++sp) m = fmaxf(m, a.pm[at(sp) * 32 + n32]);
+    for (int sp = tid >> 5; sp < splits; sp += 32) m = fmaxf(m, a.pm[at(sp) * 32 + (tid & 31)]);
+    sm_m[tid >> 5][tid & 31] = m;
+    __syncthreads();
+    m = -INFINITY;
+#pragma unroll
+    for (int k = 0; k < 32; ++k) m = fmaxf(m, sm_m[k][n32]);
     const float ref = m == -INFINITY ? 0.f : m;
     float l = 0.f;
     f32x4 o = {0, 0, 0, 0};
-    for (int sp = 0; sp < splits; ++sp) {
-      const size_t p = at(sp);
-      const float w = __builtin_amdgcn_exp2f(a.pm[p * 32 + n32] - ref);
-      l += w * a.pl[p * 32 + n32];
-      const float* img = a.po + p * MTV * PART + mt * PART + 4 * g * 64 + lane;
+    for (int s0 = h; s0 < splits; s0 += 4 * BATCH) {
+      float pm[BATCH], pl[BATCH], po[BATCH][4];
 #pragma unroll
-      for (int v = 0; v < 4; ++v) o[v] += w * img[v * 64];
+      for (int k = 0; k < BATCH; ++k) {
+        const size_t p = at(min(s0 + 4 * k, splits - 1));
+        pm[k] = a.pm[p * 32 + n32];
+        pl[k] = a.pl[p * 32 + n32];
+        const float* img = a.po + p * MTV * PART + mt * PART + 4 * g * 64 + lane;
+#pragma unroll
+        for (int v = 0; v < 4; ++v) po[k][v] = img[v * 64];
+      }
+#pragma unroll
+      for (int k = 0; k < BATCH; ++k) {
+        if (s0 + 4 * k >= splits) break;
+        const float f = __builtin_amdgcn_exp2f(pm[k] - ref);
+        l += f * pl[k];
+#pragma unroll
+        for (int v = 0; v < 4; ++v) o[v] += f * po[k][v];
+      }
     }
-    const float inv = 1.0f / l;
-    if (qi < nq) {
+    if (h > 0) sm_o[h - 1][tid & 255] = o;
+    if (g == 0 && hh == 0) sm_l[h][n32] = l;
+    __syncthreads();
+    if (h == 0 && valid && qi < nq) {  // (rows of a malformed tree are zeros already)
+      l = 0.f;
+#pragma unroll
+      for (int k = 0; k < 4; ++k) l += sm_l[k][n32];
+#pragma unroll
+      for (int k = 0; k < 3; ++k) o += sm_o[k][tid];
+      const float inv = 1.0f / l;
       const int node = qi / a.group, qhead = head * a.group + qi % a.group;
       uint16_t* dst = a.out + ((size_t)(seq.r0 + node) * a.n_kv_heads * a.group + qhead) * DH + 32 * mt + 4 * hh + 8 * g;
       const u32x2 v = {pack2bf(o[0] * inv, o[1] * inv), pack2bf(o[2] * inv, o[3] * inv)};
       *reinterpret_cast<u32x2*>(dst) = v;
     }
+    __syncthreads();  // LDS is free again
   }
 }
 
@@ -499,7 +708,7 @@ static Q8Launch q8_launch(int B, int T, int group, int n_kv_heads, int max_prefi
   Q8Launch p;
   const int queries = (T + B - 1) / B * group;  // of a sequence, if all are alike
   p.ntw = queries > 32 ? 2 : 1;
-  p.target = p.ntw == 1 ? 512 : 256;
+  p.target = 256;
   p.min_blocks = 16;
   const long items = ((long)T * group / (32 * p.ntw) + B) * n_kv_heads;  // unsplit
   const long most = ((long)max_prefix + 31) / 32 + TRJ_N_MAX / 32;       // blocks of a sequence
@@ -515,21 +724,24 @@ size_t attn_q8_ws_floats(int B, int T, int group, int n_kv_heads, int head_dim, 
   return (size_t)p.max_parts * p.ntw * (32 * head_dim + 64);
 }
 
-template <int DH, int NTW>
+template <int DH, int NT, int KS, int D, bool MANY>
 static int q8_run(const Q8Args& a, const Q8Launch& p, hipStream_t st) {
-  constexpr int KS = 4;
-  constexpr size_t lds = (size_t)NTW * (DH / 32) * (KS - 1) * 16 * 64 * 4;
+  constexpr size_t lds = q8_lds<DH, NT, KS, D>();
   static DeviceOnce once;
-  allow_lds(once, tree_attn_q8_kernel<DH, NTW, KS>, lds);
+  allow_lds(once, tree_attn_q8_kernel<DH, NT, KS, D, MANY>, lds);
   {
     ProfScope ps_(KC_ATTN, st);
-    tree_attn_q8_kernel<DH, NTW, KS><<<p.grid, KS * NTW * 64, lds, st>>>(a);
+    tree_attn_q8_kernel<DH, NT, KS, D, MANY><<<p.grid, KS * 64, lds, st>>>(a);
   }
   int rc = check_launch();
   if (rc != TRJ_OK || p.max_parts == 0) return rc;
   ProfScope ps_(KC_ATTN_COMBINE, st);
-  attn_q8_combine_kernel<DH, NTW><<<p.tiles * (DH / 32), 256, 0, st>>>(a);
+  attn_q8_combine_kernel<DH, NT, MANY><<<p.tiles * (DH / 32), 1024, 0, st>>>(a);
   return check_launch();
+}
+template <int DH, bool MANY>
+static int q8_run_tiles(const Q8Args& a, const Q8Launch& p, hipStream_t st) {
+  return p.ntw == 1 ? q8_run<DH, 1, 8, 2, MANY>(a, p, st) : q8_run<DH, 2, 4, 4, MANY>(a, p, st);
 }
 
 int launch_tree_attn_q8(const uint16_t* q, int q_stride, const void* k_pool, const void* v_pool, const float* k_scale,
@@ -544,8 +756,8 @@ int launch_tree_attn_q8(const uint16_t* q, int q_stride, const void* k_pool, con
   const Q8Args a{q, k_rows, v_rows, (const uint8_t*)k_pool, (const uint8_t*)v_pool, k_scale, v_scale, parent, node_off,
                  block_table, prefix_len, q_stride, row_stride, max_blocks, B, T, n_kv_heads, group, n_blocks, max_prefix,
                  p.target, p.min_blocks, p.max_parts, scale * 1.4426950408889634f, ws, pm, pm + tiles * 32, out, status};
-  if (head_dim == 128) return p.ntw == 1 ? q8_run<128, 1>(a, p, st) : q8_run<128, 2>(a, p, st);
-  return p.ntw == 1 ? q8_run<64, 1>(a, p, st) : q8_run<64, 2>(a, p, st);
+  if (B > 64) return head_dim == 128 ? q8_run_tiles<128, true>(a, p, st) : q8_run_tiles<64, true>(a, p, st);
+  return head_dim == 128 ? q8_run_tiles<128, false>(a, p, st) : q8_run_tiles<64, false>(a, p, st);
 }
 
 }  // namespace trj

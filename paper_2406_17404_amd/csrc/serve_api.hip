@@ -20,6 +20,8 @@ static int check_serve_batch(int B, int T, int max_blocks, int n_blocks) {
     return TRJ_ERR_BAD_SHAPE;
   return TRJ_OK;
 }
+// elements from row to row: 32 rows' offsets stay in 32 bits
+static bool bad_stride(int stride, int64_t least) { return stride < least || (stride & 7) || stride > 1 << 24; }
 static bool on16(const void* p) { return ((uintptr_t)p & 15) == 0; }
 
 extern "C" {
@@ -49,7 +51,7 @@ int32_t kv_append_q8(void* k_pool, void* v_pool, float* k_scale, float* v_scale,
   if (dtype != TRJ_BF16) return TRJ_ERR_BAD_DTYPE;
   TRJ_TRY(check_serve_batch(B, T, max_blocks, n_blocks));
   if (T < 1 || n_layers < 1 || n_layers > 32767 || n_kv_heads < 1 || n_kv_heads > 65535 ||
-      (head_dim != 64 && head_dim != 128) || row_stride < n_kv_heads * (int64_t)head_dim || (row_stride & 7) ||
+      (head_dim != 64 && head_dim != 128) || bad_stride(row_stride, n_kv_heads * (int64_t)head_dim) ||
       (row_layer_stride & 7) || !on16(k_pool) || !on16(v_pool) || !on16(k_rows) || !on16(v_rows))
     return TRJ_ERR_BAD_SHAPE;
   return launch_kv_append_q8(k_pool, v_pool, k_scale, v_scale, k_rows, v_rows, row_stride, row_layer_stride, path,
@@ -85,8 +87,8 @@ int32_t tree_attention_q8(const void* q_rows, int32_t q_stride, const void* k_po
   if (dtype != TRJ_BF16) return TRJ_ERR_BAD_DTYPE;
   TRJ_TRY(check_attention(B, T, n_heads, n_kv_heads, head_dim, max_prefix));
   TRJ_TRY(check_serve_batch(B, T, max_blocks, n_blocks));
-  if (!(scale > 0.f) || !(scale < INFINITY) || q_stride < n_heads * (int64_t)head_dim || (q_stride & 7) ||
-      row_stride < n_kv_heads * (int64_t)head_dim || (row_stride & 7) || !on16(q_rows) || !on16(k_pool) || !on16(v_pool) ||
+  if (!(scale > 0.f) || !(scale < INFINITY) || bad_stride(q_stride, n_heads * (int64_t)head_dim) ||
+      bad_stride(row_stride, n_kv_heads * (int64_t)head_dim) || !on16(q_rows) || !on16(k_pool) || !on16(v_pool) ||
       !on16(k_rows) || !on16(v_rows) || !on16(out))
     return TRJ_ERR_BAD_SHAPE;
   // the scratch starts at the workspace's first multiple of 16
