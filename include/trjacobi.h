@@ -355,7 +355,8 @@ int32_t tr_jacobi_generate(const trj_model_desc* desc, const trj_weights* weight
  * TRJ_ERR_BAD_DTYPE), head_dim 64 or 128.  At most TRJ_SERVE_MAX_SEQS sequences per call.
  *
  * node_off need not cover all T rows, and a sequence may have no rows; rows that no sequence
- * owns are left as they were in every output.  What the device finds wrong with a
+ * owns are left as they were in every output.  No row belongs to two sequences: what is written for
+ * rows that overlap, and for the sequences behind them, is undefined.  What the device finds wrong with a
  * sequence sets status_dev[s] = 1 (else 0) and is stated at each call. */
 #define TRJ_SERVE_MAX_SEQS 4096
 

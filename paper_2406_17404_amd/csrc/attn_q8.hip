@@ -142,119 +142,114 @@ __device__ inline bf16x8 operand(uint32_t a, uint32_t b, float scale) {  // 8 co
   return __builtin_bit_cast(bf16x8, v);
 }
 
-// Running softmax of one tile of 32 queries, a query per lane and its partner lane + 32: products of
+// Running softmax of one tile of 32 queries, a query per lane and its partner lane + 32: products with
 // 32 keys in (times f: log2 scores), -infinity where not visible; bf16 weights out (the B operand of the
-// second product).  Weights are relative to a reference, the largest score when it was last
-// set; it is set again once a score exceeds it by more than SLACK, so weights are at most 2^SLACK, which
-// costs nothing (they are floating-point numbers) and spares most of the rescaling of the sums:
-// with the running maximum itself some query of a tile moves it in nearly every block.
-constexpr float SLACK = 8.f;
+// second product).  Weights are relative to a reference: the largest score when it was last lifted, which
+// happens once a score exceeds it by more than SLACK.  Weights of up to 2^SLACK cost no
+// precision (they are floating-point numbers), and with the running maximum itself some query of a tile
+// would move it, and have the sums rescaled, in nearly every block.
+constexpr float SLACK = 16.f, NO_REFERENCE = -3.4028235e38f;
 struct Softmax {
-  float m = -INFINITY, l = 0.f;
-  __device__ __forceinline__ float take(const f32x16& s, float f, u32x4 (&pk)[2]) {  // the factor of the sums so far
-#pragma clang fp contract(off)
+  float m = NO_REFERENCE, l = 0.f;
+  __device__ __forceinline__ static float largest(const f32x16& s, float f) {
     float mx = s[0];
 #pragma unroll
     for (int v = 1; v < 16; ++v) mx = fmaxf(mx, s[v]);
     const auto both = __builtin_amdgcn_permlane32_swap(__float_as_uint(mx), __float_as_uint(mx), false, false);
-    mx = fmaxf(__uint_as_float(both[0]), __uint_as_float(both[1])) * f;
-    const float top = mx > m + SLACK || m == -INFINITY ? fmaxf(m, mx) : m;
-    const float ref = top == -INFINITY ? 0.f : top;  // nothing visible yet: weights 2^-inf = 0
-    const float alpha = __builtin_amdgcn_exp2f(m - ref);
+    return fmaxf(__uint_as_float(both[0]), __uint_as_float(both[1])) * f;
+  }
+  __device__ __forceinline__ bool too_low(float top) const { return top > m + SLACK; }
+  __device__ __forceinline__ float lift(float top) {  // the factor of the sums so far
+    const float ref = fmaxf(m, top), alpha = __builtin_amdgcn_exp2f(m - ref);
+    l *= alpha;
+    m = ref;
+    return alpha;
+  }
+  __device__ __forceinline__ void weigh(const f32x16& s, float f, u32x4 (&pk)[2]) {
+#pragma clang fp contract(off)
     float p[16], sum = 0.f;
     // product and difference rounded one by one: fused, the rounding of the reference's own product would
     // stay in the exponent, 1 and more for scores beyond 2^24
 #pragma unroll
     for (int v = 0; v < 16; ++v) {
       const float x = s[v] * f;
-      p[v] = __builtin_amdgcn_exp2f(x - ref);
+      p[v] = __builtin_amdgcn_exp2f(x - m);
       sum += p[v];
     }
-    l = l * alpha + sum;
-    m = top;
+    l += sum;
 #pragma unroll
     for (int kg = 0; kg < 2; ++kg)
 #pragma unroll
       for (int e = 0; e < 4; ++e) pk[kg][e] = pack2bf(p[8 * kg + 2 * e], p[8 * kg + 2 * e + 1]);
-    return alpha;
   }
 };
 
 template <int MTV>
 __device__ inline void q8_rescale(f32x16 (&o)[MTV], float alpha) {
-  if (__builtin_amdgcn_ballot_w64(alpha != 1.0f) == 0) return;
 #pragma unroll
-  for (int mt = 0; mt < MTV; ++mt)
+  for (int mt = 0; mt < MTV; ++mt) {
 #pragma unroll
     for (int v = 0; v < 16; ++v) o[mt][v] *= alpha;
-}
-
-// Scheduling of what stands in front of it: after every matrix product N vector instructions.
-template <int PRODUCTS, int N>
-__device__ __forceinline__ void interleave() {
-#pragma unroll
-  for (int i = 0; i < PRODUCTS; ++i) {
-    __builtin_amdgcn_sched_group_barrier(0x8, 1, 0);
-    __builtin_amdgcn_sched_group_barrier(0x2, N, 0);
+    __builtin_amdgcn_sched_barrier(0);  // part after part, for registers
   }
 }
 
 // An infinity or NaN among the tree's V rows: times the weight 0 of a row that does not see it it
-// would be NaN.  Such values are left out of the operand and added here to the rows that do see
-// them.  rows: V row of the block's first key, this K/V head.
-template <int NT, int MTV>
-__device__ __forceinline__ void q8_add_odd_values(f32x16 (&o)[NT][MTV], const u32x4 (&pk)[NT][2], const uint32_t (&sees)[NT],
-                                                  const uint16_t* rows, int stride, int keys) {
-  const int lane = threadIdx.x & 63, hh = lane >> 5;
+// would be NaN.  Such values are left out of the products; what they make of the rows that do see
+// them does not depend on the weights, which are positive: it is added to the results here, rarely, by
+// a walk up the tree.  Queries q0 .. q1 - 1 of a K/V head, columns c0 .. c0 + width - 1 of their results, which
+// have been stored (all threads of the workgroup come).
+__device__ inline void q8_add_odd_values(const Q8Args& a, int r0, int head, int dh, int q0, int q1, int c0, int width) {
+  __builtin_amdgcn_s_waitcnt(0);  // the stores are in the L2
+  __syncthreads();
 #pragma unroll 1
-  for (int key = 0; key < keys; ++key) {
-    const int v = (key >> 3) * 4 + (key & 3);  // the register with its weight, on half (key >> 2) & 1
-    const uint16_t* p = rows + (size_t)key * stride + 4 * hh;
-    float w[NT];
+  for (int u = threadIdx.x; u < (q1 - q0) * (width >> 1); u += blockDim.x) {
+    const int q = q0 + u / (width >> 1), c = c0 + u % (width >> 1) * 2, node = q / a.group;
+    const uint16_t* v = a.v_rows + (size_t)head * dh + c;
+    float sum[2] = {0.f, 0.f};
+    bool odd = false;
+#pragma unroll 1
+    for (int j = node; j >= 0; j = a.parent[r0 + j]) {
 #pragma unroll
-    for (int t = 0; t < NT; ++t) {
-      uint32_t word = 0;
-#pragma unroll
-      for (int i = 0; i < 8; ++i)
-        if (i == v >> 1) word = pk[t][i >> 2][i & 3];
-      word = (uint32_t)__shfl((int)word, (lane & 31) + 32 * ((key >> 2) & 1));
-      w[t] = bf2f((uint16_t)(v & 1 ? word >> 16 : word));
+      for (int e = 0; e < 2; ++e) {
+        const uint16_t x = v[(size_t)(r0 + j) * a.row_stride + e];
+        if ((x & 0x7f80) == 0x7f80) sum[e] += bf2f(x), odd = true;
+      }
     }
-#pragma unroll
-    for (int mt = 0; mt < MTV; ++mt)
-#pragma unroll
-      for (int g = 0; g < 4; ++g)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const uint16_t x = p[32 * mt + 8 * g + i];
-          if ((x & 0x7f80) != 0x7f80) continue;
-#pragma unroll
-          for (int t = 0; t < NT; ++t)
-            if ((sees[t] >> key) & 1) o[t][mt][4 * g + i] += w[t] * bf2f(x);
-        }
+    if (!odd) continue;
+    uint32_t* const at = reinterpret_cast<uint32_t*>(a.out + ((size_t)(r0 + node) * a.n_kv_heads * a.group + head * a.group + q % a.group) * dh + c);
+    const uint32_t was = __hip_atomic_load(at, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);  // from there
+    *at = pack2bf(bf2f((uint16_t)was) + sum[0], bf2f((uint16_t)(was >> 16)) + sum[1]);
   }
 }
 
 // A stream's ring in LDS is its wavefront's own: loads go there without registers (1 KiB each, in
 // order), nobody else reads it and nobody waits.  Slot of 32 keys: K pieces, then V pieces.
 // No branch that the compiler sees: it would copy the accumulators around it.
-// all loads have landed but those of `later` further blocks (P each, up to 3 of them) and EXTRA; MOST, if
-// later is 4
-template <int P, int EXTRA, int MOST>
-__device__ __forceinline__ void wait_blocks(int blocks) {
-  const int later = __builtin_amdgcn_readfirstlane(blocks);
+// All loads have landed but the newest N0 .. N5 for sel 0 .. 5.
+template <int N0, int N1, int N2, int N3, int N4, int N5>
+__device__ __forceinline__ void wait_loads(int sel_) {
+  const int sel = __builtin_amdgcn_readfirstlane(sel_);
   asm volatile(
-      "s_cmp_lt_u32 %0, 1\n\ts_cbranch_scc1 1f\n\t"
-      "s_cmp_lt_u32 %0, 2\n\ts_cbranch_scc1 2f\n\t"
-      "s_cmp_lt_u32 %0, 3\n\ts_cbranch_scc1 3f\n\t"
-      "s_cmp_lt_u32 %0, 4\n\ts_cbranch_scc1 4f\n\t"
-      "s_waitcnt vmcnt(%5)\n\ts_branch 5f\n"
-      "1:\n\ts_waitcnt vmcnt(%1)\n\ts_branch 5f\n"
-      "2:\n\ts_waitcnt vmcnt(%2)\n\ts_branch 5f\n"
-      "3:\n\ts_waitcnt vmcnt(%3)\n\ts_branch 5f\n"
-      "4:\n\ts_waitcnt vmcnt(%4)\n"
-      "5:" ::"s"(later), "n"(EXTRA), "n"(P + EXTRA), "n"(2 * P + EXTRA), "n"(3 * P + EXTRA), "n"(MOST) : "memory", "scc");
+      "s_cmp_gt_u32 %0, 4\n\ts_cbranch_scc1 5f\n\t"
+      "s_cmp_eq_u32 %0, 0\n\ts_cbranch_scc1 0f\n\t"
+      "s_cmp_eq_u32 %0, 1\n\ts_cbranch_scc1 1f\n\t"
+      "s_cmp_eq_u32 %0, 2\n\ts_cbranch_scc1 2f\n\t"
+      "s_cmp_eq_u32 %0, 3\n\ts_cbranch_scc1 3f\n\t"
+      "s_waitcnt vmcnt(%5)\n\ts_branch 6f\n"
+      "0:\n\ts_waitcnt vmcnt(%1)\n\ts_branch 6f\n"
+      "1:\n\ts_waitcnt vmcnt(%2)\n\ts_branch 6f\n"
+      "2:\n\ts_waitcnt vmcnt(%3)\n\ts_branch 6f\n"
+      "3:\n\ts_waitcnt vmcnt(%4)\n\ts_branch 6f\n"
+      "5:\n\ts_waitcnt vmcnt(%6)\n"
+      "6:" ::"s"(sel), "n"(N0), "n"(N1), "n"(N2), "n"(N3), "n"(N4), "n"(N5) : "memory", "scc");
 }
+// How many K and V are on the way behind the one that is waited for, with r blocks behind the current one and
+// rings of d.  They are asked for in the order K 0, V 0, K 1, V 1, ..
+constexpr int at_most(int a, int b) { return a < b ? a : b; }
+constexpr int behind_k0(int r, int d) { return 1 + 2 * at_most(r, d - 1); }  // K of the current block, V up to d - 1 blocks ahead
+constexpr int behind_v(int r, int d) { return 2 * at_most(r, d - 1) + (r >= d); }  // V of it, K up to d blocks ahead
+constexpr int behind_k1(int r, int d) { return r < 1 ? 15 : 1 + 2 * at_most(r - 1, d - 1); }  // K of the next, V up to d ahead
 #pragma clang diagnostic push
 #pragma clang diagnostic ignored "-Winline-asm"
 // P pieces of 1 KiB from base (uniform) to LDS at `lds` (uniform) if `yes`
@@ -297,21 +292,20 @@ __global__ __launch_bounds__(KS * 64, KS / 4) void tree_attn_q8_kernel(Q8Args a)
   static_assert(D >= 2 && KS >= TRJ_N_MAX / 32 && NT <= 2, "a stream's ring takes a block of the tree's rows");
   extern __shared__ __align__(16) uint8_t smem[];  // rings, then parts handed over
   __shared__ float sm_m[KS][NT][32], sm_l[KS][NT][32];
-  const int tid = threadIdx.x, lane = tid & 63, n32 = lane & 31, hh = lane >> 5;
-  const int ks = __builtin_amdgcn_readfirstlane(tid >> 6);
-
   Q8Plan<MANY, QUERIES> plan(a);
   if (blockIdx.x == 0) {  // sequences without work
-    if (!MANY && ks == 0 && lane < a.B && plan.mine.blocks == 0) a.status[plan.id] = plan.mine.nodes < 0;
+    if (!MANY && threadIdx.x < a.B && plan.mine.blocks == 0) a.status[plan.id] = plan.mine.nodes < 0;
     if (MANY)
-      for (int s = tid; s < a.B; s += KS * 64) {
+      for (int s = threadIdx.x; s < a.B; s += KS * 64) {
         const Q8Seq q = q8_seq(a, s);
         if (q.blocks == 0) a.status[s] = q.nodes < 0;
       }
   }
-  for (int x = blockIdx.x;; x += gridDim.x) {
+  {
     Q8Work w;
-    if (!plan.template find<0>(x, w)) return;
+    if (!plan.template find<0>(blockIdx.x, w)) return;
+    const int tid = threadIdx.x;
+    const int lane = tid & 63, n32 = lane & 31, hh = lane >> 5, ks = __builtin_amdgcn_readfirstlane(tid >> 6);
     const Q8Seq seq = w.seq;
     const int splits = w.splits, n = seq.nodes, nq = n * a.group;
     const int head = w.nth % a.n_kv_heads, sp = w.nth / a.n_kv_heads % splits, qg = w.nth / a.n_kv_heads / splits;
@@ -326,7 +320,7 @@ __global__ __launch_bounds__(KS * 64, KS / 4) void tree_attn_q8_kernel(Q8Args a)
           *reinterpret_cast<u32x2*>(a.out + (size_t)(seq.r0 + i / width) * row_len + head * a.group * DH + i % width * 4) = z;
         if (head == 0 && tid == 0) a.status[w.s] = 1;
       }
-      continue;
+      return;
     }
     const int32_t* table = a.block_table + (size_t)w.s * a.max_blocks;
     const int cached = seq.cached();
@@ -341,26 +335,77 @@ __global__ __launch_bounds__(KS * 64, KS / 4) void tree_attn_q8_kernel(Q8Args a)
     auto look_up = [&](int i0) {
       const int i = i0 + lane;
       ids = i < mine ? table[b0 + ks + i * KS] : 0;
+    };
+    // Then no load that the compiler knows of is on the way: it would wait for it later, and with it for the
+    // rings, which it does not know.
+    auto look_up_scales = [&]() {
       const bool ok = (unsigned)ids < (unsigned)a.n_blocks;
       ids = ok ? ids : 0;
       ksc = ok ? a.k_scale[plane + ids] : NAN;  // a page that is not there makes its rows NaN
       vsc = a.v_scale[plane + ids];
+      __builtin_amdgcn_s_waitcnt(0x0f70);  // vmcnt(0)
     };
-    if (mine > 0) look_up(0);
+    look_up(0);
     // queries: tile t, column n32; step 2j + i of the product: columns 32j + 16hh + 8i ..
-    int node[NT], qhead[NT];
-    bool live[NT];
+    // (worked out where they are used: they would take registers over the whole walk)
+    struct Query {
+      int node, head;
+      bool live;
+    };
+    auto query = [&](int t) {
+      int l = threadIdx.x & 31;
+      asm volatile("" : "+v"(l));
+      const int qi = (qg * NT + t) * 32 + l, qc = min(qi, nq - 1);
+      return Query{qc / a.group, head * a.group + qc % a.group, qi < nq};
+    };
     bf16x8 qreg[NT][2 * MTV];
 #pragma unroll
     for (int t = 0; t < NT; ++t) {
-      const int qi = (qg * NT + t) * 32 + n32, qc = min(qi, nq - 1);
-      node[t] = qc / a.group;
-      qhead[t] = head * a.group + qc % a.group;
-      live[t] = qi < nq;
-      const uint16_t* qp = a.q + (size_t)(seq.r0 + node[t]) * a.q_stride + (size_t)qhead[t] * DH + hh * 16;
+      const Query u = query(t);
+      const uint16_t* qp = a.q + (size_t)(seq.r0 + u.node) * a.q_stride + (size_t)u.head * DH + hh * 16;
 #pragma unroll
       for (int j = 0; j < 2 * MTV; ++j) qreg[t][j] = *reinterpret_cast<const bf16x8*>(qp + 32 * (j >> 1) + 8 * (j & 1));
     }
+    // The tree's own rows of this range go to LDS, into the order of the operands, each block into the ring of
+    // the stream that takes it, which asks for its cached blocks later.  A thread moves two rows, 8 columns.
+    const int t0 = max(b0, cached), tree = max(0, b1 - t0);  // blocks
+    const int tb = (ks - (t0 - b0) % KS + KS) % KS;          // this stream's of them
+    constexpr int UNITS = TRJ_N_MAX / 32 * 16 * CH / (KS * 64);
+    bool odd = false;
+    if (tree > 0) {
+      u32x4 raw[UNITS][4];
+#pragma unroll
+      for (int i = 0; i < UNITS; ++i) {
+        const int u = tid + i * KS * 64, b = u / (16 * CH), rr = u / CH % 16 * 2, c = u % CH, key = (t0 + b - cached) * 32 + rr;
+        if (b >= tree) continue;
+        const size_t lo = (size_t)(seq.r0 + min(key, n - 1)) * a.row_stride + (size_t)head * DH + 8 * c;
+        const size_t hi = (size_t)(seq.r0 + min(key + 1, n - 1)) * a.row_stride + (size_t)head * DH + 8 * c;
+        raw[i][0] = *reinterpret_cast<const u32x4*>(a.k_rows + lo);
+        raw[i][1] = *reinterpret_cast<const u32x4*>(a.k_rows + hi);
+        raw[i][2] = *reinterpret_cast<const u32x4*>(a.v_rows + lo);
+        raw[i][3] = *reinterpret_cast<const u32x4*>(a.v_rows + hi);
+      }
+#pragma unroll
+      for (int i = 0; i < UNITS; ++i) {
+        const int u = tid + i * KS * 64, b = u / (16 * CH), rr = u / CH % 16 * 2, c = u % CH;
+        if (b >= tree) continue;
+        uint8_t* const kt = smem + (size_t)((t0 - b0 + b) % KS) * D * SLOT;
+        u32x4* const kd = reinterpret_cast<u32x4*>(kt + ((c >> 2) * 2 + (c & 1)) * 1024 + ((c >> 1) & 1) * 512 + rr * 16);
+        kd[0] = raw[i][0];
+        kd[1] = raw[i][1];
+        uint32_t* const vd = reinterpret_cast<uint32_t*>(kt + TILE + (c >> 2) * 2048 + (rr >> 4) * 1024 + ((rr >> 2) & 1) * 512 +
+                                                         (c & 3) * 128 + ((rr >> 3) & 1) * 8 + (rr & 3) * 2);
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+          const uint32_t v0 = raw[i][2][k >> 1], v1 = raw[i][3][k >> 1];
+          uint32_t x = k & 1 ? v0 >> 16 : v0 & 0xffffu, y = k & 1 ? v1 & 0xffff0000u : v1 << 16;
+          if ((x & 0x7f80u) == 0x7f80u) odd = true, x = 0;
+          if ((y & 0x7f800000u) == 0x7f800000u) odd = true, y = 0;
+          vd[4 * k] = x | y;
+        }
+      }
+    }
+    look_up_scales();
     f32x16 o[NT][MTV];
     Softmax sm[NT];
 #pragma unroll
@@ -370,6 +415,20 @@ __global__ __launch_bounds__(KS * 64, KS / 4) void tree_attn_q8_kernel(Q8Args a)
 #pragma unroll
         for (int v = 0; v < 16; ++v) o[t][mt][v] = 0.f;
 
+    // With two tiles of heads of 128 queries and sums fill the accumulation registers, from where the products read
+    // and write them; said at the loop's ends, or the compiler moves all of them there and back.
+    auto keep = [&](auto& x) {
+      if constexpr (NT * MTV > 4) asm volatile("" : "+a"(x));
+    };
+    auto keep_all = [&]() {
+#pragma unroll
+      for (int t = 0; t < NT; ++t) {
+#pragma unroll
+        for (int j = 0; j < 2 * MTV; ++j) keep(qreg[t][j]);
+#pragma unroll
+        for (int mt = 0; mt < MTV; ++mt) keep(o[t][mt]);
+      }
+    };
     const uint32_t ring = __builtin_amdgcn_readfirstlane((uint32_t)(size_t)(__attribute__((address_space(3))) uint8_t*)smem + ks * D * SLOT);
     const u32x4* const ring_r = reinterpret_cast<const u32x4*>(smem + (size_t)ks * D * SLOT) + lane;
     auto ask = [&](const uint8_t* pool, int i, int part, int yes) {  // block i of this stream, K (0) or V (1)
@@ -381,6 +440,13 @@ __global__ __launch_bounds__(KS * 64, KS / 4) void tree_attn_q8_kernel(Q8Args a)
 #pragma unroll
       for (int j = 0; j < P; ++j) kraw[j] = ring_r[(i % D) * (SLOT / 16) + j * 64];
     };
+    f32x16 sacc[NT];  // products of the queries with a block's keys
+    auto scores = [&](int t, const bf16x8 (&kop)[2 * MTV], f32x16& to) {
+#pragma unroll
+      for (int v = 0; v < 16; ++v) to[v] = 0.f;
+#pragma unroll
+      for (int j = 0; j < 2 * MTV; ++j) to = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kop[j], qreg[t][j], to, 0, 0, 0);
+    };
     auto values = [&](int t, const bf16x8 (&vop)[2 * MTV], const u32x4 (&pk)[2]) {
 #pragma unroll
       for (int mt = 0; mt < MTV; ++mt)
@@ -388,70 +454,13 @@ __global__ __launch_bounds__(KS * 64, KS / 4) void tree_attn_q8_kernel(Q8Args a)
         for (int kg = 0; kg < 2; ++kg)
           o[t][mt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vop[2 * mt + kg], __builtin_bit_cast(bf16x8, pk[kg]), o[t][mt], 0, 0, 0);
     };
-    // Block i of those up to c1; its K is in kraw, its V and up to D - 1 blocks are on the way.  LAST: `rest` of its
-    // 32 keys exist.  With two tiles the products of one run while the softmax of the other does.
-    auto block = [&](int i, int c1, auto last_c, int rest) {
-      constexpr bool LAST = decltype(last_c)::value;
-      const float kscale = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(ksc), i & 63));
-      const float vscale = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(vsc), i & 63));
-      const float f = kscale == kscale ? a.scale_log2e : NAN;  // a page that is not there
-      const int later = min(D - 1, c1 - 1 - i);
-      const bool more = i + D < c1;
-      bf16x8 kop[2 * MTV], vop[2 * MTV];
+    auto operands = [&](bf16x8 (&op)[2 * MTV], const u32x4 (&raw)[P], float scale) {
 #pragma unroll
-      for (int j = 0; j < 2 * MTV; ++j) kop[j] = operand(kraw[j >> 1][2 * (j & 1)], kraw[j >> 1][2 * (j & 1) + 1], kscale);
-      f32x16 sacc[NT];
-      auto scores = [&](int t) {
-#pragma unroll
-        for (int v = 0; v < 16; ++v) sacc[t][v] = 0.f;
-#pragma unroll
-        for (int j = 0; j < 2 * MTV; ++j) sacc[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kop[j], qreg[t][j], sacc[t], 0, 0, 0);
-      };
-      auto hide = [&](int t) {
-        if (LAST)
-#pragma unroll
-          for (int v = 0; v < 16; ++v)
-            if (8 * (v >> 2) + 4 * hh + (v & 3) >= rest) sacc[t][v] = -INFINITY;
-      };
-      ask(a.k_pool, i + D, 0, more);
-      scores(0);
-      // V: behind it the later blocks and, if asked for, K of block i + D
-      wait_blocks<2 * P, 0, 2 * P * (D - 1) + P>(more ? 4 : later);
-      u32x4 vraw[P];
-#pragma unroll
-      for (int j = 0; j < P; ++j) vraw[j] = ring_r[(i % D) * (SLOT / 16) + (P + j) * 64];
-      u32x4 pk[NT][2];
-      float alpha[NT];
-      if constexpr (NT == 2) scores(1);
-      hide(0);
-      alpha[0] = sm[0].take(sacc[0], f, pk[0]);
-      if (LAST) {
-        // slots past the end may hold anything: their weights are 0, their values have to be numbers
-#pragma unroll
-        for (int d = 0; d < 4; ++d) {
-          const int keep = min(max(rest - 8 * d - 4 * hh, 0), 4);
-          const uint32_t mask = keep == 4 ? 0xffffffffu : (1u << (8 * keep)) - 1u;
-#pragma unroll
-          for (int j = 0; j < P; ++j) vraw[j][d] &= mask;
-        }
-      }
-#pragma unroll
-      for (int j = 0; j < 2 * MTV; ++j) vop[j] = operand(vraw[j >> 1][2 * (j & 1)], vraw[j >> 1][2 * (j & 1) + 1], vscale);
-      if constexpr (NT == 2) interleave<8, 10>();
-      ask(a.v_pool, i + D, 1, more);
-      q8_rescale<MTV>(o[0], alpha[0]);
-      if constexpr (NT == 2) {
-        values(0, vop, pk[0]);
-        hide(1);
-        alpha[1] = sm[1].take(sacc[1], f, pk[1]);
-        interleave<2 * MTV, 10>();
-        q8_rescale<MTV>(o[1], alpha[1]);
-      }
-      // K of the next block (behind the last one: whatever is there)
-      wait_blocks<2 * P, P, 2 * P * (D - 1) + P>(more ? 4 : max(later - 1, 0));
-      read_k(i + 1);
-      values(NT - 1, vop, pk[NT - 1]);
+      for (int j = 0; j < 2 * MTV; ++j) op[j] = operand(raw[j >> 1][2 * (j & 1)], raw[j >> 1][2 * (j & 1) + 1], scale);
     };
+    auto scale_of = [&](float of, int i) { return __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(of), i & 63)); };
+    // (a page that is not there makes every weight NaN)
+    auto factor = [&](int i) { const float k = scale_of(ksc, i); return k == k ? a.scale_log2e : NAN; };
     auto fill = [&](int c0, int c1) {
 #pragma unroll
       for (int i = 0; i < D; ++i) {
@@ -459,33 +468,8 @@ __global__ __launch_bounds__(KS * 64, KS / 4) void tree_attn_q8_kernel(Q8Args a)
         ask(a.v_pool, c0 + i, 1, c0 + i < c1);
       }
     };
-    // ---- the tree's own rows first: they need no table, and the cached blocks come meanwhile.  Everybody puts
-    // them into the order of the operands, each block into the ring of the stream that takes it, which asks for
-    // its cached blocks later.
-    const int t0 = max(b0, cached), tree = max(0, b1 - t0);  // blocks
-    const int tb = (ks - (t0 - b0) % KS + KS) % KS;          // this stream's of them
+    // ---- the tree's own rows first, while the cached blocks come
     if (tb >= tree) fill(0, min(mine, 64));
-    bool odd = false;
-    for (int u = tid; u < tree * 16 * CH; u += KS * 64) {  // two rows, 8 columns
-      const int b = u / (16 * CH), r = u / CH % 16 * 2, c = u % CH, key = (t0 + b - cached) * 32 + r;
-      const size_t lo = (size_t)(seq.r0 + min(key, n - 1)) * a.row_stride + (size_t)head * DH + 8 * c;
-      const size_t hi = (size_t)(seq.r0 + min(key + 1, n - 1)) * a.row_stride + (size_t)head * DH + 8 * c;
-      const u32x4 k0 = *reinterpret_cast<const u32x4*>(a.k_rows + lo), k1 = *reinterpret_cast<const u32x4*>(a.k_rows + hi);
-      const u32x4 v0 = *reinterpret_cast<const u32x4*>(a.v_rows + lo), v1 = *reinterpret_cast<const u32x4*>(a.v_rows + hi);
-      uint8_t* const kt = smem + (size_t)((t0 - b0 + b) % KS) * D * SLOT;
-      u32x4* const kd = reinterpret_cast<u32x4*>(kt + ((c >> 2) * 2 + (c & 1)) * 1024 + ((c >> 1) & 1) * 512 + r * 16);
-      kd[0] = k0;
-      kd[1] = k1;
-      uint32_t* const vd = reinterpret_cast<uint32_t*>(kt + TILE + (c >> 2) * 2048 + (r >> 4) * 1024 + ((r >> 2) & 1) * 512 +
-                                                       (c & 3) * 128 + ((r >> 3) & 1) * 8 + (r & 3) * 2);
-#pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        uint32_t x = i & 1 ? v0[i >> 1] >> 16 : v0[i >> 1] & 0xffffu, y = i & 1 ? v1[i >> 1] & 0xffff0000u : v1[i >> 1] << 16;
-        if ((x & 0x7f80u) == 0x7f80u) odd = true, x = 0;
-        if ((y & 0x7f800000u) == 0x7f800000u) odd = true, y = 0;
-        vd[4 * i] = x | y;
-      }
-    }
     bool any_odd = false;
     if (tree > 0) any_odd = __syncthreads_or(odd);
     if (tb < tree) {
@@ -493,10 +477,15 @@ __global__ __launch_bounds__(KS * 64, KS / 4) void tree_attn_q8_kernel(Q8Args a)
         const TreeBits bits = tree_bits(par, n);
         const int key0 = (t0 + tb - cached) * 32;
         uint32_t sees[NT];
+        int word[2];  // of the nodes' paths, this block's
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+          word[h] = key0 == 0 ? bits.w[0][h] : key0 == 32 ? bits.w[1][h] : key0 == 64 ? bits.w[2][h] : bits.w[3][h];
 #pragma unroll
         for (int t = 0; t < NT; ++t) {
-          const int lo = from_node(key0 < 64 ? (key0 ? bits.w[1] : bits.w[0]) : (key0 == 64 ? bits.w[2] : bits.w[3]), node[t]);
-          sees[t] = live[t] ? (uint32_t)lo : 0u;
+          const Query u = query(t);
+          const int lo = from_node(word, u.node);
+          sees[t] = u.live ? (uint32_t)lo : 0u;
         }
         const u32x4* const kt = reinterpret_cast<const u32x4*>(smem + (size_t)ks * D * SLOT) + lane;
         f32x16 sacc[NT];
@@ -516,7 +505,8 @@ __global__ __launch_bounds__(KS * 64, KS / 4) void tree_attn_q8_kernel(Q8Args a)
 #pragma unroll
           for (int v = 0; v < 16; ++v)
             if (!((sees[t] >> (8 * (v >> 2) + 4 * hh + (v & 3))) & 1)) sacc[t][v] = -INFINITY;
-          q8_rescale<MTV>(o[t], sm[t].take(sacc[t], a.scale_log2e, pk[t]));
+          q8_rescale<MTV>(o[t], sm[t].lift(Softmax::largest(sacc[t], a.scale_log2e)));
+          sm[t].weigh(sacc[t], a.scale_log2e, pk[t]);
         }
 #pragma unroll
         for (int mt = 0; mt < MTV; ++mt)
@@ -527,9 +517,6 @@ __global__ __launch_bounds__(KS * 64, KS / 4) void tree_attn_q8_kernel(Q8Args a)
             for (int t = 0; t < NT; ++t)
               o[t][mt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vop, __builtin_bit_cast(bf16x8, pk[t][kg]), o[t][mt], 0, 0, 0);
           }
-        if (any_odd)
-          q8_add_odd_values(o, pk, sees, a.v_rows + (size_t)(seq.r0 + key0) * a.row_stride + (size_t)head * DH, a.row_stride,
-                            min(32, n - key0));
       }
       fill(0, min(mine, 64));
     }
@@ -539,14 +526,84 @@ __global__ __launch_bounds__(KS * 64, KS / 4) void tree_attn_q8_kernel(Q8Args a)
       const int c1 = min(mine, c0 + 64);
       if (c0 > 0) {
         look_up(c0);
+        look_up_scales();
         fill(c0, c1);
       }
-      const int rest = seq.L - (b0 + ks + (c1 - 1) * KS) * 32;
-      const int whole = rest < 32 ? c1 - 1 : c1;
-      wait_blocks<2 * P, P, 0>(min(D - 1, c1 - 1 - c0));
+      const int rest = seq.L - (b0 + ks + (c1 - 1) * KS) * 32;  // keys of the last block, if fewer than 32
+#define Q8_WAIT(behind, r) \
+  wait_loads<P * behind(0, D), P * behind(1, D), P * behind(2, D), P * behind(3, D), P * behind(4, D), P * behind(5, D)>(r)
+      // K of a block is in registers when its turn begins.  With two tiles the softmax of one runs while the matrix
+      // units work on the other.  The loop has one way out, in front of a reference that has to be lifted: a
+      // condition around the accumulators inside it would have them copied every time.
+      bf16x8 kop[2 * MTV], vop[2 * MTV];
+      u32x4 pk[NT][2];
+      float top[NT], f;
+      Q8_WAIT(behind_k0, c1 - 1 - c0);
       read_k(c0);
-      for (int i = c0; i < whole; ++i) block(i, c1, std::false_type{}, 32);
-      if (whole < c1) block(whole, c1, std::true_type{}, rest);
+      keep_all();
+      int i = c0;
+      for (;;) {
+        bool last;
+        for (;; ++i) {
+          f = factor(i);
+          operands(kop, kraw, scale_of(ksc, i));
+#pragma unroll
+          for (int t = 0; t < NT; ++t) scores(t, kop, sacc[t]);
+#pragma unroll
+          for (int t = 0; t < NT; ++t) top[t] = Softmax::largest(sacc[t], f);
+          last = i == c1 - 1;
+          bool low = last || sm[0].too_low(top[0]);
+          if constexpr (NT == 2) low = low || sm[1].too_low(top[1]);
+          if (__ballot(low)) break;
+          ask(a.k_pool, i + D, 0, i + D < c1);
+          sm[0].weigh(sacc[0], f, pk[0]);
+          Q8_WAIT(behind_v, c1 - 1 - i);
+          u32x4 vraw[P];
+#pragma unroll
+          for (int j = 0; j < P; ++j) vraw[j] = ring_r[(i % D) * (SLOT / 16) + (P + j) * 64];
+          operands(vop, vraw, scale_of(vsc, i));
+          ask(a.v_pool, i + D, 1, i + D < c1);
+          if constexpr (NT == 2) {
+            values(0, vop, pk[0]);
+            sm[1].weigh(sacc[1], f, pk[1]);
+          }
+          Q8_WAIT(behind_k1, c1 - 1 - i);
+          read_k(i + 1);  // (behind the last one whatever is there)
+          values(NT - 1, vop, pk[NT - 1]);
+        }
+        keep_all();
+        if (last) {
+#pragma unroll
+          for (int t = 0; t < NT; ++t) {
+#pragma unroll
+            for (int v = 0; v < 16; ++v)
+              if (8 * (v >> 2) + 4 * hh + (v & 3) >= rest) sacc[t][v] = -INFINITY;
+            top[t] = Softmax::largest(sacc[t], f);
+          }
+        }
+#pragma unroll
+        for (int t = 0; t < NT; ++t) q8_rescale<MTV>(o[t], sm[t].lift(top[t]));
+        keep_all();
+        if (last) break;
+      }
+      wait_loads<0, 0, 0, 0, 0, 0>(0);
+      u32x4 vraw[P];
+#pragma unroll
+      for (int j = 0; j < P; ++j) vraw[j] = ring_r[(i % D) * (SLOT / 16) + (P + j) * 64];
+      // slots past the end may hold anything: their weights are 0, their values have to be numbers
+#pragma unroll
+      for (int d = 0; d < 4; ++d) {
+        const int keep = min(max(rest - 8 * d - 4 * hh, 0), 4);
+        const uint32_t mask = keep == 4 ? 0xffffffffu : (1u << (8 * keep)) - 1u;
+#pragma unroll
+        for (int j = 0; j < P; ++j) vraw[j][d] &= mask;
+      }
+      operands(vop, vraw, scale_of(vsc, i));
+#pragma unroll
+      for (int t = 0; t < NT; ++t) {
+        sm[t].weigh(sacc[t], f, pk[t]);
+        values(t, vop, pk[t]);
+      }
     }
     if (first && head == 0) {  // the verdict on the sequence's pages
       bool bad = false;
@@ -571,13 +628,12 @@ __global__ __launch_bounds__(KS * 64, KS / 4) void tree_attn_q8_kernel(Q8Args a)
 #pragma unroll
     for (int t = 0; t < NT; ++t) {  // tile by tile: all at once do not fit LDS
       if (t > 0) __syncthreads();
-      float mg = -INFINITY, lg = 0.f;
+      float mg = NO_REFERENCE, lg = 0.f;
 #pragma unroll
       for (int k = 0; k < KS; ++k) mg = fmaxf(mg, sm_m[k][t][n32]);
-      const float ref = mg == -INFINITY ? 0.f : mg;
 #pragma unroll
-      for (int k = 0; k < KS; ++k) lg += sm_l[k][t][n32] * __builtin_amdgcn_exp2f(sm_m[k][t][n32] - ref);
-      const float f = __builtin_amdgcn_exp2f(sm[t].m - ref);
+      for (int k = 0; k < KS; ++k) lg += sm_l[k][t][n32] * __builtin_amdgcn_exp2f(sm_m[k][t][n32] - mg);
+      const float f = __builtin_amdgcn_exp2f(sm[t].m - mg);
 #pragma unroll
       for (int mt = 0; mt < MTV; ++mt) {
 #pragma unroll
@@ -596,7 +652,7 @@ __global__ __launch_bounds__(KS * 64, KS / 4) void tree_attn_q8_kernel(Q8Args a)
       const size_t tile = (size_t)part * NT + t;
       if (splits > 1 && ks == 0 && hh == 0) {
         a.pm[tile * 32 + n32] = mg;
-        a.pl[tile * 32 + n32] = lg;
+        a.pl[tile * 32 + n32] = any_odd ? -lg : lg;  // (a sum of weights is not negative)
       }
       const float inv = 1.0f / lg;
 #pragma unroll
@@ -608,8 +664,9 @@ __global__ __launch_bounds__(KS * 64, KS / 4) void tree_attn_q8_kernel(Q8Args a)
 #pragma unroll
           for (int v = 0; v < 16; ++v) o[t][mt][v] += src[(k * 16 + v) * 64];
         if (splits == 1) {
-          if (live[t]) {
-            uint16_t* dst = a.out + (size_t)(seq.r0 + node[t]) * row_len + (size_t)qhead[t] * DH + 32 * mt + 4 * hh;
+          const Query u = query(t);
+          if (u.live) {
+            uint16_t* dst = a.out + (size_t)(seq.r0 + u.node) * row_len + (size_t)u.head * DH + 32 * mt + 4 * hh;
 #pragma unroll
             for (int g = 0; g < 4; ++g) {
               const u32x2 v = {pack2bf(o[t][mt][4 * g] * inv, o[t][mt][4 * g + 1] * inv),
@@ -624,18 +681,18 @@ __global__ __launch_bounds__(KS * 64, KS / 4) void tree_attn_q8_kernel(Q8Args a)
         }
       }
     }
-    __syncthreads();  // LDS is free again
+    if (any_odd && splits == 1) q8_add_odd_values(a, seq.r0, head, DH, qg * QUERIES, min(nq, (qg + 1) * QUERIES), 0, DH);
   }
 }
 
 // Merges the partials of a (sequence, query tile, K/V head) in split order, one 32-column part of the
 // rows per workgroup.  Thread (lane, g, h) adds the accumulator registers 4g .. 4g+3 that lane held, over
-// every fourth split from h on; the four sums are added through LDS.  All loads of a batch are asked
-// for together (clamped, never predicated): one after the other 32 splits took 35 us.
+// every fourth split from h on, with a running maximum; the four sums are joined through LDS.  All loads of a
+// batch are asked for together (clamped, never predicated): one after the other 32 splits took 35 us.
 template <int DH, int NT, bool MANY>
 __global__ __launch_bounds__(1024) void attn_q8_combine_kernel(Q8Args a) {
   constexpr int MTV = DH / 32, PART = 16 * 64, BATCH = 4;
-  __shared__ float sm_m[32][33], sm_l[4][32];
+  __shared__ float sm_m[4][32], sm_l[4][32];
   __shared__ f32x4 sm_o[3][256];
   const int tid = threadIdx.x, lane = tid & 63, n32 = lane & 31, hh = lane >> 5, g = (tid >> 6) & 3, h = tid >> 8;
   Q8Plan<MANY, 32 * NT> plan(a);
@@ -648,53 +705,65 @@ __global__ __launch_bounds__(1024) void attn_q8_combine_kernel(Q8Args a) {
     const int nq = seq.nodes * a.group, qi = (qg * NT + nt) * 32 + n32;
     if ((qg * NT + nt) * 32 >= nq) continue;
     if (w.part0 + (qg + 1) * splits * a.n_kv_heads > a.max_parts) continue;  // see there
-    const bool valid = tree_valid(load_parents(a.parent, seq.r0, seq.nodes), seq.nodes);  // uniform
-    auto at = [&](int sp) { return (size_t)(w.part0 + (qg * splits + sp) * a.n_kv_heads + head) * NT + nt; };
-    // largest maximum: thread (row of 32 splits, query)
-    float m = -INFINITY;
-    for (int sp = tid >> 5; sp < splits; sp += 32) m = fmaxf(m, a.pm[at(sp) * 32 + (tid & 31)]);
-    sm_m[tid >> 5][tid & 31] = m;
-    __syncthreads();
-    m = -INFINITY;
-#pragma unroll
-    for (int k = 0; k < 32; ++k) m = fmaxf(m, sm_m[k][n32]);
-    const float ref = m == -INFINITY ? 0.f : m;
-    float l = 0.f;
+    const TreeParents par = load_parents(a.parent, seq.r0, seq.nodes);
+    float m = NO_REFERENCE, l = 0.f;
+    bool odd = false;
     f32x4 o = {0, 0, 0, 0};
     for (int s0 = h; s0 < splits; s0 += 4 * BATCH) {
       float pm[BATCH], pl[BATCH], po[BATCH][4];
 #pragma unroll
       for (int k = 0; k < BATCH; ++k) {
-        const size_t p = at(min(s0 + 4 * k, splits - 1));
+        const int sp = min(s0 + 4 * k, splits - 1);
+        const size_t p = (size_t)(w.part0 + (qg * splits + sp) * a.n_kv_heads + head) * NT + nt;
         pm[k] = a.pm[p * 32 + n32];
         pl[k] = a.pl[p * 32 + n32];
         const float* img = a.po + p * MTV * PART + mt * PART + 4 * g * 64 + lane;
 #pragma unroll
         for (int v = 0; v < 4; ++v) po[k][v] = img[v * 64];
       }
+      float top = m;
+#pragma unroll
+      for (int k = 0; k < BATCH; ++k) top = fmaxf(top, pm[k]);
+      const float alpha = __builtin_amdgcn_exp2f(m - top);
+      m = top;
+      l *= alpha;
+      o *= alpha;
 #pragma unroll
       for (int k = 0; k < BATCH; ++k) {
         if (s0 + 4 * k >= splits) break;
-        const float f = __builtin_amdgcn_exp2f(pm[k] - ref);
-        l += f * pl[k];
+        const float f = __builtin_amdgcn_exp2f(pm[k] - m);
+        odd = odd || (__float_as_uint(pl[k]) >> 31) != 0;
+        l += f * fabsf(pl[k]);
 #pragma unroll
         for (int v = 0; v < 4; ++v) o[v] += f * po[k][v];
       }
     }
     if (h > 0) sm_o[h - 1][tid & 255] = o;
-    if (g == 0 && hh == 0) sm_l[h][n32] = l;
-    __syncthreads();
-    if (h == 0 && valid && qi < nq) {  // (rows of a malformed tree are zeros already)
-      l = 0.f;
+    if (g == 0 && hh == 0) sm_m[h][n32] = m, sm_l[h][n32] = l;
+    const bool valid = tree_valid(par, seq.nodes);  // else its rows are zeros already
+    const bool any_odd = __syncthreads_or(odd);
+    if (h == 0 && valid && qi < nq) {
+      float top = m;
 #pragma unroll
-      for (int k = 0; k < 4; ++k) l += sm_l[k][n32];
+      for (int k = 1; k < 4; ++k) top = fmaxf(top, sm_m[k][n32]);
+      const float alpha = __builtin_amdgcn_exp2f(m - top);
+      l *= alpha;
+      o *= alpha;
 #pragma unroll
-      for (int k = 0; k < 3; ++k) o += sm_o[k][tid];
+      for (int k = 1; k < 4; ++k) {
+        const float f = __builtin_amdgcn_exp2f(sm_m[k][n32] - top);
+        l += f * sm_l[k][n32];
+        o += f * sm_o[k - 1][tid];
+      }
       const float inv = 1.0f / l;
       const int node = qi / a.group, qhead = head * a.group + qi % a.group;
       uint16_t* dst = a.out + ((size_t)(seq.r0 + node) * a.n_kv_heads * a.group + qhead) * DH + 32 * mt + 4 * hh + 8 * g;
       const u32x2 v = {pack2bf(o[0] * inv, o[1] * inv), pack2bf(o[2] * inv, o[3] * inv)};
       *reinterpret_cast<u32x2*>(dst) = v;
+    }
+    if (any_odd && valid) {
+      const int q0 = (qg * NT + nt) * 32;
+      q8_add_odd_values(a, seq.r0, head, DH, q0, min(nq, q0 + 32), mt * 32, 32);
     }
     __syncthreads();  // LDS is free again
   }
@@ -716,7 +785,7 @@ static Q8Launch q8_launch(int B, int T, int group, int n_kv_heads, int max_prefi
   const long parts = most <= p.min_blocks ? 0 : std::min(2l * p.target, items * ((most + p.min_blocks - 1) / p.min_blocks));
   p.max_parts = (int)parts;
   p.grid = (int)std::min(items + (parts ? p.target : 0), 1l << 20);
-  p.tiles = (int)std::min(parts * p.ntw, 256l);
+  p.tiles = (int)std::min(std::min(parts, items) * p.ntw, 64l);
   return p;
 }
 size_t attn_q8_ws_floats(int B, int T, int group, int n_kv_heads, int head_dim, int max_prefix) {
