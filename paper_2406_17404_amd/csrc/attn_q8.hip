@@ -33,8 +33,6 @@ struct Q8Args {
   const float *k_scale, *v_scale;
   const int32_t *parent, *node_off, *block_table, *prefix_len;
   int q_stride, row_stride, max_blocks, B, T, n_kv_heads, group, n_blocks, max_prefix;
-  int target;  // workgroups aimed at
-  int min_blocks;  // of a split, at least
   int max_parts;   // images that the workspace holds
   float scale_log2e;
   float *po, *pm, *pl;  // un-normalised partials: [part][tile] images of the accumulators, maxima and sums of 32 queries
@@ -67,8 +65,14 @@ template <class T>
 __device__ inline T lane_value(T v, int lane) { return (T)__builtin_amdgcn_readlane((int)v, lane); }
 
 // The plan, the same on every wavefront of every workgroup: a split has `chunk` blocks at most, of one
-// sequence evenly many.  Sequences come longest first (up to 64 of them; index order beyond), so that what
-// starts last is short.
+// sequence evenly many.  32 sizes are weighed at once, one per lane: the longest sequence in 1 .. 32 splits.
+//   cost = rounds of workgroups * (START + blocks of one) + MERGE if anything is split
+// in times that a compute unit takes for a block of its own (0.33 us): a workgroup's way to its first block and
+// from its last to the result takes 8 us, the merge launch 5.
+// Sequences come longest first, so that what starts last is short.  Beyond 64 sequences neither is done:
+// index order, and chunks of an even share.
+constexpr float START = 24.f, MERGE = 16.f, RESIDENT = 256.f;  // one workgroup per compute unit at a time
+constexpr int MAX_PARTS = 512;  // partials that a call may leave to the merge
 struct Q8Work {  // of an item
   Q8Seq seq;
   int s, nth, splits, part0;  // nth item of sequence s; its first partial
@@ -81,28 +85,62 @@ struct Q8Plan {
 
   __device__ inline explicit Q8Plan(const Q8Args& args) : a(args) {
     const int lane = threadIdx.x & 63;
-    long work = 0;
+    float work = 0.f;
     for (int s0 = 0; s0 < (MANY ? a.B : 1); s0 += 64) {
       mine = q8_seq(a, s0 + lane);
-      long w = (long)q8_groups(a, mine, QUERIES) * mine.blocks;
-#pragma unroll
-      for (int o = 32; o > 0; o >>= 1) w += __shfl_xor(w, o);
-      work += w;
+      if (!MANY && a.B == 1) break;
+      work += wave_sum((float)q8_groups(a, mine, QUERIES) * (float)mine.blocks);
     }
     work *= a.n_kv_heads;
-    chunk = __builtin_amdgcn_readfirstlane((int)max((work + a.target - 1) / a.target, (long)a.min_blocks));
     id = lane;
-    if (!MANY && a.B > 1) {  // longest first
+    if (MANY) {  // (a split sequence has at most twice its share of parts)
+      chunk = (int)fminf(fmaxf(ceilf(work * (1.0001f * 2 / MAX_PARTS)), 16.f), 1e9f);
+      return;
+    }
+    int longest = 0;
+    if (a.B == 1) {
+      longest = lane_value(mine.blocks, 0);
+    } else {  // longest first
       int rank = 0;
-      for (int t = 0; t < a.B; ++t) {
-        const int b = lane_value(mine.blocks, t);
-        rank += b > mine.blocks || (b == mine.blocks && t < lane);
-      }
+      for (int t0 = 0; t0 < a.B; t0 += 8)  // (lanes behind the last sequence have no blocks)
+#pragma unroll
+        for (int t = t0; t < t0 + 8; ++t) {
+          const int b = lane_value(mine.blocks, t);
+          rank += b > mine.blocks || (b == mine.blocks && t < lane);
+        }
       rank = lane < a.B ? rank : lane;
       auto to = [&](int v) { return __builtin_amdgcn_ds_permute(rank << 2, v); };
       mine = Q8Seq{to(mine.r0), to(mine.nodes), to(mine.L), to(mine.blocks)};
       id = to(lane);
+      longest = lane_value(mine.blocks, 0);
     }
+    if (a.max_parts == 0 || longest <= 1) {
+      chunk = max(longest, 1);
+      return;
+    }
+    const int groups = q8_groups(a, mine, QUERIES) * a.n_kv_heads;
+    const float items = wave_sum((float)groups);
+    if (items >= RESIDENT) {  // enough workgroups: only what would outlast them all is split
+      const float share = work * (1.0001f * 2 / MAX_PARTS);
+      chunk = longest > 2.f * share + START ? (int)ceilf(fmaxf(share, 16.f)) : longest;
+      return;
+    }
+    const int c = (longest + (lane & 31)) / ((lane & 31) + 1);
+    const float each = __builtin_amdgcn_rcpf((float)c);
+    float n = 0.f, parts = 0.f;
+    if (a.B == 1) work = (float)lane_value(groups, 0) * (float)longest;
+    for (int t = 0; t < a.B; ++t) {
+      const int b = lane_value(mine.blocks, t), g = lane_value(groups, t);
+      const float k = floorf(((float)(b + c) - 0.5f) * each);  // ceil(b / c)
+      n += g * k;
+      parts += k > 1.f ? g * k : 0.f;
+    }
+    const float rounds = ceilf(n * (1.f / RESIDENT));
+    const float whole = START + c, even = START + work * __builtin_amdgcn_rcpf(n);
+    float cost = (rounds > 1.f ? fmaxf(whole, rounds * even) : whole) + (parts > 0.f ? MERGE : 0.f);
+    if (parts > a.max_parts) cost = 1e6f;
+    const uint32_t best = wave_min((uint32_t)fminf(cost * 8.f, 60e6f) << 6 | lane);
+    chunk = lane_value(c, best & 63);
   }
   __device__ inline int splits(const Q8Seq& q) const { return (q.blocks + chunk - 1) / chunk; }
   // item x of all, of which every (sequence, query group, K/V head) counts its splits, or, TILES > 0, once per
@@ -110,6 +148,14 @@ struct Q8Plan {
   template <int TILES>
   __device__ inline bool find(int x, Q8Work& w) {
     const int lane = threadIdx.x & 63;
+    if (!MANY && a.B == 1) {
+      w.seq = Q8Seq{lane_value(mine.r0, 0), lane_value(mine.nodes, 0), lane_value(mine.L, 0), lane_value(mine.blocks, 0)};
+      w.s = w.part0 = 0;
+      w.nth = x;
+      w.splits = splits(w.seq);
+      const int g = q8_groups(a, w.seq, QUERIES) * a.n_kv_heads;
+      return x < (TILES == 0 ? g * w.splits : w.splits > 1 ? g * TILES : 0);
+    }
     int base = 0, parts = 0;
     for (int s0 = 0; s0 < (MANY ? a.B : 1); s0 += 64) {
       if (MANY) mine = q8_seq(a, s0 + lane), id = s0 + lane;
@@ -371,6 +417,7 @@ __global__ __launch_bounds__(KS * 64, KS / 4) void tree_attn_q8_kernel(Q8Args a)
     const int t0 = max(b0, cached), tree = max(0, b1 - t0);  // blocks
     const int tb = (ks - (t0 - b0) % KS + KS) % KS;          // this stream's of them
     constexpr int UNITS = TRJ_N_MAX / 32 * 16 * CH / (KS * 64);
+    constexpr int EARLY = D - 2, TREE_AT = EARLY * SLOT;  // blocks that fit in front of it
     bool odd = false;
     if (tree > 0) {
       u32x4 raw[UNITS][4];
@@ -389,7 +436,7 @@ __global__ __launch_bounds__(KS * 64, KS / 4) void tree_attn_q8_kernel(Q8Args a)
       for (int i = 0; i < UNITS; ++i) {
         const int u = tid + i * KS * 64, b = u / (16 * CH), rr = u / CH % 16 * 2, c = u % CH;
         if (b >= tree) continue;
-        uint8_t* const kt = smem + (size_t)((t0 - b0 + b) % KS) * D * SLOT;
+        uint8_t* const kt = smem + (size_t)((t0 - b0 + b) % KS) * D * SLOT + TREE_AT;
         u32x4* const kd = reinterpret_cast<u32x4*>(kt + ((c >> 2) * 2 + (c & 1)) * 1024 + ((c >> 1) & 1) * 512 + rr * 16);
         kd[0] = raw[i][0];
         kd[1] = raw[i][1];
@@ -461,15 +508,18 @@ __global__ __launch_bounds__(KS * 64, KS / 4) void tree_attn_q8_kernel(Q8Args a)
     auto scale_of = [&](float of, int i) { return __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(of), i & 63)); };
     // (a page that is not there makes every weight NaN)
     auto factor = [&](int i) { const float k = scale_of(ksc, i); return k == k ? a.scale_log2e : NAN; };
-    auto fill = [&](int c0, int c1) {
+    auto fill = [&](int c0, int c1, auto from_c, auto to_c) {
 #pragma unroll
-      for (int i = 0; i < D; ++i) {
+      for (int i = decltype(from_c)::value; i < decltype(to_c)::value; ++i) {
         ask(a.k_pool, c0 + i, 0, c0 + i < c1);
         ask(a.v_pool, c0 + i, 1, c0 + i < c1);
       }
     };
     // ---- the tree's own rows first, while the cached blocks come
-    if (tb >= tree) fill(0, min(mine, 64));
+    using std::integral_constant;
+    const int first_end = min(mine, 64);
+    fill(0, first_end, integral_constant<int, 0>{}, integral_constant<int, EARLY>{});
+    if (tb >= tree) fill(0, first_end, integral_constant<int, EARLY>{}, integral_constant<int, D>{});
     bool any_odd = false;
     if (tree > 0) any_odd = __syncthreads_or(odd);
     if (tb < tree) {
@@ -487,7 +537,7 @@ __global__ __launch_bounds__(KS * 64, KS / 4) void tree_attn_q8_kernel(Q8Args a)
           const int lo = from_node(word, u.node);
           sees[t] = u.live ? (uint32_t)lo : 0u;
         }
-        const u32x4* const kt = reinterpret_cast<const u32x4*>(smem + (size_t)ks * D * SLOT) + lane;
+        const u32x4* const kt = reinterpret_cast<const u32x4*>(smem + (size_t)ks * D * SLOT + TREE_AT) + lane;
         f32x16 sacc[NT];
 #pragma unroll
         for (int t = 0; t < NT; ++t)
@@ -518,7 +568,7 @@ __global__ __launch_bounds__(KS * 64, KS / 4) void tree_attn_q8_kernel(Q8Args a)
               o[t][mt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vop, __builtin_bit_cast(bf16x8, pk[t][kg]), o[t][mt], 0, 0, 0);
           }
       }
-      fill(0, min(mine, 64));
+      fill(0, first_end, integral_constant<int, EARLY>{}, integral_constant<int, D>{});
     }
 
     // ---- the cached blocks
@@ -527,7 +577,7 @@ __global__ __launch_bounds__(KS * 64, KS / 4) void tree_attn_q8_kernel(Q8Args a)
       if (c0 > 0) {
         look_up(c0);
         look_up_scales();
-        fill(c0, c1);
+        fill(c0, c1, integral_constant<int, 0>{}, integral_constant<int, D>{});
       }
       const int rest = seq.L - (b0 + ks + (c1 - 1) * KS) * 32;  // keys of the last block, if fewer than 32
 #define Q8_WAIT(behind, r) \
@@ -770,22 +820,22 @@ __global__ __launch_bounds__(1024) void attn_q8_combine_kernel(Q8Args a) {
 }
 
 // ------------------------------------------------------------------ launch
+// Two tiles of queries per workgroup where a sequence has more than 32 (as the average of the batch has it):
+// the codes are then converted once for both, on four streams; one tile on eight.  (Four streams and two
+// workgroups per compute unit gain nothing for one tile: 64 sequences of one row on 8 K/V heads, up to 1000
+// slots 48.3 against 47.0 us.)
 struct Q8Launch {
-  int ntw, target, min_blocks, max_parts, grid, tiles;
+  int ntw, max_parts, grid, tiles;
 };
 static Q8Launch q8_launch(int B, int T, int group, int n_kv_heads, int max_prefix) {
   Q8Launch p;
-  const int queries = (T + B - 1) / B * group;  // of a sequence, if all are alike
+  const long queries = ((long)T + B - 1) / B * group;  // of a sequence, if all are alike
   p.ntw = queries > 32 ? 2 : 1;
-  p.target = 256;
-  p.min_blocks = 16;
   const long items = ((long)T * group / (32 * p.ntw) + B) * n_kv_heads;  // unsplit
   const long most = ((long)max_prefix + 31) / 32 + TRJ_N_MAX / 32;       // blocks of a sequence
-  // splits: a split sequence has more than `chunk` blocks, so at most twice as many splits as whole chunks
-  const long parts = most <= p.min_blocks ? 0 : std::min(2l * p.target, items * ((most + p.min_blocks - 1) / p.min_blocks));
-  p.max_parts = (int)parts;
-  p.grid = (int)std::min(items + (parts ? p.target : 0), 1l << 20);
-  p.tiles = (int)std::min(std::min(parts, items) * p.ntw, 64l);
+  p.max_parts = most <= MERGE ? 0 : MAX_PARTS;
+  p.grid = (int)std::min(items + p.max_parts, 1l << 30);
+  p.tiles = (int)std::min(items * p.ntw, 64l);
   return p;
 }
 size_t attn_q8_ws_floats(int B, int T, int group, int n_kv_heads, int head_dim, int max_prefix) {
@@ -824,7 +874,7 @@ int launch_tree_attn_q8(const uint16_t* q, int q_stride, const void* k_pool, con
   float* const pm = ws + tiles * 32 * head_dim;
   const Q8Args a{q, k_rows, v_rows, (const uint8_t*)k_pool, (const uint8_t*)v_pool, k_scale, v_scale, parent, node_off,
                  block_table, prefix_len, q_stride, row_stride, max_blocks, B, T, n_kv_heads, group, n_blocks, max_prefix,
-                 p.target, p.min_blocks, p.max_parts, scale * 1.4426950408889634f, ws, pm, pm + tiles * 32, out, status};
+                 p.max_parts, scale * 1.4426950408889634f, ws, pm, pm + tiles * 32, out, status};
   if (B > 64) return head_dim == 128 ? q8_run_tiles<128, true>(a, p, st) : q8_run_tiles<64, true>(a, p, st);
   return head_dim == 128 ? q8_run_tiles<128, false>(a, p, st) : q8_run_tiles<64, false>(a, p, st);
 }

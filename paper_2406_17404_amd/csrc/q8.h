@@ -34,14 +34,31 @@ __device__ inline uint32_t q8_codes(float a, float b) {
   return (fabsf(a) < INFINITY ? c & 0xffu : 0x7fu) | (fabsf(b) < INFINITY ? c & 0xff00u : 0x7f00u);
 }
 
-__device__ inline int wave_scan(int x) {  // inclusive sum over the lanes
-  const int lane = threadIdx.x & 63;
-#pragma unroll
-  for (int o = 1; o < 64; o <<= 1) {
-    const int y = __shfl_up(x, o);
-    if (lane >= o) x += y;
-  }
+// Sums over the lanes by data-parallel moves inside the vector unit: rows of 16 lanes, then the rows' last lanes
+// into the rows behind them.  (Through __shfl, which goes by way of LDS, a scan took 0.4 us.)
+template <int MOVE, int ROWS>
+__device__ inline int moved(int none, int x) {
+  return __builtin_amdgcn_update_dpp(none, x, MOVE, ROWS, 0xf, false);
+}
+#define TRJ_WAVE_STEPS(STEP) \
+  STEP(0x111, 0xf) STEP(0x112, 0xf) STEP(0x114, 0xf) STEP(0x118, 0xf) STEP(0x142, 0xa) STEP(0x143, 0xc)
+__device__ inline int wave_scan(int x) {  // inclusive sum
+#define TRJ_STEP(MOVE, ROWS) x += moved<MOVE, ROWS>(0, x);
+  TRJ_WAVE_STEPS(TRJ_STEP)
+#undef TRJ_STEP
   return x;
+}
+__device__ inline float wave_sum(float x) {  // the same for all lanes
+#define TRJ_STEP(MOVE, ROWS) x += __int_as_float(moved<MOVE, ROWS>(0, __float_as_int(x)));
+  TRJ_WAVE_STEPS(TRJ_STEP)
+#undef TRJ_STEP
+  return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(x), 63));
+}
+__device__ inline uint32_t wave_min(uint32_t x) {
+#define TRJ_STEP(MOVE, ROWS) x = min(x, (uint32_t)moved<MOVE, ROWS>(-1, (int)x));
+  TRJ_WAVE_STEPS(TRJ_STEP)
+#undef TRJ_STEP
+  return (uint32_t)__builtin_amdgcn_readlane((int)x, 63);
 }
 // The sequence that owns item x when sequence s has count(s) items, and which of its items it is; false
 // behind the last item.  Every wavefront by itself, 64 sequences a round, uniform answers.
@@ -56,12 +73,10 @@ __device__ inline bool find_seq(int x, int B, F count, int& s, int& nth) {
     if (here) {
       const int l = __builtin_ctzll(here);
       s = s0 + l;
-      nth = x - (__shfl(upto, l) - __shfl(c, l));
-      s = __builtin_amdgcn_readfirstlane(s);
-      nth = __builtin_amdgcn_readfirstlane(nth);
+      nth = x - (__builtin_amdgcn_readlane(upto, l) - __builtin_amdgcn_readlane(c, l));
       return true;
     }
-    base = __shfl(upto, 63);
+    base = __builtin_amdgcn_readlane(upto, 63);
   }
   return false;
 }
