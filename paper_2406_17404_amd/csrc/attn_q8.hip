@@ -179,6 +179,7 @@ struct Q8Plan {
   }
 };
 
+typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
 __device__ inline uint32_t bf16_pair(uint32_t codes, float scale, bool hi) {
   return hi ? __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(codes, scale, true))
             : __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(codes, scale, false));
@@ -323,10 +324,10 @@ __device__ __forceinline__ void request(const void* base, uint32_t lane16, uint3
 }
 #pragma clang diagnostic pop
 
-// rings; in the same place what the streams hand over at the end
+// rings and, with one tile, a block of the tree's rows; in the same place what the streams hand over at the end
 template <int DH, int NT, int KS, int D>
 constexpr size_t q8_lds() {
-  const size_t ring = (size_t)KS * D * 64 * DH, merge = (size_t)(DH / 32) * (KS - 1) * 4096;
+  const size_t ring = (size_t)KS * D * 64 * DH + (NT == 1 ? 2 * 64 * DH : 0), merge = (size_t)(DH / 32) * (KS - 1) * 4096;
   return ring > merge ? ring : merge;
 }
 
@@ -335,6 +336,7 @@ template <int DH, int NT, int KS, int D, bool MANY>
 __global__ __launch_bounds__(KS * 64, KS / 4) void tree_attn_q8_kernel(Q8Args a) {
   constexpr int MTV = DH / 32, OW = MTV * 16 * 64, P = MTV, SLOT = 64 * DH, QUERIES = 32 * NT;
   constexpr int TILE = 64 * DH, CH = DH / 8;
+  constexpr bool TREE_LDS = NT == 1;
   static_assert(D >= 2 && KS >= TRJ_N_MAX / 32 && NT <= 2, "a stream's ring takes a block of the tree's rows");
   extern __shared__ __align__(16) uint8_t smem[];  // rings, then parts handed over
   __shared__ float sm_m[KS][NT][32], sm_l[KS][NT][32];
@@ -392,6 +394,9 @@ __global__ __launch_bounds__(KS * 64, KS / 4) void tree_attn_q8_kernel(Q8Args a)
       __builtin_amdgcn_s_waitcnt(0x0f70);  // vmcnt(0)
     };
     look_up(0);
+    // the verdict on the sequence's pages, by its first workgroup: most of them are asked for here, judged at the end
+    const bool judge = first && head == 0;
+    int32_t seen_page = judge && tid < cached ? table[tid] : 0;
     // queries: tile t, column n32; step 2j + i of the product: columns 32j + 16hh + 8i ..
     // (worked out where they are used: they would take registers over the whole walk)
     struct Query {
@@ -412,44 +417,47 @@ __global__ __launch_bounds__(KS * 64, KS / 4) void tree_attn_q8_kernel(Q8Args a)
 #pragma unroll
       for (int j = 0; j < 2 * MTV; ++j) qreg[t][j] = *reinterpret_cast<const bf16x8*>(qp + 32 * (j >> 1) + 8 * (j & 1));
     }
-    // The tree's own rows of this range go to LDS, into the order of the operands, each block into the ring of
-    // the stream that takes it, which asks for its cached blocks later.  A thread moves two rows, 8 columns.
+    // The tree's own rows of this range go to LDS as they are, each block to the stream that takes it: the first to a
+    // place of its own, if there is one (TREE_LDS), others into that stream's ring, which is then filled later.
+    // 16-byte piece c of row r lies at c ^ r of its row, so that neither writing rows nor reading columns meets
+    // a bank twice.
     const int t0 = max(b0, cached), tree = max(0, b1 - t0);  // blocks
     const int tb = (ks - (t0 - b0) % KS + KS) % KS;          // this stream's of them
-    constexpr int UNITS = TRJ_N_MAX / 32 * 16 * CH / (KS * 64);
-    constexpr int EARLY = D - 2, TREE_AT = EARLY * SLOT;  // blocks that fit in front of it
+    constexpr int UNITS = TRJ_N_MAX / 32 * 32 * CH / (KS * 64);
+    constexpr int EARLY = D - 2;  // blocks that fit in front of it
+    auto tree_at = [&](int b) {
+      return TREE_LDS && b == 0 ? smem + (size_t)KS * D * SLOT : smem + ((size_t)((t0 - b0 + b) % KS) * D + EARLY) * SLOT;
+    };
     bool odd = false;
     if (tree > 0) {
-      u32x4 raw[UNITS][4];
+      u32x4 raw[UNITS][2];
 #pragma unroll
       for (int i = 0; i < UNITS; ++i) {
-        const int u = tid + i * KS * 64, b = u / (16 * CH), rr = u / CH % 16 * 2, c = u % CH, key = (t0 + b - cached) * 32 + rr;
-        if (b >= tree) continue;
-        const size_t lo = (size_t)(seq.r0 + min(key, n - 1)) * a.row_stride + (size_t)head * DH + 8 * c;
-        const size_t hi = (size_t)(seq.r0 + min(key + 1, n - 1)) * a.row_stride + (size_t)head * DH + 8 * c;
-        raw[i][0] = *reinterpret_cast<const u32x4*>(a.k_rows + lo);
-        raw[i][1] = *reinterpret_cast<const u32x4*>(a.k_rows + hi);
-        raw[i][2] = *reinterpret_cast<const u32x4*>(a.v_rows + lo);
-        raw[i][3] = *reinterpret_cast<const u32x4*>(a.v_rows + hi);
+        const int u = tid + i * KS * 64, rr = u / CH, c = u % CH;  // of all blocks' rows
+        if (rr >= tree * 32) break;
+        const size_t at = (size_t)(seq.r0 + min((t0 - cached) * 32 + rr, n - 1)) * a.row_stride + (size_t)head * DH + 8 * c;
+        raw[i][0] = *reinterpret_cast<const u32x4*>(a.k_rows + at);
+        raw[i][1] = *reinterpret_cast<const u32x4*>(a.v_rows + at);
       }
 #pragma unroll
       for (int i = 0; i < UNITS; ++i) {
-        const int u = tid + i * KS * 64, b = u / (16 * CH), rr = u / CH % 16 * 2, c = u % CH;
-        if (b >= tree) continue;
-        uint8_t* const kt = smem + (size_t)((t0 - b0 + b) % KS) * D * SLOT + TREE_AT;
-        u32x4* const kd = reinterpret_cast<u32x4*>(kt + ((c >> 2) * 2 + (c & 1)) * 1024 + ((c >> 1) & 1) * 512 + rr * 16);
-        kd[0] = raw[i][0];
-        kd[1] = raw[i][1];
-        uint32_t* const vd = reinterpret_cast<uint32_t*>(kt + TILE + (c >> 2) * 2048 + (rr >> 4) * 1024 + ((rr >> 2) & 1) * 512 +
-                                                         (c & 3) * 128 + ((rr >> 3) & 1) * 8 + (rr & 3) * 2);
+        const int u = tid + i * KS * 64, rr = u / CH, c = u % CH;
+        if (rr >= tree * 32) break;
+        uint8_t* const dst = tree_at(rr >> 5) + (rr & 31) * 2 * DH + (c ^ (rr & (CH - 1))) * 16;
+        u32x4 v = raw[i][1];
+        bool mine_odd = false;
 #pragma unroll
-        for (int k = 0; k < 8; ++k) {
-          const uint32_t v0 = raw[i][2][k >> 1], v1 = raw[i][3][k >> 1];
-          uint32_t x = k & 1 ? v0 >> 16 : v0 & 0xffffu, y = k & 1 ? v1 & 0xffff0000u : v1 << 16;
-          if ((x & 0x7f80u) == 0x7f80u) odd = true, x = 0;
-          if ((y & 0x7f800000u) == 0x7f800000u) odd = true, y = 0;
-          vd[4 * k] = x | y;
+        for (int e = 0; e < 4; ++e) mine_odd = mine_odd || (v[e] & 0x7f80u) == 0x7f80u || (v[e] & 0x7f800000u) == 0x7f800000u;
+        if (mine_odd) {  // left out of the products, see q8_add_odd_values
+          odd = true;
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            if ((v[e] & 0x7f80u) == 0x7f80u) v[e] &= 0xffff0000u;
+            if ((v[e] & 0x7f800000u) == 0x7f800000u) v[e] &= 0xffffu;
+          }
         }
+        *reinterpret_cast<u32x4*>(dst) = raw[i][0];
+        *reinterpret_cast<u32x4*>(dst + TILE) = v;
       }
     }
     look_up_scales();
@@ -519,7 +527,8 @@ __global__ __launch_bounds__(KS * 64, KS / 4) void tree_attn_q8_kernel(Q8Args a)
     using std::integral_constant;
     const int first_end = min(mine, 64);
     fill(0, first_end, integral_constant<int, 0>{}, integral_constant<int, EARLY>{});
-    if (tb >= tree) fill(0, first_end, integral_constant<int, EARLY>{}, integral_constant<int, D>{});
+    const bool own_place = TREE_LDS && tb == 0;
+    if (tb >= tree || own_place) fill(0, first_end, integral_constant<int, EARLY>{}, integral_constant<int, D>{});
     bool any_odd = false;
     if (tree > 0) any_odd = __syncthreads_or(odd);
     if (tb < tree) {
@@ -537,7 +546,20 @@ __global__ __launch_bounds__(KS * 64, KS / 4) void tree_attn_q8_kernel(Q8Args a)
           const int lo = from_node(word, u.node);
           sees[t] = u.live ? (uint32_t)lo : 0u;
         }
-        const u32x4* const kt = reinterpret_cast<const u32x4*>(smem + (size_t)ks * D * SLOT + TREE_AT) + lane;
+        const uint8_t* const rows = tree_at(tb);
+        auto key_piece = [&](int j) {  // row n32, columns 32 (j / 2) + 16 hh + 8 (j % 2) ..
+          const int c = (j >> 1) * 4 + hh * 2 + (j & 1);
+          return *reinterpret_cast<const u32x4*>(rows + n32 * 2 * DH + (c ^ (n32 & (CH - 1))) * 16);
+        };
+        auto value_pair = [&](int mt, int kg, int e) {  // rows 16 kg + 8 (e / 2) + 4 hh + 2 (e % 2) and the next, column 32 mt + n32
+          u16x2 x;
+#pragma unroll
+          for (int i = 0; i < 2; ++i) {
+            const int key = 16 * kg + 8 * (e >> 1) + 4 * hh + 2 * (e & 1) + i, c = 4 * mt + (n32 >> 3);
+            x[i] = *reinterpret_cast<const uint16_t*>(rows + TILE + key * 2 * DH + (c ^ (key & (CH - 1))) * 16 + (n32 & 7) * 2);
+          }
+          return __builtin_bit_cast(uint32_t, x);
+        };
         f32x16 sacc[NT];
 #pragma unroll
         for (int t = 0; t < NT; ++t)
@@ -545,7 +567,7 @@ __global__ __launch_bounds__(KS * 64, KS / 4) void tree_attn_q8_kernel(Q8Args a)
           for (int v = 0; v < 16; ++v) sacc[t][v] = 0.f;
 #pragma unroll
         for (int j = 0; j < 2 * MTV; ++j) {
-          const bf16x8 kop = __builtin_bit_cast(bf16x8, kt[j * 64]);
+          const bf16x8 kop = __builtin_bit_cast(bf16x8, key_piece(j));
 #pragma unroll
           for (int t = 0; t < NT; ++t) sacc[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kop, qreg[t][j], sacc[t], 0, 0, 0);
         }
@@ -562,13 +584,13 @@ __global__ __launch_bounds__(KS * 64, KS / 4) void tree_attn_q8_kernel(Q8Args a)
         for (int mt = 0; mt < MTV; ++mt)
 #pragma unroll
           for (int kg = 0; kg < 2; ++kg) {
-            const bf16x8 vop = __builtin_bit_cast(bf16x8, kt[TILE / 16 + (mt * 2 + kg) * 64]);
+            const bf16x8 vop = __builtin_bit_cast(bf16x8, u32x4{value_pair(mt, kg, 0), value_pair(mt, kg, 1), value_pair(mt, kg, 2), value_pair(mt, kg, 3)});
 #pragma unroll
             for (int t = 0; t < NT; ++t)
               o[t][mt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vop, __builtin_bit_cast(bf16x8, pk[t][kg]), o[t][mt], 0, 0, 0);
           }
       }
-      fill(0, first_end, integral_constant<int, EARLY>{}, integral_constant<int, D>{});
+      if (!own_place) fill(0, first_end, integral_constant<int, EARLY>{}, integral_constant<int, D>{});
     }
 
     // ---- the cached blocks
@@ -588,19 +610,22 @@ __global__ __launch_bounds__(KS * 64, KS / 4) void tree_attn_q8_kernel(Q8Args a)
       bf16x8 kop[2 * MTV], vop[2 * MTV];
       u32x4 pk[NT][2];
       float top[NT], f;
+      auto begin = [&](int i) {  // products and their maxima, from K in registers
+        f = factor(i);
+        operands(kop, kraw, scale_of(ksc, i));
+#pragma unroll
+        for (int t = 0; t < NT; ++t) scores(t, kop, sacc[t]);
+#pragma unroll
+        for (int t = 0; t < NT; ++t) top[t] = Softmax::largest(sacc[t], f);
+      };
       Q8_WAIT(behind_k0, c1 - 1 - c0);
       read_k(c0);
       keep_all();
+      begin(c0);
       int i = c0;
       for (;;) {
         bool last;
-        for (;; ++i) {
-          f = factor(i);
-          operands(kop, kraw, scale_of(ksc, i));
-#pragma unroll
-          for (int t = 0; t < NT; ++t) scores(t, kop, sacc[t]);
-#pragma unroll
-          for (int t = 0; t < NT; ++t) top[t] = Softmax::largest(sacc[t], f);
+        for (;;) {
           last = i == c1 - 1;
           bool low = last || sm[0].too_low(top[0]);
           if constexpr (NT == 2) low = low || sm[1].too_low(top[1]);
@@ -618,8 +643,10 @@ __global__ __launch_bounds__(KS * 64, KS / 4) void tree_attn_q8_kernel(Q8Args a)
             sm[1].weigh(sacc[1], f, pk[1]);
           }
           Q8_WAIT(behind_k1, c1 - 1 - i);
-          read_k(i + 1);  // (behind the last one whatever is there)
+          ++i;
+          read_k(i);
           values(NT - 1, vop, pk[NT - 1]);
+          begin(i);
         }
         keep_all();
         if (last) {
@@ -655,15 +682,9 @@ __global__ __launch_bounds__(KS * 64, KS / 4) void tree_attn_q8_kernel(Q8Args a)
         values(t, vop, pk[t]);
       }
     }
-    if (first && head == 0) {  // the verdict on the sequence's pages
-      bool bad = false;
-      for (int j = tid; j < cached; j += KS * 64) bad = bad || (unsigned)table[j] >= (unsigned)a.n_blocks;
-      bad = __syncthreads_or(bad);
-      if (tid == 0) a.status[w.s] = bad;
-    }
-
-    // ---- merge the key streams of every query tile in a fixed order: stream mt (second tile: mt + KS / 2)
-    // owns part mt
+    // ---- merge the key streams of every query tile in a fixed order: stream k adds up registers R k .. of the tile
+    constexpr int R = MTV * 16 / KS;
+    static_assert(R % 4 == 0, "");
 #pragma unroll
     for (int t = 0; t < NT; ++t) {
       const float l = sm[t].l + __shfl_xor(sm[t].l, 32);
@@ -673,8 +694,7 @@ __global__ __launch_bounds__(KS * 64, KS / 4) void tree_attn_q8_kernel(Q8Args a)
       }
     }
     __syncthreads();  // the rings are free, too
-    float* const red = reinterpret_cast<float*>(smem);
-    constexpr int PART = 16 * 64;
+    f32x4* const red = reinterpret_cast<f32x4*>(smem);
 #pragma unroll
     for (int t = 0; t < NT; ++t) {  // tile by tile: all at once do not fit LDS
       if (t > 0) __syncthreads();
@@ -684,15 +704,16 @@ __global__ __launch_bounds__(KS * 64, KS / 4) void tree_attn_q8_kernel(Q8Args a)
 #pragma unroll
       for (int k = 0; k < KS; ++k) lg += sm_l[k][t][n32] * __builtin_amdgcn_exp2f(sm_m[k][t][n32] - mg);
       const float f = __builtin_amdgcn_exp2f(sm[t].m - mg);
+      f32x4 sum[R / 4];
 #pragma unroll
-      for (int mt = 0; mt < MTV; ++mt) {
+      for (int k = 0; k < KS; ++k) {  // to stream k
 #pragma unroll
-        for (int v = 0; v < 16; ++v) o[t][mt][v] *= f;
-        const int owner = (mt + t * (KS / 2)) % KS;
-        if (ks != owner) {
-          float* dst = red + ((mt * (KS - 1)) + (ks < owner ? ks : ks - 1)) * PART + lane;
-#pragma unroll
-          for (int v = 0; v < 16; ++v) dst[v * 64] = o[t][mt][v];
+        for (int q = 0; q < R / 4; ++q) {
+          const int reg = k * R + 4 * q;
+          const f32x4 x = {o[t][reg >> 4][reg & 15] * f, o[t][reg >> 4][(reg & 15) + 1] * f, o[t][reg >> 4][(reg & 15) + 2] * f,
+                           o[t][reg >> 4][(reg & 15) + 3] * f};
+          if (ks == k) sum[q] = x;
+          else red[((k * (KS - 1) + (ks < k ? ks : ks - 1)) * (R / 4) + q) * 64 + lane] = x;
         }
       }
       __syncthreads();
@@ -704,32 +725,32 @@ __global__ __launch_bounds__(KS * 64, KS / 4) void tree_attn_q8_kernel(Q8Args a)
         a.pm[tile * 32 + n32] = mg;
         a.pl[tile * 32 + n32] = any_odd ? -lg : lg;  // (a sum of weights is not negative)
       }
-      const float inv = 1.0f / lg;
 #pragma unroll
-      for (int mt = 0; mt < MTV; ++mt) {
-        if (ks != (mt + t * (KS / 2)) % KS) continue;
-        const float* src = red + (mt * (KS - 1)) * PART + lane;
+      for (int k = 0; k < KS - 1; ++k)
 #pragma unroll
-        for (int k = 0; k < KS - 1; ++k)
+        for (int q = 0; q < R / 4; ++q) sum[q] += red[((ks * (KS - 1) + k) * (R / 4) + q) * 64 + lane];
+      const int reg0 = ks * R;  // 32-column part reg0 / 16, columns 8 (v / 4) + 4 hh + v % 4 of it
+      if (splits == 1) {
+        const float inv = 1.0f / lg;
+        const Query u = query(t);
+        if (u.live) {
+          uint16_t* dst = a.out + (size_t)(seq.r0 + u.node) * row_len + (size_t)u.head * DH + 4 * hh + (reg0 >> 4) * 32 + (reg0 & 15) * 2;
 #pragma unroll
-          for (int v = 0; v < 16; ++v) o[t][mt][v] += src[(k * 16 + v) * 64];
-        if (splits == 1) {
-          const Query u = query(t);
-          if (u.live) {
-            uint16_t* dst = a.out + (size_t)(seq.r0 + u.node) * row_len + (size_t)u.head * DH + 32 * mt + 4 * hh;
-#pragma unroll
-            for (int g = 0; g < 4; ++g) {
-              const u32x2 v = {pack2bf(o[t][mt][4 * g] * inv, o[t][mt][4 * g + 1] * inv),
-                               pack2bf(o[t][mt][4 * g + 2] * inv, o[t][mt][4 * g + 3] * inv)};
-              *reinterpret_cast<u32x2*>(dst + 8 * g) = v;
-            }
+          for (int q = 0; q < R / 4; ++q) {
+            const u32x2 v = {pack2bf(sum[q][0] * inv, sum[q][1] * inv), pack2bf(sum[q][2] * inv, sum[q][3] * inv)};
+            *reinterpret_cast<u32x2*>(dst + 8 * q) = v;
           }
-        } else {
-          float* img = a.po + tile * OW + mt * PART + lane;
-#pragma unroll
-          for (int v = 0; v < 16; ++v) img[v * 64] = o[t][mt][v];
         }
+      } else {
+#pragma unroll
+        for (int q = 0; q < R / 4; ++q) *reinterpret_cast<f32x4*>(a.po + tile * OW + ((reg0 >> 2) + q) * 256 + lane * 4) = sum[q];
       }
+    }
+    if (judge) {
+      bool bad = (unsigned)seen_page >= (unsigned)a.n_blocks;
+      for (int j = tid + KS * 64; j < cached; j += KS * 64) bad = bad || (unsigned)table[j] >= (unsigned)a.n_blocks;
+      bad = __syncthreads_or(bad);
+      if (tid == 0) a.status[w.s] = bad;
     }
     if (any_odd && splits == 1) q8_add_odd_values(a, seq.r0, head, DH, qg * QUERIES, min(nq, (qg + 1) * QUERIES), 0, DH);
   }
@@ -760,16 +781,15 @@ __global__ __launch_bounds__(1024) void attn_q8_combine_kernel(Q8Args a) {
     bool odd = false;
     f32x4 o = {0, 0, 0, 0};
     for (int s0 = h; s0 < splits; s0 += 4 * BATCH) {
-      float pm[BATCH], pl[BATCH], po[BATCH][4];
+      float pm[BATCH], pl[BATCH];
+      f32x4 po[BATCH];
 #pragma unroll
       for (int k = 0; k < BATCH; ++k) {
         const int sp = min(s0 + 4 * k, splits - 1);
         const size_t p = (size_t)(w.part0 + (qg * splits + sp) * a.n_kv_heads + head) * NT + nt;
         pm[k] = a.pm[p * 32 + n32];
         pl[k] = a.pl[p * 32 + n32];
-        const float* img = a.po + p * MTV * PART + mt * PART + 4 * g * 64 + lane;
-#pragma unroll
-        for (int v = 0; v < 4; ++v) po[k][v] = img[v * 64];
+        po[k] = *reinterpret_cast<const f32x4*>(a.po + p * MTV * PART + (mt * 4 + g) * 256 + lane * 4);
       }
       float top = m;
 #pragma unroll
@@ -784,8 +804,7 @@ __global__ __launch_bounds__(1024) void attn_q8_combine_kernel(Q8Args a) {
         const float f = __builtin_amdgcn_exp2f(pm[k] - m);
         odd = odd || (__float_as_uint(pl[k]) >> 31) != 0;
         l += f * fabsf(pl[k]);
-#pragma unroll
-        for (int v = 0; v < 4; ++v) o[v] += f * po[k][v];
+        o += f * po[k];
       }
     }
     if (h > 0) sm_o[h - 1][tid & 255] = o;
