@@ -1,4 +1,6 @@
 // Pages that follow lengths, and the append that quantises rows into the paged 8-bit cache.
+#include <algorithm>
+
 #include "kernels.h"
 #include "q8.h"
 
@@ -142,12 +144,14 @@ int launch_block_tables(int32_t* block_table, int max_blocks, const int32_t* hel
 }
 
 // ------------------------------------------------------------------ append
-// A workgroup quantises one page of one head, K or V: 32 x DH values, 16 of a row per thread.
+// A wavefront quantises one page of one head, K or V: 32 x DH values, a lane 4 rows x 8 columns at a time.
 //   top = max |x| over the page's new rows;  2^k with top <= 448 * 2^k;  code = e4m3(x * 2^-k)
 // With a power of two the products are exact, so a page whose scale grows is requantised by
-// multiplying its codes with the (power of two) ratio.
-// Bound by memory for prompts (2 bytes read, 1 written per value) and by latency for a few rows: count,
-// table entry, rows, maximum over the workgroup, codes.
+// multiplying its codes with the (power of two) ratio.  K's bytes are stored as they are; V's, four rows
+// to a word, go through LDS, where they meet those of rows that stay.
+// Bound by memory for prompts (2 bytes read, 1 written per value), by a chain of latencies for a few rows
+// (lengths, page number, rows, codes), so a workgroup finds its page once for several heads and
+// layers, and no wavefront waits for another.
 struct AppendArgs {
   uint8_t* pool[2];
   float* scale[2];
@@ -187,16 +191,134 @@ __device__ inline bool append_valid(const AppendArgs& a, int s, int L, int m) {
   return __ballot(bad) == 0;
 }
 
-template <int DH>
-__global__ __launch_bounds__(2 * DH) void kv_append_kernel(AppendArgs a) {
-  constexpr int THREADS = 2 * DH, WAVES = THREADS / 64, CH = DH / 16;
-  __shared__ __align__(16) uint8_t tile[32 * DH];
-  __shared__ uint32_t tops[WAVES];
-  const int tid = threadIdx.x, lane = tid & 63, wv = tid >> 6;
-  const int head = blockIdx.y, layer = blockIdx.z >> 1, which = blockIdx.z & 1;
+// place of 16-byte group g of a V page in LDS: the columns that a wavefront writes at once would meet a quarter of
+// the banks
+__device__ inline int v_group_place(int g) { return g ^ ((g >> 3) & 3) ^ (((g >> 6) & 1) << 2); }
 
-  if (blockIdx.y == 0 && blockIdx.z == 0) {  // the verdicts
-    for (int s = blockIdx.x * WAVES + wv; s < a.B; s += gridDim.x * WAVES) {
+template <int DH>
+__global__ __launch_bounds__(256, 3) void kv_append_kernel(AppendArgs a, int planes) {
+  constexpr int C8 = DH / 8, PASSES = 8 * C8 / 64, GROUPS = 2 * DH / 64;  // 16-byte groups of a page per lane
+  __shared__ __align__(16) uint8_t tiles[4][32 * DH];
+  const int lane = threadIdx.x & 63, wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  uint8_t* const tile = tiles[wv];
+  for (int x = blockIdx.x;; x += gridDim.x) {
+    int s, nth;
+    if (!find_seq(x, a.B, [&](int q) { return pages_touched(a.prefix_len[q], append_rows(a, q)); }, s, nth)) break;
+    const int L = a.prefix_len[s], m = append_rows(a, s), r0 = a.node_off[s];
+    const int pg = L / TRJ_KV_BLOCK + nth, page = a.block_table[(size_t)s * a.max_blocks + pg];
+    const int old_rows = max(0, min(32, L - pg * 32)), end = min(32, L + m - pg * 32);  // new: [old_rows, end)
+    int row[PASSES][4];  // of the input, -1: none
+#pragma unroll
+    for (int p = 0; p < PASSES; ++p)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const int r = (p * 64 + lane) / C8 * 4 + i, j = pg * 32 + r - L;
+        row[p][i] = r >= old_rows && r < end ? (a.path ? a.path[(size_t)s * TRJ_N_MAX + j] : j) : -1;
+      }
+    if (!append_valid(a, s, L, m)) continue;
+    for (int pl = blockIdx.y * 4 + wv; pl < planes; pl += gridDim.y * 4) {
+      int ln = lane;
+      asm("" : "+v"(ln));  // offsets are worked out again for every plane, not held in registers
+      const int c0 = ln % C8 * 8;
+      const int which = pl & 1, head = (pl >> 1) % a.n_kv_heads, layer = (pl >> 1) / a.n_kv_heads;
+      const size_t pln = ((size_t)layer * a.n_kv_heads + head) * a.n_blocks + page;
+      float* const scale = a.scale[which] + pln;
+      uint8_t* const pool = a.pool[which] + pln * 32 * DH;
+      const uint16_t* const src = a.rows[which] + layer * a.row_layer_stride + (size_t)head * DH + c0;
+      u32x4 raw[PASSES][4];
+#pragma unroll
+      for (int p = 0; p < PASSES; ++p)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          raw[p][i] = u32x4{0, 0, 0, 0};
+          if (row[p][i] >= 0) raw[p][i] = *reinterpret_cast<const u32x4*>(src + (size_t)(r0 + row[p][i]) * a.row_stride);
+        }
+      const bool keeps = which == 1 && (old_rows > 0 || end < 32);  // V words hold rows that stay
+      u32x4 had[GROUPS];
+      if (keeps)
+#pragma unroll
+        for (int k = 0; k < GROUPS; ++k) had[k] = reinterpret_cast<const u32x4*>(pool)[k * 64 + ln];
+      int e_old = Q8_MIN_EXP;
+      if (old_rows > 0) e_old = q8_exp_of(*scale);
+      uint32_t top = 0;  // bits of the largest finite magnitude
+#pragma unroll
+      for (int p = 0; p < PASSES; ++p)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+          const uint32_t w = raw[p][i >> 2][i & 3], lo = (w << 16) & 0x7fffffffu, hi = w & 0x7fff0000u;
+          top = max(top, max(lo < 0x7f800000u ? lo : 0u, hi < 0x7f800000u ? hi : 0u));
+        }
+      const int e = max(q8_exp(wave_max(top)), e_old);
+      const float inv = q8_pow2(-e), ratio = q8_pow2(max(e_old - e, -126));
+      const bool grew = old_rows > 0 && e > e_old;
+      if (lane == 0) *scale = q8_pow2(e);
+      auto lower = [&](uint32_t codes) {  // earlier codes to the new scale
+        const f32x2 p = __builtin_amdgcn_cvt_pk_f32_fp8((int)codes, false), q = __builtin_amdgcn_cvt_pk_f32_fp8((int)codes, true);
+        return q8_codes(p[0] * ratio, p[1] * ratio) | q8_codes(q[0] * ratio, q[1] * ratio) << 16;
+      };
+#pragma unroll
+      for (int p = 0; p < PASSES; ++p) {
+        const int q = (p * 64 + ln) / C8;  // rows 4q ..
+        uint32_t code[4][2];
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+          for (int h = 0; h < 2; ++h) {
+            const uint32_t u = raw[p][i][2 * h], v = raw[p][i][2 * h + 1];
+            code[i][h] = q8_codes(__uint_as_float(u << 16) * inv, __uint_as_float(u & 0xffff0000u) * inv) |
+                         q8_codes(__uint_as_float(v << 16) * inv, __uint_as_float(v & 0xffff0000u) * inv) << 16;
+          }
+        if (which == 0) {
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            u32x2* const dst = reinterpret_cast<u32x2*>(pool + q8_k_off(4 * q + i, c0));
+            if (row[p][i] >= 0) *dst = u32x2{code[i][0], code[i][1]};
+            else if (grew && 4 * q + i < old_rows) {
+              const u32x2 o = *dst;
+              *dst = u32x2{lower(o[0]), lower(o[1])};
+            }
+          }
+        } else {
+#pragma unroll
+          for (int c = 0; c < 8; ++c) {
+            const uint32_t sel = 0x0c0c0400u + 0x0101u * (c & 3);  // byte c % 4 of each of two words
+            const uint32_t ab = __builtin_amdgcn_perm(code[1][c >> 2], code[0][c >> 2], sel);
+            const uint32_t cd = __builtin_amdgcn_perm(code[3][c >> 2], code[2][c >> 2], sel);
+            const int g = q8_v_off(4 * q, c0 + c) >> 4;
+            *reinterpret_cast<uint32_t*>(tile + v_group_place(g) * 16 + (q >> 1) * 4) = ab | cd << 16;
+          }
+        }
+        __builtin_amdgcn_sched_barrier(0);  // one pass after the other: registers
+      }
+      if (which == 1) {
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // this wavefront's words, which it reads itself
+#pragma unroll
+        for (int k = 0; k < GROUPS; ++k) {
+          const int g = k * 64 + ln;
+          const u32x4 fresh = *reinterpret_cast<const u32x4*>(tile + v_group_place(g) * 16);
+          u32x4 put = fresh;
+          if (keeps)
+#pragma unroll
+            for (int d = 0; d < 4; ++d) {  // rows 8d + 4 ((g / 32) % 2) ..
+              uint32_t is_new = 0, is_old = 0;
+#pragma unroll
+              for (int i = 0; i < 4; ++i) {
+                const int r = 8 * d + 4 * ((g >> 5) & 1) + i;
+                if (r < old_rows) is_old |= 0xffu << (8 * i);
+                else if (r < end) is_new |= 0xffu << (8 * i);
+              }
+              const uint32_t kept = grew ? lower(had[k][d]) : had[k][d];
+              put[d] = (fresh[d] & is_new) | (kept & is_old) | (had[k][d] & ~(is_new | is_old));
+            }
+          reinterpret_cast<u32x4*>(pool)[g] = put;
+          __builtin_amdgcn_sched_barrier(0);
+        }
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // read before the next page's are written
+      }
+    }
+  }
+  if (blockIdx.y == 0) {  // the verdicts
+    for (int s = blockIdx.x * 4 + wv; s < a.B; s += gridDim.x * 4) {
       const int m = append_rows(a, s);
       const bool ok = m >= 0 && append_valid(a, s, a.prefix_len[s], m);
       if (lane == 0) {
@@ -204,99 +326,6 @@ __global__ __launch_bounds__(2 * DH) void kv_append_kernel(AppendArgs a) {
         a.status[s] = !ok;
       }
     }
-  }
-  for (int x = blockIdx.x;; x += gridDim.x) {
-    int s, nth;
-    if (!find_seq(x, a.B, [&](int q) { return pages_touched(a.prefix_len[q], append_rows(a, q)); }, s, nth)) return;
-    const int L = a.prefix_len[s], m = append_rows(a, s), r0 = a.node_off[s];
-    if (!append_valid(a, s, L, m)) continue;  // uniform over the workgroup
-    const int pg = L / TRJ_KV_BLOCK + nth, page = a.block_table[(size_t)s * a.max_blocks + pg];
-    const int old_rows = max(0, min(32, L - pg * 32)), end = min(32, L + m - pg * 32);  // new: [old_rows, end)
-
-    // 16 values of row r
-    const int r = tid / CH, c0 = (tid % CH) * 16;
-    const bool mine = r >= old_rows && r < end;
-    u32x4 raw[2] = {{0, 0, 0, 0}, {0, 0, 0, 0}};
-    if (mine) {
-      const int j = pg * 32 + r - L;
-      const int row = r0 + (a.path ? a.path[(size_t)s * TRJ_N_MAX + j] : j);
-      const u32x4* src = reinterpret_cast<const u32x4*>(a.rows[which] + layer * a.row_layer_stride + (size_t)row * a.row_stride +
-                                                        (size_t)head * DH + c0);
-      raw[0] = src[0];
-      raw[1] = src[1];
-    }
-    uint32_t top = 0;  // bits of the largest finite magnitude
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      const uint32_t w = raw[i >> 2][i & 3], lo = (w << 16) & 0x7fffffffu, hi = w & 0x7fff0000u;
-      top = max(top, max(lo < 0x7f800000u ? lo : 0u, hi < 0x7f800000u ? hi : 0u));
-    }
-    for (int o = 32; o > 0; o >>= 1) top = max(top, (uint32_t)__shfl_xor((int)top, o));
-    if (lane == 0) tops[wv] = top;
-    __syncthreads();
-#pragma unroll
-    for (int w = 0; w < WAVES; ++w) top = max(top, tops[w]);
-    const size_t plane = ((size_t)layer * a.n_kv_heads + head) * a.n_blocks + page;
-    float* const scale = a.scale[which] + plane;
-    int e = q8_exp(top), e_old = 0;
-    if (old_rows > 0) {
-      e_old = q8_exp_of(*scale);
-      e = max(e, e_old);
-    }
-    const float inv = q8_pow2(-e);
-    u32x4 codes;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      uint32_t c[2];
-#pragma unroll
-      for (int k = 0; k < 2; ++k) {
-        const uint32_t w = raw[i >> 1][(i & 1) * 2 + k];
-        c[k] = q8_codes(__uint_as_float(w << 16) * inv, __uint_as_float(w & 0xffff0000u) * inv);
-      }
-      codes[i] = c[0] | c[1] << 16;
-    }
-    // through LDS into the page's order
-    if (which == 0) {
-      *reinterpret_cast<u32x4*>(tile + q8_k_off(r, c0)) = codes;
-    } else {
-#pragma unroll
-      for (int i = 0; i < 16; ++i) tile[q8_v_off(r, c0 + i)] = (uint8_t)(codes[i >> 2] >> (8 * (i & 3)));
-    }
-    __syncthreads();  // every thread has read the old scale as well
-    if (tid == 0) *scale = q8_pow2(e);
-    u32x4* const dst = reinterpret_cast<u32x4*>(a.pool[which] + plane * 32 * DH) + tid;
-    const bool grew = old_rows > 0 && e > e_old;
-    const float ratio = grew ? q8_pow2(max(e_old - e, -126)) : 1.f;
-    const u32x4 fresh = reinterpret_cast<const u32x4*>(tile)[tid];
-    // byte i of dword d of this thread's 16: row
-    const bool whole = old_rows == 0 && end == 32;
-    u32x4 old = {0, 0, 0, 0};
-    const int kr = tid & 31;  // K: all 16 bytes belong to one row
-    const bool k_new = kr >= old_rows && kr < end;
-    if (which == 0 ? (grew && kr < old_rows) : !whole) old = *dst;
-    u32x4 put;
-#pragma unroll
-    for (int d = 0; d < 4; ++d) {
-      uint32_t kept = old[d];
-      if (grew) {
-        const f32x2 p = __builtin_amdgcn_cvt_pk_f32_fp8((int)kept, false), q = __builtin_amdgcn_cvt_pk_f32_fp8((int)kept, true);
-        kept = q8_codes(p[0] * ratio, p[1] * ratio) | q8_codes(q[0] * ratio, q[1] * ratio) << 16;
-      }
-      if (which == 0) {
-        put[d] = k_new ? fresh[d] : kept;
-      } else {
-        uint32_t is_new = 0, is_old = 0;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const int row = 8 * d + 4 * ((tid >> 5) & 1) + i;
-          if (row < old_rows) is_old |= 0xffu << (8 * i);
-          else if (row < end) is_new |= 0xffu << (8 * i);
-        }
-        put[d] = (fresh[d] & is_new) | (kept & is_old) | (old[d] & ~(is_new | is_old));
-      }
-    }
-    if (which == 0 ? (k_new || (grew && kr < old_rows)) : true) *dst = put;
-    __syncthreads();  // the tile is free again
   }
 }
 
@@ -309,9 +338,13 @@ int launch_kv_append_q8(void* k_pool, void* v_pool, float* k_scale, float* v_sca
                      row_stride, row_layer_stride, path, accept_len, node_off, block_table, prefix_len, max_blocks, B, T,
                      n_kv_heads, n_blocks, new_len, status};
   // all rows: a sequence touches at most two pages more than its rows fill; a path mostly one or two
-  const dim3 grid(path ? 2 * B : T / TRJ_KV_BLOCK + 2 * B, n_kv_heads, 2 * n_layers);
-  if (head_dim == 128) kv_append_kernel<128><<<grid, 256, 0, st>>>(a);
-  else kv_append_kernel<64><<<grid, 128, 0, st>>>(a);
+  const int pages = path ? 2 * B : T / TRJ_KV_BLOCK + 2 * B, planes = 2 * n_layers * n_kv_heads;
+  // several planes per wavefront where there are more than the chip holds wavefronts of: what finds the page is
+  // then done once for them
+  const int each = (int)std::min(std::max((long)pages * planes / 6144, 1l), 8l);
+  const dim3 grid(pages, std::min((planes + 4 * each - 1) / (4 * each), 65535));
+  if (head_dim == 128) kv_append_kernel<128><<<grid, 256, 0, st>>>(a, planes);
+  else kv_append_kernel<64><<<grid, 256, 0, st>>>(a, planes);
   return check_launch();
 }
 

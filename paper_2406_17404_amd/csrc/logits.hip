@@ -15,9 +15,14 @@
 
 namespace trj {
 
-constexpr int LG_THREADS = 256, LG_SLICE = 4 * LG_THREADS;
-typedef float f32x4_any __attribute__((ext_vector_type(4), aligned(4)));  // rows of odd length start anywhere
+constexpr int LG_THREADS = 256, LG_SLICE = 4 * LG_THREADS, LG_BATCH = 4;
+typedef float f32x4_any __attribute__((ext_vector_type(4), aligned(4)));
+typedef int i32x4_any __attribute__((ext_vector_type(4), aligned(4)));  // rows of odd length start anywhere
 
+struct LogitsBatch {  // four tokens of each of some rows, with the words of their masks
+  float x[LG_BATCH][4];
+  uint32_t words[LG_BATCH];
+};
 struct LogitsArgs {
   const float* x;
   const int32_t *tok, *parent, *node_off;
@@ -42,13 +47,31 @@ __device__ inline uint64_t pick_key(float x, int i) {
   const uint32_t ord = x != x ? 0u : (u >> 31 ? ~u : u | 0x80000000u);
   return (uint64_t)ord << 32 | (uint32_t)~i;
 }
-__device__ inline uint64_t wave_max(uint64_t k) {
+__device__ inline uint64_t wave_max_key(uint64_t k) {
 #pragma unroll
   for (int o = 32; o > 0; o >>= 1) {
     const uint64_t u = (uint64_t)(uint32_t)__shfl_xor((int)(k >> 32), o) << 32 | (uint32_t)__shfl_xor((int)k, o);
     k = u > k ? u : k;
   }
   return k;
+}
+// The best of four tokens from `first` on, of all lanes; tokens that are not allowed are -infinity.  mine, top:
+// the largest of a lane and of all
+__device__ inline uint64_t wave_pick(const float (&x)[4], uint32_t may, int first, float mine, float top) {
+  if (top > -INFINITY) {  // the first lane that has it, of it the first token
+    const int at = first + (x[0] == top ? 0 : x[1] == top ? 1 : x[2] == top ? 2 : 3);
+    return pick_key(top, __builtin_amdgcn_readlane(at, __builtin_ctzll(__ballot(mine == top))));
+  }
+  uint64_t k = 0;  // nothing but -infinity, NaN and what is not allowed
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    const uint64_t u = (may >> e) & 1 ? pick_key(x[e], first + e) : 0;
+    k = u > k ? u : k;
+  }
+  return wave_max_key(k);
+}
+__device__ inline uint64_t uniform(uint64_t x) {
+  return (uint64_t)__builtin_amdgcn_readfirstlane((int)(x >> 32)) << 32 | (uint32_t)__builtin_amdgcn_readfirstlane((int)x);
 }
 __device__ inline int picked(uint64_t key) { return key == 0 ? -1 : (int)~(uint32_t)key; }
 
@@ -63,12 +86,14 @@ __device__ inline int logits_rows(const LogitsArgs& a, int s) {
 
 __global__ __launch_bounds__(LG_THREADS) void tree_logits_kernel(LogitsArgs a) {
   __shared__ int seen_n[LG_SLICE], made_n[LG_SLICE], bias_at[LG_SLICE];
-  __shared__ uint32_t above[TRJ_N_MAX][4];  // drafts of this slice on the path to a node
+  __shared__ __align__(16) uint32_t above[TRJ_N_MAX][4];  // drafts of this slice on the path to a node
+  __shared__ uint64_t under[2];             // nodes below such drafts
   __shared__ int draft[TRJ_N_MAX];          // a draft's place in the slice
   __shared__ uint64_t best[TRJ_N_MAX][LG_THREADS / 64];
   const int tid = threadIdx.x, lane = tid & 63, wv = tid >> 6;
   const int v0 = blockIdx.x * LG_SLICE, mine = v0 + 4 * tid;
   const int words = (a.V + 31) >> 5;
+  const uint32_t there = mine >= a.V ? 0u : mine + 4 <= a.V ? 15u : (1u << (a.V - mine)) - 1u;  // tokens of the vocabulary
 
   if (blockIdx.x == 0 && blockIdx.y == 0) {  // sequences without rows
     for (int s = tid; s < a.B; s += LG_THREADS) {
@@ -79,15 +104,34 @@ __global__ __launch_bounds__(LG_THREADS) void tree_logits_kernel(LogitsArgs a) {
   for (int y = blockIdx.y;; y += gridDim.y) {
     int s, nth;
     if (!find_seq(y, a.B, [&](int q) { return max(0, (logits_rows(a, q) + a.rows - 1) / a.rows); }, s, nth)) return;
-    const int r0 = a.node_off[s], n = a.node_off[s + 1] - r0;
+    const int r0 = a.node_off[s], n = a.node_off[s + 1] - r0, i0 = nth * a.rows, i1 = min(n, i0 + a.rows);
+    auto load = [&](LogitsBatch& b, int ib) {
+#pragma unroll
+      for (int u = 0; u < LG_BATCH; ++u) {  // (the last row again behind the end)
+        const size_t t = r0 + min(ib + u, i1 - 1);
+        const float* src = a.x + t * a.V + mine;
+        if (mine + 4 <= a.V) {
+          const f32x4_any v = *reinterpret_cast<const f32x4_any*>(src);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) b.x[u][e] = v[e];
+        } else {
+#pragma unroll
+          for (int e = 0; e < 4; ++e) b.x[u][e] = mine + e < a.V ? src[e] : 0.f;
+        }
+        b.words[u] = ~0u;
+        if (a.allowed && mine < a.V) b.words[u] = a.allowed[t * words + (mine >> 5)];
+      }
+    };
+    LogitsBatch even, odd;
+    load(even, i0);  // while the text is scanned
     const TreeParents par = load_parents(a.parent, r0, n);
     const bool ok = tree_valid(par, n);
     if (blockIdx.x == 0 && nth == 0 && tid == 0) a.status[s] = !ok;
     if (!ok) continue;  // uniform over the workgroup
-    const int i0 = nth * a.rows, i1 = min(n, i0 + a.rows);
 
     int seen[4] = {0, 0, 0, 0}, made[4] = {0, 0, 0, 0};
     float bias[4] = {0.f, 0.f, 0.f, 0.f}, rep = 1.f, freq = 0.f, pres = 0.f;
+    uint64_t below[2] = {0, 0};
     if (a.pen || a.bias_off) {
       for (int k = tid; k < LG_SLICE; k += LG_THREADS) seen_n[k] = made_n[k] = bias_at[k] = 0;
       __syncthreads();
@@ -95,12 +139,25 @@ __global__ __launch_bounds__(LG_THREADS) void tree_logits_kernel(LogitsArgs a) {
         rep = a.pen[3 * s], freq = a.pen[3 * s + 1], pres = a.pen[3 * s + 2];
         if (a.ctx) {
           const int c0 = a.ctx_off[s], c1 = a.ctx_off[s + 1], g0 = a.gen_start[s];
-          for (int k = c0 + tid; k < c1; k += LG_THREADS) {
-            const int v = a.ctx[k] - v0;
-            if (a.ctx[k] >= 0 && (unsigned)v < (unsigned)LG_SLICE) {
-              atomicAdd(&seen_n[v], 1);
-              if (k - c0 >= g0) atomicAdd(&made_n[v], 1);
+          for (int k0 = c0 + 4 * tid; k0 < c1; k0 += 16 * LG_THREADS) {  // 16 tokens of a thread together
+            i32x4_any t[4];
+#pragma unroll
+            for (int u = 0; u < 4; ++u) {
+              const int k = k0 + u * 4 * LG_THREADS;
+              if (k + 4 <= c1) t[u] = *reinterpret_cast<const i32x4_any*>(a.ctx + k);
+              else
+#pragma unroll
+                for (int e = 0; e < 4; ++e) t[u][e] = k + e < c1 ? a.ctx[k + e] : -1;
             }
+#pragma unroll
+            for (int u = 0; u < 4; ++u)
+#pragma unroll
+              for (int e = 0; e < 4; ++e) {
+                const int v = t[u][e] - v0;
+                if (t[u][e] < 0 || (unsigned)v >= (unsigned)LG_SLICE) continue;
+                atomicAdd(&seen_n[v], 1);
+                if (k0 + u * 4 * LG_THREADS + e - c0 >= g0) atomicAdd(&made_n[v], 1);
+              }
           }
         }
         if (wv == 0) {  // the drafts of this slice, and where they lie above a node
@@ -120,6 +177,14 @@ __global__ __launch_bounds__(LG_THREADS) void tree_logits_kernel(LogitsArgs a) {
           for (int h = 0; h < 2; ++h)
 #pragma unroll
             for (int k = 0; k < 4; ++k) above[lane + 64 * h][k] = (uint32_t)bits.w[k][h] & in[k];
+#pragma unroll
+          for (int h = 0; h < 2; ++h) {
+            uint32_t any = 0;
+#pragma unroll
+            for (int k = 0; k < 4; ++k) any |= (uint32_t)bits.w[k][h] & in[k];
+            const uint64_t b = __ballot(any != 0);
+            if (lane == 0) under[h] = b;
+          }
         }
       }
       if (a.bias_off) {
@@ -137,69 +202,74 @@ __global__ __launch_bounds__(LG_THREADS) void tree_logits_kernel(LogitsArgs a) {
         const int at = bias_at[4 * tid + e];
         if (at > 0) bias[e] = a.bias_val[a.bias_off[s] + at - 1];
       }
+      if (a.pen) below[0] = uniform(under[0]), below[1] = uniform(under[1]);
     }
-
-    for (int i = i0; i < i1; ++i) {
-      const size_t t = r0 + i;
-      const float* src = a.x + t * a.V + mine;
-      float x[4];
-      if (mine + 4 <= a.V) {
-        const f32x4_any v = *reinterpret_cast<const f32x4_any*>(src);
-#pragma unroll
-        for (int e = 0; e < 4; ++e) x[e] = v[e];
-      } else {
-#pragma unroll
-        for (int e = 0; e < 4; ++e) x[e] = mine + e < a.V ? src[e] : 0.f;
-      }
-      uint32_t may = mine < a.V ? 15u : 0u;
-      if (a.allowed && mine < a.V) may = a.allowed[t * words + (mine >> 5)] >> (mine & 31);
-#pragma unroll
-      for (int e = 0; e < 4; ++e)
-        if (mine + e >= a.V) may &= ~(1u << e);
-      if (a.pen) {
+    auto finish = [&](LogitsBatch& b, int ib) {
 #pragma clang fp contract(off)
-        int n_seen[4], n_made[4];
+      float(&x)[LG_BATCH][4] = b.x;
+      uint32_t may[LG_BATCH];
 #pragma unroll
-        for (int e = 0; e < 4; ++e) n_seen[e] = seen[e], n_made[e] = made[e];
+      for (int u = 0; u < LG_BATCH; ++u) {
+        const int i = ib + u;
+        may[u] = (b.words[u] >> (mine & 31)) & there;
+        if (a.pen) {
+          int n_seen[4], n_made[4];
 #pragma unroll
-        for (int k = 0; k < 4; ++k)
-          for (uint32_t b = above[i][k]; b; b &= b - 1) {
-            const int v = draft[32 * k + __builtin_ctz(b)];
+          for (int e = 0; e < 4; ++e) n_seen[e] = seen[e], n_made[e] = made[e];
+          if (i < i1 && (below[i >> 6] >> (i & 63)) & 1) {  // uniform, and rare
 #pragma unroll
-            for (int e = 0; e < 4; ++e)
-              if (v == 4 * tid + e) ++n_seen[e], ++n_made[e];
+            for (int k = 0; k < 4; ++k)
+              for (uint32_t m = __builtin_amdgcn_readfirstlane(above[i][k]); m; m &= m - 1) {
+                const int v = draft[32 * k + __builtin_ctz(m)];
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                  if (v == 4 * tid + e) ++n_seen[e], ++n_made[e];
+              }
           }
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          if (n_seen[e]) x[e] = x[e] > 0.f ? x[e] / rep : x[e] * rep;
-          const float f = freq * (float)n_made[e];
-          x[e] = x[e] - f;
-          x[e] = x[e] - (n_made[e] ? pres : 0.f);
+          for (int e = 0; e < 4; ++e) {
+            if (n_seen[e]) x[u][e] = x[u][e] > 0.f ? x[u][e] / rep : x[u][e] * rep;
+            const float f = freq * (float)n_made[e];
+            x[u][e] = x[u][e] - f;
+            x[u][e] = x[u][e] - (n_made[e] ? pres : 0.f);
+          }
         }
-      }
-      uint64_t top = 0;
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        if (a.bias_off) x[e] = x[e] + bias[e];
-        const bool yes = (may >> e) & 1;
-        if (!yes) x[e] = -INFINITY;
-        const uint64_t k = yes ? pick_key(x[e], mine + e) : 0;
-        top = k > top ? k : top;
-      }
-      if (a.out) {
-        float* dst = a.out + t * a.V + mine;
-        if (mine + 4 <= a.V) {
-          *reinterpret_cast<f32x4_any*>(dst) = f32x4_any{x[0], x[1], x[2], x[3]};
-        } else {
+        for (int e = 0; e < 4; ++e) {
+          if (a.bias_off) x[u][e] = x[u][e] + bias[e];
+          if (!((may[u] >> e) & 1)) x[u][e] = -INFINITY;
+        }
+        if (a.out && i < i1) {
+          float* dst = a.out + (size_t)(r0 + i) * a.V + mine;
+          if (mine + 4 <= a.V) {
+            *reinterpret_cast<f32x4_any*>(dst) = f32x4_any{x[u][0], x[u][1], x[u][2], x[u][3]};
+          } else {
 #pragma unroll
-          for (int e = 0; e < 4; ++e)
-            if (mine + e < a.V) dst[e] = x[e];
+            for (int e = 0; e < 4; ++e)
+              if (mine + e < a.V) dst[e] = x[u][e];
+          }
         }
       }
       if (a.argmax) {
-        top = wave_max(top);
-        if (lane == 0) best[i - i0][wv] = top;
+        float top[LG_BATCH], most[LG_BATCH];
+#pragma unroll
+        for (int u = 0; u < LG_BATCH; ++u) {
+          most[u] = fmaxf(fmaxf(x[u][0], x[u][1]), fmaxf(x[u][2], x[u][3]));
+          top[u] = wave_max(most[u]);
+        }
+#pragma unroll
+        for (int u = 0; u < LG_BATCH; ++u) {
+          const uint64_t k = wave_pick(x[u], may[u], mine, most[u], top[u]);
+          if (lane == 0 && ib + u < i1) best[ib + u - i0][wv] = k;
+        }
       }
+    };
+
+    for (int ib = i0; ib < i1; ib += 2 * LG_BATCH) {
+      if (ib + LG_BATCH < i1) load(odd, ib + LG_BATCH);
+      finish(even, ib);
+      if (ib + 2 * LG_BATCH < i1) load(even, ib + 2 * LG_BATCH);
+      if (ib + LG_BATCH < i1) finish(odd, ib + LG_BATCH);
     }
     __syncthreads();
     if (a.argmax)
@@ -220,14 +290,14 @@ __global__ __launch_bounds__(256) void logits_pick_kernel(LogitsArgs a, int slic
   const int lane = threadIdx.x & 63, w = blockIdx.x * 4 + (threadIdx.x >> 6);
   int s, i;
   if (!find_seq(w, a.B, [&](int q) { return max(0, logits_rows(a, q)); }, s, i)) return;
-  const int r0 = a.node_off[s], n = a.node_off[s + 1] - r0;
-  if (!tree_valid(load_parents(a.parent, r0, n), n)) return;
+  const int r0 = a.node_off[s];
+  if (a.status[s]) return;  // (as the launch before has found)
   uint64_t k = 0;
   for (int c = lane; c < slices; c += 64) {
     const uint64_t u = a.cand[(size_t)(r0 + i) * slices + c];
     k = u > k ? u : k;
   }
-  k = wave_max(k);
+  k = wave_max_key(k);
   if (lane == 0) a.argmax[r0 + i] = picked(k);
 }
 
@@ -242,10 +312,8 @@ int launch_tree_logits(const float* x, const int32_t* tok, const int32_t* parent
                        const int32_t* bias_tok, const float* bias_val, int n_bias, const int32_t* bias_off, const uint32_t* allowed,
                        float* out, int32_t* argmax, uint64_t* cand, int32_t* status, hipStream_t st) {
   const int slices = logits_slices(V);
-  // rows per workgroup: enough workgroups to fill the chip, few scans of the text
-  int rows = 8;
-  while (rows < 64 && (long)slices * T / rows > 4096) rows *= 2;
-  while (rows > 1 && (long)slices * T / rows < 512) rows /= 2;
+  // rows per workgroup: two workgroups per compute unit, and few scans of the text
+  const int rows = (int)std::min(std::max((long)slices * T / 512, 1l), (long)TRJ_N_MAX);
   const LogitsArgs a{x, tok, parent, node_off, B, T, V, ctx, ctx_off, gen_start, n_ctx, n_bias, pen, bias_tok, bias_val, bias_off, allowed,
                      out, argmax, cand, status, rows};
   const dim3 grid(slices, std::min((long)T / rows + B, 65535l));
