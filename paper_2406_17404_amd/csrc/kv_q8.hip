@@ -196,7 +196,7 @@ __device__ inline bool append_valid(const AppendArgs& a, int s, int L, int m) {
 __device__ inline int v_group_place(int g) { return g ^ ((g >> 3) & 3) ^ (((g >> 6) & 1) << 2); }
 
 template <int DH>
-__global__ __launch_bounds__(256, 3) void kv_append_kernel(AppendArgs a, int planes) {
+__global__ __launch_bounds__(256, 4) void kv_append_kernel(AppendArgs a, int planes) {
   constexpr int C8 = DH / 8, PASSES = 8 * C8 / 64, GROUPS = 2 * DH / 64;  // 16-byte groups of a page per lane
   __shared__ __align__(16) uint8_t tiles[4][32 * DH];
   const int lane = threadIdx.x & 63, wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);

@@ -15,7 +15,7 @@
 
 namespace trj {
 
-constexpr int LG_THREADS = 256, LG_SLICE = 4 * LG_THREADS, LG_BATCH = 4;
+constexpr int LG_THREADS = 256, LG_SLICE = 4 * LG_THREADS, LG_BATCH = 4, LG_WGS = 1024;
 typedef float f32x4_any __attribute__((ext_vector_type(4), aligned(4)));
 typedef int i32x4_any __attribute__((ext_vector_type(4), aligned(4)));  // rows of odd length start anywhere
 
@@ -55,32 +55,57 @@ __device__ inline uint64_t wave_max_key(uint64_t k) {
   }
   return k;
 }
-// The best of four tokens from `first` on, of all lanes; tokens that are not allowed are -infinity.  mine, top:
-// the largest of a lane and of all
-__device__ inline uint64_t wave_pick(const float (&x)[4], uint32_t may, int first, float mine, float top) {
-  if (top > -INFINITY) {  // the first lane that has it, of it the first token
-    const int at = first + (x[0] == top ? 0 : x[1] == top ? 1 : x[2] == top ? 2 : 3);
-    return pick_key(top, __builtin_amdgcn_readlane(at, __builtin_ctzll(__ballot(mine == top))));
+// The largest of all lanes for four values at once, NaN passed over while there is a number.  The four take turns,
+// which covers the two instructions that have to lie between a register's write and its move between lanes.
+__device__ inline void wave_max4(float (&x)[4]) {
+#define TRJ_STEP(MOVE)                                                                                    \
+  "v_max_f32_dpp %0, %0, %0 " MOVE "\n v_max_f32_dpp %1, %1, %1 " MOVE "\n v_max_f32_dpp %2, %2, %2 " MOVE \
+  "\n v_max_f32_dpp %3, %3, %3 " MOVE "\n "
+  asm("s_nop 1\n " TRJ_STEP("row_shr:1 row_mask:0xf bank_mask:0xf") TRJ_STEP("row_shr:2 row_mask:0xf bank_mask:0xf")
+          TRJ_STEP("row_shr:4 row_mask:0xf bank_mask:0xf") TRJ_STEP("row_shr:8 row_mask:0xf bank_mask:0xf")
+              TRJ_STEP("row_bcast:15 row_mask:0xa bank_mask:0xf") TRJ_STEP("row_bcast:31 row_mask:0xc bank_mask:0xf")
+      : "+v"(x[0]), "+v"(x[1]), "+v"(x[2]), "+v"(x[3]));
+#undef TRJ_STEP
+#pragma unroll
+  for (int u = 0; u < 4; ++u) x[u] = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(x[u]), 63));
+}
+// The best of 256 tokens from `first` on, lane l's those from first + 4 l; tokens that are not allowed are -infinity.
+// top: the largest of all.
+__device__ inline uint64_t wave_pick(const float (&x)[4], uint32_t may, int first, float top) {
+  if (top > -INFINITY) {  // the first token that has it
+    uint32_t at = ~0u;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const uint64_t have = __ballot(x[e] == top);
+      if (have) at = min(at, 4u * __builtin_ctzll(have) + e);
+    }
+    return pick_key(top, first + (int)at);
   }
   uint64_t k = 0;  // nothing but -infinity, NaN and what is not allowed
 #pragma unroll
   for (int e = 0; e < 4; ++e) {
-    const uint64_t u = (may >> e) & 1 ? pick_key(x[e], first + e) : 0;
+    const uint64_t u = (may >> e) & 1 ? pick_key(x[e], first + 4 * (int)(threadIdx.x & 63) + e) : 0;
     k = u > k ? u : k;
   }
   return wave_max_key(k);
+}
+// a where m's bits are set, b where not; all of them or none are
+__device__ inline float choose(uint32_t m, float a, float b) {
+  return __uint_as_float((m & __float_as_uint(a)) | (~m & __float_as_uint(b)));
 }
 __device__ inline uint64_t uniform(uint64_t x) {
   return (uint64_t)__builtin_amdgcn_readfirstlane((int)(x >> 32)) << 32 | (uint32_t)__builtin_amdgcn_readfirstlane((int)x);
 }
 __device__ inline int picked(uint64_t key) { return key == 0 ? -1 : (int)~(uint32_t)key; }
 
-// rows of sequence s, -1: malformed offsets
+// rows of sequence s, -1: malformed offsets.  All of them are asked for at once.
 __device__ inline int logits_rows(const LogitsArgs& a, int s) {
   const int r0 = a.node_off[s], r1 = a.node_off[s + 1];
-  bool bad = r0 < 0 || r1 < r0 || r1 > a.T || r1 - r0 > TRJ_N_MAX;
-  if (a.ctx && a.pen) bad = bad || a.ctx_off[s] < 0 || a.ctx_off[s + 1] < a.ctx_off[s] || a.ctx_off[s + 1] > a.n_ctx;
-  if (a.bias_off) bad = bad || a.bias_off[s] < 0 || a.bias_off[s + 1] < a.bias_off[s] || a.bias_off[s + 1] > a.n_bias;
+  int c0 = 0, c1 = 0, b0 = 0, b1 = 0;
+  if (a.ctx && a.pen) c0 = a.ctx_off[s], c1 = a.ctx_off[s + 1];
+  if (a.bias_off) b0 = a.bias_off[s], b1 = a.bias_off[s + 1];
+  const bool bad = (r0 < 0) | (r1 < r0) | (r1 > a.T) | (r1 - r0 > TRJ_N_MAX) | (c0 < 0) | (c1 < c0) | (c1 > a.n_ctx) | (b0 < 0) | (b1 < b0) |
+                   (b1 > a.n_bias);
   return bad ? -1 : r1 - r0;
 }
 
@@ -122,14 +147,15 @@ __global__ __launch_bounds__(LG_THREADS) void tree_logits_kernel(LogitsArgs a) {
         if (a.allowed && mine < a.V) b.words[u] = a.allowed[t * words + (mine >> 5)];
       }
     };
-    LogitsBatch even, odd;
-    load(even, i0);  // while the text is scanned
+    LogitsBatch next;
+    load(next, i0);  // while the text is scanned
     const TreeParents par = load_parents(a.parent, r0, n);
     const bool ok = tree_valid(par, n);
     if (blockIdx.x == 0 && nth == 0 && tid == 0) a.status[s] = !ok;
     if (!ok) continue;  // uniform over the workgroup
 
-    int seen[4] = {0, 0, 0, 0}, made[4] = {0, 0, 0, 0};
+    int made[4] = {0, 0, 0, 0};
+    uint32_t seen[4] = {0, 0, 0, 0};  // all bits or none
     float bias[4] = {0.f, 0.f, 0.f, 0.f}, rep = 1.f, freq = 0.f, pres = 0.f;
     uint64_t below[2] = {0, 0};
     if (a.pen || a.bias_off) {
@@ -197,50 +223,78 @@ __global__ __launch_bounds__(LG_THREADS) void tree_logits_kernel(LogitsArgs a) {
       __syncthreads();
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
-        seen[e] = seen_n[4 * tid + e];
+        seen[e] = seen_n[4 * tid + e] ? ~0u : 0u;
         made[e] = made_n[4 * tid + e];
         const int at = bias_at[4 * tid + e];
         if (at > 0) bias[e] = a.bias_val[a.bias_off[s] + at - 1];
       }
       if (a.pen) below[0] = uniform(under[0]), below[1] = uniform(under[1]);
     }
-    auto finish = [&](LogitsBatch& b, int ib) {
+    // x / rep from the rounded reciprocal, corrected twice with the exact remainder: the second correction rounds
+    // as the division does, as long as nothing leaves the range of normal numbers
+    const float one_rep = 1.f / rep;
+    const bool plain_rep = rep >= 0x1p-30f && rep <= 0x1p30f;
+    float freqs[4], press[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      freqs[e] = freq * (float)made[e];
+      press[e] = made[e] ? pres : 0.f;
+    }
+    for (int ib = i0; ib < i1; ib += LG_BATCH) {
 #pragma clang fp contract(off)
-      float(&x)[LG_BATCH][4] = b.x;
+      float x[LG_BATCH][4];
       uint32_t may[LG_BATCH];
 #pragma unroll
       for (int u = 0; u < LG_BATCH; ++u) {
         const int i = ib + u;
-        may[u] = (b.words[u] >> (mine & 31)) & there;
-        if (a.pen) {
-          int n_seen[4], n_made[4];
+        may[u] = (next.words[u] >> (mine & 31)) & there;
 #pragma unroll
-          for (int e = 0; e < 4; ++e) n_seen[e] = seen[e], n_made[e] = made[e];
-          if (i < i1 && (below[i >> 6] >> (i & 63)) & 1) {  // uniform, and rare
+        for (int e = 0; e < 4; ++e) x[u][e] = next.x[u][e];
+        if (a.pen && i < i1) {
+          uint32_t had[4];
+          float f[4], p[4];
+#pragma unroll
+          for (int e = 0; e < 4; ++e) had[e] = seen[e], f[e] = freqs[e], p[e] = press[e];
+          if ((below[i >> 6] >> (i & 63)) & 1) {  // uniform, and rare
+            int more[4] = {0, 0, 0, 0};
 #pragma unroll
             for (int k = 0; k < 4; ++k)
               for (uint32_t m = __builtin_amdgcn_readfirstlane(above[i][k]); m; m &= m - 1) {
                 const int v = draft[32 * k + __builtin_ctz(m)];
 #pragma unroll
-                for (int e = 0; e < 4; ++e)
-                  if (v == 4 * tid + e) ++n_seen[e], ++n_made[e];
+                for (int e = 0; e < 4; ++e) more[e] += v == 4 * tid + e;
+              }
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+              if (more[e]) {
+                had[e] = ~0u;
+                f[e] = freq * (float)(made_n[4 * tid + e] + more[e]);
+                p[e] = pres;
               }
           }
 #pragma unroll
           for (int e = 0; e < 4; ++e) {
-            if (n_seen[e]) x[u][e] = x[u][e] > 0.f ? x[u][e] / rep : x[u][e] * rep;
-            const float f = freq * (float)n_made[e];
-            x[u][e] = x[u][e] - f;
-            x[u][e] = x[u][e] - (n_made[e] ? pres : 0.f);
+            const float y = x[u][e];
+            float q = y * one_rep;
+            q = __builtin_fmaf(__builtin_fmaf(-q, rep, y), one_rep, q);
+            q = __builtin_fmaf(__builtin_fmaf(-q, rep, y), one_rep, q);
+            if (y > 0.f && !(plain_rep && y >= 0x1p-60f && y <= 0x1p60f)) q = y / rep;  // rare
+            x[u][e] = choose(had[e], y > 0.f ? q : y * rep, y) - f[e];
+            x[u][e] = x[u][e] - p[e];
           }
         }
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
           if (a.bias_off) x[u][e] = x[u][e] + bias[e];
-          if (!((may[u] >> e) & 1)) x[u][e] = -INFINITY;
+          x[u][e] = choose((uint32_t)((int)(may[u] << (31 - e)) >> 31), x[u][e], -INFINITY);
         }
-        if (a.out && i < i1) {
-          float* dst = a.out + (size_t)(r0 + i) * a.V + mine;
+      }
+      if (ib + LG_BATCH < i1) load(next, ib + LG_BATCH);
+      if (a.out)
+#pragma unroll
+        for (int u = 0; u < LG_BATCH; ++u) {
+          if (ib + u >= i1) break;
+          float* dst = a.out + (size_t)(r0 + ib + u) * a.V + mine;
           if (mine + 4 <= a.V) {
             *reinterpret_cast<f32x4_any*>(dst) = f32x4_any{x[u][0], x[u][1], x[u][2], x[u][3]};
           } else {
@@ -249,27 +303,18 @@ __global__ __launch_bounds__(LG_THREADS) void tree_logits_kernel(LogitsArgs a) {
               if (mine + e < a.V) dst[e] = x[u][e];
           }
         }
-      }
       if (a.argmax) {
-        float top[LG_BATCH], most[LG_BATCH];
+        float top[LG_BATCH];
+#pragma unroll
+        for (int u = 0; u < LG_BATCH; ++u) top[u] = fmaxf(fmaxf(x[u][0], x[u][1]), fmaxf(x[u][2], x[u][3]));
+        wave_max4(top);
 #pragma unroll
         for (int u = 0; u < LG_BATCH; ++u) {
-          most[u] = fmaxf(fmaxf(x[u][0], x[u][1]), fmaxf(x[u][2], x[u][3]));
-          top[u] = wave_max(most[u]);
-        }
-#pragma unroll
-        for (int u = 0; u < LG_BATCH; ++u) {
-          const uint64_t k = wave_pick(x[u], may[u], mine, most[u], top[u]);
-          if (lane == 0 && ib + u < i1) best[ib + u - i0][wv] = k;
+          if (ib + u >= i1) break;
+          const uint64_t k = wave_pick(x[u], may[u], v0 + 256 * wv, top[u]);
+          if (lane == 0) best[ib + u - i0][wv] = k;
         }
       }
-    };
-
-    for (int ib = i0; ib < i1; ib += 2 * LG_BATCH) {
-      if (ib + LG_BATCH < i1) load(odd, ib + LG_BATCH);
-      finish(even, ib);
-      if (ib + 2 * LG_BATCH < i1) load(even, ib + 2 * LG_BATCH);
-      if (ib + LG_BATCH < i1) finish(odd, ib + LG_BATCH);
     }
     __syncthreads();
     if (a.argmax)
@@ -312,8 +357,9 @@ int launch_tree_logits(const float* x, const int32_t* tok, const int32_t* parent
                        const int32_t* bias_tok, const float* bias_val, int n_bias, const int32_t* bias_off, const uint32_t* allowed,
                        float* out, int32_t* argmax, uint64_t* cand, int32_t* status, hipStream_t st) {
   const int slices = logits_slices(V);
-  // rows per workgroup: two workgroups per compute unit, and few scans of the text
-  const int rows = (int)std::min(std::max((long)slices * T / 512, 1l), (long)TRJ_N_MAX);
+  // rows per workgroup: the chip holds four workgroups per compute unit (half as many took 80 us instead of 57 for 16 x 64
+  // nodes over 32000 tokens, twice as many 62)
+  const int rows = (int)std::min(std::max((long)slices * T / LG_WGS, 1l), (long)TRJ_N_MAX);
   const LogitsArgs a{x, tok, parent, node_off, B, T, V, ctx, ctx_off, gen_start, n_ctx, n_bias, pen, bias_tok, bias_val, bias_off, allowed,
                      out, argmax, cand, status, rows};
   const dim3 grid(slices, std::min((long)T / rows + B, 65535l));
