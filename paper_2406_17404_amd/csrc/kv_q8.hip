@@ -152,6 +152,7 @@ int launch_block_tables(int32_t* block_table, int max_blocks, const int32_t* hel
 // Bound by memory for prompts (2 bytes read, 1 written per value), by a chain of latencies for a few rows
 // (lengths, page number, rows, codes), so a workgroup finds its page once for several heads and
 // layers, and no wavefront waits for another.
+typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
 struct AppendArgs {
   uint8_t* pool[2];
   float* scale[2];
@@ -191,6 +192,8 @@ __device__ inline bool append_valid(const AppendArgs& a, int s, int L, int m) {
   return __ballot(bad) == 0;
 }
 
+// the lowest n bytes of a word, all of them from 4 on
+__device__ inline uint32_t bytes_below(int n) { return n <= 0 ? 0u : n >= 4 ? ~0u : (1u << (8 * n)) - 1u; }
 // place of 16-byte group g of a V page in LDS: the columns that a wavefront writes at once would meet a quarter of
 // the banks
 __device__ inline int v_group_place(int g) { return g ^ ((g >> 3) & 3) ^ (((g >> 6) & 1) << 2); }
@@ -240,15 +243,27 @@ __global__ __launch_bounds__(256, 4) void kv_append_kernel(AppendArgs a, int pla
         for (int k = 0; k < GROUPS; ++k) had[k] = reinterpret_cast<const u32x4*>(pool)[k * 64 + ln];
       int e_old = Q8_MIN_EXP;
       if (old_rows > 0) e_old = q8_exp_of(*scale);
-      uint32_t top = 0;  // bits of the largest finite magnitude
+      // the largest magnitude, two rows' halves at a time; only a page with numbers that are not finite looks at
+      // them one by one
+      u16x2 pair = {0, 0};
 #pragma unroll
       for (int p = 0; p < PASSES; ++p)
 #pragma unroll
-        for (int i = 0; i < 16; ++i) {
-          const uint32_t w = raw[p][i >> 2][i & 3], lo = (w << 16) & 0x7fffffffu, hi = w & 0x7fff0000u;
-          top = max(top, max(lo < 0x7f800000u ? lo : 0u, hi < 0x7f800000u ? hi : 0u));
-        }
-      const int e = max(q8_exp(wave_max(top)), e_old);
+        for (int i = 0; i < 16; ++i) pair = __builtin_elementwise_max(pair, __builtin_bit_cast(u16x2, raw[p][i >> 2][i & 3] & 0x7fff7fffu));
+      uint32_t top = wave_max((uint32_t)max(pair[0], pair[1]) << 16);
+      const bool odd_ones = top >= 0x7f800000u;  // uniform
+      if (odd_ones) {
+        top = 0;
+#pragma unroll
+        for (int p = 0; p < PASSES; ++p)
+#pragma unroll
+          for (int i = 0; i < 16; ++i) {
+            const uint32_t w = raw[p][i >> 2][i & 3], lo = (w << 16) & 0x7fffffffu, hi = w & 0x7fff0000u;
+            top = max(top, max(lo < 0x7f800000u ? lo : 0u, hi < 0x7f800000u ? hi : 0u));
+          }
+        top = wave_max(top);
+      }
+      const int e = max(q8_exp(top), e_old);
       const float inv = q8_pow2(-e), ratio = q8_pow2(max(e_old - e, -126));
       const bool grew = old_rows > 0 && e > e_old;
       if (lane == 0) *scale = q8_pow2(e);
@@ -258,6 +273,16 @@ __global__ __launch_bounds__(256, 4) void kv_append_kernel(AppendArgs a, int pla
       };
 #pragma unroll
       for (int p = 0; p < PASSES; ++p) {
+        if (old_rows >= (p + 1) * 4 * 64 / C8 || end <= p * 4 * 64 / C8) {  // no new rows here (uniform)
+          if (which == 0 && grew && old_rows > p * 4 * 64 / C8)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              u32x2* const dst = reinterpret_cast<u32x2*>(pool + q8_k_off((p * 64 + ln) / C8 * 4 + i, c0));
+              const u32x2 o = *dst;
+              *dst = u32x2{lower(o[0]), lower(o[1])};
+            }
+          continue;
+        }
         const int q = (p * 64 + ln) / C8;  // rows 4q ..
         uint32_t code[4][2];
 #pragma unroll
@@ -265,9 +290,18 @@ __global__ __launch_bounds__(256, 4) void kv_append_kernel(AppendArgs a, int pla
 #pragma unroll
           for (int h = 0; h < 2; ++h) {
             const uint32_t u = raw[p][i][2 * h], v = raw[p][i][2 * h + 1];
-            code[i][h] = q8_codes(__uint_as_float(u << 16) * inv, __uint_as_float(u & 0xffff0000u) * inv) |
-                         q8_codes(__uint_as_float(v << 16) * inv, __uint_as_float(v & 0xffff0000u) * inv) << 16;
+            int c = __builtin_amdgcn_cvt_pk_fp8_f32(__uint_as_float(u << 16) * inv, __uint_as_float(u & 0xffff0000u) * inv, 0, false);
+            code[i][h] = __builtin_amdgcn_cvt_pk_fp8_f32(__uint_as_float(v << 16) * inv, __uint_as_float(v & 0xffff0000u) * inv, c, true);
           }
+        if (odd_ones)
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+              const uint32_t u = raw[p][i][2 * h], v = raw[p][i][2 * h + 1];
+              code[i][h] = q8_codes(__uint_as_float(u << 16) * inv, __uint_as_float(u & 0xffff0000u) * inv) |
+                           q8_codes(__uint_as_float(v << 16) * inv, __uint_as_float(v & 0xffff0000u) * inv) << 16;
+            }
         if (which == 0) {
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
@@ -288,30 +322,30 @@ __global__ __launch_bounds__(256, 4) void kv_append_kernel(AppendArgs a, int pla
             *reinterpret_cast<uint32_t*>(tile + v_group_place(g) * 16 + (q >> 1) * 4) = ab | cd << 16;
           }
         }
-        __builtin_amdgcn_sched_barrier(0);  // one pass after the other: registers
       }
       if (which == 1) {
+        uint32_t is_new[4], is_old[4];  // bytes of a group's words: rows 8d + 4 ((ln / 32) % 2) ..
+#pragma unroll
+        for (int d = 0; d < 4; ++d) {
+          const int r = 8 * d + 4 * ((ln >> 5) & 1);
+          const uint32_t below_old = bytes_below(old_rows - r), below_end = bytes_below(end - r);
+          is_old[d] = below_old;
+          is_new[d] = below_end & ~below_old;
+        }
+        if (grew)
+#pragma unroll
+          for (int k = 0; k < GROUPS; ++k)
+#pragma unroll
+            for (int d = 0; d < 4; ++d) had[k][d] = (lower(had[k][d]) & is_old[d]) | (had[k][d] & ~is_old[d]);
         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // this wavefront's words, which it reads itself
 #pragma unroll
         for (int k = 0; k < GROUPS; ++k) {
           const int g = k * 64 + ln;
-          const u32x4 fresh = *reinterpret_cast<const u32x4*>(tile + v_group_place(g) * 16);
-          u32x4 put = fresh;
+          u32x4 put = *reinterpret_cast<const u32x4*>(tile + v_group_place(g) * 16);
           if (keeps)
 #pragma unroll
-            for (int d = 0; d < 4; ++d) {  // rows 8d + 4 ((g / 32) % 2) ..
-              uint32_t is_new = 0, is_old = 0;
-#pragma unroll
-              for (int i = 0; i < 4; ++i) {
-                const int r = 8 * d + 4 * ((g >> 5) & 1) + i;
-                if (r < old_rows) is_old |= 0xffu << (8 * i);
-                else if (r < end) is_new |= 0xffu << (8 * i);
-              }
-              const uint32_t kept = grew ? lower(had[k][d]) : had[k][d];
-              put[d] = (fresh[d] & is_new) | (kept & is_old) | (had[k][d] & ~(is_new | is_old));
-            }
+            for (int d = 0; d < 4; ++d) put[d] = (put[d] & is_new[d]) | (had[k][d] & ~is_new[d]);
           reinterpret_cast<u32x4*>(pool)[g] = put;
-          __builtin_amdgcn_sched_barrier(0);
         }
         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // read before the next page's are written
       }
