@@ -373,9 +373,10 @@ int launch_kv_append_q8(void* k_pool, void* v_pool, float* k_scale, float* v_sca
                      n_kv_heads, n_blocks, new_len, status};
   // all rows: a sequence touches at most two pages more than its rows fill; a path mostly one or two
   const int pages = path ? 2 * B : T / TRJ_KV_BLOCK + 2 * B, planes = 2 * n_layers * n_kv_heads;
-  // several planes per wavefront where there are more than the chip holds wavefronts of: what finds the page is
-  // then done once for them
-  const int each = (int)std::min(std::max((long)pages * planes / 6144, 1l), 8l);
+  // several planes per wavefront where there are more than the 4096 wavefronts that the chip holds at a time: what
+  // finds the page is then done once for them (16 accepted paths, 32 layers, 8 heads: one plane 32 us, two 26, three or
+  // four 23, five to eight 25 to 27)
+  const int each = (int)std::min(std::max((long)pages * planes / 4096, 1l), 8l);
   const dim3 grid(pages, std::min((planes + 4 * each - 1) / (4 * each), 65535));
   if (head_dim == 128) kv_append_kernel<128><<<grid, 256, 0, st>>>(a, planes);
   else kv_append_kernel<64><<<grid, 256, 0, st>>>(a, planes);
