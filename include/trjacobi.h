@@ -391,7 +391,8 @@ int32_t kv_block_tables(int32_t* block_table, int32_t max_blocks, const int32_t*
  * the earlier codes are rounded to it (exact down to the type's subnormal values).  Codes
  * round to nearest, ties to even.  A value that is not finite is stored as NaN and has no part
  * in the scale.  Slots of a page behind the last row keep their bytes.
- * new_len[s] = prefix_len[s] + rows stored.  Repeating a call changes nothing.
+ * new_len[s] = prefix_len[s] + rows stored, in a buffer that must not overlap prefix_len
+ * (TRJ_ERR_BAD_SHAPE).  Repeating a call changes nothing.
  * Pools: n_layers of the layout above, one behind the other; rows of layer l start
  * l * row_layer_stride elements behind layer 0's (a multiple of 8).
  * Nothing is stored, new_len = prefix_len and status 1: accept_len[s] < 0 or >= N_s, a path
@@ -447,7 +448,7 @@ int32_t tree_logits_workspace_bytes(int32_t B, int32_t T, int32_t V, size_t* h_b
  * ids outside [0, V) are passed over in ctx, tok and bias_tok.
  * Parts may be left out: ctx NULL (with ctx_off, gen_start): the drafts are the only text; penalties
  * NULL: none, ctx and tok are not looked at; bias_off NULL; allowed NULL.  n_ctx, n_bias: how many tokens
- * ctx, and entries bias_tok and bias_val, hold.
+ * ctx, and entries bias_tok and bias_val, hold, at most 2^30 (TRJ_ERR_BAD_SHAPE).
  * logits_out: [T][V], may be logits itself, NULL if only predictions are wanted; argmax_out[T], may
  * be NULL (not both): the lowest index of the largest value among the allowed tokens, NaN below all
  * numbers (of nothing but NaN the first), -1 if the mask allows none, which no draft

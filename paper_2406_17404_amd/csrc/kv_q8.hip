@@ -166,15 +166,13 @@ struct AppendArgs {
 // rows to store of sequence s; -1: the sequence is refused
 __device__ inline int append_rows(const AppendArgs& a, int s) {
   const int L = a.prefix_len[s], r0 = a.node_off[s], r1 = a.node_off[s + 1];
-  if (L < 0 || r0 < 0 || r1 < r0 || r1 > a.T) return -1;
-  const int n = r1 - r0;
-  int m = n;
-  if (a.path) {
-    const int acc = a.accept_len[s];
-    if (n > TRJ_N_MAX || acc < 0 || acc >= n) return -1;
-    m = acc + 1;
-  }
-  return (long)L + m > (long)a.max_blocks * TRJ_KV_BLOCK ? -1 : m;
+  int acc = 0;
+  if (a.path) acc = a.accept_len[s];
+  bool bad = (L < 0) | (r0 < 0) | (r1 < r0) | (r1 > a.T);
+  const int n = bad ? 0 : r1 - r0;
+  if (a.path) bad |= (n > TRJ_N_MAX) | (acc < 0) | (acc >= n);
+  const int m = a.path && !bad ? acc + 1 : n;
+  return bad || (long)L + m > (long)a.max_blocks * TRJ_KV_BLOCK ? -1 : m;
 }
 __device__ inline int pages_touched(int L, int m) {
   return m <= 0 ? 0 : (L + m - 1) / TRJ_KV_BLOCK - L / TRJ_KV_BLOCK + 1;
@@ -184,7 +182,18 @@ __device__ inline bool append_valid(const AppendArgs& a, int s, int L, int m) {
   const int lane = threadIdx.x & 63;
   bool bad = false;
   const int p0 = L / TRJ_KV_BLOCK, p1 = p0 + pages_touched(L, m);
-  for (int p = p0 + lane; p < p1; p += 64) bad = bad || (unsigned)a.block_table[(size_t)s * a.max_blocks + p] >= (unsigned)a.n_blocks;
+  const int32_t* const table = a.block_table + (size_t)s * a.max_blocks;
+  if (p1 - p0 <= 64) {
+    if (p0 + lane < p1) bad = (unsigned)table[p0 + lane] >= (unsigned)a.n_blocks;
+  } else {  // long prompts: eight entries of a lane are asked for together
+    for (int p = p0; p < p1; p += 512) {
+      int pages[8];
+#pragma unroll
+      for (int u = 0; u < 8; ++u) pages[u] = table[min(p + 64 * u + lane, p1 - 1)];
+#pragma unroll
+      for (int u = 0; u < 8; ++u) bad |= (unsigned)pages[u] >= (unsigned)a.n_blocks;
+    }
+  }
   if (a.path) {
     const int n = a.node_off[s + 1] - a.node_off[s];
     for (int j = lane; j < m; j += 64) bad = bad || (unsigned)a.path[(size_t)s * TRJ_N_MAX + j] >= (unsigned)n;
@@ -377,7 +386,7 @@ int launch_kv_append_q8(void* k_pool, void* v_pool, float* k_scale, float* v_sca
   // finds the page is then done once for them (16 accepted paths, 32 layers, 8 heads: one plane 32 us, two 26, three or
   // four 23, five to eight 25 to 27)
   const int each = (int)std::min(std::max((long)pages * planes / 4096, 1l), 8l);
-  const dim3 grid(pages, std::min((planes + 4 * each - 1) / (4 * each), 65535));
+  const dim3 grid(std::min(pages, 1 << 20), std::min((planes + 4 * each - 1) / (4 * each), 65535));
   if (head_dim == 128) kv_append_kernel<128><<<grid, 256, 0, st>>>(a, planes);
   else kv_append_kernel<64><<<grid, 256, 0, st>>>(a, planes);
   return check_launch();

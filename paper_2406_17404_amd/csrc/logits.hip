@@ -109,7 +109,7 @@ __device__ inline int logits_rows(const LogitsArgs& a, int s) {
   return bad ? -1 : r1 - r0;
 }
 
-__global__ __launch_bounds__(LG_THREADS) void tree_logits_kernel(LogitsArgs a) {
+__global__ __launch_bounds__(LG_THREADS, 4) void tree_logits_kernel(LogitsArgs a) {
   __shared__ int seen_n[LG_SLICE], made_n[LG_SLICE], bias_at[LG_SLICE];
   __shared__ __align__(16) uint32_t above[TRJ_N_MAX][4];  // drafts of this slice on the path to a node
   __shared__ uint64_t under[2];             // nodes below such drafts

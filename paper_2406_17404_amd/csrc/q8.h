@@ -73,22 +73,30 @@ __device__ inline float wave_max(float x) {  // NaN is passed over while there i
   return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(x), 63));
 }
 // The sequence that owns item x when sequence s has count(s) items, and which of its items it is; false
-// behind the last item.  Every wavefront by itself, 64 sequences a round, uniform answers.
+// behind the last item.  Every wavefront by itself, 128 sequences a round, uniform answers.
 template <class F>
 __device__ inline bool find_seq(int x, int B, F count, int& s, int& nth) {
   const int lane = threadIdx.x & 63;
   int base = 0;
-  for (int s0 = 0; s0 < B; s0 += 64) {
-    const int c = s0 + lane < B ? count(s0 + lane) : 0;
-    const int upto = base + wave_scan(c);
-    const uint64_t here = __ballot(x < upto);
-    if (here) {
-      const int l = __builtin_ctzll(here);
-      s = s0 + l;
-      nth = x - (__builtin_amdgcn_readlane(upto, l) - __builtin_amdgcn_readlane(c, l));
-      return true;
+  for (int s0 = 0; s0 < B; s0 += 128) {
+    int c[2];
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {  // both asked for together
+      const int q = s0 + 64 * u + lane, n = count(min(q, B - 1));
+      c[u] = q < B ? n : 0;
     }
-    base = __builtin_amdgcn_readlane(upto, 63);
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+      const int upto = base + wave_scan(c[u]);
+      const uint64_t here = __ballot(x < upto);
+      if (here) {
+        const int l = __builtin_ctzll(here);
+        s = s0 + 64 * u + l;
+        nth = x - (__builtin_amdgcn_readlane(upto, l) - __builtin_amdgcn_readlane(c[u], l));
+        return true;
+      }
+      base = __builtin_amdgcn_readlane(upto, 63);
+    }
   }
   return false;
 }

@@ -54,6 +54,7 @@ int32_t kv_append_q8(void* k_pool, void* v_pool, float* k_scale, float* v_scale,
       (head_dim != 64 && head_dim != 128) || bad_stride(row_stride, n_kv_heads * (int64_t)head_dim) ||
       (row_layer_stride & 7) || !on16(k_pool) || !on16(v_pool) || !on16(k_rows) || !on16(v_rows))
     return TRJ_ERR_BAD_SHAPE;
+  if (new_len < prefix_len + B && prefix_len < new_len + B) return TRJ_ERR_BAD_SHAPE;
   return launch_kv_append_q8(k_pool, v_pool, k_scale, v_scale, k_rows, v_rows, row_stride, row_layer_stride, path,
                              accept_len, node_off, block_table, max_blocks, prefix_len, B, T, n_layers, n_kv_heads, head_dim,
                              n_blocks, new_len, status_dev, (hipStream_t)stream);
@@ -124,7 +125,7 @@ int32_t tree_logits(const float* logits, const int32_t* tok, const int32_t* pare
       (bias_off && (!bias_tok || !bias_val)) || (!logits_out && !argmax_out) || !workspace || !status_dev)
     return TRJ_ERR_NULLPTR;
   TRJ_TRY(check_logits(B, T, V));
-  if ((ctx && n_ctx < 0) || (bias_off && n_bias < 0)) return TRJ_ERR_BAD_SHAPE;
+  if ((ctx && (n_ctx < 0 || n_ctx > 1 << 30)) || (bias_off && (n_bias < 0 || n_bias > 1 << 30))) return TRJ_ERR_BAD_SHAPE;
   const size_t skip = (16 - ((uintptr_t)workspace & 15)) & 15;
   if (ws_bytes < skip || ws_bytes - skip < tree_logits_ws_bytes(T, V)) return TRJ_ERR_WORKSPACE_TOO_SMALL;
   return launch_tree_logits(logits, tok, parent, node_off, B, T, V, ctx, n_ctx, ctx_off, gen_start, penalties, bias_tok, bias_val,

@@ -51,6 +51,34 @@ def test_all_rows(dh, heads, layers, lens, sizes):
     check(cache, *rows_of(rng, layers, int(off[-1]) + 2, heads, dh), off, wide=8 * (lens[0] % 3))
 
 
+@pytest.mark.parametrize("dh", [64, 128])
+@pytest.mark.parametrize("L", [3, 8, 15, 16, 17, 20, 31])
+@pytest.mark.parametrize("n,std", [(1, 100.0), (1, 0.01), (7, 30.0), (14, 1e-3)])
+def test_pages_that_fill_up_while_their_scales_grow_or_stay(dh, L, n, std):
+    rng = np.random.default_rng(L * 100 + n)
+    cache = Paged(rng, [L, L + 32], 2, dh, room=40)
+    check(cache, *rows_of(rng, 1, 2 * n, 2, dh, std), offsets_of([n, n]))
+
+
+@pytest.mark.parametrize("n", [65 * 32, 520 * 32 + 7])
+@pytest.mark.parametrize("bad", [None, 0, -1])
+def test_long_prompts(n, bad):
+    rng = np.random.default_rng(n)
+    cache = Paged(rng, [20, 5], 1, 64, room=n)
+    if bad is not None:  # one page that does not exist, of all that rows go to: nothing is stored
+        cache.table[0, bad if bad == 0 else (20 + n - 1) // 32] = cache.n_blocks
+    status = check(cache, *rows_of(rng, 1, n + 3, 1, 64), offsets_of([n, 3]))
+    assert list(status) == [bad is not None, 0]
+
+
+@pytest.mark.parametrize("B", [64, 65, 128, 129, 300])
+def test_many_sequences(B):
+    rng = np.random.default_rng(B)
+    sizes = rng.choice([0, 1, 3], B)
+    cache = Paged(rng, rng.choice([0, 1, 31, 40], B), 1, 64, room=4)
+    check(cache, *rows_of(rng, 1, int(sum(sizes)) + 1, 1, 64), offsets_of(sizes))
+
+
 @pytest.mark.parametrize("seed", range(6))
 def test_accepted_paths(seed):
     rng = np.random.default_rng(50 + seed)

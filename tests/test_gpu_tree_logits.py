@@ -170,6 +170,31 @@ def test_repeated_and_foreign_tokens():
     c.check()
 
 
+@pytest.mark.parametrize("rep", [1.5, 1.0, 2.0 ** -30, 2.0 ** 30, 1e-12, 1e12, 0.0, float("inf")])
+@pytest.mark.parametrize("masked", [False, True])
+def test_quotients_of_numbers_of_any_size(rep, masked):
+    """Seen tokens from the smallest subnormal to infinity: bit for bit what a division gives."""
+    rng = np.random.default_rng(11)
+    c = Call(rng, [9, 3], 1100, [200, 5], masked=masked)
+    seen = np.unique(c.ctx[0][c.ctx[0] < 1100])
+    size = np.ldexp(rng.uniform(1, 2, (9, len(seen))), rng.integers(-149, 127, (9, len(seen))))
+    c.x[:9, seen] = (size * rng.choice([-1, 1], size.shape)).astype(np.float32)
+    c.x[3, seen[:4]] = [0.0, -0.0, np.inf, -np.inf]
+    c.x[4, seen[0]] = np.nan
+    c.x[5, :] = 3.0  # nothing unusual in this row
+    c.pen[:, 0] = rep
+    args = c.device()
+    b.tree_logits(*args)
+    torch.cuda.synchronize()
+    out, best = args[12].cpu().numpy(), args[13].cpu().numpy()
+    with np.errstate(all="ignore"):
+        for s in range(2):
+            r = slice(c.off[s], c.off[s + 1])
+            y, picks = c.want(s, np.float32)
+            assert np.array_equal(out[r], y, equal_nan=True), np.argwhere(~((out[r] == y) | np.isnan(y)))[:4]
+            assert np.array_equal(best[r], picks)
+
+
 @pytest.mark.parametrize("gen", [-5, 0, 59, 60, 1000])
 def test_where_generation_starts(gen):
     c = Call(np.random.default_rng(9), [4], 200, [60])

@@ -29,7 +29,7 @@ def test_tables(change, status):
 
 
 APPEND = dict(k=P, v=P, ks=P, vs=P, kr=P, vr=P, stride=1024, layer=1 << 20, path=None, acc=None, off=P, table=P, max_blocks=8,
-              prefix=P, B=4, T=9, layers=2, heads=8, dh=128, n_blocks=64, dtype=b.BF16, new_len=P, status=P)
+              prefix=P, B=4, T=9, layers=2, heads=8, dh=128, n_blocks=64, dtype=b.BF16, new_len=2 * P, status=P)
 
 
 @pytest.mark.parametrize("change,status", [
@@ -37,7 +37,8 @@ APPEND = dict(k=P, v=P, ks=P, vs=P, kr=P, vr=P, stride=1024, layer=1 << 20, path
     (dict(dtype=b.F32), DTYPE), (dict(dtype=9), DTYPE), (dict(dh=96), SHAPE), (dict(dh=32), SHAPE), (dict(T=0), SHAPE),
     (dict(layers=0), SHAPE), (dict(layers=40000), SHAPE), (dict(heads=0), SHAPE), (dict(heads=70000), SHAPE),
     (dict(stride=1016), SHAPE), (dict(stride=1028), SHAPE), (dict(layer=4), SHAPE), (dict(kr=P + 8), SHAPE),
-    (dict(v=P + 2), SHAPE), (dict(n_blocks=0), SHAPE), (dict(B=5000), SHAPE), (dict(max_blocks=0), SHAPE)])
+    (dict(v=P + 2), SHAPE), (dict(n_blocks=0), SHAPE), (dict(B=5000), SHAPE), (dict(max_blocks=0), SHAPE),
+    (dict(new_len=P), SHAPE), (dict(new_len=P + 12), SHAPE), (dict(new_len=P - 12), SHAPE)])
 def test_append(change, status):
     assert call("kv_append_q8", list(APPEND), APPEND, **change) == status
 
@@ -67,6 +68,7 @@ LOGITS = dict(x=P, tok=P, parent=P, off=P, B=4, T=9, V=32000, ctx=P, n_ctx=7, ct
     (dict(x=None), NULL), (dict(tok=None), NULL), (dict(ctx_off=None), NULL), (dict(gen=None), NULL), (dict(bv=None), NULL),
     (dict(out=None, argmax=None), NULL), (dict(ws=None), NULL), (dict(status=None), NULL), (dict(V=0), SHAPE),
     (dict(V=1 << 25), SHAPE), (dict(T=0), SHAPE), (dict(T=513), TREE), (dict(n_ctx=-1), SHAPE), (dict(n_bias=-1), SHAPE),
+    (dict(n_ctx=(1 << 30) + 1), SHAPE), (dict(n_bias=(1 << 30) + 1), SHAPE),
     (dict(B=4097, T=4097), SHAPE), (dict(ws_bytes=8), WS)])
 def test_logits(change, status):
     assert call("tree_logits", list(LOGITS), LOGITS, **change) == status
