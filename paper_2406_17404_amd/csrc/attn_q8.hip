@@ -5,8 +5,8 @@
 //
 // The work is streaming the sequence's codes once.  All query heads of a K/V head are worked on
 // together: query p of a sequence is (node p / G, head p % G of the group).  A workgroup owns a
-// contiguous range of 32-key blocks of one (sequence, K/V head) and NTW tiles of 32 queries;
-// wavefront (key stream, tile) walks every KS-th block for one tile:
+// contiguous range of 32-key blocks of one (sequence, K/V head) and NT tiles of 32 queries; each of its
+// KS wavefronts is a key stream, which walks every KS-th block for all of them:
 //   S^T[keys, queries] = K[keys, dh] * Q^T          (v_mfma_f32_32x32x16_bf16)
 //   O^T[dh, queries]  += V^T[dh, keys] * P^T[keys, queries]
 // A page is laid out so that 16 contiguous bytes per lane are two such A operands; codes times their
@@ -15,6 +15,12 @@
 // error 2^-9 each, independent) and the result.
 // Cached blocks come first in a range, then the blocks of the tree's own rows, which are bf16
 // in the order the projection left them; only these and the last cached page need a mask.
+//
+// Bound by memory for long prefixes: 64 rows over 32768 slots, 32 heads of 128, read 268 MB in 65 us = 4.1 TB/s (a
+// large copy moves 4.8 to 5.1, a bare read 7.1), 16 sequences of 4096 at most 361 MB in 100 us, with 43 GFLOP of
+// products.  For few rows by the way of a workgroup from the lengths over the
+// table and the scales to its first codes and, over the merge of its streams, to the result: one row over 500
+// slots takes 11 us, of which the cached blocks themselves take 2.4.
 //
 // How the keys are split is decided on the device, where the lengths are: every workgroup scans the
 // sequences (64 per round), works out the same plan and finds its own part of it.

@@ -66,12 +66,6 @@ __device__ inline uint32_t wave_max(uint32_t x) {
 #undef TRJ_STEP
   return (uint32_t)__builtin_amdgcn_readlane((int)x, 63);
 }
-__device__ inline float wave_max(float x) {  // NaN is passed over while there is a number
-#define TRJ_STEP(MOVE, ROWS) x = fmaxf(x, __int_as_float(moved<MOVE, ROWS>((int)0xff800000u, __float_as_int(x))));
-  TRJ_WAVE_STEPS(TRJ_STEP)
-#undef TRJ_STEP
-  return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(x), 63));
-}
 // The sequence that owns item x when sequence s has count(s) items, and which of its items it is; false
 // behind the last item.  Every wavefront by itself, 128 sequences a round, uniform answers.
 template <class F>
