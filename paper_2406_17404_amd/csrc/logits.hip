@@ -9,10 +9,10 @@
 // how the compiler joins them.
 // Bytes: 4 V read and, where they are kept, 4 V written per row.  Rows come in batches of four, asked for together,
 // the first while the text is scanned.  69 rows over 128256 tokens, 71 MB, take 29 us = 2.4 TB/s; 16 x 64 rows over 32000
-// tokens without output, 131 MB, 57 us = 2.3 TB/s: some 130 vector instructions per row and wavefront are half of
-// that time, and the loads wait for them more than they overlap.  (One more batch on its way at a time cost more
-// registers than the chip has for four workgroups per compute unit: 59 to 83 us; a wavefront per row and 1024
-// tokens 66 us.)
+// tokens without output, 131 MB, 57 us = 2.3 TB/s, 45 of it without any rule.  Some 130 vector instructions per row and
+// wavefront are 28 us of that; a quarter fewer of them gained nothing (60 us: rows under drafts apart), nor did one more
+// batch on its way (59; with more registers than four workgroups per compute unit have, 80), nor a wavefront per row
+// and 1024 tokens (66).
 #include <algorithm>
 
 #include "kernels.h"

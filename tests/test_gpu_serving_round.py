@@ -102,3 +102,59 @@ def test_rounds(dh, n_blocks):
         assert np.array_equal(d["new_len"].cpu().numpy(), new_len) and np.array_equal(status[4].cpu().numpy(), bad)
         prefix = new_len
     assert max(prefix) > 4
+
+
+def test_a_round_captured_into_a_graph():
+    """Replayed from a state that it has changed, with other lengths, and between eager rounds: every replay is the
+    eager round from the same state."""
+    rng = np.random.default_rng(21)
+    B, layers, kv_heads, heads, dh, V, width, n_blocks = 3, 2, 2, 8, 64, 1500, 8, 40
+    size = [7, 1, 40]
+    off, T = offsets_of(size), sum(size)
+    parent = i32(np.concatenate([I.tree_random(n, rng) for n in size]))
+    q, kr, vr = (bf16(rng.normal(size=(layers, T, h, dh))).to(DEV) for h in (heads, kv_heads, kv_heads))
+    x, tok, node_off = to_dev((rng.normal(size=(T, V)) * 3).astype(np.float32)), i32(rng.integers(0, V, T)), i32(off)
+    ctx, ctx_off, gen = i32(rng.integers(0, V, 60)), i32([0, 10, 40, 60]), i32([4, 4, 4])
+    pen = to_dev(np.tile(np.array([[1.3, 0.2, 0.1]], np.float32), (B, 1)))
+    pool, scale = ([torch.full((layers, kv_heads, n_blocks) + s, v, dtype=t, device=DEV) for _ in "kv"]
+                   for s, t, v in (((32 * dh,), torch.uint8, 0x38), ((), torch.float32, 1.0)))
+    table, held, count, prefix = i32(np.full((B, width), -1)), ints(B), i32([n_blocks]), i32([0] * B)
+    free = i32(np.arange(n_blocks))
+    held.zero_()
+    held2, count2, new_len, slot, argmax = ints(B), ints(1), ints(B), ints(T), ints(T)
+    out, y = torch.zeros_like(q), torch.zeros_like(x)
+    acc, best, path, bonus, status = ints(B), ints(B), ints((B, 128)), ints(B), [ints(B) for _ in range(4)]
+    ws = torch.empty(b.tree_attention_q8_workspace_bytes(B, T, heads, kv_heads, dh, width * 32), dtype=torch.uint8, device=DEV)
+    lws = torch.empty(b.tree_logits_workspace_bytes(B, T, V), dtype=torch.uint8, device=DEV)
+    state = [*pool, *scale, table, held, count, prefix, free]
+    results = [slot, out, y, argmax, acc, path, new_len, *status, *state]
+
+    def a_round():
+        b.kv_block_tables(table, held, prefix, node_off, T, free, count, held2, count2, slot, status[0])
+        for l in range(layers):
+            b.tree_attention_q8(q[l], pool[0][l], pool[1][l], scale[0][l], scale[1][l], kr[l], vr[l], parent, node_off, table, prefix,
+                                width * 32, dh ** -0.5, ws, out[l], status[1])
+        b.tree_logits(x, tok, parent, node_off, ctx, ctx_off, gen, pen, None, None, None, None, y, argmax, lws, status[2])
+        b.accept_path(None, tok, parent, node_off, B, T, V, argmax, acc, best, path, bonus, status[3])
+        b.kv_append_q8(*pool, *scale, kr, vr, path, acc, node_off, table, prefix, new_len, status[3])
+        held.copy_(held2)
+        count.copy_(count2)
+        prefix.copy_(new_len)
+
+    a_round()
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        a_round()
+    for _ in range(4):
+        start = [t.clone() for t in state]
+        a_round()
+        want = [t.clone() for t in results]
+        torch.cuda.synchronize()
+        for t, s in zip(state, start):
+            t.copy_(s)
+        g.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(t, w) for t, w in zip(results, want))
+        assert not status[0].any() and not status[3].any()
+    assert (prefix >= 5).all()
