@@ -8,8 +8,8 @@
 // Every step is rounded by itself (no fused multiply-add), so that a prediction does not depend on
 // how the compiler joins them.
 // Bytes: 4 V read and, where they are kept, 4 V written per row.  Rows come in batches of four, asked for together,
-// the first while the text is scanned.  69 rows over 128256 tokens, 71 MB, take 29 us = 2.4 TB/s; 16 x 64 rows over 32000
-// tokens without output, 131 MB, 57 us = 2.3 TB/s, 45 of it without any rule.  Some 130 vector instructions per row and
+// the first while the text is scanned.  69 rows over 128256 tokens, 72 MB, take 24 us = 3.0 TB/s; 16 x 64 rows over 32000
+// tokens without output, 135 MB, 56 us = 2.4 TB/s, 45 of it without any rule.  Some 130 vector instructions per row and
 // wavefront are 28 us of that; a quarter fewer of them gained nothing (60 us: rows under drafts apart), nor did one more
 // batch on its way (59; with more registers than four workgroups per compute unit have, 80), nor a wavefront per row
 // and 1024 tokens (66).
@@ -135,7 +135,8 @@ __global__ __launch_bounds__(LG_THREADS, 4) void tree_logits_kernel(LogitsArgs a
   for (int y = blockIdx.y;; y += gridDim.y) {
     int s, nth;
     if (!find_seq(y, a.B, [&](int q) { return max(0, (logits_rows(a, q) + a.rows - 1) / a.rows); }, s, nth)) return;
-    const int r0 = a.node_off[s], n = a.node_off[s + 1] - r0, i0 = nth * a.rows, i1 = min(n, i0 + a.rows);
+    const int r0 = a.node_off[s], n = a.node_off[s + 1] - r0, parts = (n + a.rows - 1) / a.rows,
+              per = (n + parts - 1) / parts, i0 = min(n, nth * per), i1 = min(n, i0 + per);  // even parts
     auto load = [&](LogitsBatch& b, int ib) {
 #pragma unroll
       for (int u = 0; u < LG_BATCH; ++u) {  // (the last row again behind the end)
@@ -363,9 +364,10 @@ int launch_tree_logits(const float* x, const int32_t* tok, const int32_t* parent
                        const int32_t* bias_tok, const float* bias_val, int n_bias, const int32_t* bias_off, const uint32_t* allowed,
                        float* out, int32_t* argmax, uint64_t* cand, int32_t* status, hipStream_t st) {
   const int slices = logits_slices(V);
-  // rows per workgroup: the chip holds four workgroups per compute unit (half as many took 80 us instead of 57 for 16 x 64
-  // nodes over 32000 tokens, twice as many 62)
-  const int rows = (int)std::min(std::max((long)slices * T / LG_WGS, 1l), (long)TRJ_N_MAX);
+  // rows per workgroup, at most: the chip holds four workgroups per compute unit, and none is to wait for another to end
+  // (rounded down instead, 69 nodes over 128256 tokens took 29 us instead of 24; half as many workgroups 80 us instead
+  // of 56 for 16 x 64 nodes over 32000 tokens, twice as many 62)
+  const int rows = (int)std::min(((long)slices * T + LG_WGS - 1) / LG_WGS, (long)TRJ_N_MAX);
   const LogitsArgs a{x, tok, parent, node_off, B, T, V, ctx, ctx_off, gen_start, n_ctx, n_bias, pen, bias_tok, bias_val, bias_off, allowed,
                      out, argmax, cand, status, rows};
   const dim3 grid(slices, std::min((long)T / rows + B, 65535l));
