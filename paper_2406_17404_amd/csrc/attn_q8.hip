@@ -319,7 +319,7 @@ __device__ __forceinline__ void request(const void* base, uint32_t lane16, uint3
         "s_add_u32 m0, %2, 0x400\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %4, %1\n\t"
         "s_add_u32 m0, %2, 0x800\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %5, %1\n\t"
         "s_add_u32 m0, %2, 0xc00\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %6, %1\n"
-        "1:" ::"v"(lane16), "s"(base), "s"(lds), "s"(yes), "v"(lane16 + 1024), "v"(lane16 + 2048), "v"(lane16 + 3072)
+        "1:" ::"v"(lane16), "s"(base), "s"(lds), "s"(yes), "v"(lane16 + 1024), "v"(lane16 + 2 * 1024), "v"(lane16 + 3 * 1024)
         : "memory", "m0", "scc");
   else
     asm volatile(
