@@ -157,7 +157,8 @@ int launch_block_tables(int32_t* block_table, int max_blocks, const int32_t* hel
 // 4096 rows of 32 heads of 128, 101 MB, take 27 us = 3.7 TB/s; the paths of 16 sequences with 6 rows each in 32 layers of 8
 // heads 23 us, of which their 34 MB of V pages (read and written whole) would need 7; one row 5.7.
 // The vector unit's work counts too: with every magnitude and every code checked by itself, and both halves of a page
-// worked on whether rows go there or not, the paths took 42 us and the prompt 32.
+// worked on whether rows go there or not, the paths took 42 us and the prompt 32.  (A plane asked for while the one
+// before it is worked on costs a third of the wavefronts their registers: 29 to 33 us for the paths, 31 for the prompt.)
 typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
 struct AppendArgs {
   uint8_t* pool[2];
@@ -239,9 +240,9 @@ __global__ __launch_bounds__(256, 4) void kv_append_kernel(AppendArgs a, int pla
       asm("" : "+v"(ln));  // offsets are worked out again for every plane, not held in registers
       const int c0 = ln % C8 * 8;
       const int which = pl & 1, head = (pl >> 1) % a.n_kv_heads, layer = (pl >> 1) / a.n_kv_heads;
-      const size_t pln = ((size_t)layer * a.n_kv_heads + head) * a.n_blocks + page;
-      float* const scale = a.scale[which] + pln;
-      uint8_t* const pool = a.pool[which] + pln * 32 * DH;
+      const size_t plane = ((size_t)layer * a.n_kv_heads + head) * a.n_blocks + page;
+      float* const scale = a.scale[which] + plane;
+      uint8_t* const pool = a.pool[which] + plane * 32 * DH;
       const uint16_t* const src = a.rows[which] + layer * a.row_layer_stride + (size_t)head * DH + c0;
       u32x4 raw[PASSES][4];
 #pragma unroll
