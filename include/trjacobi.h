@@ -368,9 +368,11 @@ int32_t tr_jacobi_generate(const trj_model_desc* desc, const trj_weights* weight
  *    behind those it holds.  Where the pages do not last for sequence s and all before it,
  *    it gets none: status_dev[s] = 1, it keeps what it holds, and so does every sequence behind it
  *    that wants more.
+ * The table entries that a sequence with status 1 wanted behind those it holds become -1: pages that
+ * it gave back from there may be another's by now, and kv_append_q8 refuses rows that would go there.
  * held_out[B], free_count_out[1]: the new counts; row_slot[T]: the slot of every row (page
  * number * 32 + position % 32), -1 for rows of sequences with status 1.
- * Also status 1, and unchanged: negative or descending sizes, more than max_blocks pages wanted
+ * Also status 1, with what it holds unchanged: negative or descending sizes, more than max_blocks pages wanted
  * or held, rows outside [0, T).  A free_count outside [0, n_blocks] counts as 0.
  * free_list has n_blocks entries, the number of pages there are; what would be stacked beyond them
  * (pages held twice) is dropped.  Page numbers are copied, not judged.  Nothing that a call reads is
@@ -397,8 +399,10 @@ int32_t kv_block_tables(int32_t* block_table, int32_t max_blocks, const int32_t*
  * l * row_layer_stride elements behind layer 0's (a multiple of 8).
  * Nothing is stored, new_len = prefix_len and status 1: accept_len[s] < 0 or >= N_s, a path
  * entry outside [0, N_s), N_s > TRJ_N_MAX with a path, rows outside [0, T), a negative size, more than
- * max_blocks pages, a page number outside [0, n_blocks).  Two sequences (or two entries
- * of one) must not name the same page where rows are stored: the result is undefined. */
+ * max_blocks pages, a page number outside [0, n_blocks).  Rows go to the pages that the table names: they have to
+ * be among those that kv_block_tables was last asked to hold, since entries behind these may be pages that the
+ * sequence gave back.  Two sequences (or two entries of one) must not name the same page where rows are
+ * stored: the result is undefined. */
 int32_t kv_append_q8(void* k_pool, void* v_pool, float* k_scale, float* v_scale, const void* k_rows,
                      const void* v_rows, int32_t row_stride, size_t row_layer_stride,
                      const int32_t* path, const int32_t* accept_len, const int32_t* node_off,

@@ -70,10 +70,12 @@ def block_tables(table, held, prefix, off, T, free, count, n_blocks):
     """Returns table, held, free list, count, row slots, status as they are afterwards."""
     table, free = table.copy(), free.copy()
     B, width = table.shape
-    status, held_out, want = np.zeros(B, int), held.copy(), np.zeros(B, int)
+    status, held_out, want, wish = np.zeros(B, int), held.copy(), np.zeros(B, int), np.zeros(B, int)
     for s in range(B):
         n = int(off[s + 1]) - int(off[s])
         want[s] = -(-(int(prefix[s]) + n) // PAGE)
+        if n >= 0 and prefix[s] >= 0 and 0 <= held[s] <= width:
+            wish[s] = min(want[s], width)
         if n < 0 or off[s] < 0 or off[s + 1] > T or prefix[s] < 0 or not 0 <= held[s] <= width or want[s] > width:
             status[s], want[s] = 1, held[s]
     stack = [int(free[i]) for i in range(count)] if 0 <= count <= n_blocks else []
@@ -95,6 +97,9 @@ def block_tables(table, held, prefix, off, T, free, count, n_blocks):
         for j in range(held[s], want[s]):
             table[s, j] = stack.pop()
         held_out[s] = want[s]
+    for s in range(B):
+        if status[s]:  # what it wanted beyond what it holds is nowhere
+            table[s, max(held[s], 0):wish[s]] = -1
     slot = np.full(T, -1)
     for s in range(B):
         if status[s] == 0:

@@ -18,6 +18,11 @@ constexpr int TABLES_THREADS = 256;
 struct SeqPages {  // of one sequence
   int held, want, bad;
 };
+// of a sequence that need not be well-formed: the table entries that its positions reach
+__device__ inline int pages_wanted(const int32_t* prefix_len, const int32_t* node_off, int max_blocks, int s) {
+  const long rows = node_off[s + 1] - (long)node_off[s], L = prefix_len[s];
+  return rows < 0 || L < 0 ? 0 : (int)min((L + rows + TRJ_KV_BLOCK - 1) / TRJ_KV_BLOCK, (long)max_blocks);
+}
 __device__ inline SeqPages seq_pages(const int32_t* held, const int32_t* prefix_len, const int32_t* node_off, int T,
                                      int max_blocks, int s) {
   const int h = held[s], L = prefix_len[s], r0 = node_off[s], r1 = node_off[s + 1];
@@ -35,9 +40,9 @@ __global__ __launch_bounds__(TABLES_THREADS) void block_tables_kernel(
   int* need_at = smem;
   int* give_at = smem + B + 1;
   __shared__ int part[2][TABLES_THREADS / 64];
-  __shared__ int mono;
+  __shared__ int mono, any_bad;
   const int tid = threadIdx.x, lane = tid & 63, wv = tid >> 6;
-  if (tid == 0) mono = 1;
+  if (tid == 0) mono = 1, any_bad = 0;
   int base_need = 0, base_give = 0;
   for (int s0 = 0; s0 < B; s0 += TABLES_THREADS) {
     const int s = s0 + tid;
@@ -48,6 +53,7 @@ __global__ __launch_bounds__(TABLES_THREADS) void block_tables_kernel(
     __syncthreads();
     if (lane == 63) part[0][wv] = a, part[1][wv] = b;
     if (s < B && node_off[s + 1] < node_off[s]) mono = 0;
+    if (p.bad) any_bad = 1;
     __syncthreads();
     int before_need = base_need, before_give = base_give;
 #pragma unroll
@@ -86,11 +92,11 @@ __global__ __launch_bounds__(TABLES_THREADS) void block_tables_kernel(
   auto served = [&](int s, const SeqPages& p) { return !p.bad && (p.want <= p.held || need_at[s + 1] <= have); };
   const int first = blockIdx.x * TABLES_THREADS + tid, step = gridDim.x * TABLES_THREADS;
   const int needed = base_need, given = have - have0;
-  // pages taken: entry x of the list belongs to its sequence if all of that sequence's entries are there
-  for (int x = first; x < min(needed, have); x += step) {
-    const int s = owner(need_at, x);
-    if (need_at[s + 1] > have) continue;
-    block_table[(size_t)s * max_blocks + held[s] + (x - need_at[s])] = stacked(have - 1 - x);
+  // pages taken: entry x of the list belongs to its sequence if all of that sequence's entries are there; else no page
+  // is where it wanted one, not the one that the sequence gave back from there earlier and another may own
+  for (unsigned x = first; x < (unsigned)needed; x += step) {
+    const int s = owner(need_at, (int)x);
+    block_table[(size_t)s * max_blocks + held[s] + (x - need_at[s])] = need_at[s + 1] <= have ? stacked(have - 1 - (int)x) : -1;
   }
   for (int x = first; x < given; x += step) free_list[have0 + x] = stacked(have0 + x);
   for (int t = first; t < T; t += step) {
@@ -123,6 +129,13 @@ __global__ __launch_bounds__(TABLES_THREADS) void block_tables_kernel(
     held_out[s] = served(s, p) ? p.want : p.held;
     status[s] = !served(s, p);
   }
+  if (any_bad)  // nor are there pages for what is malformed: rare, so all threads look for it together
+    for (int s = 0; s < B; ++s) {
+      const SeqPages p = seq_pages(held, prefix_len, node_off, T, max_blocks, s);
+      if (!p.bad || p.held < 0) continue;
+      const unsigned end = pages_wanted(prefix_len, node_off, max_blocks, s);
+      for (unsigned j = (unsigned)p.held + first; j < end; j += step) block_table[(size_t)s * max_blocks + j] = -1;
+    }
   if (first == 0) {
     int taken = needed;  // the sequences up to the first without room
     if (needed > have) {
