@@ -346,7 +346,8 @@ int32_t tr_jacobi_generate(const trj_model_desc* desc, const trj_weights* weight
  *   K: ((c/32 * 2 + c%32/16) * 32 + r) * 16 + c%16
  *   V: ((c/32 * 2 + r/4%2) * 32 + c%32) * 16 + r/16 * 8 + r/8%2 * 4 + r%4
  * block_table[B][max_blocks]: position p of sequence s is slot p % 32 of page
- * block_table[s][p / 32].  Entries behind a sequence's length are not read.
+ * block_table[s][p / 32].  Entries behind a sequence's length are not read.  Positions are int32 to the end of their
+ * page: where max_blocks is more than 2^26 - 1, a sequence can still hold no more than these.
  *
  * Rows (q_rows, k_rows, v_rows): [T][heads][head_dim] in `dtype` with *_stride elements from
  * row to row (a part of a wider row, as a common projection of q, k and v leaves it),

@@ -5,6 +5,7 @@ only.  Layouts are spelled out slot by slot."""
 import numpy as np
 
 PAGE = 32
+MAX_PAGES = (2 ** 31 - 1) // PAGE  # positions are int32, to the end of their page
 MIN_EXP = -100
 
 
@@ -76,7 +77,7 @@ def block_tables(table, held, prefix, off, T, free, count, n_blocks):
         want[s] = -(-(int(prefix[s]) + n) // PAGE)
         if n >= 0 and prefix[s] >= 0 and 0 <= held[s] <= width:
             wish[s] = min(want[s], width)
-        if n < 0 or off[s] < 0 or off[s + 1] > T or prefix[s] < 0 or not 0 <= held[s] <= width or want[s] > width:
+        if n < 0 or off[s] < 0 or off[s + 1] > T or prefix[s] < 0 or not 0 <= held[s] <= width or want[s] > min(width, MAX_PAGES):
             status[s], want[s] = 1, held[s]
     stack = [int(free[i]) for i in range(count)] if 0 <= count <= n_blocks else []
     for s in range(B):
@@ -126,7 +127,7 @@ def append(k_pool, v_pool, k_scale, v_scale, k_rows, v_rows, path, accept, off, 
                 picked = [int(i) for i in path[s][:accept[s] + 1]]
                 ok = all(0 <= i < n for i in picked)
         m = len(picked)
-        ok = ok and L + m <= table.shape[1] * PAGE
+        ok = ok and L + m <= min(table.shape[1], MAX_PAGES) * PAGE
         pages = range(L // PAGE, (L + m - 1) // PAGE + 1) if ok and m else range(0)
         ok = ok and all(0 <= table[s, p] < n_blocks for p in pages)
         if not ok:

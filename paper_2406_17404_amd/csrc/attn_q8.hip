@@ -59,7 +59,7 @@ __device__ inline Q8Seq q8_seq(const Q8Args& a, int s) {
   q.L = L;
   q.nodes = r0 < 0 || r1 < r0 || r1 > a.T ? -1 : r1 - r0;
   if (q.nodes <= 0) return q;
-  const bool fits = L >= 0 && L <= a.max_prefix && L <= (long)a.max_blocks * 32 && q.nodes <= TRJ_N_MAX;
+  const bool fits = L >= 0 && L <= a.max_prefix && L <= q8_pages_at_most(a.max_blocks) * 32 && q.nodes <= TRJ_N_MAX;
   if (!fits) q.L = -1;
   q.blocks = fits ? q.cached() + (q.nodes + 31) / 32 : 1;
   return q;

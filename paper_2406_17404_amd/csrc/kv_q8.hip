@@ -27,7 +27,8 @@ __device__ inline SeqPages seq_pages(const int32_t* held, const int32_t* prefix_
                                      int max_blocks, int s) {
   const int h = held[s], L = prefix_len[s], r0 = node_off[s], r1 = node_off[s + 1];
   const long want = ((long)L + (r1 - (long)r0) + TRJ_KV_BLOCK - 1) / TRJ_KV_BLOCK;
-  const bool bad = h < 0 || h > max_blocks || L < 0 || r0 < 0 || r1 < r0 || r1 > T || want > max_blocks;
+  const bool bad = h < 0 || h > max_blocks || L < 0 || r0 < 0 || r1 < r0 || r1 > T ||
+                   want > q8_pages_at_most(max_blocks);
   return bad ? SeqPages{h, h, 1} : SeqPages{h, (int)want, 0};
 }
 
@@ -192,7 +193,7 @@ __device__ inline int append_rows(const AppendArgs& a, int s) {
   const int n = bad ? 0 : r1 - r0;
   if (a.path) bad |= (n > TRJ_N_MAX) | (acc < 0) | (acc >= n);
   const int m = a.path && !bad ? acc + 1 : n;
-  return bad || (long)L + m > (long)a.max_blocks * TRJ_KV_BLOCK ? -1 : m;
+  return bad || (long)L + m > (long)q8_pages_at_most(a.max_blocks) * TRJ_KV_BLOCK ? -1 : m;
 }
 __device__ inline int pages_touched(int L, int m) {
   return m <= 0 ? 0 : (L + m - 1) / TRJ_KV_BLOCK - L / TRJ_KV_BLOCK + 1;

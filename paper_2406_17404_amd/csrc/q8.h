@@ -6,6 +6,10 @@
 namespace trj {
 
 constexpr int Q8_MIN_EXP = -100;  // of a scale
+// Positions and slots are int32, and so are those up to the end of their page: a table may be wider than this, a
+// sequence may not be longer.
+constexpr int Q8_MAX_PAGES = INT32_MAX / TRJ_KV_BLOCK;
+__host__ __device__ inline int q8_pages_at_most(int max_blocks) { return max_blocks < Q8_MAX_PAGES ? max_blocks : Q8_MAX_PAGES; }
 
 __host__ __device__ inline int q8_k_off(int r, int c) { return ((c >> 4) * 32 + r) * 16 + (c & 15); }
 __host__ __device__ inline int q8_v_off(int r, int c) {

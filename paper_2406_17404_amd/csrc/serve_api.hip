@@ -2,6 +2,7 @@
 #include <cstdint>
 
 #include "kernels.h"
+#include "q8.h"
 
 using namespace trj;
 
@@ -11,11 +12,8 @@ using namespace trj;
     if (rc_ != TRJ_OK) return rc_; \
   } while (0)
 
-// page numbers times the slots of a page are int32
-static const int MAX_PAGES = INT32_MAX / TRJ_KV_BLOCK;
-
 static int check_serve_batch(int B, int T, int max_blocks, int n_blocks) {
-  if (B < 1 || B > TRJ_SERVE_MAX_SEQS || T < 0 || max_blocks < 1 || n_blocks < 1 || n_blocks > MAX_PAGES ||
+  if (B < 1 || B > TRJ_SERVE_MAX_SEQS || T < 0 || max_blocks < 1 || n_blocks < 1 || n_blocks > Q8_MAX_PAGES ||
       (int64_t)B * max_blocks > INT32_MAX)
     return TRJ_ERR_BAD_SHAPE;
   return TRJ_OK;
