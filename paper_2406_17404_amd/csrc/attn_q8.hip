@@ -144,9 +144,15 @@ struct Q8Plan {
     const float rounds = ceilf(n * (1.f / RESIDENT));
     const float whole = START + c, even = START + work * __builtin_amdgcn_rcpf(n);
     float cost = (rounds > 1.f ? fmaxf(whole, rounds * even) : whole) + (parts > 0.f ? MERGE : 0.f);
-    if (parts > a.max_parts) cost = 1e6f;
-    const uint32_t best = wave_min((uint32_t)fminf(cost * 8.f, 60e6f) << 6 | lane);
+    if (parts > a.max_parts) cost = INFINITY;  // no room for its partials
+    const uint32_t best = wave_min((uint32_t)fminf(cost * 8.f, 60e6f) << 6 | lane);  // (of equals the fewest splits)
     chunk = lane_value(c, best & 63);
+    // Up to 2^16 blocks ceil(b / c) is exact as above: off by at most 33 * 1.5 * 2^-23 where the next whole number is
+    // 2^-17 away.  Beyond, whole numbers decide whether the partials have room.
+    if (longest > 1 << 16) {
+      const int k = splits(mine);
+      if (wave_sum(k > 1 ? (float)groups * (float)k : 0.f) > a.max_parts) chunk = longest;
+    }
   }
   __device__ inline int splits(const Q8Seq& q) const { return (q.blocks + chunk - 1) / chunk; }
   // item x of all, of which every (sequence, query group, K/V head) counts its splits, or, TILES > 0, once per
