@@ -79,6 +79,10 @@ __device__ inline T lane_value(T v, int lane) { return (T)__builtin_amdgcn_readl
 // index order, and chunks of an even share.
 constexpr float START = 24.f, MERGE = 16.f, RESIDENT = 256.f;  // one workgroup per compute unit at a time
 constexpr int MAX_PARTS = 512;  // partials that a call may leave to the merge
+// Blocks that a split has at least where it is not weighed: beyond 64 sequences, and with so many workgroups that only
+// what would outlast them is split.  Sequences of no more are never split, so a call without longer ones has neither
+// partials nor a merge.
+constexpr int LEAST_SPLIT = 16;
 struct Q8Work {  // of an item
   Q8Seq seq;
   int s, nth, splits, part0;  // nth item of sequence s; its first partial
@@ -100,7 +104,7 @@ struct Q8Plan {
     work *= a.n_kv_heads;
     id = lane;
     if (MANY) {  // (a split sequence has at most twice its share of parts)
-      chunk = (int)fminf(fmaxf(ceilf(work * (1.0001f * 2 / MAX_PARTS)), 16.f), 1e9f);
+      chunk = (int)fminf(fmaxf(ceilf(work * (1.0001f * 2 / MAX_PARTS)), (float)LEAST_SPLIT), 1e9f);
       return;
     }
     int longest = 0;
@@ -128,7 +132,7 @@ struct Q8Plan {
     const float items = wave_sum((float)groups);
     if (items >= RESIDENT) {  // enough workgroups: only what would outlast them all is split
       const float share = work * (1.0001f * 2 / MAX_PARTS);
-      chunk = longest > 2.f * share + START ? (int)ceilf(fmaxf(share, 16.f)) : longest;
+      chunk = longest > 2.f * share + START ? (int)ceilf(fmaxf(share, (float)LEAST_SPLIT)) : longest;
       return;
     }
     const int c = (longest + (lane & 31)) / ((lane & 31) + 1);
@@ -864,7 +868,7 @@ static Q8Launch q8_launch(int B, int T, int group, int n_kv_heads, int max_prefi
   p.ntw = queries > 32 ? 2 : 1;
   const long items = ((long)T * group / (32 * p.ntw) + B) * n_kv_heads;  // unsplit
   const long most = ((long)max_prefix + 31) / 32 + TRJ_N_MAX / 32;       // blocks of a sequence
-  p.max_parts = most <= MERGE ? 0 : MAX_PARTS;
+  p.max_parts = most <= LEAST_SPLIT ? 0 : MAX_PARTS;
   p.grid = (int)std::min(items + p.max_parts, 1l << 30);
   p.tiles = (int)std::min(items * p.ntw, 64l);
   return p;
