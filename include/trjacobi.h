@@ -421,7 +421,8 @@ int32_t tree_attention_q8_workspace_bytes(int32_t B, int32_t T, int32_t n_heads,
  * v_rows (which the cache need not hold).  A sequence of one row is plain decoding, a chain of rows a
  * causal pass.  out: [T][n_heads][head_dim].  A key that a row does not see has no part in it
  * whatever it holds, infinities and NaN included; a row that sees a value that is not finite
- * gets what the sums give.  max_prefix: host upper bound of prefix_len[s].
+ * gets what the sums give.  max_prefix: host upper bound of prefix_len[s].  scale: positive, and a
+ * finite fp32 number when multiplied by log2(e), else TRJ_ERR_BAD_SHAPE.
  * Rows of zeros and status 1: malformed tree (as trj_tree_mask), more than TRJ_N_MAX rows,
  * prefix_len[s] outside [0, max_prefix] or beyond max_blocks pages; nothing and status 1: rows outside [0, T).
  * NaN in all rows and status 1: a page number outside [0, n_blocks).

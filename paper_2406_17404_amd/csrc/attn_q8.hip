@@ -909,7 +909,7 @@ int launch_tree_attn_q8(const uint16_t* q, int q_stride, const void* k_pool, con
   float* const pm = ws + tiles * 32 * head_dim;
   const Q8Args a{q, k_rows, v_rows, (const uint8_t*)k_pool, (const uint8_t*)v_pool, k_scale, v_scale, parent, node_off,
                  block_table, prefix_len, q_stride, row_stride, max_blocks, B, T, n_kv_heads, group, n_blocks, max_prefix,
-                 p.max_parts, scale * 1.4426950408889634f, ws, pm, pm + tiles * 32, out, status};
+                 p.max_parts, scale * LOG2E, ws, pm, pm + tiles * 32, out, status};
   if (B > 64) return head_dim == 128 ? q8_run_tiles<128, true>(a, p, st) : q8_run_tiles<64, true>(a, p, st);
   return head_dim == 128 ? q8_run_tiles<128, false>(a, p, st) : q8_run_tiles<64, false>(a, p, st);
 }

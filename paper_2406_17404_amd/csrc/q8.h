@@ -6,6 +6,7 @@
 namespace trj {
 
 constexpr int Q8_MIN_EXP = -100;  // of a scale
+constexpr float LOG2E = 1.4426950408889634f;
 // Positions and slots are int32, and so are those up to the end of their page: a table may be wider than this, a
 // sequence may not be longer.
 constexpr int Q8_MAX_PAGES = INT32_MAX / TRJ_KV_BLOCK;

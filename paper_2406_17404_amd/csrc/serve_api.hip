@@ -86,7 +86,8 @@ int32_t tree_attention_q8(const void* q_rows, int32_t q_stride, const void* k_po
   if (dtype != TRJ_BF16) return TRJ_ERR_BAD_DTYPE;
   TRJ_TRY(check_attention(B, T, n_heads, n_kv_heads, head_dim, max_prefix));
   TRJ_TRY(check_serve_batch(B, T, max_blocks, n_blocks));
-  if (!(scale > 0.f) || !(scale < INFINITY) || bad_stride(q_stride, n_heads * (int64_t)head_dim) ||
+  // scores are worked out to base 2
+  if (!(scale > 0.f) || !(scale * LOG2E < INFINITY) || bad_stride(q_stride, n_heads * (int64_t)head_dim) ||
       bad_stride(row_stride, n_kv_heads * (int64_t)head_dim) || !on16(q_rows) || !on16(k_pool) || !on16(v_pool) ||
       !on16(k_rows) || !on16(v_rows) || !on16(out))
     return TRJ_ERR_BAD_SHAPE;
