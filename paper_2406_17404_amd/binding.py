@@ -356,6 +356,13 @@ def _rows(t: torch.Tensor):
     return t.data_ptr(), row, (st[0] if len(sh) == 4 and sh[0] > 1 else row * sh[-3])
 
 
+def _check_pools(k_pool, v_pool, k_scale, v_scale, pages, head_dim):
+    """pages: of all layers and heads."""
+    codes = pages * KV_BLOCK * head_dim
+    if k_pool.nbytes != codes or v_pool.nbytes != codes or k_scale.nbytes != 4 * pages or v_scale.nbytes != 4 * pages:
+        raise ValueError("pools (8 bits), scales (32 bits) and rows are not of the same layers, heads and pages")
+
+
 def kv_block_tables(block_table, held, prefix_len, node_off, T, free_list, free_count, held_out, free_count_out,
                     row_slot, status_dev):
     B, max_blocks = block_table.shape
@@ -377,9 +384,9 @@ def kv_append_q8(k_pool, v_pool, k_scale, v_scale, k_rows, v_rows, path, accept_
         raise ValueError("k_rows and v_rows are laid out alike")
     n_layers = k_rows.shape[0] if k_rows.dim() == 4 else 1
     T, heads, head_dim = k_rows.shape[-3:]
-    if heads != n_kv_heads or k_pool.numel() != n_layers * n_kv_heads * n_blocks * KV_BLOCK * head_dim or \
-            v_pool.numel() != k_pool.numel() or v_scale.shape != k_scale.shape:
-        raise ValueError("pools, scales and rows are not of the same layers, heads and pages")
+    if heads != n_kv_heads:
+        raise ValueError("rows are not of the pool's heads")
+    _check_pools(k_pool, v_pool, k_scale, v_scale, n_layers * n_kv_heads * n_blocks, head_dim)
     _check("kv_append_q8", lib().kv_append_q8(
         _ptr(k_pool), _ptr(v_pool), _ptr(k_scale), _ptr(v_scale), kp, vp, stride, layer_stride, _ptr(path),
         _ptr(accept_len), _ptr(node_off), _ptr(block_table), max_blocks, _ptr(prefix_len), B, T, n_layers, n_kv_heads,
@@ -406,9 +413,9 @@ def tree_attention_q8(q_rows, k_pool, v_pool, k_scale, v_scale, k_rows, v_rows, 
     if k_rows.shape != (T, n_kv_heads, head_dim) or v_rows.shape != k_rows.shape or stride != v_stride or \
             k_rows.dtype != q_rows.dtype or v_rows.dtype != q_rows.dtype or out.dtype != q_rows.dtype:
         raise ValueError("k_rows and v_rows are laid out alike, of q_rows' type and the pool's heads")
-    if k_pool.numel() != n_kv_heads * n_blocks * KV_BLOCK * head_dim or v_pool.numel() != k_pool.numel() or \
-            v_scale.shape != k_scale.shape or out.shape != q_rows.shape:
-        raise ValueError("pools, scales, rows and out are not of the same heads and pages")
+    _check_pools(k_pool, v_pool, k_scale, v_scale, n_kv_heads * n_blocks, head_dim)
+    if out.shape != q_rows.shape:
+        raise ValueError("out is laid out like q_rows")
     _check("tree_attention_q8", lib().tree_attention_q8(
         qp, q_stride, _ptr(k_pool), _ptr(v_pool), _ptr(k_scale), _ptr(v_scale), kp, vp, stride, _ptr(parent),
         _ptr(node_off), _ptr(block_table), max_blocks, _ptr(prefix_len), B, T, n_heads, n_kv_heads, head_dim, n_blocks,
@@ -426,6 +433,10 @@ def tree_logits(logits, tok, parent, node_off, ctx, ctx_off, gen_start, penaltie
                 allowed, logits_out, argmax_out, workspace, status_dev):
     T, V = logits.shape
     B = node_off.shape[0] - 1
+    if logits.dtype != torch.float32 or (logits_out is not None and logits_out.nbytes < 4 * T * V):
+        raise ValueError("logits and logits_out are fp32 of the same shape")
+    if allowed is not None and allowed.nbytes < 4 * T * ((V + 31) // 32):
+        raise ValueError("allowed has ceil(V / 32) words of 32 bits per row")
     _check("tree_logits", lib().tree_logits(
         _ptr(logits), _ptr(tok), _ptr(parent), _ptr(node_off), B, T, V, _ptr(ctx), 0 if ctx is None else ctx.numel(),
         _ptr(ctx_off), _ptr(gen_start),
