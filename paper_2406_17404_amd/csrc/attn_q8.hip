@@ -11,16 +11,17 @@
 //   O^T[dh, queries]  += V^T[dh, keys] * P^T[keys, queries]
 // A page is laid out so that 16 contiguous bytes per lane are two such A operands; codes times their
 // power-of-two scale are bf16 numbers, exactly, in one instruction per two (v_cvt_scalef32_pk_bf16_fp8),
-// so what is rounded to 16 bits is what the 16-bit attention rounds: the weights w (relative
-// error 2^-9 each, independent) and the result.
+// so what is rounded to 16 bits is what the 16-bit attention rounds: the weights w (by at most
+// 2^-8 of each) and the result.
 // Cached blocks come first in a range, then the blocks of the tree's own rows, which are bf16
 // in the order the projection left them; only these and the last cached page need a mask.
 //
-// Bound by memory for long prefixes: 64 rows over 32768 slots, 32 heads of 128, read 268 MB in 65 us = 4.1 TB/s (a
-// large copy moves 4.8 to 5.1, a bare read 7.1), 16 sequences of 4096 at most 361 MB in 100 us, with 43 GFLOP of
-// products.  For few rows by the way of a workgroup from the lengths over the
-// table and the scales to its first codes and, over the merge of its streams, to the result: one row over 500
-// slots takes 11 us, of which the cached blocks themselves take 2.4.
+// Bound by memory for long prefixes: 64 rows over 32768 slots, 32 heads of 128, read 271 MB in 65 us = 4.2 TB/s (a
+// large copy moves 4.5 to 4.7, a bare read 6.0), with the matrix units at work for a fifth of that time and the vector
+// units for a third; 16 sequences of 4096 at most 362 MB in 99 to 107 us, with 43 GFLOP of products.  For few rows by the
+// way of a workgroup from the lengths over the table and the scales to its first codes and, over the merge of its
+// streams, to the result: one row over 500 slots takes 11 us, of which the cached blocks themselves take 2.4, and 69
+// rows of 32 heads on 8 over 3001 slots 21, of which their products need 2.6 at the rate of a large one.
 //
 // How the keys are split is decided on the device, where the lengths are: every workgroup scans the
 // sequences (64 per round), works out the same plan and finds its own part of it.
@@ -856,9 +857,14 @@ __global__ __launch_bounds__(1024) void attn_q8_combine_kernel(Q8Args a) {
 
 // ------------------------------------------------------------------ launch
 // Two tiles of queries per workgroup where a sequence has more than 32 (as the average of the batch has it):
-// the codes are then converted once for both, on four streams; one tile on eight.  (Four streams and two
-// workgroups per compute unit gain nothing for one tile: 64 sequences of one row on 8 K/V heads, up to 1000
-// slots 48.3 against 47.0 us.)
+// the codes are then converted once for both, on four streams; one tile on eight.  That pays for heads of 128 where the chip is
+// full, which this rule does not look at (us per call with two tiles and with one):
+//   16 sequences of 64 rows, up to 4096 slots   32 on 32 heads 103 117, 32 on 8 88 99, 16 on 16 heads of 64 43 34
+//   64 and 128 sequences of 16 rows, up to 2048 32 on 8 heads 79 99, 134 153
+//   one of 64 rows, 32 on 32 heads              over 500 24 17, 3001 27 22, 32768 72 to 76 69
+//   one of 69 rows, 32 on 8 heads               over 500 25 18, 3001 29 24, 8000 37 30, 32768 75 75
+// (Four streams and two workgroups per compute unit gain nothing for one tile: 64 sequences of one row on 8 K/V heads, up to
+// 1000 slots 48.3 against 47.0 us.)
 struct Q8Launch {
   int ntw, max_parts, grid, tiles;
 };

@@ -12,7 +12,7 @@ namespace trj {
 // launch to do it, then the workgroups share out table entries, released pages and rows.
 // Nothing that one of them reads is written by another: pages taken by this call that this
 // call released are read from the table row they leave, not from the stack.
-// 16 sequences take 4.0 us, 1024 take 10.0 (four sequences of a thread asked for together, their first rows in
+// 16 sequences take 4.0 us, 1024 take 10.1 (four sequences of a thread asked for together, their first rows in
 // LDS: 4.6 and 9.5).
 constexpr int TABLES_THREADS = 256;
 struct SeqPages {  // of one sequence
@@ -169,7 +169,7 @@ int launch_block_tables(int32_t* block_table, int max_blocks, const int32_t* hel
 // (lengths, page number, rows, codes), so a workgroup finds its page once for several heads and
 // layers, and no wavefront waits for another.
 // 4096 rows of 32 heads of 128, 101 MB, take 27 us = 3.7 TB/s; the paths of 16 sequences with 6 rows each in 32 layers of 8
-// heads 23 us, of which their 34 MB of V pages (read and written whole) would need 7; one row 5.7.
+// heads 23 us, of which the 53 MB that they move (V pages read and written whole) would need 11; one row 5.8.
 // The vector unit's work counts too: with every magnitude and every code checked by itself, and both halves of a page
 // worked on whether rows go there or not, the paths took 42 us and the prompt 32.  (A plane asked for while the one
 // before it is worked on costs a third of the wavefronts their registers: 29 to 33 us for the paths, 31 for the prompt.)

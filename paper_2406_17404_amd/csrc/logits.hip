@@ -9,8 +9,8 @@
 // how the compiler joins them.
 // Bytes: 4 V read and, where they are kept, 4 V written per row.  Rows come in batches of four, asked for together,
 // the first while the text is scanned.  69 rows over 128256 tokens, 72 MB, take 24 us = 3.0 TB/s; 16 x 64 rows over 32000
-// tokens without output, 135 MB, 56 us = 2.4 TB/s, 45 of it without any rule.  Some 130 vector instructions per row and
-// wavefront are 28 us of that; a quarter fewer of them gained nothing (60 us: rows under drafts apart), nor did one more
+// tokens without output, 135 MB, 56 us = 2.4 TB/s, 45 of it without any rule.  Some 150 vector instructions per row and
+// wavefront, by the counters, are 32 us of that; a quarter fewer of them gained nothing (60 us: rows under drafts apart), nor did one more
 // batch on its way (59; with more registers than four workgroups per compute unit have, 80), nor a wavefront per row
 // and 1024 tokens (66).
 #include <algorithm>
