@@ -468,6 +468,91 @@ int32_t tree_logits(const float* logits, const int32_t* tok, const int32_t* pare
                     const uint32_t* allowed, float* logits_out, int32_t* argmax_out, void* workspace,
                     size_t ws_bytes, int32_t* status_dev, void* stream);
 
+/* ---- Prompts and sampled tokens on the paged 8-bit cache -------------------------------
+ * What a serving program needs between its own projections besides the calls above: rotary_rows
+ * turns the rows of a projection to their positions, chunk_attention_q8 takes prompts of any length
+ * beside sequences that decode, tree_sample chooses tokens under sampling rules where accept_path
+ * would else be given greedy predictions.  The rules of the section above hold here too: rows that no
+ * sequence owns are left as they were, no row belongs to two sequences, at most TRJ_SERVE_MAX_SEQS of
+ * them, status_dev[s] = 1 (else 0) for what the device finds wrong with sequence s. */
+typedef enum {
+  TRJ_ROTARY_HALVES = 0, /* pair j: columns j and j + rot_dim/2 */
+  TRJ_ROTARY_PAIRS = 1   /* pair j: columns 2j and 2j + 1 */
+} trj_rotary_layout;
+typedef enum {
+  TRJ_ROTARY_PLAIN = 0, /* f_j = theta^(-2j/rot_dim) */
+  TRJ_ROTARY_LINEAR = 1, /* f_j / factor: positions of a text that is factor times as long as the trained one */
+  TRJ_ROTARY_TURNS = 2,  /* by the turns that pair j makes in the trained length, t = trained * f_j / (2 pi): f_j / factor
+                          * up to low of them, f_j from high on, between them f_j / factor * (1 - g) + f_j * g with
+                          * g = (t - low) / (high - low) */
+  TRJ_ROTARY_RAMP = 3    /* by the pair's number: f_j up to the pair that makes high turns, f_j / factor from the one that makes
+                          * low turns on, between them in even steps: a = max(0, floor(pair(high))), b = min(rot_dim - 1,
+                          * ceil(pair(low))), pair(t) = rot_dim * ln(trained / (2 pi t)) / (2 ln theta), r = (j - a) / (b - a)
+                          * (b = a: b = a + 0.001) kept to 0 .. 1: f_j * (1 - r) + f_j / factor * r; rotated rows times
+                          * 0.1 ln(factor) + 1 */
+} trj_rotary_scaling;
+
+/* Frequencies for rotary_rows, on the host (no GPU is touched): h_freqs[rot_dim / 2], *h_magnitude.  factor >= 1, 0 < low < high
+ * and trained > 0 where the rule reads them; theta > 1. */
+int32_t trj_rotary_freqs(int32_t rot_dim, float theta, int32_t scaling, float factor, float low, float high,
+                         int32_t trained, double* h_freqs, float* h_magnitude);
+
+/* Rotary positions: (x1, x2) of pair j becomes magnitude * (x1 cos a - x2 sin a, x1 sin a + x2 cos a), a = position * freqs[j],
+ * for j < rot_dim / 2 in every head of q_rows [T][n_heads][head_dim] and k_rows [T][n_kv_heads][head_dim]; columns from
+ * rot_dim on are copied.  The angle is worked out in 64 bits, products in 32, each result rounded once.
+ * Position: prefix_len[s] + depth of the node in its tree, or with parent NULL prefix_len[s] + j for row j of a sequence of
+ * any number of rows.  freqs: DEVICE [rot_dim / 2] doubles.  head_dim a multiple of 8 up to 1024, rot_dim even and from 2 to
+ * head_dim, rows of TRJ_BF16 or TRJ_F32, addresses multiples of 16 bytes, strides of 8 elements.  Results may take the place of
+ * their inputs (same address and stride, else TRJ_ERR_BAD_SHAPE); other overlaps are undefined.
+ * Nothing and status 1: malformed tree (as trj_tree_mask), rows outside [0, T), a negative
+ * prefix_len, prefix_len[s] + N_s beyond 2^31.  At most 2^20 rows in all. */
+int32_t rotary_rows(const void* q_rows, int32_t q_stride, const void* k_rows, int32_t k_stride, const int32_t* parent,
+                    const int32_t* node_off, const int32_t* prefix_len, int32_t B, int32_t T, int32_t n_heads,
+                    int32_t n_kv_heads, int32_t head_dim, int32_t rot_dim, int32_t layout, const double* freqs,
+                    float magnitude, int32_t dtype, void* q_out, int32_t q_out_stride, void* k_out, int32_t k_out_stride,
+                    int32_t* status_dev, void* stream);
+
+/* Bytes of device scratch for chunk_attention_q8 with these sizes. */
+int32_t chunk_attention_q8_workspace_bytes(int32_t B, int32_t T, int32_t n_heads, int32_t n_kv_heads,
+                                           int32_t head_dim, int32_t max_prefix, size_t* h_bytes);
+
+/* Causal attention of new rows over one layer of the paged cache: row i of sequence s sees the prefix_len[s]
+ * positions of the cache and the rows 0 .. i of its own in k_rows, v_rows (which the cache need not hold).  A sequence has any
+ * number of rows: chunks of prompts and sequences that decode one row go in one call.  Arguments and what is said of
+ * values that are not finite as in tree_attention_q8.  At most 2^20 rows in all, T * n_heads at most 2^30, max_prefix + T at
+ * most 2^31 - 64 (TRJ_ERR_BAD_SHAPE).
+ * Rows of zeros and status 1: prefix_len[s] outside [0, max_prefix] or beyond max_blocks pages; nothing and status 1: rows
+ * outside [0, T).  NaN in all rows and status 1: a page number outside [0, n_blocks).
+ * Calls that overlap in time need workspaces of their own; nothing in one needs clearing. */
+int32_t chunk_attention_q8(const void* q_rows, int32_t q_stride, const void* k_pool, const void* v_pool,
+                           const float* k_scale, const float* v_scale, const void* k_rows, const void* v_rows,
+                           int32_t row_stride, const int32_t* node_off, const int32_t* block_table, int32_t max_blocks,
+                           const int32_t* prefix_len, int32_t B, int32_t T, int32_t n_heads, int32_t n_kv_heads,
+                           int32_t head_dim, int32_t n_blocks, int32_t max_prefix, int32_t dtype, float scale,
+                           void* workspace, size_t ws_bytes, void* out, int32_t* status_dev, void* stream);
+
+/* Bytes of device scratch for tree_sample with these sizes. */
+int32_t tree_sample_workspace_bytes(int32_t B, int32_t T, int32_t V, size_t* h_bytes);
+
+/* A token for every row of logits [T][V] (fp32; any number of rows per sequence), for accept_path to compare drafts with (its
+ * argmax_out, with logits NULL).  rules[B][4] = temperature, top-k, top-p, min-p of a sequence; uniform[T]: a random number of
+ * [0, 1) per row (kept to 0 .. 1 - 2^-24, NaN: 0).  Where nodes of one position are given that position's number, what is
+ * accepted equals token-by-token sampling with the same numbers.
+ * Tokens are taken in order: larger logits first, of equal ones the lowest index first.  A token's weight is
+ * exp((x - largest x) / temperature), held as a whole number of 2^-38, rounded to nearest; sums of weights are exact.
+ *   top-k k >= 1 (of a number with a fraction the whole part): the first k tokens; less: all.
+ *   top-p p < 1: of these the fewest first ones whose weights' sum is at least ceil(p * sum of these); p <= 0: the first one.
+ *   min-p m > 0: of these those of weight ceil(m * 2^38) or more; m > 1: as 1.
+ *   target = floor(uniform * sum of the kept); the token is the first one with which the running sum exceeds target.
+ * Products in 64-bit floating point.  temperature 0: the first token, whatever the other rules.
+ * -infinity and NaN are no tokens: a row of nothing else gets token -1, probability 0.  An infinity is a largest x, others
+ * then weigh nothing.  prob_out[T] (may be NULL): the token's share of the sum of the kept.
+ * V at most 2^24.  Left as they were, and status 1: rows outside [0, T), a temperature that is negative or not finite, a rule
+ * that is NaN. */
+int32_t tree_sample(const float* logits, const int32_t* node_off, int32_t B, int32_t T, int32_t V, const float* rules,
+                    const float* uniform, int32_t* token_out, float* prob_out, void* workspace, size_t ws_bytes,
+                    int32_t* status_dev, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -25,6 +25,8 @@ KV_BLOCK = 32
 STATIC_SCRATCH_BYTES = 32 << 20
 F32, BF16 = 0, 1
 PACK_PLAIN, PACK_QKV, PACK_GATE_UP = 0, 1, 2
+ROTARY_HALVES, ROTARY_PAIRS = 0, 1
+ROTARY_PLAIN, ROTARY_LINEAR, ROTARY_TURNS, ROTARY_RAMP = 0, 1, 2, 3
 STATUS = {0: "TRJ_OK", -1: "TRJ_ERR_NULLPTR", -2: "TRJ_ERR_BAD_SHAPE", -3: "TRJ_ERR_BAD_DTYPE",
           -4: "TRJ_ERR_TREE_TOO_LARGE", -5: "TRJ_ERR_WORKSPACE_TOO_SMALL", -6: "TRJ_ERR_HIP"}
 
@@ -108,6 +110,13 @@ _SIGS = {
                           [_f, _vp, _sz] + [_vp] * 3),
     "tree_logits_workspace_bytes": (_i32, [_i32] * 3 + [C.POINTER(_sz)]),
     "tree_logits": (_i32, [_vp] * 4 + [_i32] * 3 + [_vp, _i32] + [_vp] * 5 + [_i32] + [_vp] * 5 + [_sz] + [_vp] * 2),
+    "trj_rotary_freqs": (_i32, [_i32, _f, _i32, _f, _f, _f, _i32, C.POINTER(C.c_double), C.POINTER(_f)]),
+    "rotary_rows": (_i32, [_vp, _i32, _vp, _i32] + [_vp] * 3 + [_i32] * 7 + [_vp, _f, _i32, _vp, _i32, _vp, _i32, _vp, _vp]),
+    "chunk_attention_q8_workspace_bytes": (_i32, [_i32] * 6 + [C.POINTER(_sz)]),
+    "chunk_attention_q8": (_i32, [_vp, _i32] + [_vp] * 6 + [_i32] + [_vp] * 2 + [_i32, _vp] + [_i32] * 8 +
+                           [_f, _vp, _sz] + [_vp] * 3),
+    "tree_sample_workspace_bytes": (_i32, [_i32] * 3 + [C.POINTER(_sz)]),
+    "tree_sample": (_i32, [_vp] * 2 + [_i32] * 3 + [_vp] * 5 + [_sz] + [_vp] * 2),
 }
 
 
@@ -443,6 +452,78 @@ def tree_logits(logits, tok, parent, node_off, ctx, ctx_off, gen_start, penaltie
         _ptr(penalties), _ptr(bias_tok), _ptr(bias_val),
         0 if bias_val is None else min(bias_tok.numel(), bias_val.numel()), _ptr(bias_off), _ptr(allowed), _ptr(logits_out),
         _ptr(argmax_out), _ptr(workspace), workspace.numel() * workspace.element_size(), _ptr(status_dev), _stream()))
+
+
+def trj_rotary_freqs(rot_dim, theta, scaling=ROTARY_PLAIN, factor=1.0, low=1.0, high=4.0, trained=1):
+    """(frequencies as a host tensor of 64-bit numbers, magnitude)"""
+    freqs, magnitude = torch.zeros(max(0, rot_dim // 2), dtype=torch.float64), _f(0)
+    _check("trj_rotary_freqs", lib().trj_rotary_freqs(
+        rot_dim, theta, scaling, factor, low, high, trained, C.cast(freqs.data_ptr(), C.POINTER(C.c_double)),
+        C.byref(magnitude)))
+    return freqs, float(magnitude.value)
+
+
+def rotary_rows(q_rows, k_rows, parent, node_off, prefix_len, freqs, magnitude, layout, q_out, k_out, status_dev):
+    """Rows [T, heads, head_dim], results of the same shapes (or the rows themselves); freqs [rot_dim / 2]."""
+    T, n_heads, head_dim = q_rows.shape
+    n_kv_heads = k_rows.shape[1]
+    if k_rows.shape != (T, n_kv_heads, head_dim) or q_out.shape != q_rows.shape or k_out.shape != k_rows.shape or \
+            not q_rows.dtype == k_rows.dtype == q_out.dtype == k_out.dtype:
+        raise ValueError("rows and results are of the same type, rows and head_dim")
+    if freqs.dtype != torch.float64:
+        raise ValueError("freqs are numbers of 64 bits")
+    (qp, q_stride, _), (kp, k_stride, _), (qo, qo_stride, _), (ko, ko_stride, _) = map(_rows, (q_rows, k_rows, q_out, k_out))
+    _check("rotary_rows", lib().rotary_rows(
+        qp, q_stride, kp, k_stride, _ptr(parent), _ptr(node_off), _ptr(prefix_len), node_off.shape[0] - 1, T, n_heads,
+        n_kv_heads, head_dim, 2 * freqs.numel(), layout, _ptr(freqs), magnitude, dtype_code(q_rows.dtype), qo, qo_stride, ko,
+        ko_stride, _ptr(status_dev), _stream()))
+
+
+def chunk_attention_q8_workspace_bytes(B, T, n_heads, n_kv_heads, head_dim, max_prefix) -> int:
+    n = _sz(0)
+    _check("chunk_attention_q8_workspace_bytes", lib().chunk_attention_q8_workspace_bytes(
+        B, T, n_heads, n_kv_heads, head_dim, max_prefix, C.byref(n)))
+    return int(n.value)
+
+
+def chunk_attention_q8(q_rows, k_pool, v_pool, k_scale, v_scale, k_rows, v_rows, node_off, block_table, prefix_len,
+                       max_prefix, scale, workspace, out, status_dev):
+    """One layer, laid out as for tree_attention_q8."""
+    B, max_blocks = block_table.shape
+    n_kv_heads, n_blocks = k_scale.shape
+    T, n_heads, head_dim = q_rows.shape
+    qp, q_stride, _ = _rows(q_rows)
+    kp, stride, _ = _rows(k_rows)
+    vp, v_stride, _ = _rows(v_rows)
+    if k_rows.shape != (T, n_kv_heads, head_dim) or v_rows.shape != k_rows.shape or stride != v_stride or \
+            k_rows.dtype != q_rows.dtype or v_rows.dtype != q_rows.dtype or out.dtype != q_rows.dtype:
+        raise ValueError("k_rows and v_rows are laid out alike, of q_rows' type and the pool's heads")
+    _check_pools(k_pool, v_pool, k_scale, v_scale, n_kv_heads * n_blocks, head_dim)
+    if out.shape != q_rows.shape:
+        raise ValueError("out is laid out like q_rows")
+    _check("chunk_attention_q8", lib().chunk_attention_q8(
+        qp, q_stride, _ptr(k_pool), _ptr(v_pool), _ptr(k_scale), _ptr(v_scale), kp, vp, stride, _ptr(node_off),
+        _ptr(block_table), max_blocks, _ptr(prefix_len), B, T, n_heads, n_kv_heads, head_dim, n_blocks, max_prefix,
+        dtype_code(q_rows.dtype), scale, _ptr(workspace), workspace.numel() * workspace.element_size(), _ptr(out),
+        _ptr(status_dev), _stream()))
+
+
+def tree_sample_workspace_bytes(B: int, T: int, V: int) -> int:
+    n = _sz(0)
+    _check("tree_sample_workspace_bytes", lib().tree_sample_workspace_bytes(B, T, V, C.byref(n)))
+    return int(n.value)
+
+
+def tree_sample(logits, node_off, rules, uniform, token_out, prob_out, workspace, status_dev):
+    T, V = logits.shape
+    B = node_off.shape[0] - 1
+    if logits.dtype != torch.float32 or rules.dtype != torch.float32 or uniform.dtype != torch.float32 or \
+            rules.shape != (B, 4) or uniform.numel() < T or token_out.numel() < T or \
+            (prob_out is not None and (prob_out.dtype != torch.float32 or prob_out.numel() < T)):
+        raise ValueError("logits [T, V], rules [B, 4], uniform [T] and prob_out [T] are fp32")
+    _check("tree_sample", lib().tree_sample(
+        _ptr(logits), _ptr(node_off), B, T, V, _ptr(rules), _ptr(uniform), _ptr(token_out), _ptr(prob_out),
+        _ptr(workspace), workspace.numel() * workspace.element_size(), _ptr(status_dev), _stream()))
 
 
 # ------------------------------------------------------------------ decoding loop

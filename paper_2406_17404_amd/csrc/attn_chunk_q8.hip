@@ -1,0 +1,465 @@
+// Causal attention of chunks of new rows over the paged 8-bit cache, fp32 softmax and accumulation.
+//
+//   out_i = sum_j w_ij v_j / sum_j w_ij,  w_ij = 2^(s_ij - max_j s_ij),  s_ij = scale * log2(e) * q_i . k_j
+// over the cached positions j < prefix and the sequence's own rows j <= i.
+//
+// All query heads of a K/V head are worked on together: query p of a sequence is (row p / G, head p % G of the group).
+// A workgroup owns QUERIES of them, 32 per wavefront, and a contiguous range of blocks of 64 keys, which its
+// wavefronts bring to LDS together, as operands of
+//   S^T[keys, queries] = K[keys, dh] * Q^T          (v_mfma_f32_32x32x16_bf16)
+//   O^T[dh, queries]  += V^T[dh, keys] * P^T[keys, queries]
+// Cached blocks (two pages) are converted on the way, codes times their power-of-two scale being bf16 numbers
+// exactly; the sequence's own rows are bf16 already and V is transposed.
+#include <algorithm>
+
+#include "attn_q8.h"
+#include "kernels.h"
+
+namespace trj {
+
+struct ChunkArgs {
+  const uint16_t *q, *k_rows, *v_rows;
+  const uint8_t *k_pool, *v_pool;
+  const float *k_scale, *v_scale;
+  const int32_t *node_off, *block_table, *prefix_len;
+  int q_stride, row_stride, max_blocks, B, T, n_kv_heads, group, n_blocks, max_prefix;
+  int max_parts;
+  float scale_log2e;
+  float *po, *pm, *pl;  // un-normalised partials: [part][wavefront] images of the accumulators, maxima and sums of 32 queries
+  uint16_t* out;
+  int32_t* status;
+};
+constexpr int CH_WAVES = 8, CH_THREADS = 64 * CH_WAVES, CH_QUERIES = 32 * CH_WAVES, CH_KEYS = 64;
+constexpr int CH_MAX_PARTS = 512, CH_TARGET = CH_MAX_PARTS / 2, CH_LEAST = 4;
+
+struct ChunkSeq {
+  int r0, n, L, tiles;  // n < 0: refused, with nothing written; L < 0: refused, rows of zeros
+  __device__ inline int cached() const { return (L + CH_KEYS - 1) / CH_KEYS; }
+  __device__ inline int blocks() const { return n <= 0 ? 0 : L < 0 ? 1 : cached() + (n + CH_KEYS - 1) / CH_KEYS; }
+};
+__device__ inline ChunkSeq chunk_seq(const ChunkArgs& a, int s) {
+  ChunkSeq q{0, 0, 0, 0};
+  if (s >= a.B) return q;
+  const int r0 = a.node_off[s], r1 = a.node_off[s + 1], L = a.prefix_len[s];
+  q.r0 = r0;
+  q.n = r0 < 0 || r1 < r0 || r1 > a.T ? -1 : r1 - r0;
+  q.L = L >= 0 && L <= a.max_prefix && L <= (int64_t)q8_pages_at_most(a.max_blocks) * 32 ? L : -1;
+  q.tiles = q.n <= 0 ? 0 : (q.n * a.group + CH_QUERIES - 1) / CH_QUERIES;
+  return q;
+}
+
+struct ChunkWork {
+  ChunkSeq seq;
+  int s, nth, splits, part0;
+};
+// The same on every wavefront of every workgroup: a split has `span` blocks at most, of one sequence evenly many.
+struct ChunkPlan {
+  const ChunkArgs& a;
+  int span;
+  __device__ inline explicit ChunkPlan(const ChunkArgs& args) : a(args) {
+    const int lane = threadIdx.x & 63;
+    float work = 0.f;
+    for (int s0 = 0; s0 < a.B; s0 += 64) {
+      const ChunkSeq q = chunk_seq(a, s0 + lane);
+      work += wave_sum((float)q.tiles * (float)q.blocks());
+    }
+    work *= a.n_kv_heads;  // (a split sequence has at most twice its share of parts)
+    span = a.max_parts == 0 ? INT32_MAX >> 1 : (int)fminf(fmaxf(ceilf(work * (1.0001f / CH_TARGET)), (float)CH_LEAST), 1e9f);
+  }
+  __device__ inline int splits(const ChunkSeq& q) const { return (q.blocks() + span - 1) / span; }
+  // item x of all; of which a (sequence, tile, K/V head) counts its splits, or, MERGE, once if there are several
+  template <bool MERGE>
+  __device__ inline bool find(int x, ChunkWork& w) const {
+    const int lane = threadIdx.x & 63;
+    int base = 0, parts = 0;
+    for (int s0 = 0; s0 < a.B; s0 += 64) {
+      const ChunkSeq q = chunk_seq(a, s0 + lane);
+      const int k = splits(q), g = q.tiles * a.n_kv_heads, n = MERGE ? (k > 1 ? g : 0) : g * k;
+      const int upto = base + wave_scan(n), pupto = parts + wave_scan(k > 1 ? g * k : 0);
+      const uint64_t here = __ballot(x < upto);
+      if (here) {
+        const int l = __builtin_ctzll(here);
+        w.seq = ChunkSeq{lane_value(q.r0, l), lane_value(q.n, l), lane_value(q.L, l), lane_value(q.tiles, l)};
+        w.s = s0 + l;
+        w.nth = x - (lane_value(upto, l) - lane_value(n, l));
+        w.splits = lane_value(k, l);
+        w.part0 = lane_value(pupto, l) - (w.splits > 1 ? lane_value(g, l) * w.splits : 0);
+        return true;
+      }
+      base = lane_value(upto, 63);
+      parts = lane_value(pupto, 63);
+    }
+    return false;
+  }
+};
+
+// Infinities and NaN among V rows that some query of the tile does not see are left out of the products (times
+// the weight 0 they would be NaN) and added here, rarely, to the stored results of those who do see them: rows
+// from..row of the sequence.
+__device__ inline void chunk_add_odd_values(const ChunkArgs& a, const ChunkSeq& seq, int head, int dh, int q0, int q1, int from) {
+  __builtin_amdgcn_s_waitcnt(0);  // the stores are in the L2
+  __syncthreads();
+#pragma unroll 1
+  for (int u = threadIdx.x; u < (q1 - q0) * (dh >> 1); u += blockDim.x) {
+    const int q = q0 + u / (dh >> 1), c = u % (dh >> 1) * 2, row = q / a.group;
+    const uint16_t* v = a.v_rows + (size_t)head * dh + c;
+    float sum[2] = {0.f, 0.f};
+    bool odd = false;
+#pragma unroll 1
+    for (int j = from; j <= row; ++j) {
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        const uint16_t x = v[(size_t)(seq.r0 + j) * a.row_stride + e];
+        if ((x & 0x7f80) == 0x7f80) sum[e] += bf2f(x), odd = true;
+      }
+    }
+    if (!odd) continue;
+    uint32_t* const at = reinterpret_cast<uint32_t*>(a.out + ((size_t)(seq.r0 + row) * a.n_kv_heads * a.group + head * a.group + q % a.group) * dh + c);
+    const uint32_t was = __hip_atomic_load(at, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    *at = pack2bf(bf2f((uint16_t)was) + sum[0], bf2f((uint16_t)(was >> 16)) + sum[1]);
+  }
+}
+// first key of the sequence's own blocks with a key that row `row` does not see
+__device__ inline int first_partly_seen(int row) { return (row + 1) / CH_KEYS * CH_KEYS; }
+
+// Where a block keeps its operands in LDS: key tile kt of 32, 1 KiB per operand, 16 bytes per lane; lanes in an order
+// with which neither reading operands nor writing them from codes or rows meets a bank twice.
+template <int DH>
+struct ChunkLds {
+  static constexpr int STEPS = DH / 16, PART = CH_KEYS * DH * 2, BUFFER = 2 * PART;
+  // K: step 2j + i holds columns 32 j + 16 hh + 8 i ..
+  __device__ static inline int k_at(int kt, int step, int hh, int r) {
+    const int p = (step >> 1) * 4 + hh * 2 + (step & 1);
+    return ((kt * STEPS + step) * 64 + hh * 32 + (r ^ (p & 15))) * 16;
+  }
+  // V^T: columns 32 mt .., keys 16 kg + 8 b + 4 hh ..
+  __device__ static inline int v_at(int kt, int mt, int kg, int hh, int c32) {
+    return PART + ((kt * STEPS + 2 * mt + kg) * 64 + hh * 32 + (c32 ^ ((mt & 1) * 4 + (c32 >> 3)))) * 16;
+  }
+};
+
+template <int DH>
+__global__ __launch_bounds__(CH_THREADS, 2) void chunk_attn_q8_kernel(ChunkArgs a) {
+  using Lds = ChunkLds<DH>;
+  constexpr int MT = DH / 32, STEPS = DH / 16, OW = MT * 16 * 64;
+  extern __shared__ __align__(16) uint8_t smem[];
+  const int tid = threadIdx.x, lane = tid & 63, n32 = lane & 31, hh = lane >> 5;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  if (blockIdx.x == 0)  // sequences without work
+    for (int s = tid; s < a.B; s += CH_THREADS) {
+      const ChunkSeq q = chunk_seq(a, s);
+      if (q.n <= 0) a.status[s] = q.n < 0;
+    }
+  const ChunkPlan plan(a);
+  ChunkWork w;
+  if (!plan.find<false>(blockIdx.x, w)) return;
+  const ChunkSeq seq = w.seq;
+  const int nq = seq.n * a.group, splits = w.splits;
+  const int head = w.nth % a.n_kv_heads, sp = w.nth / a.n_kv_heads % splits, tile = seq.tiles - 1 - w.nth / a.n_kv_heads / splits;
+  const int row_len = a.n_kv_heads * a.group * DH;
+  const int q0 = tile * CH_QUERIES, q1 = min(nq, q0 + CH_QUERIES);
+  const bool judge = head == 0 && sp == 0 && tile == 0;
+  if (seq.L < 0) {
+    const int width = DH / 4;
+    for (int i = tid; i < (q1 - q0) * width; i += CH_THREADS) {
+      const int q = q0 + i / width;
+      *reinterpret_cast<u32x2*>(a.out + (size_t)(seq.r0 + q / a.group) * row_len + (head * a.group + q % a.group) * DH + i % width * 4) = u32x2{0, 0};
+    }
+    if (judge && tid == 0) a.status[w.s] = 1;
+    return;
+  }
+  const int32_t* table = a.block_table + (size_t)w.s * a.max_blocks;
+  const int row_first = q0 / a.group, row_last = (q1 - 1) / a.group;
+  const int cached = seq.cached(), blocks = cached + row_last / CH_KEYS + 1;  // of this tile
+  const int b0 = (int)((int64_t)blocks * sp / splits), b1 = (int)((int64_t)blocks * (sp + 1) / splits);
+  const size_t plane = (size_t)head * a.n_blocks;
+
+  // queries: column n32; step 2j + i of the product: columns 32 j + 16 hh + 8 i ..
+  const int qw = q0 + wave * 32, qi = min(qw + n32, nq - 1), my_row = qi / a.group;
+  const bool live_wave = qw < nq;
+  const int wave_last = __builtin_amdgcn_readfirstlane((min(qw + 31, nq - 1)) / a.group);
+  bf16x8 qreg[STEPS];
+  {
+    const uint16_t* qp = a.q + (size_t)(seq.r0 + my_row) * a.q_stride + (size_t)(head * a.group + qi % a.group) * DH + hh * 16;
+#pragma unroll
+    for (int j = 0; j < STEPS; ++j) qreg[j] = *reinterpret_cast<const bf16x8*>(qp + 32 * (j >> 1) + 8 * (j & 1));
+  }
+  f32x16 o[MT];
+#pragma unroll
+  for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+    for (int v = 0; v < 16; ++v) o[mt][v] = 0.f;
+  Softmax sm;
+  bool odd = false;
+
+  // ---- bringing a block to LDS: from memory to registers, then, a block later, to LDS
+  constexpr int PIECES = 4 * DH, UNITS = 2 * PIECES / CH_THREADS;  // 16 codes each, of K or V; per thread
+  u32x4 raw[4];
+  float piece_scale[2];
+  int ids = 0, ids_from = -(1 << 30);  // pages ids_from .. + 63 of the sequence, one per lane, and their scales
+  float ksc = 1.f, vsc = 1.f;
+  auto load = [&](int b) {
+    if (b < cached) {
+      if (b * 2 >= ids_from + 64 || ids_from < 0) {
+        ids_from = b * 2;
+        const int p = ids_from + lane;
+        const bool there = p * 32 < seq.L;
+        ids = there ? table[p] : 0;
+        const bool ok = (unsigned)ids < (unsigned)a.n_blocks;
+        ids = ok ? ids : 0;
+        ksc = !there ? 1.f : ok ? a.k_scale[plane + ids] : NAN;  // a page that is not there makes its rows NaN
+        vsc = there ? a.v_scale[plane + ids] : 1.f;
+      }
+#pragma unroll
+      for (int i = 0; i < UNITS; ++i) {
+        const int u = tid + i * CH_THREADS;
+        const bool is_v = __builtin_amdgcn_readfirstlane(u / PIECES) != 0;
+        const int kt = __builtin_amdgcn_readfirstlane(u % PIECES / (2 * DH)), piece = u % (2 * DH);
+        const int p = 2 * b + kt;
+        const int page = __builtin_amdgcn_readlane(ids, p - ids_from);
+        piece_scale[i] = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(is_v ? vsc : ksc), p - ids_from));
+        const uint8_t* pool = is_v ? a.v_pool : a.k_pool;
+        raw[i] = *reinterpret_cast<const u32x4*>(pool + (plane + (uint32_t)page) * (32 * DH) + piece * 16);
+      }
+    } else {
+      const int key0 = (b - cached) * CH_KEYS;
+#pragma unroll
+      for (int i = 0; i < DH / 64; ++i) {
+        const int u = tid + i * CH_THREADS, row = u / (DH / 8), p = u % (DH / 8);
+        raw[i] = *reinterpret_cast<const u32x4*>(a.k_rows + (size_t)(seq.r0 + min(key0 + row, seq.n - 1)) * a.row_stride + (size_t)head * DH + 8 * p);
+      }
+      if (tid < 4 * DH) {  // four rows, four columns
+        const int quad = tid / (DH / 4), cq = tid % (DH / 4);
+        u32x2 v[4];
+#pragma unroll
+        for (int d = 0; d < 4; ++d)
+          v[d] = *reinterpret_cast<const u32x2*>(a.v_rows + (size_t)(seq.r0 + min(key0 + 4 * quad + d, seq.n - 1)) * a.row_stride + (size_t)head * DH + 4 * cq);
+        raw[2] = u32x4{v[0][0], v[0][1], v[1][0], v[1][1]};
+        raw[3] = u32x4{v[2][0], v[2][1], v[3][0], v[3][1]};
+      }
+    }
+  };
+  auto store = [&](int b, uint8_t* buf) {
+    if (b < cached) {
+#pragma unroll
+      for (int i = 0; i < UNITS; ++i) {
+        const int u = tid + i * CH_THREADS;
+        const bool is_v = __builtin_amdgcn_readfirstlane(u / PIECES) != 0;
+        const int kt = __builtin_amdgcn_readfirstlane(u % PIECES / (2 * DH)), piece = u % (2 * DH);
+        const int c16 = piece >> 5, h = c16 & 1, at = piece & 31;  // K: columns 16 c16 .. of row at; V: column at of 32 (c16 / 2)
+        u32x4 x = raw[i];
+        const float scale = piece_scale[i];
+        if (is_v) {  // slots past the end may hold anything: their weights are 0, their values have to be numbers
+          const int rest = seq.L - (2 * b + kt) * 32;
+          if (rest < 32) {
+#pragma unroll
+            for (int d = 0; d < 4; ++d) {
+              const int keep = min(max(rest - 8 * d - 4 * h, 0), 4);
+              x[d] &= keep == 4 ? 0xffffffffu : (1u << (8 * keep)) - 1u;
+            }
+          }
+        }
+        bf16x8 lo = operand(x[0], x[1], scale), hi = operand(x[2], x[3], scale);
+        if (!is_v && scale != scale) {
+          const u32x4 none = {0x7fc07fc0u, 0x7fc07fc0u, 0x7fc07fc0u, 0x7fc07fc0u};
+          lo = hi = __builtin_bit_cast(bf16x8, none);
+        }
+        const int j = c16 >> 1;
+        *reinterpret_cast<bf16x8*>(buf + (is_v ? Lds::v_at(kt, j, 0, h, at) : Lds::k_at(kt, 2 * j, h, at))) = lo;
+        *reinterpret_cast<bf16x8*>(buf + (is_v ? Lds::v_at(kt, j, 1, h, at) : Lds::k_at(kt, 2 * j + 1, h, at))) = hi;
+      }
+    } else {
+      const int key0 = (b - cached) * CH_KEYS;
+#pragma unroll
+      for (int i = 0; i < DH / 64; ++i) {
+        const int u = tid + i * CH_THREADS, row = u / (DH / 8), p = u % (DH / 8);
+        *reinterpret_cast<u32x4*>(buf + Lds::k_at(row >> 5, (p >> 2) * 2 + (p & 1), (p >> 1) & 1, row & 31)) = raw[i];
+      }
+      if (tid < 4 * DH) {
+        const int quad = tid / (DH / 4), cq = tid % (DH / 4);
+        uint32_t v[4][2] = {{raw[2][0], raw[2][1]}, {raw[2][2], raw[2][3]}, {raw[3][0], raw[3][1]}, {raw[3][2], raw[3][3]}};
+        if (key0 >= first_partly_seen(row_first)) {
+#pragma unroll
+          for (int d = 0; d < 4; ++d)
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+              if ((v[d][e] & 0x7f80u) == 0x7f80u) v[d][e] &= 0xffff0000u, odd = true;
+              if ((v[d][e] & 0x7f800000u) == 0x7f800000u) v[d][e] &= 0xffffu, odd = true;
+            }
+        }
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const int c = 4 * cq + e, sh = e & 1;
+          const uint32_t x0 = v[0][e >> 1], x1 = v[1][e >> 1], x2 = v[2][e >> 1], x3 = v[3][e >> 1];
+          const u32x2 col = sh ? u32x2{(x0 >> 16) | (x1 & 0xffff0000u), (x2 >> 16) | (x3 & 0xffff0000u)}
+                               : u32x2{(x0 & 0xffffu) | (x1 << 16), (x2 & 0xffffu) | (x3 << 16)};
+          *reinterpret_cast<u32x2*>(buf + Lds::v_at(quad >> 3, c >> 5, (quad >> 2) & 1, quad & 1, c & 31) + ((quad >> 1) & 1) * 8) = col;
+        }
+      }
+    }
+  };
+
+  if (b0 < b1) load(b0);
+  for (int b = b0; b < b1; ++b) {
+    uint8_t* const buf = smem + ((b - b0) & 1) * Lds::BUFFER;
+    store(b, buf);
+    if (b + 1 < b1) load(b + 1);
+    __syncthreads();  // (the other buffer was read before the barrier of the block before)
+    const bool own = b >= cached;
+    const int key0 = (own ? b - cached : b) * CH_KEYS;
+    if (!live_wave || (own && key0 > wave_last)) continue;
+    f32x16 s[2];
+#pragma unroll
+    for (int kt = 0; kt < 2; ++kt) {
+#pragma unroll
+      for (int v = 0; v < 16; ++v) s[kt][v] = 0.f;
+#pragma unroll
+      for (int j = 0; j < STEPS; ++j) {
+        const bf16x8 kop = *reinterpret_cast<const bf16x8*>(buf + Lds::k_at(kt, j, hh, n32));
+        s[kt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kop, qreg[j], s[kt], 0, 0, 0);
+      }
+    }
+    const int limit = (own ? my_row + 1 : seq.L) - key0;
+    if (own ? key0 + CH_KEYS > row_first + 1 : limit < CH_KEYS) {
+#pragma unroll
+      for (int kt = 0; kt < 2; ++kt)
+#pragma unroll
+        for (int v = 0; v < 16; ++v)
+          if (32 * kt + 8 * (v >> 2) + 4 * hh + (v & 3) >= limit) s[kt][v] = -INFINITY;
+    }
+    const float f = a.scale_log2e;
+    const float top = fmaxf(Softmax::largest(s[0], f), Softmax::largest(s[1], f));
+    // (each query by itself: its result does not depend on those beside it)
+    const bool low = sm.too_low(top);
+    if (__ballot(low)) q8_rescale<MT>(o, sm.lift(low ? top : NO_REFERENCE));
+    u32x4 pk[2][2];
+    sm.weigh(s[0], f, pk[0]);
+    sm.weigh(s[1], f, pk[1]);
+#pragma unroll
+    for (int kt = 0; kt < 2; ++kt)
+#pragma unroll
+      for (int kg = 0; kg < 2; ++kg)
+#pragma unroll
+        for (int mt = 0; mt < MT; ++mt) {
+          const bf16x8 vop = *reinterpret_cast<const bf16x8*>(buf + Lds::v_at(kt, mt, kg, hh, n32));
+          o[mt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vop, __builtin_bit_cast(bf16x8, pk[kt][kg]), o[mt], 0, 0, 0);
+        }
+  }
+  const bool any_odd = __syncthreads_or(odd);
+
+  const float l = sm.l + __shfl_xor(sm.l, 32);
+  if (splits == 1) {
+    if (qw + n32 < nq) {
+      const float inv = 1.0f / l;
+      uint16_t* dst = a.out + (size_t)(seq.r0 + my_row) * row_len + (size_t)(head * a.group + qi % a.group) * DH + 4 * hh;
+#pragma unroll
+      for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+        for (int g = 0; g < 4; ++g) {
+          const u32x2 v = {pack2bf(o[mt][4 * g] * inv, o[mt][4 * g + 1] * inv), pack2bf(o[mt][4 * g + 2] * inv, o[mt][4 * g + 3] * inv)};
+          *reinterpret_cast<u32x2*>(dst + 32 * mt + 8 * g) = v;
+        }
+    }
+    if (any_odd) chunk_add_odd_values(a, seq, head, DH, q0, q1, first_partly_seen(row_first));
+  } else {
+    const int part = w.part0 + w.nth;
+    if (live_wave && part < a.max_parts) {  // (else more work than T rows can be: ranges that overlap)
+      const size_t image = (size_t)part * CH_WAVES + wave;
+      if (hh == 0) {
+        a.pm[image * 32 + n32] = sm.m;
+        a.pl[image * 32 + n32] = any_odd ? -l : l;  // (a sum of weights is not negative)
+      }
+#pragma unroll
+      for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+        for (int g = 0; g < 4; ++g)
+          *reinterpret_cast<f32x4*>(a.po + image * OW + (mt * 4 + g) * 256 + lane * 4) =
+              f32x4{o[mt][4 * g], o[mt][4 * g + 1], o[mt][4 * g + 2], o[mt][4 * g + 3]};
+    }
+  }
+  if (judge) {
+    bool bad = false;
+    for (int j = tid; j * 32 < seq.L; j += CH_THREADS) bad = bad || (unsigned)table[j] >= (unsigned)a.n_blocks;
+    bad = __syncthreads_or(bad);
+    if (tid == 0) a.status[w.s] = bad;
+  }
+}
+
+// Merges the partials of 32 queries of a (sequence, tile, K/V head) in split order, 32 columns per wavefront.
+template <int DH>
+__global__ __launch_bounds__(64 * (DH / 32)) void chunk_merge_kernel(ChunkArgs a) {
+  constexpr int MT = DH / 32, OW = MT * 16 * 64;
+  const int tid = threadIdx.x, lane = tid & 63, n32 = lane & 31, hh = lane >> 5, mt = tid >> 6;
+  const ChunkPlan plan(a);
+  for (int x = blockIdx.x / CH_WAVES;; x += gridDim.x / CH_WAVES) {
+    const int wave = blockIdx.x % CH_WAVES;
+    ChunkWork w;
+    if (!plan.find<true>(x, w)) return;
+    const ChunkSeq seq = w.seq;
+    const int nq = seq.n * a.group, splits = w.splits, head = w.nth % a.n_kv_heads, rest = w.nth / a.n_kv_heads;
+    const int tile = seq.tiles - 1 - rest, q0 = tile * CH_QUERIES, qw = q0 + wave * 32, qi = qw + n32;
+    if (qw >= nq || w.part0 + (rest + 1) * splits * a.n_kv_heads > a.max_parts) continue;
+    float m = NO_REFERENCE, l = 0.f;
+    bool odd = false;
+    f32x4 o[4] = {};
+    for (int sp = 0; sp < splits; ++sp) {
+      const size_t image = (size_t)(w.part0 + (rest * splits + sp) * a.n_kv_heads + head) * CH_WAVES + wave;
+      const float pm = a.pm[image * 32 + n32], pl = a.pl[image * 32 + n32];
+      const float top = fmaxf(m, pm), keep = __builtin_amdgcn_exp2f(m - top), f = __builtin_amdgcn_exp2f(pm - top);
+      odd = odd || (__float_as_uint(pl) >> 31) != 0;
+      l = l * keep + fabsf(pl) * f;
+      m = top;
+#pragma unroll
+      for (int g = 0; g < 4; ++g)
+        o[g] = o[g] * keep + *reinterpret_cast<const f32x4*>(a.po + image * OW + (mt * 4 + g) * 256 + lane * 4) * f;
+    }
+    if (qi < nq) {
+      const float inv = 1.0f / l;
+      uint16_t* dst = a.out + ((size_t)(seq.r0 + qi / a.group) * a.n_kv_heads * a.group + head * a.group + qi % a.group) * DH + 32 * mt + 4 * hh;
+#pragma unroll
+      for (int g = 0; g < 4; ++g)
+        *reinterpret_cast<u32x2*>(dst + 8 * g) = u32x2{pack2bf(o[g][0] * inv, o[g][1] * inv), pack2bf(o[g][2] * inv, o[g][3] * inv)};
+    }
+    if (__syncthreads_or(odd)) chunk_add_odd_values(a, seq, head, DH, qw, min(nq, qw + 32), first_partly_seen(q0 / a.group));
+    __syncthreads();
+  }
+}
+
+// ------------------------------------------------------------------ launch
+static int chunk_max_parts(int T, int max_prefix) {
+  const long most = ((long)max_prefix + CH_KEYS - 1) / CH_KEYS + ((long)T + CH_KEYS - 1) / CH_KEYS;  // blocks of a sequence
+  return most <= CH_LEAST ? 0 : CH_MAX_PARTS;
+}
+size_t attn_chunk_ws_floats(int B, int T, int group, int n_kv_heads, int head_dim, int max_prefix) {
+  return (size_t)chunk_max_parts(T, max_prefix) * CH_WAVES * (32 * head_dim + 64);
+}
+
+template <int DH>
+static int chunk_run(const ChunkArgs& a, hipStream_t st) {
+  constexpr size_t lds = 2 * ChunkLds<DH>::BUFFER;
+  static DeviceOnce once;
+  allow_lds(once, chunk_attn_q8_kernel<DH>, lds);
+  const long items = ((long)a.T * a.group / CH_QUERIES + a.B) * a.n_kv_heads;
+  const int grid = (int)std::min(items + a.max_parts, 1l << 30);
+  chunk_attn_q8_kernel<DH><<<grid, CH_THREADS, lds, st>>>(a);
+  int rc = check_launch();
+  if (rc != TRJ_OK || a.max_parts == 0) return rc;
+  chunk_merge_kernel<DH><<<CH_WAVES * (int)std::min(items, 128l), 64 * (DH / 32), 0, st>>>(a);
+  return check_launch();
+}
+
+int launch_attn_chunk_q8(const uint16_t* q, int q_stride, const void* k_pool, const void* v_pool, const float* k_scale,
+                         const float* v_scale, const uint16_t* k_rows, const uint16_t* v_rows, int row_stride,
+                         const int32_t* node_off, const int32_t* block_table, int max_blocks, const int32_t* prefix_len,
+                         int B, int T, int n_heads, int n_kv_heads, int head_dim, int n_blocks, int max_prefix, float scale,
+                         float* ws, uint16_t* out, int32_t* status, hipStream_t st) {
+  const int group = n_heads / n_kv_heads, parts = chunk_max_parts(T, max_prefix);
+  const size_t images = (size_t)parts * CH_WAVES;
+  float* const pm = ws + images * 32 * head_dim;
+  const ChunkArgs a{q, k_rows, v_rows, (const uint8_t*)k_pool, (const uint8_t*)v_pool, k_scale, v_scale, node_off, block_table,
+                    prefix_len, q_stride, row_stride, max_blocks, B, T, n_kv_heads, group, n_blocks, max_prefix, parts,
+                    scale * LOG2E, ws, pm, pm + images * 32, out, status};
+  return head_dim == 128 ? chunk_run<128>(a, st) : chunk_run<64>(a, st);
+}
+
+}  // namespace trj

@@ -307,4 +307,19 @@ int launch_tree_logits(const float* x, const int32_t* tok, const int32_t* parent
                        const int32_t* bias_tok, const float* bias_val, int n_bias, const int32_t* bias_off, const uint32_t* allowed,
                        float* out, int32_t* argmax, uint64_t* cand, int32_t* status, hipStream_t st);
 
+// rotary.hip, attn_chunk_q8.hip, sample.hip: prompts and sampled tokens (arguments as in trjacobi.h)
+int launch_rotary_rows(const void* q, int q_stride, const void* k, int k_stride, const int32_t* parent,
+                       const int32_t* node_off, const int32_t* prefix_len, int B, int T, int n_heads, int n_kv_heads,
+                       int head_dim, int rot_dim, int layout, const double* freqs, float magnitude, int dtype, void* q_out,
+                       int q_out_stride, void* k_out, int k_out_stride, int32_t* status, hipStream_t st);
+size_t attn_chunk_ws_floats(int B, int T, int group, int n_kv_heads, int head_dim, int max_prefix);
+int launch_attn_chunk_q8(const uint16_t* q, int q_stride, const void* k_pool, const void* v_pool, const float* k_scale,
+                         const float* v_scale, const uint16_t* k_rows, const uint16_t* v_rows, int row_stride,
+                         const int32_t* node_off, const int32_t* block_table, int max_blocks, const int32_t* prefix_len,
+                         int B, int T, int n_heads, int n_kv_heads, int head_dim, int n_blocks, int max_prefix, float scale,
+                         float* ws, uint16_t* out, int32_t* status, hipStream_t st);
+size_t tree_sample_ws_bytes(int T, int V);
+int launch_tree_sample(const float* x, const int32_t* node_off, int B, int T, int V, const float* rules,
+                       const float* uniform, int32_t* token, float* prob, void* ws, int32_t* status, hipStream_t st);
+
 }  // namespace trj

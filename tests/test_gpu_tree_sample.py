@@ -1,0 +1,189 @@
+"""tree_sample against the oracle: tokens equal, probabilities to 32-bit rounding.
+
+Weights are whole numbers of 2^-38, each off by at most one between two 64-bit exponentials that are right to
+a few units of their last place; a token can differ where the target lies within the sum of these of a border: n of 2^38 for
+n tokens, which inputs that are drawn meet with a chance below 1e-6 per row.  A probability is then off by less than n 2^-38
+and its rounding to fp32, half a step of 2^-24."""
+import numpy as np
+import pytest
+import torch
+
+from gpu_util import DEV, i32, to_dev
+from oracle import tr_prompt as P
+from paper_2406_17404_amd import binding as b
+from serve_util import ints, offsets_of
+
+pytestmark = pytest.mark.gpu
+INF, NAN = np.inf, np.nan
+
+
+class Call:
+    def __init__(self, x, sizes, rules, u):
+        self.x, self.off = np.asarray(x, np.float32), offsets_of(sizes)
+        self.rules, self.u = np.asarray(rules, np.float32).reshape(-1, 4), np.asarray(u, np.float32)
+
+    def device(self):
+        T, V = self.x.shape
+        B = len(self.off) - 1
+        ws = torch.full((b.tree_sample_workspace_bytes(B, T, V),), 255, dtype=torch.uint8, device=DEV)
+        return [to_dev(self.x), i32(self.off), to_dev(self.rules), to_dev(self.u), ints(T), torch.full((T,), 9.0, device=DEV), ws,
+                ints(B)]
+
+    def run(self):
+        args = self.device()
+        b.tree_sample(*args)
+        torch.cuda.synchronize()
+        self.status = list(args[-1].cpu().numpy())
+        return args[4].cpu().numpy(), args[5].double().cpu().numpy()
+
+    def check(self, bad=()):
+        token, prob = self.run()
+        V = self.x.shape[1]
+        covered = np.zeros(len(self.x), bool)
+        for s in range(len(self.off) - 1):
+            for t in range(self.off[s], self.off[s + 1]):
+                if s in bad:
+                    continue
+                covered[t] = True
+                want, p = P.sample(self.x[t], self.rules[s], self.u[t])
+                assert token[t] == want, (s, t, token[t], want, self.rules[s], self.u[t])
+                assert abs(prob[t] - p) <= 2.0 ** -24 * p + V * 2.0 ** -38
+        assert (token[~covered] == -7).all() and (prob[~covered] == 9.0).all()
+        assert self.status == [int(s in bad) for s in range(len(self.off) - 1)]
+        return token, prob
+
+
+RULES = [(1, 0, 1, 0), (0.7, 0, 1, 0), (1, 1, 1, 0), (1, 40, 1, 0), (0.9, 0, 0.9, 0), (1, 0, 1, 0.05), (1.3, 50, 0.8, 0.02),
+         (0, 5, 0.5, 0.1), (1, 0, 0, 0), (1, 0, 1, 1), (1, 3.9, 1, 0), (1, 1e9, 2, -1), (0.8, -3, -1, 7), (0.01, 0, 1, 0),
+         (1e-30, 0, 1, 0), (1e30, 0, 1, 0), (100, 5000, 0.5, 0), (1, INF, INF, 0)]
+
+
+@pytest.mark.parametrize("V", [1, 2, 3, 5, 63, 64, 65, 1000, 4095, 4096, 4097, 32000, 40001])
+def test_rules(V):
+    rng = np.random.default_rng(V)
+    n = len(RULES)
+    u = rng.random(n).astype(np.float32)
+    Call(rng.normal(size=(n, V)) * 3, [1] * n, RULES, u).check()
+
+
+@pytest.mark.parametrize("V", [128256, 151936])
+def test_large_vocabularies(V):
+    rng = np.random.default_rng(V)
+    rules = [RULES[i] for i in (0, 3, 4, 5, 6, 16)]
+    Call(rng.normal(size=(12, V)) * 3, [2] * 6, rules, rng.random(12)).check()
+
+
+@pytest.mark.parametrize("scale", [0.0, 1e-3, 0.25, 1.0, 8.0])
+def test_ties_and_crowded_logits(scale):
+    # steps of `scale`: many equal logits, all equal for 0
+    rng = np.random.default_rng(1)
+    x = np.round(rng.normal(size=(16, 9000)) * 2) * scale
+    for rules in ((1, 0, 1, 0), (1, 2500, 1, 0), (1, 0, 0.37, 0), (1, 5000, 0.5, 0.3)):
+        Call(x, [4] * 4, [rules] * 4, rng.random(16)).check()
+
+
+def test_coarse_logits_of_many_tokens():
+    rng = np.random.default_rng(2)
+    x = torch.from_numpy(rng.normal(size=(6, 60000)) * 3).bfloat16().float().numpy()
+    Call(x, [6], [(1, 0, 0.95, 0)], rng.random(6)).check()
+    Call(x * 0.01, [6], [(1, 30000, 0.95, 0)], rng.random(6)).check()
+
+
+@pytest.mark.parametrize("u", [0.0, 0.25, 0.5, 1 - 2.0 ** -24, 1.0, 2.0, -1.0, NAN])
+def test_borders_that_are_met_exactly(u):
+    x = np.zeros((4, 1024))
+    x[1, ::2] = -INF
+    x[2, 512:] = -np.log(2.0)  # not exact: the oracle's weights are
+    x[3] = np.where(np.arange(1024) % 3 == 0, 4.0, -INF)
+    for rules in ((1, 0, 1, 0), (1, 256, 1, 0), (1, 0, 0.25, 0), (1, 512, 0.5, 0), (1, 0, 1, 1)):
+        Call(x, [4], [rules], [u] * 4).check()
+
+
+def test_rows_without_tokens_and_infinities():
+    x = np.full((8, 300), -INF)
+    x[1] = NAN
+    x[2, 7] = -5.0
+    x[3, [4, 250]] = INF
+    x[3, 9] = 3e38
+    x[4] = np.where(np.arange(300) % 2, NAN, 1.0)
+    x[5] = np.where(np.arange(300) % 2, 3e38, -3e38)
+    x[6] = np.arange(300) * 1e-45
+    x[7] = [-0.0, 0.0] * 150
+    for rules in RULES:
+        Call(x, [8], [rules], np.linspace(0, 0.999, 8)).check()
+
+
+def test_sequences_rules_and_refusals():
+    rng = np.random.default_rng(3)
+    sizes = [3, 0, 130, 5, 1, 2, 2, 2, 2, 2]
+    rules = [(1, 0, 1, 0), (1, 0, 1, 0), (0.8, 20, 0.9, 0), (-1, 0, 1, 0), (0, 0, 1, 0), (INF, 0, 1, 0), (NAN, 0, 1, 0),
+             (1, NAN, 1, 0), (1, 0, NAN, 0), (1, 0, 1, NAN)]
+    c = Call(rng.normal(size=(sum(sizes) + 3, 500)) * 2, sizes, rules, rng.random(sum(sizes) + 3))
+    c.check(bad=(3, 5, 6, 7, 8, 9))
+    args = c.device()
+    args[1] = i32([0, 3, 2, 2, 400, 500, 600, 600, 600, 600, 700])
+    b.tree_sample(*args)
+    torch.cuda.synchronize()
+    assert list(args[-1].cpu().numpy()) == [0, 1, 0, 1, 1, 1, 1, 1, 1, 1]
+    assert (args[4][3:] == -7).all() and (args[4][:3] >= 0).all()
+
+
+def test_many_sequences():
+    rng = np.random.default_rng(4)
+    Call(rng.normal(size=(300, 100)) * 2, [1] * 300, [RULES[i % 7] for i in range(300)], rng.random(300)).check()
+
+
+def test_shares_follow_the_probabilities():
+    # an even grid of numbers: counts are the kept probabilities to one in either direction of each border
+    rng = np.random.default_rng(5)
+    row, n = (rng.normal(size=2000) * 2).astype(np.float32), 4096
+    rules = (0.9, 100, 0.95, 0.01)
+    token, _ = Call(np.tile(row, (n, 1)), [n], [rules], (np.arange(n) + 0.5) / n).run()
+    some, w = P.kept(row, rules)
+    got = np.bincount(token, minlength=2000)
+    want = np.zeros(2000)
+    want[some] = np.array([float(v) for v in w]) / float(sum(w)) * n
+    assert np.abs(got - want).max() <= 1
+
+
+def test_without_probabilities_captured_and_replayed():
+    rng = np.random.default_rng(6)
+    c = Call(rng.normal(size=(70, 5000)) * 3, [64, 6], [(0.8, 50, 0.9, 0.01), (1, 0, 0.9, 0)], rng.random(70))
+    want, _ = c.check()
+    args = c.device()
+    args[5] = None
+    g = torch.cuda.CUDAGraph()
+    b.tree_sample(*args)
+    torch.cuda.synchronize()
+    with torch.cuda.graph(g):
+        b.tree_sample(*args)
+    numbers = args[3].clone()
+    for i in range(3):
+        args[3].copy_(1 - numbers)
+        g.replay()
+        torch.cuda.synchronize()
+        other = args[4].clone()
+        b.tree_sample(*args)
+        torch.cuda.synchronize()
+        assert torch.equal(other, args[4])
+        args[3].copy_(numbers)
+        args[4].fill_(-9)
+        g.replay()
+        torch.cuda.synchronize()
+        assert np.array_equal(args[4].cpu().numpy(), want)
+
+
+def test_two_streams_with_workspaces_of_their_own():
+    rng = np.random.default_rng(7)
+    calls = [Call(rng.normal(size=(9, 70001)), [9], [(1, 0, 0.9, 0)], rng.random(9)),
+             Call(rng.normal(size=(90, 3000)), [90], [(1, 20, 1, 0)], rng.random(90))]
+    want = [c.check()[0] for c in calls]
+    args = [c.device() for c in calls]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in calls]
+    for _ in range(3):
+        for st, a in zip(streams, args):
+            with torch.cuda.stream(st):
+                b.tree_sample(*a)
+    torch.cuda.synchronize()
+    assert all(np.array_equal(a[4].cpu().numpy(), w) for a, w in zip(args, want))
