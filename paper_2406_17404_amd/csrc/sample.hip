@@ -6,8 +6,11 @@
 //
 // Weights are whole numbers, so that sums do not depend on their order and every comparison with a border is exact.
 // As all three rules keep first parts, only the sum of what each keeps matters: of the smallest the target is a share.  No
-// row is sorted: a histogram over max x - x finds the bin in which a count or a running sum crosses a border, and the
-// tokens of that bin alone are put in order.
+// row is sorted.  Two ways:
+//   the short list  where top-k (or min-p without top-p) leaves few tokens: of the 1024 threads' largest logits the k-th is
+//                   a bound that k tokens reach and few more; those are collected, put in order and weighed
+//   the histogram   of the weights over max x - x, which finds the bin in which a running sum (or count) crosses a
+//                   border; the tokens of that bin alone are put in order
 #include <algorithm>
 
 #include "kernels.h"
@@ -15,7 +18,8 @@
 
 namespace trj {
 
-constexpr int SMP_THREADS = 1024, SMP_BINS = 2048, SMP_LIST = 2048;
+constexpr int SMP_ABREAST = 2;
+constexpr int SMP_THREADS = 512, SMP_WAVES = SMP_THREADS / 64, SMP_BINS = 2048, SMP_LIST = 2048;
 constexpr double SMP_UNIT = 274877906944.0;      // 2^38
 constexpr float SMP_RANGE = 27.1f;               // exp(-27.1) * 2^38 rounds to 0
 typedef float f32x4_row __attribute__((ext_vector_type(4), aligned(4)));  // rows of odd length start anywhere
@@ -32,29 +36,60 @@ struct SampleArgs {
 
 __device__ inline bool is_token(float x) { return x > -INFINITY; }  // neither -infinity nor NaN
 // Place in the order, larger first: the logit's bits, ascending, then the index from behind.  Never 0 for a token.
-__device__ inline uint64_t place_key(float x, int i) {
+__device__ inline uint32_t place_bits(float x) {
   const uint32_t u = __float_as_uint(x + 0.f);  // the zeros are equal
-  return (uint64_t)(u >> 31 ? ~u : u | 0x80000000u) << 24 | (uint32_t)(0xffffff - i);
+  return u >> 31 ? ~u : u | 0x80000000u;
 }
-__device__ inline float key_logit(uint64_t k) {
-  const uint32_t u = (uint32_t)(k >> 24);
-  return __uint_as_float(u >> 31 ? u & 0x7fffffffu : ~u);
-}
+__device__ inline float bits_logit(uint32_t u) { return __uint_as_float(u >> 31 ? u & 0x7fffffffu : ~u); }
+__device__ inline uint64_t place_key(float x, int i) { return (uint64_t)place_bits(x) << 24 | (uint32_t)(0xffffff - i); }
+__device__ inline float key_logit(uint64_t k) { return bits_logit((uint32_t)(k >> 24)); }
 __device__ inline int key_index(uint64_t k) { return 0xffffff - (int)(k & 0xffffff); }
 
-struct SampleRow {
-  float top, per_bin;  // largest logit; bins per logit
-  double inv;          // 1 / temperature
-  __device__ inline SampleRow(float m, float t) : top(m), per_bin(SMP_BINS / (SMP_RANGE * t)), inv(1.0 / (double)t) {}
-  __device__ inline uint64_t weight(float x) const {
-    if (x == top) return (uint64_t)SMP_UNIT;
-    const double y = ((double)x - (double)top) * inv;
-    return y > -(double)SMP_RANGE ? (uint64_t)rint(exp(y) * SMP_UNIT) : 0;
+struct SampleRules {
+  float t, top_k, top_p;
+  uint64_t least;  // of a weight, by min-p
+  bool bad;
+  __device__ inline SampleRules(const float* r) : t(r[0]), top_k(r[1]), top_p(r[2]) {
+    const float m = r[3];
+    bad = !(t >= 0.f && t < INFINITY) || top_k != top_k || top_p != top_p || m != m;
+    least = m > 0.f ? (uint64_t)ceil((double)fminf(m, 1.f) * SMP_UNIT) : 0;
   }
-  __device__ inline int bin(float x) const { return x == top ? 0 : (int)fminf((top - x) * per_bin, (float)(SMP_BINS - 1)); }
+  __device__ inline bool short_by_k() const { return top_k >= 1.f && top_k <= SMP_THREADS / 2; }
+  __device__ inline bool short_by_min() const { return least > 0 && !(top_p < 1.f) && !(top_k >= 1.f); }
 };
 
-// sums over the workgroup
+// What a row's weights and bins are worked out from.  Weights: 2^(y / 64), y <= 0, is a table's 2^(j / 64) times Taylor's
+// polynomial on |f| <= ln(2) / 128 times a power of two; the first missing term is below 4e-17.  Without branches: what lies
+// far below (-infinity, NaN) is taken for 2^-40, a quarter of a unit, and rounds to 0.
+constexpr int SMP_STEPS = 64;
+struct SampleScale {
+  float half_top, per_bin;  // half the largest logit; bins per half a logit
+  double top, inv;          // 64 log2(e) / temperature
+  bool infinite;            // then the infinities count as 0 and all others as -infinity
+  __device__ inline SampleScale(float m, float t)
+      : half_top(m == INFINITY ? 0.f : 0.5f * m), per_bin(fminf((2 * SMP_BINS / SMP_RANGE) / t, 1e30f)),
+        top(m == INFINITY ? 0.0 : (double)m), inv(SMP_STEPS * 1.4426950408889634 / (double)t), infinite(m == INFINITY) {}
+  __device__ inline float seen(float x) const { return !infinite ? x : x == INFINITY ? 0.f : -INFINITY; }
+  __device__ inline uint64_t weight(float x, const double* table) const {
+    constexpr double L = 0.6931471805599453 / SMP_STEPS;
+    const double y = fmax(((double)x - top) * inv, -40.0 * SMP_STEPS), n = rint(y), f = y - n;
+    double p = L * L * L * L * L / 120;
+    p = fma(p, f, L * L * L * L / 24);
+    p = fma(p, f, L * L * L / 6);
+    p = fma(p, f, L * L / 2);
+    p = fma(p, f, L);
+    const int k = (int)n;
+    const double root = table[k & (SMP_STEPS - 1)];
+    p = fma(p * f, root, root);
+    // the sum's last bit is worth 1: the whole number is in its low bits
+    const double whole = ldexp(p, (k >> 6) + 38) + 4503599627370496.0;
+    return (uint64_t)__double_as_longlong(whole) & 0xfffffffffffffull;
+  }
+  // Falling with x.  The last bin's tokens weigh nothing: exp(-27.1 * 2047 / 2048) * 2^38 = 0.47.
+  __device__ inline int bin(float x) const { return (int)fminf(fmaf(-0.5f, x, half_top) * per_bin, (float)(SMP_BINS - 1)); }
+};
+
+// ---- sums over the workgroup
 __device__ inline uint64_t lane_up64(uint64_t v, int d) {
   return (uint64_t)(uint32_t)__shfl_up((int)(v >> 32), d) << 32 | (uint32_t)__shfl_up((int)v, d);
 }
@@ -67,25 +102,53 @@ __device__ inline uint64_t wave_scan64(uint64_t v) {  // inclusive
   }
   return v;
 }
+struct Parts {
+  uint64_t w[SMP_WAVES], n[SMP_WAVES];
+  float f[SMP_WAVES];
+};
 template <class F>
-__device__ inline uint64_t wave_all64(uint64_t v, F join) {
+__device__ inline uint64_t block_all64(uint64_t v, Parts& part, F join) {
 #pragma unroll
   for (int d = 32; d > 0; d >>= 1) v = join(v, (uint64_t)(uint32_t)__shfl_xor((int)(v >> 32), d) << 32 | (uint32_t)__shfl_xor((int)v, d));
-  return v;
-}
-template <class F>
-__device__ inline uint64_t block_all64(uint64_t v, uint64_t (&part)[SMP_THREADS / 64], F join) {
-  v = wave_all64(v, join);
   __syncthreads();
-  if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = v;
+  if ((threadIdx.x & 63) == 0) part.w[threadIdx.x >> 6] = v;
   __syncthreads();
-  v = part[0];
+  v = part.w[0];
 #pragma unroll
-  for (int w = 1; w < SMP_THREADS / 64; ++w) v = join(v, part[w]);
+  for (int w = 1; w < SMP_WAVES; ++w) v = join(v, part.w[w]);
   return v;
 }
+__device__ inline float block_max(float v, Parts& part) {  // of numbers
+#pragma unroll
+  for (int d = 32; d > 0; d >>= 1) v = fmaxf(v, __shfl_xor(v, d));
+  __syncthreads();
+  if ((threadIdx.x & 63) == 0) part.f[threadIdx.x >> 6] = v;
+  __syncthreads();
+  v = part.f[0];
+#pragma unroll
+  for (int w = 1; w < SMP_WAVES; ++w) v = fmaxf(v, part.f[w]);
+  return v;
+}
+// exclusive sum over the threads, and the whole
+__device__ inline uint64_t block_before64(uint64_t v, uint64_t (&part)[SMP_WAVES], uint64_t& all) {
+  const uint64_t upto = wave_scan64(v);
+  __syncthreads();
+  if ((threadIdx.x & 63) == 63) part[threadIdx.x >> 6] = upto;
+  __syncthreads();
+  uint64_t before = upto - v;
+  all = 0;
+#pragma unroll
+  for (int k = 0; k < SMP_WAVES; ++k) {
+    if (k < (int)(threadIdx.x >> 6)) before += part[k];
+    all += part[k];
+  }
+  return before;
+}
+struct Larger { __device__ uint64_t operator()(uint64_t p, uint64_t q) const { return p > q ? p : q; } };
+struct Smaller { __device__ uint64_t operator()(uint64_t p, uint64_t q) const { return p < q ? p : q; } };
+struct Plus { __device__ uint64_t operator()(uint64_t p, uint64_t q) const { return p + q; } };
 
-// Tokens per bin and the sum of their weights; after scan() those of all bins before, [SMP_BINS]: all.
+// Tokens per bin and the sum of their weights; after sum_bins() those of all bins before, [SMP_BINS]: all.
 struct Histogram {
   uint64_t w[SMP_BINS + 1];
   uint32_t n[SMP_BINS + 1];
@@ -96,199 +159,703 @@ struct Histogram {
     atomicAdd((unsigned long long*)&w[b], (unsigned long long)weight);
     atomicAdd(&n[b], 1u);
   }
-  __device__ inline void scan(uint64_t (&part_w)[SMP_THREADS / 64], uint64_t (&part_n)[SMP_THREADS / 64]) {
-    constexpr int PER = SMP_BINS / SMP_THREADS;
-    const int tid = threadIdx.x, wave = tid >> 6;
-    __syncthreads();
-    uint64_t mw = 0, mn = 0, cw[PER], cn[PER];
-#pragma unroll
-    for (int i = 0; i < PER; ++i) {
-      cw[i] = w[tid * PER + i], cn[i] = n[tid * PER + i];
-      mw += cw[i], mn += cn[i];
-    }
-    uint64_t sw = wave_scan64(mw), sn = wave_scan64(mn);
-    if ((tid & 63) == 63) part_w[wave] = sw, part_n[wave] = sn;
-    __syncthreads();
-    for (int k = 0; k < wave; ++k) sw += part_w[k], sn += part_n[k];
-    if (tid == SMP_THREADS - 1) w[SMP_BINS] = sw, n[SMP_BINS] = (uint32_t)sn;
-    sw -= mw, sn -= mn;
-#pragma unroll
-    for (int i = 0; i < PER; ++i) {
-      w[tid * PER + i] = sw, n[tid * PER + i] = (uint32_t)sn;
-      sw += cw[i], sn += cn[i];
-    }
-    __syncthreads();
-  }
-  // the bin with which the running count (or sum) exceeds `target`
-  __device__ inline int crossing(bool by_count, uint64_t target) const {
-    int lo = 0, hi = SMP_BINS;  // before(lo) <= target < before(hi)
-    while (hi - lo > 1) {
-      const int m = (lo + hi) >> 1;
-      if ((by_count ? (uint64_t)n[m] : w[m]) <= target) lo = m;
-      else hi = m;
-    }
-    return lo;
-  }
 };
 
-__global__ __launch_bounds__(SMP_THREADS) void sample_kernel(SampleArgs a) {
-  __shared__ Histogram first;
-  __shared__ union {  // never both at once
-    Histogram hist;
-    struct { uint64_t key[SMP_LIST], w[SMP_LIST]; } list;
-  } second;
-  Histogram& zoom = second.hist;
-  uint64_t *const list_key = second.list.key, *const list_w = second.list.w;
-  __shared__ uint64_t part_w[SMP_THREADS / 64], part_n[SMP_THREADS / 64];
-  __shared__ uint64_t found_key, found_w, found_upto;
-  __shared__ int list_n;
-  const int tid = threadIdx.x, lane = tid & 63, t = blockIdx.x;
-  if (t == 0)  // sequences without rows of their own
-    for (int s = tid; s < a.B; s += SMP_THREADS) {
-      const int r0 = a.node_off[s], r1 = a.node_off[s + 1];
-      const bool bad = r0 < 0 || r1 < r0 || r1 > a.T;
-      if (bad || r0 == r1) a.status[s] = bad;
-    }
-  int s = -1, r0 = 0;
-  for (int s0 = 0; s0 < a.B && s < 0; s0 += 64) {
-    const int q = min(s0 + lane, a.B - 1), b = a.node_off[q], e = a.node_off[q + 1];
-    const uint64_t here = __ballot(s0 + lane < a.B && b >= 0 && b <= t && t < e && e <= a.T);
-    if (here) {
-      const int l = __builtin_ctzll(here);
-      s = s0 + l;
-      r0 = __builtin_amdgcn_readlane(b, l);
-    }
-  }
-  if (s < 0) return;
-  const float temperature = a.rules[4 * s], top_k = a.rules[4 * s + 1], top_p = a.rules[4 * s + 2], min_p = a.rules[4 * s + 3];
-  const bool bad = !(temperature >= 0.f && temperature < INFINITY) || top_k != top_k || top_p != top_p || min_p != min_p;
-  if (t == r0 && tid == 0) a.status[s] = bad;
-  if (bad) return;
-
-  const float* const x = a.x + (size_t)t * a.V;
-  auto each = [&](auto f) {
-    for (int i = tid * 4; i < a.V; i += SMP_THREADS * 4) {
-      if (i + 4 <= a.V) {
-        const f32x4_row v = *reinterpret_cast<const f32x4_row*>(x + i);
-#pragma unroll
-        for (int e = 0; e < 4; ++e) f(v[e], i + e);
-      } else {
-        for (int e = i; e < a.V; ++e) f(x[e], e);
-      }
-    }
+struct SampleLds {
+  union {
+    struct {
+      uint64_t before[SMP_BINS + 1];  // weights per bin; after from_weights() of all bins before, [SMP_BINS]: all
+      union {
+        Histogram zoom;
+        struct { uint64_t key[SMP_LIST], w[SMP_LIST]; } list;
+        uint32_t count[SMP_BINS + 1];
+      };
+    } hist;
+    struct {
+      uint64_t key[SMP_LIST], sorted[SMP_LIST], upto[SMP_LIST];
+    } few;
+    uint32_t bins[SMP_BINS + 1];  // of the threads' largest logits
   };
-  auto larger = [](uint64_t p, uint64_t q) { return p > q ? p : q; };
-  auto smaller = [](uint64_t p, uint64_t q) { return p < q ? p : q; };
-  auto plus = [](uint64_t p, uint64_t q) { return p + q; };
-
-  uint64_t best = 0;
-  each([&](float v, int i) {
-    if (is_token(v)) best = larger(best, place_key(v, i));
-  });
-  best = block_all64(best, part_w, larger);
-  if (best == 0 || temperature == 0.f) {
-    if (tid == 0) {
-      a.token[t] = best == 0 ? -1 : key_index(best);
-      if (a.prob) a.prob[t] = best == 0 ? 0.f : 1.f;
-    }
-    return;
+  Parts part;
+  double table[SMP_STEPS];  // 2^(j / 64)
+  uint64_t found_key, found_w, found_upto;
+  uint32_t bound;
+  int list_n;
+  __device__ inline void make_table() {
+    if (threadIdx.x < SMP_STEPS) table[threadIdx.x] = exp2((double)threadIdx.x / SMP_STEPS);
   }
-  const SampleRow row(key_logit(best), temperature);
-  const uint64_t least = min_p > 0.f ? (uint64_t)ceil((double)fminf(min_p, 1.f) * SMP_UNIT) : 0;
-  first.clear();
+};
+template <class T>
+__device__ inline int crossing(const T (&before)[SMP_BINS + 1], uint64_t target) {  // before[lo] <= target < before[lo + 1]
+  int lo = 0, hi = SMP_BINS;
+  while (hi - lo > 1) {
+    const int m = (lo + hi) >> 1;
+    if (before[m] <= target) lo = m;
+    else hi = m;
+  }
+  return lo;
+}
+// counts or weights per bin to those of all bins before; the sum of all
+template <class T>
+__device__ inline uint64_t sum_bins(T (&x)[SMP_BINS + 1], Parts& part) {
+  constexpr int PER = SMP_BINS / SMP_THREADS;
+  const int tid = threadIdx.x;
   __syncthreads();
-  uint64_t over = 0;  // weights of `least` or more
-  each([&](float v, int i) {
-    if (!is_token(v)) return;
-    const uint64_t w = row.weight(v);
-    if (w == 0) return;
-    first.add(row.bin(v), w);
-    if (w >= least) over += w;
-  });
-  first.scan(part_w, part_n);
-  over = block_all64(over, part_n, plus);
+  T c[PER];
+  uint64_t sum = 0, all;
+#pragma unroll
+  for (int i = 0; i < PER; ++i) c[i] = x[tid * PER + i], sum += c[i];
+  uint64_t before = block_before64(sum, part.w, all);
+  if (tid == 0) x[SMP_BINS] = (T)all;
+#pragma unroll
+  for (int i = 0; i < PER; ++i) x[tid * PER + i] = (T)before, before += c[i];
+  __syncthreads();
+  return all;
+}
 
-  uint64_t kept = first.w[SMP_BINS];
+// the first position at which the running sum has to be at least this much, by top-p, less one
+__device__ inline uint64_t top_p_target(float p, uint64_t sum) {
+  const double need = ceil((double)p * (double)sum);
+  return need > 1.0 ? (uint64_t)need - 1 : 0;
+}
+__device__ inline uint64_t uniform_target(float u, uint64_t kept) {
+  const double v = fmin(fmax((double)u, 0.0), 1.0 - 1.0 / (1 << 24));  // NaN: 0
+  const uint64_t target = (uint64_t)floor(v * (double)kept);
+  return target < kept ? target : kept - 1;
+}
+__device__ inline void give(const SampleArgs& a, int t, uint64_t key, uint64_t w, uint64_t kept) {
+  a.token[t] = key_index(key);
+  if (a.prob) a.prob[t] = (float)((double)w / (double)kept);
+}
+
+// The n tokens of few.key, unsorted, among which the first n_keep (n or fewer) are all that top-k keeps.
+__device__ inline void finish_list(const SampleArgs& a, int t, const SampleRules& r, const SampleScale& sc, SampleLds& l, int n, int n_keep) {
+  const int tid = threadIdx.x;
+  auto& f = l.few;
+  // place of every token: the number of tokens ahead of it; several threads count for one where there are few
+  int wide = SMP_THREADS;
+  while (wide >> 1 >= n && wide > 64) wide >>= 1;
+  const int share = SMP_THREADS / wide, part = tid / wide;
+  uint32_t* const rank = reinterpret_cast<uint32_t*>(f.upto);
+  for (int e = tid; e < n; e += SMP_THREADS) rank[e] = 0;
+  __syncthreads();
+  for (int e = tid % wide; e < n; e += wide) {
+    const uint64_t k = f.key[e];
+    const int j1 = (int)((part + 1) * (long)n / share);
+    int ahead = 0;
+#pragma unroll 4
+    for (int j = (int)(part * (long)n / share); j < j1; ++j) ahead += f.key[j] > k;
+    if (share == 1) rank[e] = ahead;
+    else if (ahead) atomicAdd(&rank[e], (uint32_t)ahead);
+  }
+  __syncthreads();
+  for (int e = tid; e < n; e += SMP_THREADS) f.sorted[rank[e]] = f.key[e];
+  __syncthreads();
+  constexpr int PER = SMP_LIST / SMP_THREADS;
+  uint64_t key[PER], w[PER], upto[PER], sum = 0, kept;
+#pragma unroll
+  for (int i = 0; i < PER; ++i) {
+    const int e = tid * PER + i;
+    key[i] = e < n_keep ? f.sorted[e] : 0;
+    w[i] = e < n_keep ? sc.weight(sc.seen(key_logit(key[i])), l.table) : 0;
+    sum += w[i];
+    upto[i] = sum;
+  }
+  const uint64_t before = block_before64(sum, l.part.w, kept);
+#pragma unroll
+  for (int i = 0; i < PER; ++i) upto[i] += before;
+  // the token with which the running sum exceeds a target is in one thread's hands
+  auto crosses = [&](int i, uint64_t target) { return upto[i] - w[i] <= target && target < upto[i]; };
+  if (r.top_p < 1.f) {
+    const uint64_t target = top_p_target(r.top_p, kept);
+#pragma unroll
+    for (int i = 0; i < PER; ++i)
+      if (crosses(i, target)) l.found_upto = upto[i];
+    __syncthreads();
+    kept = l.found_upto;
+  }
+  if (r.least > 0) {
+    uint64_t over = 0;
+#pragma unroll
+    for (int i = 0; i < PER; ++i) over += w[i] >= r.least ? w[i] : 0;
+    over = block_all64(over, l.part, Plus());
+    kept = over < kept ? over : kept;
+  }
+  const uint64_t target = uniform_target(a.uniform[t], kept);
+#pragma unroll
+  for (int i = 0; i < PER; ++i)
+    if (crosses(i, target)) give(a, t, key[i], w[i], kept);
+}
+
+// From the weights per bin (hist.before, summed), with `scan` over all tokens of the row (others may be among them); over:
+// the sum of the weights that min-p allows.  False, with nothing given, where a
+// count decides or a bin is too full for the list.
+template <class Scan>
+__device__ inline bool finish_bins(const SampleArgs& a, int t, const SampleRules& r, const SampleScale& sc, SampleLds& l,
+                                   uint64_t over, Scan scan) {
+  if (r.top_k >= 1.f && r.top_k < (float)a.V) return false;
+  const int tid = threadIdx.x;
+  auto& h = l.hist;
+  uint64_t kept = h.before[SMP_BINS];
+#pragma unroll 1
+  for (int step = r.top_p < 1.f ? 0 : 1; step < 2; ++step) {  // top-p, the token
+    if (step == 1) kept = over < kept ? over : kept;
+    const uint64_t target = step == 0 ? top_p_target(r.top_p, kept) : uniform_target(a.uniform[t], kept);
+    const int b = crossing(h.before, target);
+    __syncthreads();
+    if (tid == 0) l.list_n = 0;
+    __syncthreads();
+    SampleScale q = sc;  // nothing of it is to be kept from before, in registers for every logit
+    asm volatile("" : "+v"(q.half_top), "+v"(q.per_bin));
+    scan([&](float v, int i) {
+      if (q.bin(v) != b) return;  // (what is no token is in the last bin, in which nothing crosses)
+      const int at = atomicAdd(&l.list_n, 1);
+      if (at < SMP_LIST) h.list.key[at] = place_key(v, i);
+    });
+    __syncthreads();
+    const int n = l.list_n;
+    if (n > SMP_LIST) return false;
+    for (int e = tid; e < n; e += SMP_THREADS) h.list.w[e] = sc.weight(key_logit(h.list.key[e]), l.table);
+    __syncthreads();
+    for (int e = tid; e < n; e += SMP_THREADS) {
+      const uint64_t k = h.list.key[e], w = h.list.w[e];
+      uint64_t sum = h.before[b];
+#pragma unroll 4
+      for (int j = 0; j < n; ++j)
+        if (h.list.key[j] > k) sum += h.list.w[j];
+      if (sum <= target && target < sum + w) l.found_key = k, l.found_w = w, l.found_upto = sum + w;
+    }
+    __syncthreads();
+    if (step == 0) kept = l.found_upto;
+  }
+  if (tid == 0) give(a, t, l.found_key, l.found_w, kept);
+  return true;
+}
+
+// The same for every row, with `each` over its tokens.
+template <class Each>
+__device__ inline void finish_histogram(const SampleArgs& a, int t, const SampleRules& r, const SampleScale& sc, SampleLds& l,
+                                        uint64_t over, Each each) {
+  const int tid = threadIdx.x;
+  auto& h = l.hist;
+  uint64_t kept = h.before[SMP_BINS];
 #pragma unroll 1
   for (int step = 0; step < 3; ++step) {  // top-k, top-p, the token
-    bool by_count = false;
-    uint64_t target;  // the first token with which the running count or sum exceeds it is wanted
+    const bool by_count = step == 0;
+    uint64_t target, before_n = 0;  // the first token with which the running count or sum exceeds it is wanted
+    int b;
     if (step == 0) {
-      if (!(top_k >= 1.f) || top_k >= (float)first.n[SMP_BINS]) continue;
-      by_count = true;
-      target = (uint64_t)top_k - 1;
-    } else if (step == 1) {
-      if (!(top_p < 1.f)) continue;
-      const double need = ceil((double)top_p * (double)kept);
-      target = need > 1.0 ? (uint64_t)need - 1 : 0;
+      if (!(r.top_k >= 1.f) || r.top_k >= (float)a.V) continue;
+      target = (uint64_t)r.top_k - 1;
+      for (int i = tid; i <= SMP_BINS; i += SMP_THREADS) h.count[i] = 0;
+      __syncthreads();
+      each([&](float v, int) { atomicAdd(&h.count[sc.bin(v)], 1u); });
+      sum_bins(h.count, l.part);
+      if (target >= h.count[SMP_BINS - 1]) continue;  // among those that weigh nothing, or beyond all
+      b = crossing(h.count, target);
+      before_n = h.count[b];
+      __syncthreads();
     } else {
-      kept = smaller(kept, over);
-      const double u = fmin(fmax((double)a.uniform[t], 0.0), 1.0 - 1.0 / (1 << 24));
-      target = smaller((uint64_t)floor(u * (double)kept), kept - 1);
+      if (step == 1) {
+        if (!(r.top_p < 1.f)) continue;
+        target = top_p_target(r.top_p, kept);
+      } else {
+        kept = over < kept ? over : kept;
+        target = uniform_target(a.uniform[t], kept);
+      }
+      b = crossing(h.before, target);
     }
-    const int b = first.crossing(by_count, target);
-    uint64_t before_w = first.w[b], lo = 0, hi = ~0ull;
-    uint32_t before_n = first.n[b], n = first.n[b + 1] - before_n;
+    uint64_t before_w = h.before[b], lo = 0, hi = ~0ull;
+    // the tokens lo .. hi of bin b; their number, and as many as there is room for in the list
+    auto list = [&]() {
+      __syncthreads();
+      if (tid == 0) l.list_n = 0;
+      __syncthreads();
+      each([&](float v, int i) {
+        if (sc.bin(v) != b) return;
+        const uint64_t k = place_key(v, i);
+        if (k < lo || k > hi) return;
+        const int at = atomicAdd(&l.list_n, 1);
+        if (at < SMP_LIST) h.list.key[at] = k, h.list.w[at] = sc.weight(v, l.table);
+      });
+      __syncthreads();
+      return l.list_n;
+    };
+    int n = list();
     if (n > SMP_LIST) {  // many alike: closer, over the whole order
       uint64_t kmin = ~0ull, kmax = 0;
       each([&](float v, int i) {
-        if (is_token(v) && row.bin(v) == b && row.weight(v) > 0) kmin = smaller(kmin, place_key(v, i)), kmax = larger(kmax, place_key(v, i));
+        if (sc.bin(v) == b) kmin = Smaller()(kmin, place_key(v, i)), kmax = Larger()(kmax, place_key(v, i));
       });
-      lo = block_all64(kmin, part_w, smaller);
-      hi = block_all64(kmax, part_w, larger);
-      while (n > SMP_LIST) {
+      lo = block_all64(kmin, l.part, Smaller());
+      hi = block_all64(kmax, l.part, Larger());
+      do {
         const int bits = 64 - __clzll((long long)(hi - lo)), shift = max(0, bits - 11);  // (hi - lo) >> shift < SMP_BINS
-        zoom.clear();
+        __syncthreads();
+        h.zoom.clear();
         __syncthreads();
         each([&](float v, int i) {
-          if (!is_token(v) || row.bin(v) != b) return;
-          const uint64_t k = place_key(v, i), w = row.weight(v);
-          if (k >= lo && k <= hi && w > 0) zoom.add((int)((hi - k) >> shift), w);
+          if (sc.bin(v) != b) return;
+          const uint64_t k = place_key(v, i);
+          if (k >= lo && k <= hi) h.zoom.add((int)((hi - k) >> shift), sc.weight(v, l.table));
         });
-        zoom.scan(part_w, part_n);
-        const int z = zoom.crossing(by_count, target - (by_count ? before_n : before_w));
-        before_w += zoom.w[z];
-        before_n += zoom.n[z];
-        n = zoom.n[z + 1] - zoom.n[z];
+        sum_bins(h.zoom.w, l.part);
+        sum_bins(h.zoom.n, l.part);
+        const int z = by_count ? crossing(h.zoom.n, target - before_n) : crossing(h.zoom.w, target - before_w);
+        before_w += h.zoom.w[z];
+        before_n += h.zoom.n[z];
+        n = h.zoom.n[z + 1] - h.zoom.n[z];
         const uint64_t top = hi - ((uint64_t)z << shift);
         const uint64_t width = (1ull << shift) - 1;
         lo = top - lo > width ? top - width : lo;
         hi = top;
-        __syncthreads();
-      }
+      } while (n > SMP_LIST);
+      list();
     }
-    if (tid == 0) list_n = 0;
-    __syncthreads();
-    each([&](float v, int i) {
-      if (!is_token(v) || row.bin(v) != b) return;
-      const uint64_t k = place_key(v, i), w = row.weight(v);
-      if (w == 0 || k < lo || k > hi) return;
-      const int at = atomicAdd(&list_n, 1);
-      if (at < SMP_LIST) list_key[at] = k, list_w[at] = w;
-    });
-    __syncthreads();
-    for (int e = tid; e < (int)n; e += SMP_THREADS) {
-      const uint64_t k = list_key[e], w = list_w[e];
+    for (int e = tid; e < n; e += SMP_THREADS) {
+      const uint64_t k = h.list.key[e], w = h.list.w[e];
       uint64_t sum = before_w, rank = before_n;
-      for (int j = 0; j < (int)n; ++j)
-        if (list_key[j] > k) sum += list_w[j], ++rank;
-      if (by_count ? rank == target : (sum <= target && target < sum + w)) found_key = k, found_w = w, found_upto = sum + w;
+#pragma unroll 4
+      for (int j = 0; j < n; ++j)
+        if (h.list.key[j] > k) sum += h.list.w[j], ++rank;
+      if (by_count ? rank == target : (sum <= target && target < sum + w)) l.found_key = k, l.found_w = w, l.found_upto = sum + w;
     }
     __syncthreads();
-    if (step < 2) kept = found_upto;
+    if (step < 2) kept = l.found_upto;
   }
-  if (tid == 0) {
-    a.token[t] = key_index(found_key);
-    if (a.prob) a.prob[t] = (float)((double)found_w / (double)kept);
+  if (tid == 0) give(a, t, l.found_key, l.found_w, kept);
+}
+
+// The sequence of row t, -1: none; the same on all lanes.  Its first row's workgroup answers for its rules.
+__device__ inline int sample_sequence(const SampleArgs& a, int t, bool& first_row) {
+  const int lane = threadIdx.x & 63;
+  for (int s0 = 0; s0 < a.B; s0 += 64) {
+    const int q = min(s0 + lane, a.B - 1), b = a.node_off[q], e = a.node_off[q + 1];
+    const uint64_t here = __ballot(s0 + lane < a.B && b >= 0 && b <= t && t < e && e <= a.T);
+    if (here) {
+      const int l = __builtin_ctzll(here);
+      first_row = __builtin_amdgcn_readlane(b, l) == t;
+      return s0 + l;
+    }
+  }
+  return -1;
+}
+__device__ inline void empty_sequences(const SampleArgs& a) {
+  for (int s = threadIdx.x; s < a.B; s += SMP_THREADS) {
+    const int r0 = a.node_off[s], r1 = a.node_off[s + 1];
+    const bool bad = r0 < 0 || r1 < r0 || r1 > a.T;
+    if (bad || r0 == r1) a.status[s] = bad;
   }
 }
 
-size_t tree_sample_ws_bytes(int, int) { return 16; }
-int launch_tree_sample(const float* x, const int32_t* node_off, int B, int T, int V, const float* rules,
-                       const float* uniform, int32_t* token, float* prob, void*, int32_t* status, hipStream_t st) {
-  const SampleArgs a{x, node_off, B, T, V, rules, uniform, token, prob, status};
-  sample_kernel<<<T, SMP_THREADS, 0, st>>>(a);
+// Every token of a row, read from memory.
+struct Streamed {
+  const float* x;
+  int V;
+  SampleScale sc;
+  template <class F>
+  __device__ inline void operator()(F f) const {
+#pragma unroll 1
+    for (int i = (int)threadIdx.x * 4; i < V; i += SMP_THREADS * 4) {
+      float v[4];
+      if (i + 4 <= V) {
+        const f32x4_row q = *reinterpret_cast<const f32x4_row*>(x + i);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[e] = q[e];
+      } else {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[e] = i + e < V ? x[i + e] : -INFINITY;
+      }
+#pragma unroll 1
+      for (int e = 0; e < 4; ++e) {
+        const float u = sc.seen(e == 0 ? v[0] : e == 1 ? v[1] : e == 2 ? v[2] : v[3]);
+        if (is_token(u)) f(u, i + e);
+      }
+    }
+  }
+};
+// 4 * NV logits per thread of x[0 .. n), 2048 apart in groups of four, -infinity where there are none.
+template <int NV>
+struct Held {
+  float v[NV][4];
+  __device__ inline void load(const float* x, int n) {
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+      const int at = (i * SMP_THREADS + threadIdx.x) * 4;
+      if (at + 4 <= n) {
+        const f32x4_row q = *reinterpret_cast<const f32x4_row*>(x + at);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[i][e] = q[e];
+      } else {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[i][e] = at + e < n ? x[at + e] : -INFINITY;
+      }
+    }
+  }
+  __device__ inline float top() const {
+    float m = -INFINITY;  // (NaN is passed over)
+#pragma unroll
+    for (int i = 0; i < NV; ++i)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) m = fmaxf(m, v[i][e]);
+    return m;
+  }
+  template <class F>
+  __device__ inline void each(F f) const {
+#pragma unroll
+    for (int i = 0; i < NV; ++i)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) f(v[i][e], (i * SMP_THREADS + (int)threadIdx.x) * 4 + e);
+  }
+  __device__ inline void only_infinities() {
+#pragma unroll
+    for (int i = 0; i < NV; ++i)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) v[i][e] = v[i][e] == INFINITY ? 0.f : -INFINITY;
+  }
+  // weights per bin; the sum of this thread's of `least` or more
+  __device__ inline uint64_t add_weights(const SampleScale& sc, uint64_t least, SampleLds& l) const {
+    uint64_t over = 0;
+#pragma unroll
+    for (int i = 0; i < NV; ++i)
+#pragma unroll
+      for (int g = 0; g < 4; g += SMP_ABREAST) {
+        uint64_t w[SMP_ABREAST];
+        int b[SMP_ABREAST];
+#pragma unroll
+        for (int e = 0; e < SMP_ABREAST; ++e) {
+          w[e] = sc.weight(v[i][g + e], l.table), b[e] = sc.bin(v[i][g + e]);
+        }
+#pragma unroll
+        for (int e = 0; e < SMP_ABREAST; ++e) {
+          atomicAdd((unsigned long long*)&l.hist.before[b[e]], (unsigned long long)w[e]);
+          over += w[e] >= least ? w[e] : 0;
+        }
+        __builtin_amdgcn_sched_barrier(0);  // group after group, for registers
+      }
+    return over;
+  }
+};
+// All logits of a part of a row, piece after piece from memory.
+struct Pieces {
+  const float* x;
+  int from, to;
+  template <class F>
+  __device__ inline void held(F f) const {
+#pragma unroll 1
+    for (int i = from; i < to; i += 16 * SMP_THREADS) {
+      Held<4> h;
+      h.load(x + i, to - i);
+      f(h, i);
+    }
+  }
+  template <class F>
+  __device__ inline void operator()(F f) const {
+    held([&](Held<4>& h, int i0) { h.each([&](float v, int i) { f(v, i0 + i); }); });
+  }
+};
+// A logit that at least k tokens of the workgroup reach, and few more: the threads' largest ones, by bins below the top.
+// -infinity where fewer than k threads hold tokens that can weigh anything.
+__device__ inline float reached_by(uint32_t k, float mine, const SampleScale& sc, SampleLds& l) {
+  const int tid = threadIdx.x;
+  __syncthreads();
+  for (int i = tid; i < SMP_BINS; i += SMP_THREADS) l.bins[i] = 0;
+  if (tid == 0) l.bound = 0xffffffffu;
+  __syncthreads();
+  const int b = sc.bin(sc.seen(mine));
+  const bool counts = b < SMP_BINS - 1;
+  if (counts) atomicAdd(&l.bins[b], 1u);
+  __syncthreads();
+  const uint64_t all = sum_bins(l.bins, l.part);
+  if (all < k) return -INFINITY;
+  if (counts && l.bins[b] < k) atomicMin(&l.bound, place_bits(mine));
+  __syncthreads();
+  return bits_logit(l.bound);
+}
+// Tokens from `bound` on to out[0 .. cap), in any order; their number
+template <int NV>
+__device__ inline int collect(const Held<NV>& x, float bound, int first_index, uint64_t* out, int cap, SampleLds& l) {
+  __syncthreads();
+  if (threadIdx.x == 0) l.list_n = 0;
+  __syncthreads();
+  x.each([&](float v, int i) {
+    if (!(v >= bound)) return;
+    const int at = atomicAdd(&l.list_n, 1);
+    if (at < cap) out[at] = place_key(v, first_index + i);
+  });
+  __syncthreads();
+  return l.list_n;
+}
+// Row t without tokens, or greedy
+__device__ inline void give_first(const SampleArgs& a, int t, uint64_t best) {
+  a.token[t] = best == 0 ? -1 : key_index(best);
+  if (a.prob) a.prob[t] = best == 0 ? 0.f : 1.f;
+}
+
+__device__ inline float min_p_bound(const SampleRules& r, float top) {
+  // a token below it weighs less than `least`, by far more than a weight's error
+  return (float)((double)top + log((double)r.least * 0.999 / SMP_UNIT) * r.t - fabs((double)top) * 1e-6);
+}
+
+// Everything from the row in memory, for the few rows that need it.
+__device__ inline void finish_slowly(const SampleArgs& a, int t, const SampleRules& r, const SampleScale& sc, SampleLds& l) {
+  const int tid = threadIdx.x;
+  const Streamed each{a.x + (size_t)t * a.V, a.V, sc};
+  __syncthreads();
+  for (int i = tid; i <= SMP_BINS; i += SMP_THREADS) l.hist.before[i] = 0;
+  __syncthreads();
+  uint64_t over = 0;
+  each([&](float v, int) {
+    const uint64_t w = sc.weight(v, l.table);
+    atomicAdd((unsigned long long*)&l.hist.before[sc.bin(v)], (unsigned long long)w);
+    over += w >= r.least ? w : 0;
+  });
+  sum_bins(l.hist.before, l.part);
+  over = block_all64(over, l.part, Plus());
+  finish_histogram(a, t, r, sc, l, over, each);
+}
+
+// One workgroup per row, the row in registers.
+template <int NV>
+__global__ __launch_bounds__(SMP_THREADS, 4) void sample_row_kernel(SampleArgs a) {
+  __shared__ SampleLds l;
+  const int tid = threadIdx.x, t = blockIdx.x;
+  if (t == 0) empty_sequences(a);
+  Held<NV> row;
+  const float* const x = a.x + (size_t)t * a.V;
+  row.load(x, a.V);
+  bool first_row = false;
+  const int s = sample_sequence(a, t, first_row);
+  if (s < 0) return;
+  const SampleRules r(a.rules + 4 * s);
+  if (first_row && tid == 0) a.status[s] = r.bad;
+  if (r.bad) return;
+  l.make_table();
+  const float mine = row.top(), top = block_max(mine, l.part);
+  if (!is_token(top) || r.t == 0.f) {
+    uint64_t best = 0;
+    row.each([&](float v, int i) {
+      if (v == top && is_token(v)) best = Larger()(best, place_key(v, i));
+    });
+    best = block_all64(best, l.part, Larger());
+    if (tid == 0) give_first(a, t, best);
+    return;
+  }
+  const SampleScale sc(top, r.t);
+  // ---- the short list
+  if (r.short_by_k() || r.short_by_min()) {
+    const int k = r.short_by_k() ? (int)r.top_k : 0;
+    const float bound = k > 0 ? reached_by(k, mine, sc, l) : min_p_bound(r, top);
+    if (bound > -INFINITY) {
+      const int n = collect(row, bound, 0, l.few.key, SMP_LIST, l);
+      if (n <= SMP_LIST) {
+        finish_list(a, t, r, sc, l, n, k > 0 ? min(n, k) : n);
+        return;
+      }
+    }
+  }
+  // ---- the histogram, from memory again (that the row kept its registers through it cost hundreds of spills)
+  const Pieces all{x, 0, a.V};
+  __syncthreads();
+  for (int i = tid; i <= SMP_BINS; i += SMP_THREADS) l.hist.before[i] = 0;
+  __syncthreads();
+  uint64_t over = 0;
+  all.held([&](Held<4>& h, int) {
+    if (sc.infinite) h.only_infinities();
+    over += h.add_weights(sc, r.least, l);
+  });
+  sum_bins(l.hist.before, l.part);
+  over = block_all64(over, l.part, Plus());
+  if (!finish_bins(a, t, r, sc, l, over, [&](auto f) { all([&](float v, int i) { f(sc.seen(v), i); }); })) finish_slowly(a, t, r, sc, l);
+}
+
+// ---- rows cut into chunks: what every chunk finds out by itself, then the weights of the rows that need them all, then the rows
+struct ChunkedRows {
+  int row0, rows, chunks, size;  // of the launch; per row; logits, a multiple of 4
+  float* top;                    // [rows][chunks]
+  int32_t* n;                    // tokens listed, -1: not all that top-k could keep
+  uint64_t *over, *data;         // weights that min-p allows; the list, or the weights per bin, [SMP_BINS]
+  __device__ inline size_t at(int t, int c) const { return (size_t)(t - row0) * chunks + c; }
+};
+constexpr int SMP_CHUNK_LIST = 1024;
+
+template <int NV>
+__global__ __launch_bounds__(SMP_THREADS) void sample_chunk_kernel(SampleArgs a, ChunkedRows ch) {
+  __shared__ SampleLds l;
+  const int tid = threadIdx.x, t = ch.row0 + blockIdx.x / ch.chunks, c = blockIdx.x % ch.chunks, first = c * ch.size;
+  if (blockIdx.x == 0 && ch.row0 == 0) empty_sequences(a);
+  Held<NV> row;
+  row.load(a.x + (size_t)t * a.V + first, min(ch.size, a.V - first));
+  bool first_row = false;
+  const int s = sample_sequence(a, t, first_row);
+  if (s < 0) return;
+  const SampleRules r(a.rules + 4 * s);
+  if (first_row && c == 0 && tid == 0) a.status[s] = r.bad;
+  if (r.bad) return;
+  const float mine = row.top(), top = block_max(mine, l.part);
+  const size_t at = ch.at(t, c);
+  int n = -1;
+  if (!is_token(top)) {
+    n = 0;
+  } else if (r.short_by_k() && r.t > 0.f) {
+    const float bound = reached_by((uint32_t)r.top_k, mine, SampleScale(top, r.t), l);
+    n = collect(row, fmaxf(bound, -3.4028235e38f), first, ch.data + at * SMP_BINS, SMP_CHUNK_LIST, l);
+    if (n > SMP_CHUNK_LIST) n = -1;
+  }
+  if (tid == 0) ch.top[at] = top, ch.n[at] = n;
+}
+// largest logit of a row, and whether its chunks list all that top-k could keep
+struct ChunkedTop {
+  float top;
+  bool listed;
+};
+__device__ inline ChunkedTop chunked_top(const ChunkedRows& ch, int t, const SampleRules& r) {
+  ChunkedTop x{-INFINITY, r.short_by_k()};
+  for (int c = 0; c < ch.chunks; ++c) {
+    const size_t at = ch.at(t, c);
+    x.top = fmaxf(x.top, ch.top[at]);
+    x.listed = x.listed && ch.n[at] >= 0;
+  }
+  return x;
+}
+template <int NV>
+__global__ __launch_bounds__(SMP_THREADS) void sample_weigh_kernel(SampleArgs a, ChunkedRows ch) {
+  __shared__ SampleLds l;
+  const int tid = threadIdx.x, t = ch.row0 + blockIdx.x / ch.chunks, c = blockIdx.x % ch.chunks, first = c * ch.size;
+  bool first_row = false;
+  const int s = sample_sequence(a, t, first_row);
+  if (s < 0) return;
+  const SampleRules r(a.rules + 4 * s);
+  if (r.bad || r.t == 0.f) return;
+  const ChunkedTop x = chunked_top(ch, t, r);
+  if (x.listed || !is_token(x.top)) return;
+  const SampleScale sc(x.top, r.t);
+  Held<NV> row;
+  row.load(a.x + (size_t)t * a.V + first, min(ch.size, a.V - first));
+  l.make_table();
+  for (int i = tid; i <= SMP_BINS; i += SMP_THREADS) l.hist.before[i] = 0;
+  __syncthreads();
+  if (sc.infinite) row.only_infinities();
+  uint64_t over = row.add_weights(sc, r.least, l);
+  over = block_all64(over, l.part, Plus());
+  const size_t at = ch.at(t, c);
+  for (int i = tid; i < SMP_BINS; i += SMP_THREADS) ch.data[at * SMP_BINS + i] = l.hist.before[i];
+  if (tid == 0) ch.over[at] = over;
+}
+__global__ __launch_bounds__(SMP_THREADS) void sample_finish_kernel(SampleArgs a, ChunkedRows ch) {
+  __shared__ SampleLds l;
+  const int tid = threadIdx.x, t = ch.row0 + blockIdx.x;
+  bool first_row = false;
+  const int s = sample_sequence(a, t, first_row);
+  if (s < 0) return;
+  const SampleRules r(a.rules + 4 * s);
+  if (r.bad) return;
+  l.make_table();
+  const ChunkedTop x = chunked_top(ch, t, r);
+  const float* const row = a.x + (size_t)t * a.V;
+  if (!is_token(x.top) || r.t == 0.f) {
+    uint64_t best = 0;
+    if (is_token(x.top)) {
+      int c = 0;
+      while (ch.top[ch.at(t, c)] != x.top) ++c;  // (one of them is the largest)
+      Pieces{row, c * ch.size, min(a.V, (c + 1) * ch.size)}([&](float v, int i) {
+        if (v == x.top) best = Larger()(best, place_key(v, i));
+      });
+    }
+    best = block_all64(best, l.part, Larger());
+    if (tid == 0) give_first(a, t, best);
+    return;
+  }
+  const SampleScale sc(x.top, r.t);
+  if (x.listed) {
+    const int k = (int)r.top_k;
+    auto entries = [&](auto f) {
+      for (int c = 0; c < ch.chunks; ++c) {
+        const size_t at = ch.at(t, c);
+        for (int i = tid; i < ch.n[at]; i += SMP_THREADS) f(ch.data[at * SMP_BINS + i]);
+      }
+    };
+    uint64_t best = 0;
+    entries([&](uint64_t key) { best = Larger()(best, key); });
+    float bound = reached_by(k, best == 0 ? -INFINITY : key_logit(best), sc, l);
+    __syncthreads();
+    if (tid == 0) l.list_n = 0;
+    __syncthreads();
+    entries([&](uint64_t key) {
+      if (!(key_logit(key) >= bound)) return;
+      const int at = atomicAdd(&l.list_n, 1);
+      if (at < SMP_LIST) l.few.key[at] = key;
+    });
+    __syncthreads();
+    const int n = l.list_n;
+    if (n <= SMP_LIST) {
+      finish_list(a, t, r, sc, l, n, min(n, k));
+      return;
+    }
+  }
+  // ---- the histogram of the chunks, or, where the lists were too long after all, from the row itself
+  if (!x.listed) {
+    for (int i = tid; i <= SMP_BINS; i += SMP_THREADS) {
+      uint64_t w = 0;
+      if (i < SMP_BINS)
+        for (int c = 0; c < ch.chunks; ++c) w += ch.data[ch.at(t, c) * SMP_BINS + i];
+      l.hist.before[i] = w;
+    }
+    __syncthreads();
+    uint64_t over = 0;
+    for (int c = tid; c < ch.chunks; c += SMP_THREADS) over += ch.over[ch.at(t, c)];
+    sum_bins(l.hist.before, l.part);
+    over = block_all64(over, l.part, Plus());
+    if (finish_bins(a, t, r, sc, l, over, [&](auto f) { Pieces{row, 0, a.V}([&](float v, int i) { f(sc.seen(v), i); }); })) return;
+  }
+  finish_slowly(a, t, r, sc, l);
+}
+
+// ------------------------------------------------------------------ launch
+constexpr int SMP_ROW = 64 * SMP_THREADS, SMP_CHUNK = 32 * SMP_THREADS;  // logits that a workgroup holds
+struct SampleLaunch {
+  int chunks, size, rows;  // per row; logits; rows of a launch
+};
+static SampleLaunch sample_launch(int T, int V) {
+  SampleLaunch p{0, 0, T};
+  if (V <= SMP_ROW) return p;
+  const int least = (V + SMP_CHUNK - 1) / SMP_CHUNK, most = (V + 8 * SMP_THREADS - 1) / (8 * SMP_THREADS);
+  p.chunks = std::min(std::max(least, (512 + T - 1) / T), most);
+  p.size = ((V + p.chunks - 1) / p.chunks + 3) / 4 * 4;
+  p.chunks = (V + p.size - 1) / p.size;
+  p.rows = std::max(1, std::min(T, 4096 / p.chunks));
+  return p;
+}
+size_t tree_sample_ws_bytes(int T, int V) {
+  const SampleLaunch p = sample_launch(T, V);
+  return (size_t)p.rows * p.chunks * (8 * SMP_BINS + 16) + 16;
+}
+template <int NV>
+static int sample_chunked(const SampleArgs& a, const ChunkedRows& ch, hipStream_t st) {
+  sample_chunk_kernel<NV><<<ch.rows * ch.chunks, SMP_THREADS, 0, st>>>(a, ch);
+  sample_weigh_kernel<NV><<<ch.rows * ch.chunks, SMP_THREADS, 0, st>>>(a, ch);
+  sample_finish_kernel<<<ch.rows, SMP_THREADS, 0, st>>>(a, ch);
   return check_launch();
+}
+int launch_tree_sample(const float* x, const int32_t* node_off, int B, int T, int V, const float* rules,
+                       const float* uniform, int32_t* token, float* prob, void* ws, int32_t* status, hipStream_t st) {
+  const SampleArgs a{x, node_off, B, T, V, rules, uniform, token, prob, status};
+  const SampleLaunch p = sample_launch(T, V);
+  if (p.chunks == 0) {
+    if (V <= 8 * SMP_THREADS) sample_row_kernel<2><<<T, SMP_THREADS, 0, st>>>(a);
+    else if (V <= 32 * SMP_THREADS) sample_row_kernel<8><<<T, SMP_THREADS, 0, st>>>(a);
+    else sample_row_kernel<16><<<T, SMP_THREADS, 0, st>>>(a);
+    return check_launch();
+  }
+  const size_t all = (size_t)p.rows * p.chunks;
+  uint64_t* const data = (uint64_t*)ws;
+  for (int row0 = 0; row0 < T; row0 += p.rows) {
+    const ChunkedRows ch{row0, std::min(p.rows, T - row0), p.chunks, p.size, (float*)(data + all * (SMP_BINS + 1)),
+                         (int32_t*)(data + all * (SMP_BINS + 1)) + all, data + all * SMP_BINS, data};
+    const int rc = p.size <= 8 * SMP_THREADS ? sample_chunked<2>(a, ch, st) : sample_chunked<8>(a, ch, st);
+    if (rc != TRJ_OK) return rc;
+  }
+  return TRJ_OK;
 }
 
 }  // namespace trj
