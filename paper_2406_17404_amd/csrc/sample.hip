@@ -58,32 +58,32 @@ struct SampleRules {
   __device__ inline bool short_by_min() const { return least > 0 && !(top_p < 1.f) && !(top_k >= 1.f); }
 };
 
-// What a row's weights and bins are worked out from.  Weights: 2^(y / 64), y <= 0, is a table's 2^(j / 64) times Taylor's
-// polynomial on |f| <= ln(2) / 128 times a power of two; the first missing term is below 4e-17.  Without branches: what lies
-// far below (-infinity, NaN) is taken for 2^-40, a quarter of a unit, and rounds to 0.
-constexpr int SMP_STEPS = 64;
+// What a row's weights and bins are worked out from.  Weights: 2^(y / 128), y <= 0, is a table's 2^(j / 128) times Taylor's
+// polynomial on |f| <= ln(2) / 256 times a power of two; the first missing term is below 1.3e-15, 2^-11 of a unit.  Without
+// branches: what lies far below (-infinity, NaN) is taken for 2^-40, a quarter of a unit, and rounds to 0.  Whole numbers come
+// from adding 1.5 * 2^52, which leaves them in a sum's low bits: rounding and conversion are instructions at a fraction of the rate.
+constexpr int SMP_STEPS = 128;
 struct SampleScale {
   float half_top, per_bin;  // half the largest logit; bins per half a logit
-  double top, inv;          // 64 log2(e) / temperature
+  double top, inv;          // 128 log2(e) / temperature
   bool infinite;            // then the infinities count as 0 and all others as -infinity
   __device__ inline SampleScale(float m, float t)
       : half_top(m == INFINITY ? 0.f : 0.5f * m), per_bin(fminf((2 * SMP_BINS / SMP_RANGE) / t, 1e30f)),
         top(m == INFINITY ? 0.0 : (double)m), inv(SMP_STEPS * 1.4426950408889634 / (double)t), infinite(m == INFINITY) {}
   __device__ inline float seen(float x) const { return !infinite ? x : x == INFINITY ? 0.f : -INFINITY; }
   __device__ inline uint64_t weight(float x, const double* table) const {
-    constexpr double L = 0.6931471805599453 / SMP_STEPS;
-    const double y = fmax(((double)x - top) * inv, -40.0 * SMP_STEPS), n = rint(y), f = y - n;
-    double p = L * L * L * L * L / 120;
-    p = fma(p, f, L * L * L * L / 24);
-    p = fma(p, f, L * L * L / 6);
+    constexpr double L = 0.6931471805599453 / SMP_STEPS, WHOLE = 6755399441055744.0;
+    const double y = fmax(((double)x - top) * inv, -40.0 * SMP_STEPS), n = y + WHOLE, f = y - (n - WHOLE);
+    const int k = (int)__double_as_longlong(n);
+    double p = fma(L * L * L * L / 24, f, L * L * L / 6);
     p = fma(p, f, L * L / 2);
     p = fma(p, f, L);
-    const int k = (int)n;
     const double root = table[k & (SMP_STEPS - 1)];
-    p = fma(p * f, root, root);
-    // the sum's last bit is worth 1: the whole number is in its low bits
-    const double whole = ldexp(p, (k >> 6) + 38) + 4503599627370496.0;
-    return (uint64_t)__double_as_longlong(whole) & 0xfffffffffffffull;
+    const uint64_t r = (uint64_t)__double_as_longlong(fma(p * f, root, root));
+    // times 2^(k / 128 + 38), in the exponent
+    const uint64_t scaled = (uint64_t)((uint32_t)(r >> 32) + ((uint32_t)((k >> 7) + 38) << 20)) << 32 | (uint32_t)r;
+    const double whole = __longlong_as_double((long long)scaled) + WHOLE;
+    return (uint64_t)__double_as_longlong(whole) & 0x7ffffffffffffull;
   }
   // Falling with x.  The last bin's tokens weigh nothing: exp(-27.1 * 2047 / 2048) * 2^38 = 0.47.
   __device__ inline int bin(float x) const { return (int)fminf(fmaf(-0.5f, x, half_top) * per_bin, (float)(SMP_BINS - 1)); }
@@ -103,7 +103,8 @@ __device__ inline uint64_t wave_scan64(uint64_t v) {  // inclusive
   return v;
 }
 struct Parts {
-  uint64_t w[SMP_WAVES], n[SMP_WAVES];
+  uint64_t w[SMP_WAVES];
+  uint32_t least[SMP_WAVES], most[SMP_WAVES];
   float f[SMP_WAVES];
 };
 template <class F>
@@ -162,25 +163,26 @@ struct Histogram {
 };
 
 struct SampleLds {
-  union {
+  uint64_t before[SMP_BINS + 1];  // weights per bin; after sum_bins() of all bins before, [SMP_BINS]: all
+  union {                         // never two at once
     struct {
-      uint64_t before[SMP_BINS + 1];  // weights per bin; after from_weights() of all bins before, [SMP_BINS]: all
-      union {
-        Histogram zoom;
-        struct { uint64_t key[SMP_LIST], w[SMP_LIST]; } list;
-        uint32_t count[SMP_BINS + 1];
-      };
-    } hist;
-    struct {
-      uint64_t key[SMP_LIST], sorted[SMP_LIST], upto[SMP_LIST];
+      uint64_t key[SMP_LIST], sorted[SMP_LIST];
+      uint32_t bin[SMP_BINS + 1];
     } few;
-    uint32_t bins[SMP_BINS + 1];  // of the threads' largest logits
+    Histogram zoom;
+    struct { uint64_t key[SMP_LIST], w[SMP_LIST]; } list;
+    uint32_t count[SMP_BINS + 1];
   };
   Parts part;
   double table[SMP_STEPS];  // 2^(j / 64)
   uint64_t found_key, found_w, found_upto;
   uint32_t bound;
   int list_n;
+  __device__ inline void start_list() {
+    __syncthreads();
+    if (threadIdx.x == 0) list_n = 0;
+    __syncthreads();
+  }
   __device__ inline void make_table() {
     if (threadIdx.x < SMP_STEPS) table[threadIdx.x] = exp2((double)threadIdx.x / SMP_STEPS);
   }
@@ -228,107 +230,140 @@ __device__ inline void give(const SampleArgs& a, int t, uint64_t key, uint64_t w
   if (a.prob) a.prob[t] = (float)((double)w / (double)kept);
 }
 
-// The n tokens of few.key, unsorted, among which the first n_keep (n or fewer) are all that top-k keeps.
-__device__ inline void finish_list(const SampleArgs& a, int t, const SampleRules& r, const SampleScale& sc, SampleLds& l, int n, int n_keep) {
+// few.key[0 .. n) in order: by bins over the keys' range, then within each bin, which is few but for tokens that are much alike
+__device__ inline void order_list(SampleLds& l, int n) {
+  constexpr int PER = SMP_LIST / SMP_THREADS;
   const int tid = threadIdx.x;
   auto& f = l.few;
-  // place of every token: the number of tokens ahead of it; several threads count for one where there are few
-  int wide = SMP_THREADS;
-  while (wide >> 1 >= n && wide > 64) wide >>= 1;
-  const int share = SMP_THREADS / wide, part = tid / wide;
-  uint32_t* const rank = reinterpret_cast<uint32_t*>(f.upto);
-  for (int e = tid; e < n; e += SMP_THREADS) rank[e] = 0;
-  __syncthreads();
-  for (int e = tid % wide; e < n; e += wide) {
-    const uint64_t k = f.key[e];
-    const int j1 = (int)((part + 1) * (long)n / share);
-    int ahead = 0;
-#pragma unroll 4
-    for (int j = (int)(part * (long)n / share); j < j1; ++j) ahead += f.key[j] > k;
-    if (share == 1) rank[e] = ahead;
-    else if (ahead) atomicAdd(&rank[e], (uint32_t)ahead);
-  }
-  __syncthreads();
-  for (int e = tid; e < n; e += SMP_THREADS) f.sorted[rank[e]] = f.key[e];
-  __syncthreads();
-  constexpr int PER = SMP_LIST / SMP_THREADS;
-  uint64_t key[PER], w[PER], upto[PER], sum = 0, kept;
+  for (int i = tid; i <= SMP_BINS; i += SMP_THREADS) f.bin[i] = 0;
+  uint64_t key[PER];
+  int b[PER], at[PER];
+  uint32_t lo = ~0u, hi = 0;  // of the logits' bits
 #pragma unroll
-  for (int i = 0; i < PER; ++i) {
-    const int e = tid * PER + i;
-    key[i] = e < n_keep ? f.sorted[e] : 0;
-    w[i] = e < n_keep ? sc.weight(sc.seen(key_logit(key[i])), l.table) : 0;
-    sum += w[i];
-    upto[i] = sum;
+  for (int j = 0; j < PER; ++j) {
+    const int e = tid + j * SMP_THREADS;
+    key[j] = e < n ? f.key[e] : 0;
+    if (e < n) lo = min(lo, (uint32_t)(key[j] >> 24)), hi = max(hi, (uint32_t)(key[j] >> 24));
   }
-  const uint64_t before = block_before64(sum, l.part.w, kept);
+  lo = wave_min(lo), hi = wave_max(hi);
+  if ((tid & 63) == 0) l.part.least[tid >> 6] = lo, l.part.most[tid >> 6] = hi;
+  __syncthreads();
 #pragma unroll
-  for (int i = 0; i < PER; ++i) upto[i] += before;
+  for (int w = 0; w < SMP_WAVES; ++w) lo = min(lo, l.part.least[w]), hi = max(hi, l.part.most[w]);
+  const uint64_t most = (uint64_t)hi << 24 | 0xffffff, range = most - ((uint64_t)lo << 24);
+  const int shift = max(0, 53 - __clzll((long long)range));  // range >> shift < SMP_BINS
+#pragma unroll
+  for (int j = 0; j < PER; ++j)
+    if (tid + j * SMP_THREADS < n) b[j] = (int)((most - key[j]) >> shift), at[j] = (int)atomicAdd(&f.bin[b[j]], 1u);
+  sum_bins(f.bin, l.part);
+#pragma unroll
+  for (int j = 0; j < PER; ++j)
+    if (tid + j * SMP_THREADS < n) f.sorted[f.bin[b[j]] + at[j]] = key[j];
+  __syncthreads();
+#pragma unroll
+  for (int j = 0; j < PER; ++j)
+    if (tid + j * SMP_THREADS < n) {
+      int place = (int)f.bin[b[j]];
+      const int end = (int)f.bin[b[j] + 1];
+      int ahead = 0;
+      for (int i = place; i < end; ++i) ahead += f.sorted[i] > key[j];
+      f.key[place + ahead] = key[j];
+    }
+  __syncthreads();
+}
+// The first n of the ordered list: every thread's keys, weights and running sums.
+struct Weighed {
+  static constexpr int PER = SMP_LIST / SMP_THREADS;
+  uint64_t key[PER], w[PER], upto[PER], all;
+  __device__ inline Weighed(const SampleScale& sc, SampleLds& l, int n) {
+    uint64_t sum = 0;
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+      const int e = (int)threadIdx.x * PER + i;
+      key[i] = e < n ? l.few.key[e] : 0;
+      w[i] = e < n ? sc.weight(sc.seen(key_logit(key[i])), l.table) : 0;
+      upto[i] = sum += w[i];
+    }
+    const uint64_t before = block_before64(sum, l.part.w, all);
+#pragma unroll
+    for (int i = 0; i < PER; ++i) upto[i] += before;
+  }
   // the token with which the running sum exceeds a target is in one thread's hands
-  auto crosses = [&](int i, uint64_t target) { return upto[i] - w[i] <= target && target < upto[i]; };
+  __device__ inline bool crosses(int i, uint64_t target) const { return upto[i] - w[i] <= target && target < upto[i]; }
+};
+
+// The n tokens of few.key, unsorted, among which the first n_keep (n or fewer) are all that top-k keeps.
+__device__ inline void finish_list(const SampleArgs& a, int t, const SampleRules& r, const SampleScale& sc, SampleLds& l, int n, int n_keep) {
+  order_list(l, n);
+  const Weighed x(sc, l, n_keep);
+  uint64_t kept = x.all;
   if (r.top_p < 1.f) {
     const uint64_t target = top_p_target(r.top_p, kept);
 #pragma unroll
-    for (int i = 0; i < PER; ++i)
-      if (crosses(i, target)) l.found_upto = upto[i];
+    for (int i = 0; i < Weighed::PER; ++i)
+      if (x.crosses(i, target)) l.found_upto = x.upto[i];
     __syncthreads();
     kept = l.found_upto;
   }
   if (r.least > 0) {
     uint64_t over = 0;
 #pragma unroll
-    for (int i = 0; i < PER; ++i) over += w[i] >= r.least ? w[i] : 0;
+    for (int i = 0; i < Weighed::PER; ++i) over += x.w[i] >= r.least ? x.w[i] : 0;
     over = block_all64(over, l.part, Plus());
     kept = over < kept ? over : kept;
   }
   const uint64_t target = uniform_target(a.uniform[t], kept);
 #pragma unroll
-  for (int i = 0; i < PER; ++i)
-    if (crosses(i, target)) give(a, t, key[i], w[i], kept);
+  for (int i = 0; i < Weighed::PER; ++i)
+    if (x.crosses(i, target)) give(a, t, x.key[i], x.w[i], kept);
 }
 
-// From the weights per bin (hist.before, summed), with `scan` over all tokens of the row (others may be among them); over:
-// the sum of the weights that min-p allows.  False, with nothing given, where a
-// count decides or a bin is too full for the list.
+// From the weights per bin (before, summed), with one `scan` over all tokens of the row (others may be among them); over:
+// the sum of the weights that min-p allows.  False, with nothing given, where a count decides or the list is too short.
 template <class Scan>
 __device__ inline bool finish_bins(const SampleArgs& a, int t, const SampleRules& r, const SampleScale& sc, SampleLds& l,
                                    uint64_t over, Scan scan) {
   if (r.top_k >= 1.f && r.top_k < (float)a.V) return false;
-  const int tid = threadIdx.x;
-  auto& h = l.hist;
-  uint64_t kept = h.before[SMP_BINS];
-#pragma unroll 1
-  for (int step = r.top_p < 1.f ? 0 : 1; step < 2; ++step) {  // top-p, the token
-    if (step == 1) kept = over < kept ? over : kept;
-    const uint64_t target = step == 0 ? top_p_target(r.top_p, kept) : uniform_target(a.uniform[t], kept);
-    const int b = crossing(h.before, target);
-    __syncthreads();
-    if (tid == 0) l.list_n = 0;
-    __syncthreads();
-    SampleScale q = sc;  // nothing of it is to be kept from before, in registers for every logit
-    asm volatile("" : "+v"(q.half_top), "+v"(q.per_bin));
-    scan([&](float v, int i) {
-      if (q.bin(v) != b) return;  // (what is no token is in the last bin, in which nothing crosses)
-      const int at = atomicAdd(&l.list_n, 1);
-      if (at < SMP_LIST) h.list.key[at] = place_key(v, i);
-    });
-    __syncthreads();
-    const int n = l.list_n;
-    if (n > SMP_LIST) return false;
-    for (int e = tid; e < n; e += SMP_THREADS) h.list.w[e] = sc.weight(key_logit(h.list.key[e]), l.table);
-    __syncthreads();
-    for (int e = tid; e < n; e += SMP_THREADS) {
-      const uint64_t k = h.list.key[e], w = h.list.w[e];
-      uint64_t sum = h.before[b];
-#pragma unroll 4
-      for (int j = 0; j < n; ++j)
-        if (h.list.key[j] > k) sum += h.list.w[j];
-      if (sum <= target && target < sum + w) l.found_key = k, l.found_w = w, l.found_upto = sum + w;
-    }
-    __syncthreads();
-    if (step == 0) kept = l.found_upto;
+  // top-p crosses its border in bin bp, which leaves from `least` to `most`; the token is then in bins b0 .. b1
+  const float u = a.uniform[t];
+  uint64_t least = l.before[SMP_BINS], most = least;
+  uint64_t p_target = 0;
+  int bp = SMP_BINS;
+  if (r.top_p < 1.f) {
+    p_target = top_p_target(r.top_p, most);
+    bp = crossing(l.before, p_target);
+    least = l.before[bp] + 1, most = l.before[bp + 1];
   }
-  if (tid == 0) give(a, t, l.found_key, l.found_w, kept);
+  const int b0 = crossing(l.before, uniform_target(u, least < over ? least : over));
+  const int b1 = crossing(l.before, uniform_target(u, most < over ? most : over));
+  l.start_list();
+  scan([&](float v, int i) {
+    const int b = sc.bin(sc.seen(v));
+    if (!(b == bp || (b >= b0 && b <= b1))) return;  // (what is no token is in the last bin, in which nothing crosses)
+    const int at = atomicAdd(&l.list_n, 1);
+    const uint64_t k = place_key(v, i);
+    if (at < SMP_LIST) l.few.key[at] = k;
+  });
+  __syncthreads();
+  const int n = l.list_n;
+  if (n > SMP_LIST) return false;
+  order_list(l, n);
+  const Weighed x(sc, l, n);
+  // the list's running sums lack the bins before b0, and from bp on, where that is apart, those behind b1
+  const uint64_t front = l.before[b0], back = bp > b1 ? l.before[min(bp, SMP_BINS)] - (l.before[b1 + 1] - front) : front;
+  uint64_t kept = most;
+  if (r.top_p < 1.f) {
+#pragma unroll
+    for (int i = 0; i < Weighed::PER; ++i)
+      if (x.crosses(i, p_target - back)) l.found_upto = x.upto[i] + back;
+    __syncthreads();
+    kept = l.found_upto;
+  }
+  kept = over < kept ? over : kept;
+  const uint64_t target = uniform_target(u, kept) - front;
+#pragma unroll
+  for (int i = 0; i < Weighed::PER; ++i)
+    if (x.crosses(i, target)) give(a, t, x.key[i], x.w[i], kept);
   return true;
 }
 
@@ -337,7 +372,7 @@ template <class Each>
 __device__ inline void finish_histogram(const SampleArgs& a, int t, const SampleRules& r, const SampleScale& sc, SampleLds& l,
                                         uint64_t over, Each each) {
   const int tid = threadIdx.x;
-  auto& h = l.hist;
+  SampleLds& h = l;
   uint64_t kept = h.before[SMP_BINS];
 #pragma unroll 1
   for (int step = 0; step < 3; ++step) {  // top-k, top-p, the token
@@ -513,7 +548,8 @@ struct Held {
 #pragma unroll
       for (int e = 0; e < 4; ++e) v[i][e] = v[i][e] == INFINITY ? 0.f : -INFINITY;
   }
-  // weights per bin; the sum of this thread's of `least` or more
+  // weights per bin; LEAST: the sum of this thread's of `least` or more
+  template <bool LEAST>
   __device__ inline uint64_t add_weights(const SampleScale& sc, uint64_t least, SampleLds& l) const {
     uint64_t over = 0;
 #pragma unroll
@@ -528,8 +564,8 @@ struct Held {
         }
 #pragma unroll
         for (int e = 0; e < SMP_ABREAST; ++e) {
-          atomicAdd((unsigned long long*)&l.hist.before[b[e]], (unsigned long long)w[e]);
-          over += w[e] >= least ? w[e] : 0;
+          atomicAdd((unsigned long long*)&l.before[b[e]], (unsigned long long)w[e]);
+          if (LEAST) over += w[e] >= least ? w[e] : 0;
         }
         __builtin_amdgcn_sched_barrier(0);  // group after group, for registers
       }
@@ -559,29 +595,28 @@ struct Pieces {
 __device__ inline float reached_by(uint32_t k, float mine, const SampleScale& sc, SampleLds& l) {
   const int tid = threadIdx.x;
   __syncthreads();
-  for (int i = tid; i < SMP_BINS; i += SMP_THREADS) l.bins[i] = 0;
+  for (int i = tid; i <= SMP_BINS; i += SMP_THREADS) l.count[i] = 0;
   if (tid == 0) l.bound = 0xffffffffu;
   __syncthreads();
   const int b = sc.bin(sc.seen(mine));
   const bool counts = b < SMP_BINS - 1;
-  if (counts) atomicAdd(&l.bins[b], 1u);
+  if (counts) atomicAdd(&l.count[b], 1u);
   __syncthreads();
-  const uint64_t all = sum_bins(l.bins, l.part);
+  const uint64_t all = sum_bins(l.count, l.part);
   if (all < k) return -INFINITY;
-  if (counts && l.bins[b] < k) atomicMin(&l.bound, place_bits(mine));
+  if (counts && l.count[b] < k) atomicMin(&l.bound, place_bits(mine));
   __syncthreads();
   return bits_logit(l.bound);
 }
 // Tokens from `bound` on to out[0 .. cap), in any order; their number
 template <int NV>
 __device__ inline int collect(const Held<NV>& x, float bound, int first_index, uint64_t* out, int cap, SampleLds& l) {
-  __syncthreads();
-  if (threadIdx.x == 0) l.list_n = 0;
-  __syncthreads();
+  l.start_list();
   x.each([&](float v, int i) {
     if (!(v >= bound)) return;
     const int at = atomicAdd(&l.list_n, 1);
-    if (at < cap) out[at] = place_key(v, first_index + i);
+    const uint64_t k = place_key(v, first_index + i);
+    if (at < cap) out[at] = k;
   });
   __syncthreads();
   return l.list_n;
@@ -602,15 +637,15 @@ __device__ inline void finish_slowly(const SampleArgs& a, int t, const SampleRul
   const int tid = threadIdx.x;
   const Streamed each{a.x + (size_t)t * a.V, a.V, sc};
   __syncthreads();
-  for (int i = tid; i <= SMP_BINS; i += SMP_THREADS) l.hist.before[i] = 0;
+  for (int i = tid; i <= SMP_BINS; i += SMP_THREADS) l.before[i] = 0;
   __syncthreads();
   uint64_t over = 0;
   each([&](float v, int) {
     const uint64_t w = sc.weight(v, l.table);
-    atomicAdd((unsigned long long*)&l.hist.before[sc.bin(v)], (unsigned long long)w);
+    atomicAdd((unsigned long long*)&l.before[sc.bin(v)], (unsigned long long)w);
     over += w >= r.least ? w : 0;
   });
-  sum_bins(l.hist.before, l.part);
+  sum_bins(l.before, l.part);
   over = block_all64(over, l.part, Plus());
   finish_histogram(a, t, r, sc, l, over, each);
 }
@@ -657,16 +692,16 @@ __global__ __launch_bounds__(SMP_THREADS, 4) void sample_row_kernel(SampleArgs a
   // ---- the histogram, from memory again (that the row kept its registers through it cost hundreds of spills)
   const Pieces all{x, 0, a.V};
   __syncthreads();
-  for (int i = tid; i <= SMP_BINS; i += SMP_THREADS) l.hist.before[i] = 0;
+  for (int i = tid; i <= SMP_BINS; i += SMP_THREADS) l.before[i] = 0;
   __syncthreads();
   uint64_t over = 0;
   all.held([&](Held<4>& h, int) {
     if (sc.infinite) h.only_infinities();
-    over += h.add_weights(sc, r.least, l);
+    over += r.least > 0 ? h.add_weights<true>(sc, r.least, l) : h.add_weights<false>(sc, 0, l);
   });
-  sum_bins(l.hist.before, l.part);
-  over = block_all64(over, l.part, Plus());
-  if (!finish_bins(a, t, r, sc, l, over, [&](auto f) { all([&](float v, int i) { f(sc.seen(v), i); }); })) finish_slowly(a, t, r, sc, l);
+  sum_bins(l.before, l.part);
+  over = r.least > 0 ? block_all64(over, l.part, Plus()) : l.before[SMP_BINS];
+  if (!finish_bins(a, t, r, sc, l, over, [&](auto f) { all(f); })) finish_slowly(a, t, r, sc, l);
 }
 
 // ---- rows cut into chunks: what every chunk finds out by itself, then the weights of the rows that need them all, then the rows
@@ -710,13 +745,16 @@ struct ChunkedTop {
   bool listed;
 };
 __device__ inline ChunkedTop chunked_top(const ChunkedRows& ch, int t, const SampleRules& r) {
-  ChunkedTop x{-INFINITY, r.short_by_k()};
-  for (int c = 0; c < ch.chunks; ++c) {
+  float top = -INFINITY;
+  bool listed = true;
+  for (int c = threadIdx.x & 63; c < ch.chunks; c += 64) {
     const size_t at = ch.at(t, c);
-    x.top = fmaxf(x.top, ch.top[at]);
-    x.listed = x.listed && ch.n[at] >= 0;
+    top = fmaxf(top, ch.top[at]);
+    listed = listed && ch.n[at] >= 0;
   }
-  return x;
+#pragma unroll
+  for (int d = 32; d > 0; d >>= 1) top = fmaxf(top, __shfl_xor(top, d));
+  return ChunkedTop{top, r.short_by_k() && __ballot(!listed) == 0};
 }
 template <int NV>
 __global__ __launch_bounds__(SMP_THREADS) void sample_weigh_kernel(SampleArgs a, ChunkedRows ch) {
@@ -733,13 +771,14 @@ __global__ __launch_bounds__(SMP_THREADS) void sample_weigh_kernel(SampleArgs a,
   Held<NV> row;
   row.load(a.x + (size_t)t * a.V + first, min(ch.size, a.V - first));
   l.make_table();
-  for (int i = tid; i <= SMP_BINS; i += SMP_THREADS) l.hist.before[i] = 0;
+  for (int i = tid; i <= SMP_BINS; i += SMP_THREADS) l.before[i] = 0;
   __syncthreads();
   if (sc.infinite) row.only_infinities();
-  uint64_t over = row.add_weights(sc, r.least, l);
-  over = block_all64(over, l.part, Plus());
+  uint64_t over = r.least > 0 ? row.template add_weights<true>(sc, r.least, l) : row.template add_weights<false>(sc, 0, l);
+  if (r.least > 0) over = block_all64(over, l.part, Plus());
+  __syncthreads();
   const size_t at = ch.at(t, c);
-  for (int i = tid; i < SMP_BINS; i += SMP_THREADS) ch.data[at * SMP_BINS + i] = l.hist.before[i];
+  for (int i = tid; i < SMP_BINS; i += SMP_THREADS) ch.data[at * SMP_BINS + i] = l.before[i];
   if (tid == 0) ch.over[at] = over;
 }
 __global__ __launch_bounds__(SMP_THREADS) void sample_finish_kernel(SampleArgs a, ChunkedRows ch) {
@@ -769,18 +808,21 @@ __global__ __launch_bounds__(SMP_THREADS) void sample_finish_kernel(SampleArgs a
   const SampleScale sc(x.top, r.t);
   if (x.listed) {
     const int k = (int)r.top_k;
+    // entry e of all: chunk c's from upto[c] on
+    uint32_t* const upto = l.few.bin;
+    for (int c = tid; c <= SMP_BINS; c += SMP_THREADS) upto[c] = c < ch.chunks ? ch.n[ch.at(t, c)] : 0;
+    const int all = (int)sum_bins(l.few.bin, l.part);
     auto entries = [&](auto f) {
-      for (int c = 0; c < ch.chunks; ++c) {
-        const size_t at = ch.at(t, c);
-        for (int i = tid; i < ch.n[at]; i += SMP_THREADS) f(ch.data[at * SMP_BINS + i]);
+#pragma unroll 4
+      for (int e = tid; e < all; e += SMP_THREADS) {
+        const int c = crossing(l.few.bin, e);
+        f(ch.data[ch.at(t, c) * SMP_BINS + (e - upto[c])]);
       }
     };
     uint64_t best = 0;
     entries([&](uint64_t key) { best = Larger()(best, key); });
-    float bound = reached_by(k, best == 0 ? -INFINITY : key_logit(best), sc, l);
-    __syncthreads();
-    if (tid == 0) l.list_n = 0;
-    __syncthreads();
+    const float bound = all <= SMP_LIST ? -INFINITY : reached_by(k, best == 0 ? -INFINITY : key_logit(best), sc, l);
+    l.start_list();
     entries([&](uint64_t key) {
       if (!(key_logit(key) >= bound)) return;
       const int at = atomicAdd(&l.list_n, 1);
@@ -798,15 +840,17 @@ __global__ __launch_bounds__(SMP_THREADS) void sample_finish_kernel(SampleArgs a
     for (int i = tid; i <= SMP_BINS; i += SMP_THREADS) {
       uint64_t w = 0;
       if (i < SMP_BINS)
+#pragma unroll 8
         for (int c = 0; c < ch.chunks; ++c) w += ch.data[ch.at(t, c) * SMP_BINS + i];
-      l.hist.before[i] = w;
+      l.before[i] = w;
     }
     __syncthreads();
     uint64_t over = 0;
-    for (int c = tid; c < ch.chunks; c += SMP_THREADS) over += ch.over[ch.at(t, c)];
-    sum_bins(l.hist.before, l.part);
-    over = block_all64(over, l.part, Plus());
-    if (finish_bins(a, t, r, sc, l, over, [&](auto f) { Pieces{row, 0, a.V}([&](float v, int i) { f(sc.seen(v), i); }); })) return;
+    if (r.least > 0)
+      for (int c = tid; c < ch.chunks; c += SMP_THREADS) over += ch.over[ch.at(t, c)];
+    sum_bins(l.before, l.part);
+    over = r.least > 0 ? block_all64(over, l.part, Plus()) : l.before[SMP_BINS];
+    if (finish_bins(a, t, r, sc, l, over, [&](auto f) { Pieces{row, 0, a.V}(f); })) return;
   }
   finish_slowly(a, t, r, sc, l);
 }
