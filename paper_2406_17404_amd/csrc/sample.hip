@@ -18,7 +18,10 @@
 
 namespace trj {
 
-constexpr int SMP_ABREAST = 2;
+#ifndef ABR
+#define ABR 2
+#endif
+constexpr int SMP_ABREAST = ABR;
 constexpr int SMP_THREADS = 512, SMP_WAVES = SMP_THREADS / 64, SMP_BINS = 2048, SMP_LIST = 2048;
 constexpr double SMP_UNIT = 274877906944.0;      // 2^38
 constexpr float SMP_RANGE = 27.1f;               // exp(-27.1) * 2^38 rounds to 0
@@ -63,6 +66,10 @@ struct SampleRules {
 // branches: what lies far below (-infinity, NaN) is taken for 2^-40, a quarter of a unit, and rounds to 0.  Whole numbers come
 // from adding 1.5 * 2^52, which leaves them in a sum's low bits: rounding and conversion are instructions at a fraction of the rate.
 constexpr int SMP_STEPS = 128;
+struct LogitRange {
+  float lo, hi;
+  __device__ inline bool has(float x) const { return x >= lo && x <= hi; }
+};
 struct SampleScale {
   float half_top, per_bin;  // half the largest logit; bins per half a logit
   double top, inv;          // 128 log2(e) / temperature
@@ -84,6 +91,13 @@ struct SampleScale {
     const uint64_t scaled = (uint64_t)((uint32_t)(r >> 32) + ((uint32_t)((k >> 7) + 38) << 20)) << 32 | (uint32_t)r;
     const double whole = __longlong_as_double((long long)scaled) + WHOLE;
     return (uint64_t)__double_as_longlong(whole) & 0x7ffffffffffffull;
+  }
+  // logits that bins b0 .. b1 can hold (a token's bin is off by less than 2^-20 of its place)
+  __device__ inline LogitRange range(int b0, int b1, float t) const {
+    if (infinite) return LogitRange{INFINITY, INFINITY};
+    if (t > 1e30f) return LogitRange{-INFINITY, INFINITY};
+    const float off = fabsf(half_top) * 1e-6f + 1e-37f;  // (half a subnormal number is rounded)
+    return LogitRange{2.f * (half_top - (float)(b1 + 1) / per_bin * 1.00001f - off), 2.f * (half_top - (float)b0 / per_bin * 0.99999f + off)};
   }
   // Falling with x.  The last bin's tokens weigh nothing: exp(-27.1 * 2047 / 2048) * 2^38 = 0.47.
   __device__ inline int bin(float x) const { return (int)fminf(fmaf(-0.5f, x, half_top) * per_bin, (float)(SMP_BINS - 1)); }
@@ -162,7 +176,25 @@ struct Histogram {
   }
 };
 
-struct SampleLds {
+struct ListLds {  // of what makes a list
+  Parts part;
+  uint32_t count[SMP_THREADS];
+  int list_n, bound_bin;
+  __device__ inline void start_list() {
+    __syncthreads();
+    if (threadIdx.x == 0) list_n = 0;
+    __syncthreads();
+  }
+};
+struct WeighLds {  // of what adds up weights
+  uint64_t before[SMP_BINS + 1];
+  Parts part;
+  double table[SMP_STEPS];  // 2^(j / 128)
+  __device__ inline void make_table() {
+    if (threadIdx.x < SMP_STEPS) table[threadIdx.x] = exp2((double)threadIdx.x / SMP_STEPS);
+  }
+};
+struct SampleLds : ListLds {
   uint64_t before[SMP_BINS + 1];  // weights per bin; after sum_bins() of all bins before, [SMP_BINS]: all
   union {                         // never two at once
     struct {
@@ -171,18 +203,11 @@ struct SampleLds {
     } few;
     Histogram zoom;
     struct { uint64_t key[SMP_LIST], w[SMP_LIST]; } list;
-    uint32_t count[SMP_BINS + 1];
+    uint32_t counts[SMP_BINS + 1];
   };
-  Parts part;
-  double table[SMP_STEPS];  // 2^(j / 64)
-  uint64_t found_key, found_w, found_upto;
-  uint32_t bound;
-  int list_n;
-  __device__ inline void start_list() {
-    __syncthreads();
-    if (threadIdx.x == 0) list_n = 0;
-    __syncthreads();
-  }
+  double table[SMP_STEPS];  // 2^(j / 128)
+  uint64_t found_upto;
+  uint64_t found_key, found_w;
   __device__ inline void make_table() {
     if (threadIdx.x < SMP_STEPS) table[threadIdx.x] = exp2((double)threadIdx.x / SMP_STEPS);
   }
@@ -337,7 +362,9 @@ __device__ inline bool finish_bins(const SampleArgs& a, int t, const SampleRules
   const int b0 = crossing(l.before, uniform_target(u, least < over ? least : over));
   const int b1 = crossing(l.before, uniform_target(u, most < over ? most : over));
   l.start_list();
+  const LogitRange in_t = sc.range(b0, b1, r.t), in_p = sc.range(min(bp, SMP_BINS - 1), min(bp, SMP_BINS - 1), r.t);
   scan([&](float v, int i) {
+    if (!in_t.has(v) && !in_p.has(v)) return;
     const int b = sc.bin(sc.seen(v));
     if (!(b == bp || (b >= b0 && b <= b1))) return;  // (what is no token is in the last bin, in which nothing crosses)
     const int at = atomicAdd(&l.list_n, 1);
@@ -382,13 +409,13 @@ __device__ inline void finish_histogram(const SampleArgs& a, int t, const Sample
     if (step == 0) {
       if (!(r.top_k >= 1.f) || r.top_k >= (float)a.V) continue;
       target = (uint64_t)r.top_k - 1;
-      for (int i = tid; i <= SMP_BINS; i += SMP_THREADS) h.count[i] = 0;
+      for (int i = tid; i <= SMP_BINS; i += SMP_THREADS) h.counts[i] = 0;
       __syncthreads();
-      each([&](float v, int) { atomicAdd(&h.count[sc.bin(v)], 1u); });
-      sum_bins(h.count, l.part);
-      if (target >= h.count[SMP_BINS - 1]) continue;  // among those that weigh nothing, or beyond all
-      b = crossing(h.count, target);
-      before_n = h.count[b];
+      each([&](float v, int) { atomicAdd(&h.counts[sc.bin(v)], 1u); });
+      sum_bins(h.counts, l.part);
+      if (target >= h.counts[SMP_BINS - 1]) continue;  // among those that weigh nothing, or beyond all
+      b = crossing(h.counts, target);
+      before_n = h.counts[b];
       __syncthreads();
     } else {
       if (step == 1) {
@@ -549,8 +576,8 @@ struct Held {
       for (int e = 0; e < 4; ++e) v[i][e] = v[i][e] == INFINITY ? 0.f : -INFINITY;
   }
   // weights per bin; LEAST: the sum of this thread's of `least` or more
-  template <bool LEAST>
-  __device__ inline uint64_t add_weights(const SampleScale& sc, uint64_t least, SampleLds& l) const {
+  template <bool LEAST, class Lds>
+  __device__ inline uint64_t add_weights(const SampleScale& sc, uint64_t least, Lds& l) const {
     uint64_t over = 0;
 #pragma unroll
     for (int i = 0; i < NV; ++i)
@@ -572,45 +599,71 @@ struct Held {
     return over;
   }
 };
-// All logits of a part of a row, piece after piece from memory.
+// All logits of a part of a row, piece after piece from memory, the next one on its way.
+template <int NV>
 struct Pieces {
   const float* x;
   int from, to;
   template <class F>
   __device__ inline void held(F f) const {
+    constexpr int STEP = 4 * NV * SMP_THREADS;
+    Held<NV> ahead;
+    ahead.load(x + from, to - from);
 #pragma unroll 1
-    for (int i = from; i < to; i += 16 * SMP_THREADS) {
-      Held<4> h;
-      h.load(x + i, to - i);
+    for (int i = from; i < to; i += STEP) {
+      Held<NV> h = ahead;
+      if (i + STEP < to) ahead.load(x + i + STEP, to - i - STEP);
       f(h, i);
     }
   }
   template <class F>
   __device__ inline void operator()(F f) const {
-    held([&](Held<4>& h, int i0) { h.each([&](float v, int i) { f(v, i0 + i); }); });
+    held([&](Held<NV>& h, int i0) { h.each([&](float v, int i) { f(v, i0 + i); }); });
   }
 };
-// A logit that at least k tokens of the workgroup reach, and few more: the threads' largest ones, by bins below the top.
-// -infinity where fewer than k threads hold tokens that can weigh anything.
-__device__ inline float reached_by(uint32_t k, float mine, const SampleScale& sc, SampleLds& l) {
+// Weights of a part of a row per bin (l.before, cleared here), and the sum of those of `least` or more if that is not 0.
+template <class Lds>
+__device__ inline uint64_t weigh_part(const Pieces<2>& part, const SampleScale& sc, uint64_t least, Lds& l) {
+  uint64_t over = 0;
+  __syncthreads();
+  for (int i = threadIdx.x; i <= SMP_BINS; i += SMP_THREADS) l.before[i] = 0;
+  __syncthreads();
+  part.held([&](Held<2>& h, int) {
+    if (sc.infinite) h.only_infinities();
+    if (least > 0) over += h.template add_weights<true>(sc, least, l);
+    else h.template add_weights<false>(sc, 0, l);
+  });
+  __syncthreads();
+  return over;
+}
+// A logit that at least k tokens of the workgroup reach, and few more: the lower end of the bin, of as many as threads over
+// the range that weighs anything, in which the k-th of the threads' largest ones lies.  -infinity where fewer threads hold tokens.
+__device__ inline float reached_by(int k, float mine, const SampleScale& sc, ListLds& l) {
+  constexpr float WIDE = (float)SMP_BINS / SMP_THREADS;
   const int tid = threadIdx.x;
   __syncthreads();
-  for (int i = tid; i <= SMP_BINS; i += SMP_THREADS) l.count[i] = 0;
-  if (tid == 0) l.bound = 0xffffffffu;
+  l.count[tid] = 0;
+  if (tid == 0) l.bound_bin = -1;
   __syncthreads();
   const int b = sc.bin(sc.seen(mine));
-  const bool counts = b < SMP_BINS - 1;
-  if (counts) atomicAdd(&l.count[b], 1u);
+  if (b < SMP_BINS - 1) atomicAdd(&l.count[b / (SMP_BINS / SMP_THREADS)], 1u);
   __syncthreads();
-  const uint64_t all = sum_bins(l.count, l.part);
-  if (all < k) return -INFINITY;
-  if (counts && l.count[b] < k) atomicMin(&l.bound, place_bits(mine));
+  const int c = (int)l.count[tid];
+  int upto = wave_scan(c);
+  if ((tid & 63) == 63) l.part.least[tid >> 6] = upto;
   __syncthreads();
-  return bits_logit(l.bound);
+#pragma unroll
+  for (int w = 0; w < SMP_WAVES - 1; ++w) upto += w < (tid >> 6) ? (int)l.part.least[w] : 0;
+  if (upto >= k && upto - c < k) l.bound_bin = tid;
+  __syncthreads();
+  if (l.bound_bin < 0) return -INFINITY;
+  // (a token's bin is off by less than 2^-20 of its place)
+  const float below = 2.f * ((float)(l.bound_bin + 1) * WIDE) / sc.per_bin * 1.00001f;
+  return sc.infinite ? INFINITY : 2.f * sc.half_top - below - fabsf(sc.half_top) * 1e-6f;
 }
 // Tokens from `bound` on to out[0 .. cap), in any order; their number
 template <int NV>
-__device__ inline int collect(const Held<NV>& x, float bound, int first_index, uint64_t* out, int cap, SampleLds& l) {
+__device__ inline int collect(const Held<NV>& x, float bound, int first_index, uint64_t* out, int cap, ListLds& l) {
   l.start_list();
   x.each([&](float v, int i) {
     if (!(v >= bound)) return;
@@ -689,19 +742,11 @@ __global__ __launch_bounds__(SMP_THREADS, 4) void sample_row_kernel(SampleArgs a
       }
     }
   }
-  // ---- the histogram, from memory again (that the row kept its registers through it cost hundreds of spills)
-  const Pieces all{x, 0, a.V};
-  __syncthreads();
-  for (int i = tid; i <= SMP_BINS; i += SMP_THREADS) l.before[i] = 0;
-  __syncthreads();
-  uint64_t over = 0;
-  all.held([&](Held<4>& h, int) {
-    if (sc.infinite) h.only_infinities();
-    over += r.least > 0 ? h.add_weights<true>(sc, r.least, l) : h.add_weights<false>(sc, 0, l);
-  });
+  // ---- the histogram
+  uint64_t over = weigh_part(Pieces<2>{x, 0, a.V}, sc, r.least, l);
   sum_bins(l.before, l.part);
   over = r.least > 0 ? block_all64(over, l.part, Plus()) : l.before[SMP_BINS];
-  if (!finish_bins(a, t, r, sc, l, over, [&](auto f) { all(f); })) finish_slowly(a, t, r, sc, l);
+  if (!finish_bins(a, t, r, sc, l, over, [&](auto f) { Pieces<4>{x, 0, a.V}(f); })) finish_slowly(a, t, r, sc, l);
 }
 
 // ---- rows cut into chunks: what every chunk finds out by itself, then the weights of the rows that need them all, then the rows
@@ -716,7 +761,7 @@ constexpr int SMP_CHUNK_LIST = 1024;
 
 template <int NV>
 __global__ __launch_bounds__(SMP_THREADS) void sample_chunk_kernel(SampleArgs a, ChunkedRows ch) {
-  __shared__ SampleLds l;
+  __shared__ ListLds l;
   const int tid = threadIdx.x, t = ch.row0 + blockIdx.x / ch.chunks, c = blockIdx.x % ch.chunks, first = c * ch.size;
   if (blockIdx.x == 0 && ch.row0 == 0) empty_sequences(a);
   Held<NV> row;
@@ -733,7 +778,7 @@ __global__ __launch_bounds__(SMP_THREADS) void sample_chunk_kernel(SampleArgs a,
   if (!is_token(top)) {
     n = 0;
   } else if (r.short_by_k() && r.t > 0.f) {
-    const float bound = reached_by((uint32_t)r.top_k, mine, SampleScale(top, r.t), l);
+    const float bound = reached_by((int)r.top_k, mine, SampleScale(top, r.t), l);
     n = collect(row, fmaxf(bound, -3.4028235e38f), first, ch.data + at * SMP_BINS, SMP_CHUNK_LIST, l);
     if (n > SMP_CHUNK_LIST) n = -1;
   }
@@ -756,9 +801,8 @@ __device__ inline ChunkedTop chunked_top(const ChunkedRows& ch, int t, const Sam
   for (int d = 32; d > 0; d >>= 1) top = fmaxf(top, __shfl_xor(top, d));
   return ChunkedTop{top, r.short_by_k() && __ballot(!listed) == 0};
 }
-template <int NV>
 __global__ __launch_bounds__(SMP_THREADS) void sample_weigh_kernel(SampleArgs a, ChunkedRows ch) {
-  __shared__ SampleLds l;
+  __shared__ WeighLds l;
   const int tid = threadIdx.x, t = ch.row0 + blockIdx.x / ch.chunks, c = blockIdx.x % ch.chunks, first = c * ch.size;
   bool first_row = false;
   const int s = sample_sequence(a, t, first_row);
@@ -768,15 +812,9 @@ __global__ __launch_bounds__(SMP_THREADS) void sample_weigh_kernel(SampleArgs a,
   const ChunkedTop x = chunked_top(ch, t, r);
   if (x.listed || !is_token(x.top)) return;
   const SampleScale sc(x.top, r.t);
-  Held<NV> row;
-  row.load(a.x + (size_t)t * a.V + first, min(ch.size, a.V - first));
   l.make_table();
-  for (int i = tid; i <= SMP_BINS; i += SMP_THREADS) l.before[i] = 0;
-  __syncthreads();
-  if (sc.infinite) row.only_infinities();
-  uint64_t over = r.least > 0 ? row.template add_weights<true>(sc, r.least, l) : row.template add_weights<false>(sc, 0, l);
+  uint64_t over = weigh_part(Pieces<2>{a.x + (size_t)t * a.V, first, min(first + ch.size, a.V)}, sc, r.least, l);
   if (r.least > 0) over = block_all64(over, l.part, Plus());
-  __syncthreads();
   const size_t at = ch.at(t, c);
   for (int i = tid; i < SMP_BINS; i += SMP_THREADS) ch.data[at * SMP_BINS + i] = l.before[i];
   if (tid == 0) ch.over[at] = over;
@@ -797,7 +835,7 @@ __global__ __launch_bounds__(SMP_THREADS) void sample_finish_kernel(SampleArgs a
     if (is_token(x.top)) {
       int c = 0;
       while (ch.top[ch.at(t, c)] != x.top) ++c;  // (one of them is the largest)
-      Pieces{row, c * ch.size, min(a.V, (c + 1) * ch.size)}([&](float v, int i) {
+      Pieces<8>{row, c * ch.size, min(a.V, (c + 1) * ch.size)}([&](float v, int i) {
         if (v == x.top) best = Larger()(best, place_key(v, i));
       });
     }
@@ -819,9 +857,12 @@ __global__ __launch_bounds__(SMP_THREADS) void sample_finish_kernel(SampleArgs a
         f(ch.data[ch.at(t, c) * SMP_BINS + (e - upto[c])]);
       }
     };
-    uint64_t best = 0;
-    entries([&](uint64_t key) { best = Larger()(best, key); });
-    const float bound = all <= SMP_LIST ? -INFINITY : reached_by(k, best == 0 ? -INFINITY : key_logit(best), sc, l);
+    float bound = -INFINITY;
+    if (all > SMP_LIST) {
+      uint64_t best = 0;
+      entries([&](uint64_t key) { best = Larger()(best, key); });
+      bound = reached_by(k, best == 0 ? -INFINITY : key_logit(best), sc, l);
+    }
     l.start_list();
     entries([&](uint64_t key) {
       if (!(key_logit(key) >= bound)) return;
@@ -850,7 +891,7 @@ __global__ __launch_bounds__(SMP_THREADS) void sample_finish_kernel(SampleArgs a
       for (int c = tid; c < ch.chunks; c += SMP_THREADS) over += ch.over[ch.at(t, c)];
     sum_bins(l.before, l.part);
     over = r.least > 0 ? block_all64(over, l.part, Plus()) : l.before[SMP_BINS];
-    if (finish_bins(a, t, r, sc, l, over, [&](auto f) { Pieces{row, 0, a.V}(f); })) return;
+    if (finish_bins(a, t, r, sc, l, over, [&](auto f) { Pieces<8>{row, 0, a.V}(f); })) return;
   }
   finish_slowly(a, t, r, sc, l);
 }
@@ -877,7 +918,7 @@ size_t tree_sample_ws_bytes(int T, int V) {
 template <int NV>
 static int sample_chunked(const SampleArgs& a, const ChunkedRows& ch, hipStream_t st) {
   sample_chunk_kernel<NV><<<ch.rows * ch.chunks, SMP_THREADS, 0, st>>>(a, ch);
-  sample_weigh_kernel<NV><<<ch.rows * ch.chunks, SMP_THREADS, 0, st>>>(a, ch);
+  sample_weigh_kernel<<<ch.rows * ch.chunks, SMP_THREADS, 0, st>>>(a, ch);
   sample_finish_kernel<<<ch.rows, SMP_THREADS, 0, st>>>(a, ch);
   return check_launch();
 }
