@@ -18,10 +18,7 @@
 
 namespace trj {
 
-#ifndef ABR
-#define ABR 2
-#endif
-constexpr int SMP_ABREAST = ABR;
+constexpr int SMP_ABREAST = 2;
 constexpr int SMP_THREADS = 512, SMP_WAVES = SMP_THREADS / 64, SMP_BINS = 2048, SMP_LIST = 2048;
 constexpr double SMP_UNIT = 274877906944.0;      // 2^38
 constexpr float SMP_RANGE = 27.1f;               // exp(-27.1) * 2^38 rounds to 0
@@ -61,34 +58,41 @@ struct SampleRules {
   __device__ inline bool short_by_min() const { return least > 0 && !(top_p < 1.f) && !(top_k >= 1.f); }
 };
 
-// What a row's weights and bins are worked out from.  Weights: 2^(y / 128), y <= 0, is a table's 2^(j / 128) times Taylor's
-// polynomial on |f| <= ln(2) / 256 times a power of two; the first missing term is below 1.3e-15, 2^-11 of a unit.  Without
-// branches: what lies far below (-infinity, NaN) is taken for 2^-40, a quarter of a unit, and rounds to 0.  Whole numbers come
-// from adding 1.5 * 2^52, which leaves them in a sum's low bits: rounding and conversion are instructions at a fraction of the rate.
-constexpr int SMP_STEPS = 128;
+// What a row's weights and bins are worked out from.  Weights: 2^y, y <= 0, is Taylor's polynomial of e^(f ln 2) on
+// |f| <= 1/2 times a power of two; the first missing term is below 6.3e-15, 2^-9 of a unit.  (A table of 2^(j / 128) with
+// a polynomial of five terms took as long.)  Without branches: what lies far below (-infinity, NaN) is taken for 2^-40, a quarter of a unit, and rounds to 0.  Whole numbers come from adding 1.5 * 2^52, which
+// leaves them in a sum's low bits: rounding and conversion are instructions at a fraction of the rate.
 struct LogitRange {
   float lo, hi;
-  __device__ inline bool has(float x) const { return x >= lo && x <= hi; }
+  __device__ inline int has(float x) const { return (int)(x >= lo) & (int)(x <= hi); }
 };
 struct SampleScale {
   float half_top, per_bin;  // half the largest logit; bins per half a logit
-  double top, inv;          // 128 log2(e) / temperature
+  double top, inv;          // log2(e) / temperature
   bool infinite;            // then the infinities count as 0 and all others as -infinity
   __device__ inline SampleScale(float m, float t)
       : half_top(m == INFINITY ? 0.f : 0.5f * m), per_bin(fminf((2 * SMP_BINS / SMP_RANGE) / t, 1e30f)),
-        top(m == INFINITY ? 0.0 : (double)m), inv(SMP_STEPS * 1.4426950408889634 / (double)t), infinite(m == INFINITY) {}
+        top(m == INFINITY ? 0.0 : (double)m), inv(1.4426950408889634 / (double)t), infinite(m == INFINITY) {}
   __device__ inline float seen(float x) const { return !infinite ? x : x == INFINITY ? 0.f : -INFINITY; }
-  __device__ inline uint64_t weight(float x, const double* table) const {
-    constexpr double L = 0.6931471805599453 / SMP_STEPS, WHOLE = 6755399441055744.0;
-    const double y = fmax(((double)x - top) * inv, -40.0 * SMP_STEPS), n = y + WHOLE, f = y - (n - WHOLE);
+  __device__ inline uint64_t weight(float x) const {
+    constexpr double L = 0.6931471805599453, WHOLE = 6755399441055744.0;
+    constexpr double L2 = L * L, L4 = L2 * L2, L6 = L4 * L2, L8 = L4 * L4, L10 = L8 * L2;
+    const double y = fmax(((double)x - top) * inv, -40.0), n = y + WHOLE, f = y - (n - WHOLE);
     const int k = (int)__double_as_longlong(n);
-    double p = fma(L * L * L * L / 24, f, L * L * L / 6);
-    p = fma(p, f, L * L / 2);
+    double p = fma(L10 * L / 39916800, f, L10 / 3628800);
+    p = fma(p, f, L8 * L / 362880);
+    p = fma(p, f, L8 / 40320);
+    p = fma(p, f, L6 * L / 5040);
+    p = fma(p, f, L6 / 720);
+    p = fma(p, f, L4 * L / 120);
+    p = fma(p, f, L4 / 24);
+    p = fma(p, f, L2 * L / 6);
+    p = fma(p, f, L2 / 2);
     p = fma(p, f, L);
-    const double root = table[k & (SMP_STEPS - 1)];
-    const uint64_t r = (uint64_t)__double_as_longlong(fma(p * f, root, root));
-    // times 2^(k / 128 + 38), in the exponent
-    const uint64_t scaled = (uint64_t)((uint32_t)(r >> 32) + ((uint32_t)((k >> 7) + 38) << 20)) << 32 | (uint32_t)r;
+    p = fma(p, f, 1.0);
+    const uint64_t r = (uint64_t)__double_as_longlong(p);
+    // times 2^(k + 38), in the exponent
+    const uint64_t scaled = (uint64_t)((uint32_t)(r >> 32) + ((uint32_t)(k + 38) << 20)) << 32 | (uint32_t)r;
     const double whole = __longlong_as_double((long long)scaled) + WHOLE;
     return (uint64_t)__double_as_longlong(whole) & 0x7ffffffffffffull;
   }
@@ -189,10 +193,6 @@ struct ListLds {  // of what makes a list
 struct WeighLds {  // of what adds up weights
   uint64_t before[SMP_BINS + 1];
   Parts part;
-  double table[SMP_STEPS];  // 2^(j / 128)
-  __device__ inline void make_table() {
-    if (threadIdx.x < SMP_STEPS) table[threadIdx.x] = exp2((double)threadIdx.x / SMP_STEPS);
-  }
 };
 struct SampleLds : ListLds {
   uint64_t before[SMP_BINS + 1];  // weights per bin; after sum_bins() of all bins before, [SMP_BINS]: all
@@ -205,12 +205,8 @@ struct SampleLds : ListLds {
     struct { uint64_t key[SMP_LIST], w[SMP_LIST]; } list;
     uint32_t counts[SMP_BINS + 1];
   };
-  double table[SMP_STEPS];  // 2^(j / 128)
-  uint64_t found_upto;
-  uint64_t found_key, found_w;
-  __device__ inline void make_table() {
-    if (threadIdx.x < SMP_STEPS) table[threadIdx.x] = exp2((double)threadIdx.x / SMP_STEPS);
-  }
+  uint64_t found_upto, found_key, found_w;
+  int found_bin[2];
 };
 template <class T>
 __device__ inline int crossing(const T (&before)[SMP_BINS + 1], uint64_t target) {  // before[lo] <= target < before[lo + 1]
@@ -221,6 +217,24 @@ __device__ inline int crossing(const T (&before)[SMP_BINS + 1], uint64_t target)
     else hi = m;
   }
   return lo;
+}
+// the same of l.before for two targets, by all threads at once
+struct BinPair {
+  int first, second;
+};
+__device__ inline BinPair crossings(SampleLds& l, uint64_t target0, uint64_t target1) {
+  constexpr int PER = SMP_BINS / SMP_THREADS;
+  __syncthreads();
+  uint64_t lower = l.before[threadIdx.x * PER];
+#pragma unroll
+  for (int i = 0; i < PER; ++i) {
+    const uint64_t upper = l.before[threadIdx.x * PER + i + 1];
+    if (lower <= target0 && target0 < upper) l.found_bin[0] = threadIdx.x * PER + i;
+    if (lower <= target1 && target1 < upper) l.found_bin[1] = threadIdx.x * PER + i;
+    lower = upper;
+  }
+  __syncthreads();
+  return BinPair{l.found_bin[0], l.found_bin[1]};
 }
 // counts or weights per bin to those of all bins before; the sum of all
 template <class T>
@@ -306,7 +320,7 @@ struct Weighed {
     for (int i = 0; i < PER; ++i) {
       const int e = (int)threadIdx.x * PER + i;
       key[i] = e < n ? l.few.key[e] : 0;
-      w[i] = e < n ? sc.weight(sc.seen(key_logit(key[i])), l.table) : 0;
+      w[i] = e < n ? sc.weight(sc.seen(key_logit(key[i]))) : 0;
       upto[i] = sum += w[i];
     }
     const uint64_t before = block_before64(sum, l.part.w, all);
@@ -318,7 +332,7 @@ struct Weighed {
 };
 
 // The n tokens of few.key, unsorted, among which the first n_keep (n or fewer) are all that top-k keeps.
-__device__ inline void finish_list(const SampleArgs& a, int t, const SampleRules& r, const SampleScale& sc, SampleLds& l, int n, int n_keep) {
+__device__ inline void finish_list(const SampleArgs& a, int t, float u, const SampleRules& r, const SampleScale& sc, SampleLds& l, int n, int n_keep) {
   order_list(l, n);
   const Weighed x(sc, l, n_keep);
   uint64_t kept = x.all;
@@ -337,7 +351,7 @@ __device__ inline void finish_list(const SampleArgs& a, int t, const SampleRules
     over = block_all64(over, l.part, Plus());
     kept = over < kept ? over : kept;
   }
-  const uint64_t target = uniform_target(a.uniform[t], kept);
+  const uint64_t target = uniform_target(u, kept);
 #pragma unroll
   for (int i = 0; i < Weighed::PER; ++i)
     if (x.crosses(i, target)) give(a, t, x.key[i], x.w[i], kept);
@@ -346,31 +360,35 @@ __device__ inline void finish_list(const SampleArgs& a, int t, const SampleRules
 // From the weights per bin (before, summed), with one `scan` over all tokens of the row (others may be among them); over:
 // the sum of the weights that min-p allows.  False, with nothing given, where a count decides or the list is too short.
 template <class Scan>
-__device__ inline bool finish_bins(const SampleArgs& a, int t, const SampleRules& r, const SampleScale& sc, SampleLds& l,
-                                   uint64_t over, Scan scan) {
+__device__ inline bool finish_bins(const SampleArgs& a, int t, float u, const SampleRules& r, const SampleScale& sc,
+                                   SampleLds& l, uint64_t over, Scan scan) {
   if (r.top_k >= 1.f && r.top_k < (float)a.V) return false;
   // top-p crosses its border in bin bp, which leaves from `least` to `most`; the token is then in bins b0 .. b1
-  const float u = a.uniform[t];
   uint64_t least = l.before[SMP_BINS], most = least;
   uint64_t p_target = 0;
   int bp = SMP_BINS;
   if (r.top_p < 1.f) {
     p_target = top_p_target(r.top_p, most);
-    bp = crossing(l.before, p_target);
+    bp = crossings(l, p_target, p_target).first;
     least = l.before[bp] + 1, most = l.before[bp + 1];
   }
-  const int b0 = crossing(l.before, uniform_target(u, least < over ? least : over));
-  const int b1 = crossing(l.before, uniform_target(u, most < over ? most : over));
+  const BinPair b01 = crossings(l, uniform_target(u, least < over ? least : over), uniform_target(u, most < over ? most : over));
+  const int b0 = b01.first, b1 = b01.second;
   l.start_list();
-  const LogitRange in_t = sc.range(b0, b1, r.t), in_p = sc.range(min(bp, SMP_BINS - 1), min(bp, SMP_BINS - 1), r.t);
-  scan([&](float v, int i) {
-    if (!in_t.has(v) && !in_p.has(v)) return;
+  const LogitRange in_t = sc.range(b0, b1, r.t);
+  auto take = [&](float v, int i) {
     const int b = sc.bin(sc.seen(v));
     if (!(b == bp || (b >= b0 && b <= b1))) return;  // (what is no token is in the last bin, in which nothing crosses)
     const int at = atomicAdd(&l.list_n, 1);
-    const uint64_t k = place_key(v, i);
-    if (at < SMP_LIST) l.few.key[at] = k;
-  });
+    if (at < SMP_LIST) l.few.key[at] = place_key(v, i);
+  };
+  auto any = [](const LogitRange& q, const float(&v)[4]) { return q.has(v[0]) | q.has(v[1]) | q.has(v[2]) | q.has(v[3]); };
+  if (bp == SMP_BINS || bp <= b1) {
+    scan([&](const float(&v)[4]) { return any(in_t, v) != 0; }, take);
+  } else {
+    const LogitRange in_p = sc.range(bp, bp, r.t);
+    scan([&](const float(&v)[4]) { return (any(in_t, v) | any(in_p, v)) != 0; }, take);
+  }
   __syncthreads();
   const int n = l.list_n;
   if (n > SMP_LIST) return false;
@@ -438,7 +456,7 @@ __device__ inline void finish_histogram(const SampleArgs& a, int t, const Sample
         const uint64_t k = place_key(v, i);
         if (k < lo || k > hi) return;
         const int at = atomicAdd(&l.list_n, 1);
-        if (at < SMP_LIST) h.list.key[at] = k, h.list.w[at] = sc.weight(v, l.table);
+        if (at < SMP_LIST) h.list.key[at] = k, h.list.w[at] = sc.weight(v);
       });
       __syncthreads();
       return l.list_n;
@@ -459,7 +477,7 @@ __device__ inline void finish_histogram(const SampleArgs& a, int t, const Sample
         each([&](float v, int i) {
           if (sc.bin(v) != b) return;
           const uint64_t k = place_key(v, i);
-          if (k >= lo && k <= hi) h.zoom.add((int)((hi - k) >> shift), sc.weight(v, l.table));
+          if (k >= lo && k <= hi) h.zoom.add((int)((hi - k) >> shift), sc.weight(v));
         });
         sum_bins(h.zoom.w, l.part);
         sum_bins(h.zoom.n, l.part);
@@ -569,6 +587,16 @@ struct Held {
 #pragma unroll
       for (int e = 0; e < 4; ++e) f(v[i][e], (i * SMP_THREADS + (int)threadIdx.x) * 4 + e);
   }
+  // of the groups of four of which `some`(v0, v1, v2, v3) holds: a branch per group, not per logit
+  template <class S, class F>
+  __device__ inline void each_of(S some, F f) const {
+#pragma unroll
+    for (int i = 0; i < NV; ++i)
+      if (some(v[i])) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) f(v[i][e], (i * SMP_THREADS + (int)threadIdx.x) * 4 + e);
+      }
+  }
   __device__ inline void only_infinities() {
 #pragma unroll
     for (int i = 0; i < NV; ++i)
@@ -587,7 +615,7 @@ struct Held {
         int b[SMP_ABREAST];
 #pragma unroll
         for (int e = 0; e < SMP_ABREAST; ++e) {
-          w[e] = sc.weight(v[i][g + e], l.table), b[e] = sc.bin(v[i][g + e]);
+          w[e] = sc.weight(v[i][g + e]), b[e] = sc.bin(v[i][g + e]);
         }
 #pragma unroll
         for (int e = 0; e < SMP_ABREAST; ++e) {
@@ -616,9 +644,9 @@ struct Pieces {
       f(h, i);
     }
   }
-  template <class F>
-  __device__ inline void operator()(F f) const {
-    held([&](Held<NV>& h, int i0) { h.each([&](float v, int i) { f(v, i0 + i); }); });
+  template <class S, class F>
+  __device__ inline void operator()(S some, F f) const {
+    held([&](Held<NV>& h, int i0) { h.each_of(some, [&](float v, int i) { f(v, i0 + i); }); });
   }
 };
 // Weights of a part of a row per bin (l.before, cleared here), and the sum of those of `least` or more if that is not 0.
@@ -665,7 +693,7 @@ __device__ inline float reached_by(int k, float mine, const SampleScale& sc, Lis
 template <int NV>
 __device__ inline int collect(const Held<NV>& x, float bound, int first_index, uint64_t* out, int cap, ListLds& l) {
   l.start_list();
-  x.each([&](float v, int i) {
+  x.each_of([&](const float(&v)[4]) { return fmaxf(fmaxf(v[0], v[1]), fmaxf(v[2], v[3])) >= bound; }, [&](float v, int i) {
     if (!(v >= bound)) return;
     const int at = atomicAdd(&l.list_n, 1);
     const uint64_t k = place_key(v, first_index + i);
@@ -694,7 +722,7 @@ __device__ inline void finish_slowly(const SampleArgs& a, int t, const SampleRul
   __syncthreads();
   uint64_t over = 0;
   each([&](float v, int) {
-    const uint64_t w = sc.weight(v, l.table);
+    const uint64_t w = sc.weight(v);
     atomicAdd((unsigned long long*)&l.before[sc.bin(v)], (unsigned long long)w);
     over += w >= r.least ? w : 0;
   });
@@ -716,9 +744,9 @@ __global__ __launch_bounds__(SMP_THREADS, 4) void sample_row_kernel(SampleArgs a
   const int s = sample_sequence(a, t, first_row);
   if (s < 0) return;
   const SampleRules r(a.rules + 4 * s);
+  const float u = a.uniform[t];
   if (first_row && tid == 0) a.status[s] = r.bad;
   if (r.bad) return;
-  l.make_table();
   const float mine = row.top(), top = block_max(mine, l.part);
   if (!is_token(top) || r.t == 0.f) {
     uint64_t best = 0;
@@ -737,7 +765,7 @@ __global__ __launch_bounds__(SMP_THREADS, 4) void sample_row_kernel(SampleArgs a
     if (bound > -INFINITY) {
       const int n = collect(row, bound, 0, l.few.key, SMP_LIST, l);
       if (n <= SMP_LIST) {
-        finish_list(a, t, r, sc, l, n, k > 0 ? min(n, k) : n);
+        finish_list(a, t, u, r, sc, l, n, k > 0 ? min(n, k) : n);
         return;
       }
     }
@@ -746,7 +774,7 @@ __global__ __launch_bounds__(SMP_THREADS, 4) void sample_row_kernel(SampleArgs a
   uint64_t over = weigh_part(Pieces<2>{x, 0, a.V}, sc, r.least, l);
   sum_bins(l.before, l.part);
   over = r.least > 0 ? block_all64(over, l.part, Plus()) : l.before[SMP_BINS];
-  if (!finish_bins(a, t, r, sc, l, over, [&](auto f) { Pieces<4>{x, 0, a.V}(f); })) finish_slowly(a, t, r, sc, l);
+  if (!finish_bins(a, t, u, r, sc, l, over, Pieces<4>{x, 0, a.V})) finish_slowly(a, t, r, sc, l);
 }
 
 // ---- rows cut into chunks: what every chunk finds out by itself, then the weights of the rows that need them all, then the rows
@@ -812,7 +840,6 @@ __global__ __launch_bounds__(SMP_THREADS) void sample_weigh_kernel(SampleArgs a,
   const ChunkedTop x = chunked_top(ch, t, r);
   if (x.listed || !is_token(x.top)) return;
   const SampleScale sc(x.top, r.t);
-  l.make_table();
   uint64_t over = weigh_part(Pieces<2>{a.x + (size_t)t * a.V, first, min(first + ch.size, a.V)}, sc, r.least, l);
   if (r.least > 0) over = block_all64(over, l.part, Plus());
   const size_t at = ch.at(t, c);
@@ -826,8 +853,8 @@ __global__ __launch_bounds__(SMP_THREADS) void sample_finish_kernel(SampleArgs a
   const int s = sample_sequence(a, t, first_row);
   if (s < 0) return;
   const SampleRules r(a.rules + 4 * s);
+  const float u = a.uniform[t];
   if (r.bad) return;
-  l.make_table();
   const ChunkedTop x = chunked_top(ch, t, r);
   const float* const row = a.x + (size_t)t * a.V;
   if (!is_token(x.top) || r.t == 0.f) {
@@ -835,7 +862,7 @@ __global__ __launch_bounds__(SMP_THREADS) void sample_finish_kernel(SampleArgs a
     if (is_token(x.top)) {
       int c = 0;
       while (ch.top[ch.at(t, c)] != x.top) ++c;  // (one of them is the largest)
-      Pieces<8>{row, c * ch.size, min(a.V, (c + 1) * ch.size)}([&](float v, int i) {
+      Pieces<8>{row, c * ch.size, min(a.V, (c + 1) * ch.size)}([&](const float(&v)[4]) { return fmaxf(fmaxf(v[0], v[1]), fmaxf(v[2], v[3])) == x.top; }, [&](float v, int i) {
         if (v == x.top) best = Larger()(best, place_key(v, i));
       });
     }
@@ -872,7 +899,7 @@ __global__ __launch_bounds__(SMP_THREADS) void sample_finish_kernel(SampleArgs a
     __syncthreads();
     const int n = l.list_n;
     if (n <= SMP_LIST) {
-      finish_list(a, t, r, sc, l, n, min(n, k));
+      finish_list(a, t, u, r, sc, l, n, min(n, k));
       return;
     }
   }
@@ -891,13 +918,13 @@ __global__ __launch_bounds__(SMP_THREADS) void sample_finish_kernel(SampleArgs a
       for (int c = tid; c < ch.chunks; c += SMP_THREADS) over += ch.over[ch.at(t, c)];
     sum_bins(l.before, l.part);
     over = r.least > 0 ? block_all64(over, l.part, Plus()) : l.before[SMP_BINS];
-    if (finish_bins(a, t, r, sc, l, over, [&](auto f) { Pieces<8>{row, 0, a.V}(f); })) return;
+    if (finish_bins(a, t, u, r, sc, l, over, Pieces<8>{row, 0, a.V})) return;
   }
   finish_slowly(a, t, r, sc, l);
 }
 
 // ------------------------------------------------------------------ launch
-constexpr int SMP_ROW = 64 * SMP_THREADS, SMP_CHUNK = 32 * SMP_THREADS;  // logits that a workgroup holds
+constexpr int SMP_ROW = 64 * SMP_THREADS, SMP_CHUNK = 64 * SMP_THREADS;  // logits that a workgroup holds
 struct SampleLaunch {
   int chunks, size, rows;  // per row; logits; rows of a launch
 };
@@ -905,7 +932,7 @@ static SampleLaunch sample_launch(int T, int V) {
   SampleLaunch p{0, 0, T};
   if (V <= SMP_ROW) return p;
   const int least = (V + SMP_CHUNK - 1) / SMP_CHUNK, most = (V + 8 * SMP_THREADS - 1) / (8 * SMP_THREADS);
-  p.chunks = std::min(std::max(least, (512 + T - 1) / T), most);
+  p.chunks = std::min(std::max(least, 512 / T), most);  // two workgroups per compute unit at a time
   p.size = ((V + p.chunks - 1) / p.chunks + 3) / 4 * 4;
   p.chunks = (V + p.size - 1) / p.size;
   p.rows = std::max(1, std::min(T, 4096 / p.chunks));
@@ -937,7 +964,9 @@ int launch_tree_sample(const float* x, const int32_t* node_off, int B, int T, in
   for (int row0 = 0; row0 < T; row0 += p.rows) {
     const ChunkedRows ch{row0, std::min(p.rows, T - row0), p.chunks, p.size, (float*)(data + all * (SMP_BINS + 1)),
                          (int32_t*)(data + all * (SMP_BINS + 1)) + all, data + all * SMP_BINS, data};
-    const int rc = p.size <= 8 * SMP_THREADS ? sample_chunked<2>(a, ch, st) : sample_chunked<8>(a, ch, st);
+    const int rc = p.size <= 8 * SMP_THREADS    ? sample_chunked<2>(a, ch, st)
+                   : p.size <= 32 * SMP_THREADS ? sample_chunked<8>(a, ch, st)
+                                                : sample_chunked<16>(a, ch, st);
     if (rc != TRJ_OK) return rc;
   }
   return TRJ_OK;
