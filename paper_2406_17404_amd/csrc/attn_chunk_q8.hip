@@ -11,6 +11,7 @@
 // Cached blocks (two pages) are converted on the way, codes times their power-of-two scale being bf16 numbers
 // exactly; the sequence's own rows are bf16 already and V is transposed.
 #include <algorithm>
+#include <type_traits>
 
 #include "attn_q8.h"
 #include "kernels.h"
@@ -122,19 +123,22 @@ __device__ inline void chunk_add_odd_values(const ChunkArgs& a, const ChunkSeq& 
 // first key of the sequence's own blocks with a key that row `row` does not see
 __device__ inline int first_partly_seen(int row) { return (row + 1) / CH_KEYS * CH_KEYS; }
 
-// Where a block keeps its operands in LDS: key tile kt of 32, 1 KiB per operand, 16 bytes per lane; lanes in an order
-// with which neither reading operands nor writing them from codes or rows meets a bank twice.
+// Where a block keeps its operands in LDS: an operand of 64 lanes' 16 bytes after the other, with gaps with which neither
+// reading operands nor writing them from codes or rows meets a bank more often than it has to; lane + constant, so that one
+// register addresses all of a block's.
 template <int DH>
 struct ChunkLds {
-  static constexpr int STEPS = DH / 16, PART = CH_KEYS * DH * 2, BUFFER = 2 * PART;
-  // K: step 2j + i holds columns 32 j + 16 hh + 8 i ..
-  __device__ static inline int k_at(int kt, int step, int hh, int r) {
-    const int p = (step >> 1) * 4 + hh * 2 + (step & 1);
-    return ((kt * STEPS + step) * 64 + hh * 32 + (r ^ (p & 15))) * 16;
-  }
+  static constexpr int STEPS = DH / 16;
+  static constexpr int K_HALF = 512 + 16, K_STEP = 2 * K_HALF, K_TILE = STEPS * K_STEP;
+  static constexpr int V_HALF = 512 + 64, V_STEP = 2 * V_HALF, V_TILE = STEPS * V_STEP;
+  static constexpr int V0 = 2 * K_TILE, BUFFER = V0 + 2 * V_TILE;
+  // K: step 2j + i holds columns 32 j + 16 hh + 8 i .. of row r
+  __device__ static inline int k_lane(int hh, int r) { return hh * K_HALF + r * 16; }
+  __device__ static inline int k_at(int kt, int step, int hh, int r) { return kt * K_TILE + step * K_STEP + k_lane(hh, r); }
   // V^T: columns 32 mt .., keys 16 kg + 8 b + 4 hh ..
+  __device__ static inline int v_lane(int hh, int c32) { return V0 + hh * V_HALF + c32 * 16 + (c32 >> 3) * 16; }
   __device__ static inline int v_at(int kt, int mt, int kg, int hh, int c32) {
-    return PART + ((kt * STEPS + 2 * mt + kg) * 64 + hh * 32 + (c32 ^ ((mt & 1) * 4 + (c32 >> 3)))) * 16;
+    return kt * V_TILE + (2 * mt + kg) * V_STEP + v_lane(hh, c32);
   }
 };
 
@@ -171,71 +175,78 @@ __global__ __launch_bounds__(CH_THREADS, 2) void chunk_attn_q8_kernel(ChunkArgs 
   const int32_t* table = a.block_table + (size_t)w.s * a.max_blocks;
   const int row_first = q0 / a.group, row_last = (q1 - 1) / a.group;
   const int cached = seq.cached(), blocks = cached + row_last / CH_KEYS + 1;  // of this tile
-  const int b0 = (int)((int64_t)blocks * sp / splits), b1 = (int)((int64_t)blocks * (sp + 1) / splits);
+  const int b0 = __builtin_amdgcn_readfirstlane((int)((int64_t)blocks * sp / splits));
+  const int b1 = __builtin_amdgcn_readfirstlane((int)((int64_t)blocks * (sp + 1) / splits));
   const size_t plane = (size_t)head * a.n_blocks;
 
   // queries: column n32; step 2j + i of the product: columns 32 j + 16 hh + 8 i ..
   const int qw = q0 + wave * 32, qi = min(qw + n32, nq - 1), my_row = qi / a.group;
   const bool live_wave = qw < nq;
-  const int wave_last = __builtin_amdgcn_readfirstlane((min(qw + 31, nq - 1)) / a.group);
   bf16x8 qreg[STEPS];
   {
     const uint16_t* qp = a.q + (size_t)(seq.r0 + my_row) * a.q_stride + (size_t)(head * a.group + qi % a.group) * DH + hh * 16;
 #pragma unroll
     for (int j = 0; j < STEPS; ++j) qreg[j] = *reinterpret_cast<const bf16x8*>(qp + 32 * (j >> 1) + 8 * (j & 1));
   }
-  f32x16 o[MT];
-#pragma unroll
-  for (int mt = 0; mt < MT; ++mt)
-#pragma unroll
-    for (int v = 0; v < 16; ++v) o[mt][v] = 0.f;
-  Softmax sm;
-  bool odd = false;
+  int odd = 0;
 
   // ---- bringing a block to LDS: from memory to registers, then, a block later, to LDS
+  // No branch in here that lanes take differently: the walk's accumulators would be copied around it.
+  constexpr bool V_ALL = 4 * DH == CH_THREADS;
   constexpr int PIECES = 4 * DH, UNITS = 2 * PIECES / CH_THREADS;  // 16 codes each, of K or V; per thread
-  u32x4 raw[4];
+  // of this thread's units: K or V, page of the block, place there, places in LDS of the halves (the second a step on)
+  const int page_of = wave % (PIECES / 64) / (DH / 32), piece = tid % (2 * DH);
+  auto is_v = [&](int i) { return (wave + i * CH_WAVES) / (PIECES / 64) != 0; };
+  const int c16 = piece >> 5, unit_h = c16 & 1, unit_at = piece & 31;  // K: columns 16 c16 .. of row unit_at; V: column unit_at of 32 (c16 / 2)
+  const int k_unit = Lds::k_at(page_of, c16 & ~1, unit_h, unit_at), v_unit = Lds::v_at(page_of, c16 >> 1, 0, unit_h, unit_at);
+  u32x4 raw0 = {}, raw1 = {}, raw2 = {}, raw3 = {};
   float piece_scale[2];
   int ids = 0, ids_from = -(1 << 30);  // pages ids_from .. + 63 of the sequence, one per lane, and their scales
   float ksc = 1.f, vsc = 1.f;
+  // (places are worked out where they are used: over the whole walk they would take registers)
+  auto fresh_tid = [&]() {
+    int t = threadIdx.x;
+    asm volatile("" : "+v"(t));
+    return t;
+  };
   auto load = [&](int b) {
     if (b < cached) {
       if (b * 2 >= ids_from + 64 || ids_from < 0) {
         ids_from = b * 2;
-        const int p = ids_from + lane;
-        const bool there = p * 32 < seq.L;
-        ids = there ? table[p] : 0;
-        const bool ok = (unsigned)ids < (unsigned)a.n_blocks;
-        ids = ok ? ids : 0;
-        ksc = !there ? 1.f : ok ? a.k_scale[plane + ids] : NAN;  // a page that is not there makes its rows NaN
-        vsc = there ? a.v_scale[plane + ids] : 1.f;
+        const int p = ids_from + lane, pages = (seq.L + 31) >> 5;
+        const int id = table[min(p, pages - 1)];
+        const bool there = p < pages, ok = (unsigned)id < (unsigned)a.n_blocks;
+        ids = ok ? id : 0;
+        const float of_k = a.k_scale[plane + ids], of_v = a.v_scale[plane + ids];
+        ksc = !there ? 1.f : ok ? of_k : NAN;  // a page that is not there makes its rows NaN
+        vsc = there ? of_v : 1.f;
       }
+      const int at = 2 * b + page_of - ids_from;
+      const size_t page = (plane + (uint32_t)__builtin_amdgcn_readlane(ids, at)) * (32 * DH);
 #pragma unroll
       for (int i = 0; i < UNITS; ++i) {
-        const int u = tid + i * CH_THREADS;
-        const bool is_v = __builtin_amdgcn_readfirstlane(u / PIECES) != 0;
-        const int kt = __builtin_amdgcn_readfirstlane(u % PIECES / (2 * DH)), piece = u % (2 * DH);
-        const int p = 2 * b + kt;
-        const int page = __builtin_amdgcn_readlane(ids, p - ids_from);
-        piece_scale[i] = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(is_v ? vsc : ksc), p - ids_from));
-        const uint8_t* pool = is_v ? a.v_pool : a.k_pool;
-        raw[i] = *reinterpret_cast<const u32x4*>(pool + (plane + (uint32_t)page) * (32 * DH) + piece * 16);
+        piece_scale[i] = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(is_v(i) ? vsc : ksc), at));
+        const u32x4 x = *reinterpret_cast<const u32x4*>((is_v(i) ? a.v_pool : a.k_pool) + page + piece * 16);
+        if (i == 0) raw0 = x;
+        else raw1 = x;
       }
     } else {
-      const int key0 = (b - cached) * CH_KEYS;
+      const int key0 = (b - cached) * CH_KEYS, tid = fresh_tid();
 #pragma unroll
       for (int i = 0; i < DH / 64; ++i) {
         const int u = tid + i * CH_THREADS, row = u / (DH / 8), p = u % (DH / 8);
-        raw[i] = *reinterpret_cast<const u32x4*>(a.k_rows + (size_t)(seq.r0 + min(key0 + row, seq.n - 1)) * a.row_stride + (size_t)head * DH + 8 * p);
+        const u32x4 x = *reinterpret_cast<const u32x4*>(a.k_rows + (size_t)(seq.r0 + min(key0 + row, seq.n - 1)) * a.row_stride + (size_t)head * DH + 8 * p);
+        if (i == 0) raw0 = x;
+        else raw1 = x;
       }
-      if (tid < 4 * DH) {  // four rows, four columns
+      if (V_ALL || wave < 4 * DH / 64) {  // four rows, four columns
         const int quad = tid / (DH / 4), cq = tid % (DH / 4);
         u32x2 v[4];
 #pragma unroll
         for (int d = 0; d < 4; ++d)
           v[d] = *reinterpret_cast<const u32x2*>(a.v_rows + (size_t)(seq.r0 + min(key0 + 4 * quad + d, seq.n - 1)) * a.row_stride + (size_t)head * DH + 4 * cq);
-        raw[2] = u32x4{v[0][0], v[0][1], v[1][0], v[1][1]};
-        raw[3] = u32x4{v[2][0], v[2][1], v[3][0], v[3][1]};
+        raw2 = u32x4{v[0][0], v[0][1], v[1][0], v[1][1]};
+        raw3 = u32x4{v[2][0], v[2][1], v[3][0], v[3][1]};
       }
     }
   };
@@ -243,48 +254,43 @@ __global__ __launch_bounds__(CH_THREADS, 2) void chunk_attn_q8_kernel(ChunkArgs 
     if (b < cached) {
 #pragma unroll
       for (int i = 0; i < UNITS; ++i) {
-        const int u = tid + i * CH_THREADS;
-        const bool is_v = __builtin_amdgcn_readfirstlane(u / PIECES) != 0;
-        const int kt = __builtin_amdgcn_readfirstlane(u % PIECES / (2 * DH)), piece = u % (2 * DH);
-        const int c16 = piece >> 5, h = c16 & 1, at = piece & 31;  // K: columns 16 c16 .. of row at; V: column at of 32 (c16 / 2)
-        u32x4 x = raw[i];
+        u32x4 x = i == 0 ? raw0 : raw1;
         const float scale = piece_scale[i];
-        if (is_v) {  // slots past the end may hold anything: their weights are 0, their values have to be numbers
-          const int rest = seq.L - (2 * b + kt) * 32;
-          if (rest < 32) {
+        const int rest = seq.L - (2 * b + page_of) * 32;
+        if (is_v(i) && rest < 32) {  // slots past the end may hold anything: their weights are 0, their values have to be numbers
 #pragma unroll
-            for (int d = 0; d < 4; ++d) {
-              const int keep = min(max(rest - 8 * d - 4 * h, 0), 4);
-              x[d] &= keep == 4 ? 0xffffffffu : (1u << (8 * keep)) - 1u;
-            }
+          for (int d = 0; d < 4; ++d) {
+            const int keep = min(max(rest - 8 * d - 4 * unit_h, 0), 4);
+            x[d] &= keep == 4 ? 0xffffffffu : (1u << (8 * keep)) - 1u;
           }
         }
         bf16x8 lo = operand(x[0], x[1], scale), hi = operand(x[2], x[3], scale);
-        if (!is_v && scale != scale) {
+        if (!is_v(i) && (__float_as_uint(scale) & 0x7fffffffu) > 0x7f800000u) {
           const u32x4 none = {0x7fc07fc0u, 0x7fc07fc0u, 0x7fc07fc0u, 0x7fc07fc0u};
           lo = hi = __builtin_bit_cast(bf16x8, none);
         }
-        const int j = c16 >> 1;
-        *reinterpret_cast<bf16x8*>(buf + (is_v ? Lds::v_at(kt, j, 0, h, at) : Lds::k_at(kt, 2 * j, h, at))) = lo;
-        *reinterpret_cast<bf16x8*>(buf + (is_v ? Lds::v_at(kt, j, 1, h, at) : Lds::k_at(kt, 2 * j + 1, h, at))) = hi;
+        uint8_t* const to = buf + (is_v(i) ? v_unit : k_unit);
+        *reinterpret_cast<bf16x8*>(to) = lo;
+        *reinterpret_cast<bf16x8*>(to + (is_v(i) ? Lds::V_STEP : Lds::K_STEP)) = hi;
       }
     } else {
-      const int key0 = (b - cached) * CH_KEYS;
+      const int key0 = (b - cached) * CH_KEYS, tid = fresh_tid();
 #pragma unroll
       for (int i = 0; i < DH / 64; ++i) {
         const int u = tid + i * CH_THREADS, row = u / (DH / 8), p = u % (DH / 8);
-        *reinterpret_cast<u32x4*>(buf + Lds::k_at(row >> 5, (p >> 2) * 2 + (p & 1), (p >> 1) & 1, row & 31)) = raw[i];
+        *reinterpret_cast<u32x4*>(buf + Lds::k_at(row >> 5, (p >> 2) * 2 + (p & 1), (p >> 1) & 1, row & 31)) = i == 0 ? raw0 : raw1;
       }
-      if (tid < 4 * DH) {
+      if (V_ALL || wave < 4 * DH / 64) {
         const int quad = tid / (DH / 4), cq = tid % (DH / 4);
-        uint32_t v[4][2] = {{raw[2][0], raw[2][1]}, {raw[2][2], raw[2][3]}, {raw[3][0], raw[3][1]}, {raw[3][2], raw[3][3]}};
+        uint32_t v[4][2] = {{raw2[0], raw2[1]}, {raw2[2], raw2[3]}, {raw3[0], raw3[1]}, {raw3[2], raw3[3]}};
         if (key0 >= first_partly_seen(row_first)) {
 #pragma unroll
           for (int d = 0; d < 4; ++d)
 #pragma unroll
             for (int e = 0; e < 2; ++e) {
-              if ((v[d][e] & 0x7f80u) == 0x7f80u) v[d][e] &= 0xffff0000u, odd = true;
-              if ((v[d][e] & 0x7f800000u) == 0x7f800000u) v[d][e] &= 0xffffu, odd = true;
+              const bool lo = (v[d][e] & 0x7f80u) == 0x7f80u, hi = (v[d][e] & 0x7f800000u) == 0x7f800000u;
+              v[d][e] &= (lo ? 0xffff0000u : ~0u) & (hi ? 0xffffu : ~0u);
+              odd |= (int)lo | (int)hi;
             }
         }
 #pragma unroll
@@ -299,55 +305,176 @@ __global__ __launch_bounds__(CH_THREADS, 2) void chunk_attn_q8_kernel(ChunkArgs 
     }
   };
 
-  if (b0 < b1) load(b0);
-  for (int b = b0; b < b1; ++b) {
-    uint8_t* const buf = smem + ((b - b0) & 1) * Lds::BUFFER;
-    store(b, buf);
-    if (b + 1 < b1) load(b + 1);
-    __syncthreads();  // (the other buffer was read before the barrier of the block before)
-    const bool own = b >= cached;
-    const int key0 = (own ? b - cached : b) * CH_KEYS;
-    if (!live_wave || (own && key0 > wave_last)) continue;
-    f32x16 s[2];
+  // ---- the walk, tile after tile of 32 keys, two in a block.  With a tile's scores in registers, a step has the last tile's
+  // weights times its values beside this one's exponentials, then the products with the next tile's keys.
+  f32x16 o[MT], s;
+  u32x4 pk[2] = {};  // weights of the last tile
+  float m = NO_REFERENCE, l = 0.f, top = 0.f;
+  const float f = a.scale_log2e;
 #pragma unroll
-    for (int kt = 0; kt < 2; ++kt) {
+  for (int mt = 0; mt < MT; ++mt)
 #pragma unroll
-      for (int v = 0; v < 16; ++v) s[kt][v] = 0.f;
+    for (int v = 0; v < 16; ++v) o[mt][v] = 0.f;
+  const int k_lane = Lds::k_lane(hh, n32), v_lane = Lds::v_lane(hh, n32);
+  auto scores = [&](const uint8_t* at) {
+    f32x16 to;
 #pragma unroll
-      for (int j = 0; j < STEPS; ++j) {
-        const bf16x8 kop = *reinterpret_cast<const bf16x8*>(buf + Lds::k_at(kt, j, hh, n32));
-        s[kt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kop, qreg[j], s[kt], 0, 0, 0);
-      }
+    for (int v = 0; v < 16; ++v) to[v] = 0.f;
+#pragma unroll
+    for (int j = 0; j < STEPS; ++j)
+      to = __builtin_amdgcn_mfma_f32_32x32x16_bf16(*reinterpret_cast<const bf16x8*>(at + j * Lds::K_STEP), qreg[j], to, 0, 0, 0);
+    s = to;
+  };
+  auto values = [&](const uint8_t* at) {
+#pragma unroll
+    for (int kg = 0; kg < 2; ++kg)
+#pragma unroll
+      for (int mt = 0; mt < MT; ++mt)
+        o[mt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(*reinterpret_cast<const bf16x8*>(at + (2 * mt + kg) * Lds::V_STEP),
+                                                        __builtin_bit_cast(bf16x8, pk[kg]), o[mt], 0, 0, 0);
+  };
+  auto pack = [&](const float (&p)[16]) {
+#pragma unroll
+    for (int kg = 0; kg < 2; ++kg)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) pk[kg][e] = pack2bf(p[8 * kg + 2 * e], p[8 * kg + 2 * e + 1]);
+  };
+  const int tiles = 2 * (b1 - b0);
+  // Blocks stay in LDS in turn in three places.  Block b + 1 takes the place of block b - 2, which was last read in the first
+  // step of block b - 1, before that block's barrier.
+  int b = b0, place = 0;  // of the current block
+  auto buffer = [&](int ahead) {
+    const int i = place + ahead;
+    return smem + (i - (3 & ~((i - 3) >> 31))) * Lds::BUFFER;
+  };
+  auto arrive = [&](int t) {  // in front of tile t
+    if (t & 1) {
+      __syncthreads();
+    } else {
+      if (b + 1 < b1) store(b + 1, buffer(1));
+      if (b + 2 < b1) load(b + 2);
     }
-    const int limit = (own ? my_row + 1 : seq.L) - key0;
-    if (own ? key0 + CH_KEYS > row_first + 1 : limit < CH_KEYS) {
+  };
+  auto leave = [&](int t) {
+    b += t & 1;
+    const int next = place + (t & 1);
+    place = next & ((next - 3) >> 31);
+  };
+  auto next_keys = [&](int t) { return buffer(t & 1) + (1 - (t & 1)) * Lds::K_TILE + k_lane; };
+  auto last_values = [&](int t) { return buffer(2 - 2 * (t & 1)) + (1 - (t & 1)) * Lds::V_TILE + v_lane; };
+  if (tiles > 0) {
+    load(b0);
+    store(b0, buffer(0));
+    if (b0 + 1 < b1) load(b0 + 1);
+    __syncthreads();
+  }
+  if (!live_wave) {
+    for (int t = 0; t < tiles; ++t) {
+      arrive(t);
+      leave(t);
+    }
+  } else if (tiles > 0) {
+    // tiles before `plain_end` of the cache and of the own rows are seen whole by all queries
+    const int cached_end = 2 * (min(b1, cached) - b0) - (seq.L < cached * CH_KEYS && b1 >= cached ? 2 : 0);
+    const int own_begin = max(2 * (cached - b0), 0), own_end = own_begin + 2 * ((row_first + 1) / CH_KEYS) - 2 * max(b0 - cached, 0);
+    bool far = false;
+    auto plain_until = [&](int t) {  // the first tile from t on that is not
+      const int end = t < cached_end ? cached_end : t >= own_begin && t < own_end ? own_end : t;
+      return far ? t : min(end, tiles - 1);
+    };
+    scores(buffer(0) + k_lane);
+    top = Softmax::largest(s, f);
+    int t = 0, until = 0;
+    arrive(t);
+    auto stop = [&]() {
+      return (__ballot(top > m + SLACK) | (uint64_t)(int64_t)(__builtin_amdgcn_readfirstlane(until - 1 - t) >> 31)) != 0;
+    };
+    for (;;) {
+      // The loop has one way out, at its end, in front of a tile that is masked or lifts a reference: a condition around the
+      // accumulators, or a way out before they change, would have them copied every time.
+      if (!stop()) do {
+        float p[16], sum = 0.f;
 #pragma unroll
-      for (int kt = 0; kt < 2; ++kt)
+        for (int v = 0; v < 16; ++v) p[v] = fmaf(s[v], f, -m);
+        const uint8_t *const k_from = next_keys(t), *const v_from = last_values(t);
+        // in this order: operands asked for AHEAD products before they are needed, exponentials beside the products
+        constexpr int AHEAD = 3, EXPS = 16 / STEPS;
+        bf16x8 kop[STEPS], vop[STEPS];
+        auto ask = [&](int j) {
+          kop[j] = *reinterpret_cast<const bf16x8*>(k_from + j * Lds::K_STEP);
+          vop[j] = *reinterpret_cast<const bf16x8*>(v_from + (2 * (j % MT) + j / MT) * Lds::V_STEP);
+        };
+#pragma unroll
+        for (int j = 0; j < AHEAD; ++j) ask(j);
+#pragma unroll
+        for (int v = 0; v < 16; ++v) s[v] = 0.f;
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int j = 0; j < STEPS; ++j) {
+          if (j + AHEAD < STEPS) ask(j + AHEAD);
+          s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kop[j], qreg[j], s, 0, 0, 0);
+#pragma unroll
+          for (int e = 0; e < EXPS / 2; ++e) p[EXPS * j + e] = __builtin_amdgcn_exp2f(p[EXPS * j + e]);
+          __builtin_amdgcn_sched_barrier(0);
+          o[j % MT] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vop[j], __builtin_bit_cast(bf16x8, pk[j / MT]), o[j % MT], 0, 0, 0);
+#pragma unroll
+          for (int e = EXPS / 2; e < EXPS; ++e) p[EXPS * j + e] = __builtin_amdgcn_exp2f(p[EXPS * j + e]);
+#pragma unroll
+          for (int e = 0; e < EXPS; ++e) sum += p[EXPS * j + e];
+          // (else they would be worked out where they are used, a step later)
+#pragma unroll
+          for (int e = 0; e < EXPS; ++e) asm volatile("" : "+v"(p[EXPS * j + e]));
+          asm volatile("" : "+v"(sum));
+          __builtin_amdgcn_sched_barrier(0);
+        }
+        l += sum;
+        pack(p);
+        asm volatile("" : "+v"(pk[0]), "+v"(pk[1]), "+v"(l));
+        top = Softmax::largest(s, f);
+        leave(t);
+        ++t;
+        arrive(t);
+      } while (!stop());
+      {
+        const bool own = b >= cached;
+        const int limit = (own ? my_row + 1 : seq.L) - (own ? b - cached : b) * CH_KEYS - 32 * (t & 1) - 4 * hh;
 #pragma unroll
         for (int v = 0; v < 16; ++v)
-          if (32 * kt + 8 * (v >> 2) + 4 * hh + (v & 3) >= limit) s[kt][v] = -INFINITY;
-    }
-    const float f = a.scale_log2e;
-    const float top = fmaxf(Softmax::largest(s[0], f), Softmax::largest(s[1], f));
-    // (each query by itself: its result does not depend on those beside it)
-    const bool low = sm.too_low(top);
-    if (__ballot(low)) q8_rescale<MT>(o, sm.lift(low ? top : NO_REFERENCE));
-    u32x4 pk[2][2];
-    sm.weigh(s[0], f, pk[0]);
-    sm.weigh(s[1], f, pk[1]);
+          if (8 * (v >> 2) + (v & 3) >= limit) s[v] = -INFINITY;
+      }
+      top = Softmax::largest(s, f);
+      // Each query's reference by itself: its result does not depend on those beside it.
+      const float ref = top > m + SLACK ? top : m, alpha = __builtin_amdgcn_exp2f(m - ref);
+      m = ref;
+      if (t > 0) values(last_values(t));
+      q8_rescale<MT>(o, alpha);
+      {
+#pragma clang fp contract(off)
+        // Product and difference rounded one by one.  Fused, as above, the rounding of the reference's own product would stay in
+        // the exponent, the same for all keys: next to nothing up to 2^20, but anything far beyond (`far`).
+        float p[16], sum = 0.f;
 #pragma unroll
-    for (int kt = 0; kt < 2; ++kt)
-#pragma unroll
-      for (int kg = 0; kg < 2; ++kg)
-#pragma unroll
-        for (int mt = 0; mt < MT; ++mt) {
-          const bf16x8 vop = *reinterpret_cast<const bf16x8*>(buf + Lds::v_at(kt, mt, kg, hh, n32));
-          o[mt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vop, __builtin_bit_cast(bf16x8, pk[kt][kg]), o[mt], 0, 0, 0);
+        for (int v = 0; v < 16; ++v) {
+          const float x = s[v] * f;
+          p[v] = __builtin_amdgcn_exp2f(x - m);
+          sum += p[v];
         }
+        l = l * alpha + sum;
+        pack(p);
+      }
+      far = __ballot(fabsf(m) > 1048576.f && m != NO_REFERENCE) != 0;
+      if (t == tiles - 1) break;
+      scores(next_keys(t));
+      top = Softmax::largest(s, f);
+      leave(t);
+      until = __builtin_amdgcn_readfirstlane(plain_until(++t));
+      arrive(t);
+    }
+    values(buffer(0) + Lds::V_TILE + v_lane);
   }
   const bool any_odd = __syncthreads_or(odd);
 
-  const float l = sm.l + __shfl_xor(sm.l, 32);
+  l += __shfl_xor(l, 32);
   if (splits == 1) {
     if (qw + n32 < nq) {
       const float inv = 1.0f / l;
@@ -366,7 +493,7 @@ __global__ __launch_bounds__(CH_THREADS, 2) void chunk_attn_q8_kernel(ChunkArgs 
     if (live_wave && part < a.max_parts) {  // (else more work than T rows can be: ranges that overlap)
       const size_t image = (size_t)part * CH_WAVES + wave;
       if (hh == 0) {
-        a.pm[image * 32 + n32] = sm.m;
+        a.pm[image * 32 + n32] = m;
         a.pl[image * 32 + n32] = any_odd ? -l : l;  // (a sum of weights is not negative)
       }
 #pragma unroll
@@ -436,7 +563,7 @@ size_t attn_chunk_ws_floats(int B, int T, int group, int n_kv_heads, int head_di
 
 template <int DH>
 static int chunk_run(const ChunkArgs& a, hipStream_t st) {
-  constexpr size_t lds = 2 * ChunkLds<DH>::BUFFER;
+  constexpr size_t lds = 3 * ChunkLds<DH>::BUFFER;
   static DeviceOnce once;
   allow_lds(once, chunk_attn_q8_kernel<DH>, lds);
   const long items = ((long)a.T * a.group / CH_QUERIES + a.B) * a.n_kv_heads;
