@@ -123,22 +123,22 @@ __device__ inline void chunk_add_odd_values(const ChunkArgs& a, const ChunkSeq& 
 // first key of the sequence's own blocks with a key that row `row` does not see
 __device__ inline int first_partly_seen(int row) { return (row + 1) / CH_KEYS * CH_KEYS; }
 
-// Where a block keeps its operands in LDS: an operand of 64 lanes' 16 bytes after the other, with gaps with which neither
-// reading operands nor writing them from codes or rows meets a bank more often than it has to; lane + constant, so that one
-// register addresses all of a block's.
+// LDS.  A block's operands lie one after the other, 64 lanes' 16 bytes each, with gaps with which neither reading operands
+// nor writing them from codes or rows meets a bank more often than it has to; lane + constant, so that one register
+// addresses all of a block's.  K has two places for blocks, V three.  Behind them is what comes from memory, codes or
+// rows as they are: two blocks' worth, of each wavefront its own, which nobody else reads.
 template <int DH>
 struct ChunkLds {
   static constexpr int STEPS = DH / 16;
-  static constexpr int K_HALF = 512 + 16, K_STEP = 2 * K_HALF, K_TILE = STEPS * K_STEP;
-  static constexpr int V_HALF = 512 + 64, V_STEP = 2 * V_HALF, V_TILE = STEPS * V_STEP;
-  static constexpr int V0 = 2 * K_TILE, BUFFER = V0 + 2 * V_TILE;
+  static constexpr int K_HALF = 512 + 16, K_STEP = 2 * K_HALF, K_TILE = STEPS * K_STEP, K_BLOCK = 2 * K_TILE;
+  static constexpr int V_HALF = 512 + 64, V_STEP = 2 * V_HALF, V_TILE = STEPS * V_STEP, V_BLOCK = 2 * V_TILE;
+  static constexpr int UNITS = DH / 64;  // KiB of a wavefront and block: so many of codes, twice of K rows and of V rows
+  static constexpr int V0 = 2 * K_BLOCK, RAW0 = V0 + 3 * V_BLOCK, RAW = 2 * UNITS * 1024, BYTES = RAW0 + 2 * CH_WAVES * RAW;
   // K: step 2j + i holds columns 32 j + 16 hh + 8 i .. of row r
-  __device__ static inline int k_lane(int hh, int r) { return hh * K_HALF + r * 16; }
-  __device__ static inline int k_at(int kt, int step, int hh, int r) { return kt * K_TILE + step * K_STEP + k_lane(hh, r); }
+  __device__ static inline int k_at(int kt, int step, int hh, int r) { return kt * K_TILE + step * K_STEP + hh * K_HALF + r * 16; }
   // V^T: columns 32 mt .., keys 16 kg + 8 b + 4 hh ..
-  __device__ static inline int v_lane(int hh, int c32) { return V0 + hh * V_HALF + c32 * 16 + (c32 >> 3) * 16; }
   __device__ static inline int v_at(int kt, int mt, int kg, int hh, int c32) {
-    return kt * V_TILE + (2 * mt + kg) * V_STEP + v_lane(hh, c32);
+    return kt * V_TILE + (2 * mt + kg) * V_STEP + hh * V_HALF + c32 * 16 + (c32 >> 3) * 16;
   }
 };
 
@@ -190,26 +190,25 @@ __global__ __launch_bounds__(CH_THREADS, 2) void chunk_attn_q8_kernel(ChunkArgs 
   }
   int odd = 0;
 
-  // ---- bringing a block to LDS: from memory to registers, then, a block later, to LDS
+  // ---- bringing blocks to LDS: asked for two blocks ahead, without registers, then turned into operands.
   // No branch in here that lanes take differently: the walk's accumulators would be copied around it.
-  constexpr bool V_ALL = 4 * DH == CH_THREADS;
-  constexpr int PIECES = 4 * DH, UNITS = 2 * PIECES / CH_THREADS;  // 16 codes each, of K or V; per thread
-  // of this thread's units: K or V, page of the block, place there, places in LDS of the halves (the second a step on)
+  constexpr int UNITS = Lds::UNITS, PIECES = 4 * DH;  // 16 codes each, of K or V
+  const uint32_t raw0 = __builtin_amdgcn_readfirstlane((uint32_t)(size_t)(__attribute__((address_space(3))) uint8_t*)smem + Lds::RAW0 + wave * Lds::RAW);
+  uint8_t* const raw_r = smem + Lds::RAW0 + wave * Lds::RAW;
+  constexpr int RAW_SLOT = CH_WAVES * Lds::RAW;
+  // codes: this wavefront's units are of K or V, of one page of the block; this lane's place there and in LDS
   const int page_of = wave % (PIECES / 64) / (DH / 32), piece = tid % (2 * DH);
   auto is_v = [&](int i) { return (wave + i * CH_WAVES) / (PIECES / 64) != 0; };
   const int c16 = piece >> 5, unit_h = c16 & 1, unit_at = piece & 31;  // K: columns 16 c16 .. of row unit_at; V: column unit_at of 32 (c16 / 2)
   const int k_unit = Lds::k_at(page_of, c16 & ~1, unit_h, unit_at), v_unit = Lds::v_at(page_of, c16 >> 1, 0, unit_h, unit_at);
-  u32x4 raw0 = {}, raw1 = {}, raw2 = {}, raw3 = {};
-  float piece_scale[2];
+  // rows: each wavefront has eight of the block, this lane 16 bytes of K (of the same lane of V)
+  constexpr int PER_ROW = DH / 8, ROWS_AT_ONCE = 64 / PER_ROW;
+  const int my_p = lane % PER_ROW, my_r = lane / PER_ROW;
   int ids = 0, ids_from = -(1 << 30);  // pages ids_from .. + 63 of the sequence, one per lane, and their scales
   float ksc = 1.f, vsc = 1.f;
-  // (places are worked out where they are used: over the whole walk they would take registers)
-  auto fresh_tid = [&]() {
-    int t = threadIdx.x;
-    asm volatile("" : "+v"(t));
-    return t;
-  };
-  auto load = [&](int b) {
+  float scale0[UNITS] = {}, scale1[UNITS] = {};  // of the codes on their way into slots 0 and 1
+  auto ask = [&](int b) {  // into slot b % 2
+    const uint32_t to = raw0 + (b & 1) * RAW_SLOT;
     if (b < cached) {
       if (b * 2 >= ids_from + 64 || ids_from < 0) {
         ids_from = b * 2;
@@ -220,42 +219,43 @@ __global__ __launch_bounds__(CH_THREADS, 2) void chunk_attn_q8_kernel(ChunkArgs 
         const float of_k = a.k_scale[plane + ids], of_v = a.v_scale[plane + ids];
         ksc = !there ? 1.f : ok ? of_k : NAN;  // a page that is not there makes its rows NaN
         vsc = there ? of_v : 1.f;
+        __builtin_amdgcn_s_waitcnt(0x0f70);  // vmcnt(0): the compiler would wait for these later, and for all that is asked for here
       }
       const int at = 2 * b + page_of - ids_from;
       const size_t page = (plane + (uint32_t)__builtin_amdgcn_readlane(ids, at)) * (32 * DH);
 #pragma unroll
       for (int i = 0; i < UNITS; ++i) {
-        piece_scale[i] = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(is_v(i) ? vsc : ksc), at));
-        const u32x4 x = *reinterpret_cast<const u32x4*>((is_v(i) ? a.v_pool : a.k_pool) + page + piece * 16);
-        if (i == 0) raw0 = x;
-        else raw1 = x;
+        const float scale = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(is_v(i) ? vsc : ksc), at));
+        scale0[i] = b & 1 ? scale0[i] : scale;
+        scale1[i] = b & 1 ? scale : scale1[i];
+        load_to_lds<false>((is_v(i) ? a.v_pool : a.k_pool) + page, piece * 16, to + i * 1024);
       }
     } else {
-      const int key0 = (b - cached) * CH_KEYS, tid = fresh_tid();
+      const int key0 = (b - cached) * CH_KEYS + wave * 8;
+      const size_t first = (size_t)(seq.r0 + min(key0, seq.n - 1)) * a.row_stride + (size_t)head * DH;
+      const int rows = max(seq.n - 1 - key0, 0);  // (those behind the last are the last)
 #pragma unroll
-      for (int i = 0; i < DH / 64; ++i) {
-        const int u = tid + i * CH_THREADS, row = u / (DH / 8), p = u % (DH / 8);
-        const u32x4 x = *reinterpret_cast<const u32x4*>(a.k_rows + (size_t)(seq.r0 + min(key0 + row, seq.n - 1)) * a.row_stride + (size_t)head * DH + 8 * p);
-        if (i == 0) raw0 = x;
-        else raw1 = x;
-      }
-      if (V_ALL || wave < 4 * DH / 64) {  // four rows, four columns
-        const int quad = tid / (DH / 4), cq = tid % (DH / 4);
-        u32x2 v[4];
-#pragma unroll
-        for (int d = 0; d < 4; ++d)
-          v[d] = *reinterpret_cast<const u32x2*>(a.v_rows + (size_t)(seq.r0 + min(key0 + 4 * quad + d, seq.n - 1)) * a.row_stride + (size_t)head * DH + 4 * cq);
-        raw2 = u32x4{v[0][0], v[0][1], v[1][0], v[1][1]};
-        raw3 = u32x4{v[2][0], v[2][1], v[3][0], v[3][1]};
+      for (int i = 0; i < UNITS; ++i) {
+        const uint32_t at = (uint32_t)min(i * ROWS_AT_ONCE + my_r, rows) * (uint32_t)(a.row_stride * 2) + my_p * 16;
+        load_to_lds<false>(a.k_rows + first, at, to + i * 1024);
+        load_to_lds<false>(a.v_rows + first, at, to + (UNITS + i) * 1024);
       }
     }
   };
-  auto store = [&](int b, uint8_t* buf) {
+  // block b has come; the operands of block b to its places
+  auto arrived = [&](int b) {
+    if (b + 1 >= b1) __builtin_amdgcn_s_waitcnt(0x0f70);           // vmcnt(0)
+    else if (b + 1 < cached) __builtin_amdgcn_s_waitcnt(0x0f70 + UNITS);  // all but the next block's
+    else __builtin_amdgcn_s_waitcnt(0x0f70 + 2 * UNITS);
+    asm volatile("" ::: "memory");
+  };
+  auto convert = [&](int b, uint8_t* kbuf, uint8_t* vbuf) {
+    const uint8_t* const raw = raw_r + (b & 1) * RAW_SLOT;
     if (b < cached) {
 #pragma unroll
       for (int i = 0; i < UNITS; ++i) {
-        u32x4 x = i == 0 ? raw0 : raw1;
-        const float scale = piece_scale[i];
+        u32x4 x = *reinterpret_cast<const u32x4*>(raw + i * 1024 + lane * 16);
+        const float scale = b & 1 ? scale1[i] : scale0[i];
         const int rest = seq.L - (2 * b + page_of) * 32;
         if (is_v(i) && rest < 32) {  // slots past the end may hold anything: their weights are 0, their values have to be numbers
 #pragma unroll
@@ -269,38 +269,43 @@ __global__ __launch_bounds__(CH_THREADS, 2) void chunk_attn_q8_kernel(ChunkArgs 
           const u32x4 none = {0x7fc07fc0u, 0x7fc07fc0u, 0x7fc07fc0u, 0x7fc07fc0u};
           lo = hi = __builtin_bit_cast(bf16x8, none);
         }
-        uint8_t* const to = buf + (is_v(i) ? v_unit : k_unit);
+        uint8_t* const to = is_v(i) ? vbuf + v_unit : kbuf + k_unit;
         *reinterpret_cast<bf16x8*>(to) = lo;
         *reinterpret_cast<bf16x8*>(to + (is_v(i) ? Lds::V_STEP : Lds::K_STEP)) = hi;
       }
     } else {
-      const int key0 = (b - cached) * CH_KEYS, tid = fresh_tid();
+      const int key0 = (b - cached) * CH_KEYS;
 #pragma unroll
-      for (int i = 0; i < DH / 64; ++i) {
-        const int u = tid + i * CH_THREADS, row = u / (DH / 8), p = u % (DH / 8);
-        *reinterpret_cast<u32x4*>(buf + Lds::k_at(row >> 5, (p >> 2) * 2 + (p & 1), (p >> 1) & 1, row & 31)) = i == 0 ? raw0 : raw1;
+      for (int i = 0; i < UNITS; ++i) {
+        const int row = wave * 8 + i * ROWS_AT_ONCE + my_r;
+        *reinterpret_cast<u32x4*>(kbuf + Lds::k_at(row >> 5, (my_p >> 2) * 2 + (my_p & 1), (my_p >> 1) & 1, row & 31)) =
+            *reinterpret_cast<const u32x4*>(raw + i * 1024 + lane * 16);
       }
-      if (V_ALL || wave < 4 * DH / 64) {
-        const int quad = tid / (DH / 4), cq = tid % (DH / 4);
-        uint32_t v[4][2] = {{raw2[0], raw2[1]}, {raw2[2], raw2[3]}, {raw3[0], raw3[1]}, {raw3[2], raw3[3]}};
-        if (key0 >= first_partly_seen(row_first)) {
+      // four rows, four columns (for heads of 64 the upper lanes do what the lower ones do)
+      const int quad = wave * 2 + (lane / (DH / 4) & 1), cq = lane % (DH / 4);
+      uint32_t v[4][2];
 #pragma unroll
-          for (int d = 0; d < 4; ++d)
+      for (int d = 0; d < 4; ++d) {
+        const u32x2 x = *reinterpret_cast<const u32x2*>(raw + UNITS * 1024 + ((quad & 1) * 4 + d) * (2 * DH) + cq * 8);
+        v[d][0] = x[0], v[d][1] = x[1];
+      }
+      if (key0 >= first_partly_seen(row_first)) {
 #pragma unroll
-            for (int e = 0; e < 2; ++e) {
-              const bool lo = (v[d][e] & 0x7f80u) == 0x7f80u, hi = (v[d][e] & 0x7f800000u) == 0x7f800000u;
-              v[d][e] &= (lo ? 0xffff0000u : ~0u) & (hi ? 0xffffu : ~0u);
-              odd |= (int)lo | (int)hi;
-            }
-        }
+        for (int d = 0; d < 4; ++d)
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const int c = 4 * cq + e, sh = e & 1;
-          const uint32_t x0 = v[0][e >> 1], x1 = v[1][e >> 1], x2 = v[2][e >> 1], x3 = v[3][e >> 1];
-          const u32x2 col = sh ? u32x2{(x0 >> 16) | (x1 & 0xffff0000u), (x2 >> 16) | (x3 & 0xffff0000u)}
-                               : u32x2{(x0 & 0xffffu) | (x1 << 16), (x2 & 0xffffu) | (x3 << 16)};
-          *reinterpret_cast<u32x2*>(buf + Lds::v_at(quad >> 3, c >> 5, (quad >> 2) & 1, quad & 1, c & 31) + ((quad >> 1) & 1) * 8) = col;
-        }
+          for (int e = 0; e < 2; ++e) {
+            const bool lo = (v[d][e] & 0x7f80u) == 0x7f80u, hi = (v[d][e] & 0x7f800000u) == 0x7f800000u;
+            v[d][e] &= (lo ? 0xffff0000u : ~0u) & (hi ? 0xffffu : ~0u);
+            odd |= (int)lo | (int)hi;
+          }
+      }
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const int c = 4 * cq + e;
+        const uint32_t x0 = v[0][e >> 1], x1 = v[1][e >> 1], x2 = v[2][e >> 1], x3 = v[3][e >> 1];
+        const u32x2 col = e & 1 ? u32x2{(x0 >> 16) | (x1 & 0xffff0000u), (x2 >> 16) | (x3 & 0xffff0000u)}
+                                : u32x2{(x0 & 0xffffu) | (x1 << 16), (x2 & 0xffffu) | (x3 << 16)};
+        *reinterpret_cast<u32x2*>(vbuf + Lds::v_at(quad >> 3, c >> 5, (quad >> 2) & 1, quad & 1, c & 31) + ((quad >> 1) & 1) * 8) = col;
       }
     }
   };
@@ -315,7 +320,7 @@ __global__ __launch_bounds__(CH_THREADS, 2) void chunk_attn_q8_kernel(ChunkArgs 
   for (int mt = 0; mt < MT; ++mt)
 #pragma unroll
     for (int v = 0; v < 16; ++v) o[mt][v] = 0.f;
-  const int k_lane = Lds::k_lane(hh, n32), v_lane = Lds::v_lane(hh, n32);
+  const int k_lane = Lds::k_at(0, 0, hh, n32), v_lane = Lds::V0 + Lds::v_at(0, 0, 0, hh, n32);
   auto scores = [&](const uint8_t* at) {
     f32x16 to;
 #pragma unroll
@@ -340,19 +345,24 @@ __global__ __launch_bounds__(CH_THREADS, 2) void chunk_attn_q8_kernel(ChunkArgs 
       for (int e = 0; e < 4; ++e) pk[kg][e] = pack2bf(p[8 * kg + 2 * e], p[8 * kg + 2 * e + 1]);
   };
   const int tiles = 2 * (b1 - b0);
-  // Blocks stay in LDS in turn in three places.  Block b + 1 takes the place of block b - 2, which was last read in the first
-  // step of block b - 1, before that block's barrier.
-  int b = b0, place = 0;  // of the current block
-  auto buffer = [&](int ahead) {
+  // Block b + 1 takes the K place of block b - 1 and the V place of block b - 2.  Both were last read in the first step of
+  // block b - 1, before that block's barrier.
+  int b = b0, place = 0;  // the current block, and its V place
+  auto k_block = [&](int ahead) { return smem + ((b - b0 + ahead) & 1) * Lds::K_BLOCK; };
+  auto v_block = [&](int ahead) {
     const int i = place + ahead;
-    return smem + (i - (3 & ~((i - 3) >> 31))) * Lds::BUFFER;
+    return smem + (i - (3 & ~((i - 3) >> 31))) * Lds::V_BLOCK;
   };
   auto arrive = [&](int t) {  // in front of tile t
     if (t & 1) {
       __syncthreads();
-    } else {
-      if (b + 1 < b1) store(b + 1, buffer(1));
-      if (b + 2 < b1) load(b + 2);
+    } else if (b + 1 < b1) {
+      arrived(b + 1);
+      convert(b + 1, k_block(1), v_block(1) + Lds::V0);
+      if (b + 3 < b1) {
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // what came has been read
+        ask(b + 3);
+      }
     }
   };
   auto leave = [&](int t) {
@@ -360,12 +370,17 @@ __global__ __launch_bounds__(CH_THREADS, 2) void chunk_attn_q8_kernel(ChunkArgs 
     const int next = place + (t & 1);
     place = next & ((next - 3) >> 31);
   };
-  auto next_keys = [&](int t) { return buffer(t & 1) + (1 - (t & 1)) * Lds::K_TILE + k_lane; };
-  auto last_values = [&](int t) { return buffer(2 - 2 * (t & 1)) + (1 - (t & 1)) * Lds::V_TILE + v_lane; };
+  auto next_keys = [&](int t) { return k_block(t & 1) + (1 - (t & 1)) * Lds::K_TILE + k_lane; };
+  auto last_values = [&](int t) { return v_block(2 - 2 * (t & 1)) + (1 - (t & 1)) * Lds::V_TILE + v_lane; };
   if (tiles > 0) {
-    load(b0);
-    store(b0, buffer(0));
-    if (b0 + 1 < b1) load(b0 + 1);
+    ask(b0);
+    if (b0 + 1 < b1) ask(b0 + 1);
+    arrived(b0);
+    convert(b0, k_block(0), v_block(0) + Lds::V0);
+    if (b0 + 2 < b1) {
+      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+      ask(b0 + 2);
+    }
     __syncthreads();
   }
   if (!live_wave) {
@@ -382,7 +397,7 @@ __global__ __launch_bounds__(CH_THREADS, 2) void chunk_attn_q8_kernel(ChunkArgs 
       const int end = t < cached_end ? cached_end : t >= own_begin && t < own_end ? own_end : t;
       return far ? t : min(end, tiles - 1);
     };
-    scores(buffer(0) + k_lane);
+    scores(k_block(0) + k_lane);
     top = Softmax::largest(s, f);
     int t = 0, until = 0;
     arrive(t);
@@ -470,7 +485,7 @@ __global__ __launch_bounds__(CH_THREADS, 2) void chunk_attn_q8_kernel(ChunkArgs 
       until = __builtin_amdgcn_readfirstlane(plain_until(++t));
       arrive(t);
     }
-    values(buffer(0) + Lds::V_TILE + v_lane);
+    values(v_block(0) + Lds::V_TILE + v_lane);
   }
   const bool any_odd = __syncthreads_or(odd);
 
@@ -563,7 +578,7 @@ size_t attn_chunk_ws_floats(int B, int T, int group, int n_kv_heads, int head_di
 
 template <int DH>
 static int chunk_run(const ChunkArgs& a, hipStream_t st) {
-  constexpr size_t lds = 3 * ChunkLds<DH>::BUFFER;
+  constexpr size_t lds = ChunkLds<DH>::BYTES;
   static DeviceOnce once;
   allow_lds(once, chunk_attn_q8_kernel<DH>, lds);
   const long items = ((long)a.T * a.group / CH_QUERIES + a.B) * a.n_kv_heads;
