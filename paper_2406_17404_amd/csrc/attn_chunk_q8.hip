@@ -27,11 +27,12 @@ struct ChunkArgs {
   int max_parts;
   float scale_log2e;
   float *po, *pm, *pl;  // un-normalised partials: [part][wavefront] images of the accumulators, maxima and sums of 32 queries
+  int32_t* merges;      // how many tiles there are to merge, then from word 8 on 8 words for each (ChunkMerge)
   uint16_t* out;
   int32_t* status;
 };
 constexpr int CH_WAVES = 8, CH_THREADS = 64 * CH_WAVES, CH_QUERIES = 32 * CH_WAVES, CH_KEYS = 64;
-constexpr int CH_MAX_PARTS = 512, CH_TARGET = CH_MAX_PARTS / 2, CH_LEAST = 4;
+constexpr int CH_MAX_PARTS = 512, CH_MAX_MERGES = CH_MAX_PARTS / 2, CH_LEAST = 4;  // partials that a call may leave to the merge; blocks that a split has at least
 
 struct ChunkSeq {
   int r0, n, L, tiles;  // n < 0: refused, with nothing written; L < 0: refused, rows of zeros
@@ -51,46 +52,117 @@ __device__ inline ChunkSeq chunk_seq(const ChunkArgs& a, int s) {
 
 struct ChunkWork {
   ChunkSeq seq;
-  int s, nth, splits, part0;
+  int s, nth, splits, part0, merge0;  // first partial and first merge of the sequence
 };
-// The same on every wavefront of every workgroup: a split has `span` blocks at most, of one sequence evenly many.
+struct ChunkMerge {
+  int r0, n, tile, head, splits, part, step, pad;  // partial of split k: part + k * step
+};
+// The plan, the same on every wavefront of every workgroup: a split has `span` blocks at most, of one sequence evenly
+// many.  Up to 64 sequences (not MANY) 32 spans are weighed, one per lane, the longest sequence in 1 .. 32 splits:
+//   cost = rounds of workgroups * (START + blocks of one) + MERGE if anything is split
+// in times that a compute unit takes for a block of 256 queries (2.3 us); sequences come longest first, so that what starts
+// last is short.  Beyond 64 sequences neither is done: index order, and spans of an even share.
+constexpr float START = 4.5f, MERGE = 2.5f, RESIDENT = 256.f;  // one workgroup per compute unit at a time
+template <bool MANY>
 struct ChunkPlan {
   const ChunkArgs& a;
-  int span;
+  ChunkSeq mine;  // sequence `id` (sorted)
+  int id, span;
   __device__ inline explicit ChunkPlan(const ChunkArgs& args) : a(args) {
     const int lane = threadIdx.x & 63;
     float work = 0.f;
-    for (int s0 = 0; s0 < a.B; s0 += 64) {
-      const ChunkSeq q = chunk_seq(a, s0 + lane);
-      work += wave_sum((float)q.tiles * (float)q.blocks());
+    for (int s0 = 0; s0 < (MANY ? a.B : 1); s0 += 64) {
+      mine = chunk_seq(a, s0 + lane);
+      if (!MANY && a.B == 1) break;
+      work += wave_sum((float)mine.tiles * (float)mine.blocks());
     }
-    work *= a.n_kv_heads;  // (a split sequence has at most twice its share of parts)
-    span = a.max_parts == 0 ? INT32_MAX >> 1 : (int)fminf(fmaxf(ceilf(work * (1.0001f / CH_TARGET)), (float)CH_LEAST), 1e9f);
+    work *= a.n_kv_heads;
+    id = lane;
+    if (MANY) {  // (a split sequence has at most twice its share of parts)
+      span = a.max_parts == 0 ? 1 << 30 : (int)fminf(fmaxf(ceilf(work * (1.0001f * 2 / CH_MAX_PARTS)), (float)CH_LEAST), 1e9f);
+      return;
+    }
+    if (a.B > 1) {  // longest first
+      const int blocks = mine.blocks();
+      int rank = 0;
+      for (int t0 = 0; t0 < a.B; t0 += 8)  // (lanes behind the last sequence have no blocks)
+#pragma unroll
+        for (int t = t0; t < t0 + 8; ++t) {
+          const int b = lane_value(blocks, t);
+          rank += b > blocks || (b == blocks && t < lane);
+        }
+      rank = lane < a.B ? rank : lane;
+      auto to = [&](int v) { return __builtin_amdgcn_ds_permute(rank << 2, v); };
+      mine = ChunkSeq{to(mine.r0), to(mine.n), to(mine.L), to(mine.tiles)};
+      id = to(lane);
+    }
+    const int blocks = mine.blocks(), longest = max(lane_value(blocks, 0), 1), groups = mine.tiles * a.n_kv_heads;
+    span = longest;
+    if (a.max_parts == 0 || longest == 1) return;
+    const int c = (longest + (lane & 31)) / ((lane & 31) + 1);
+    const float each = __builtin_amdgcn_rcpf((float)c);
+    float n = 0.f, parts = 0.f;
+    if (a.B == 1) work = (float)lane_value(groups, 0) * (float)longest;
+    for (int t = 0; t < a.B; ++t) {
+      const int b = lane_value(blocks, t), g = lane_value(groups, t);
+      const float k = floorf(((float)(b + c) - 0.5f) * each);  // ceil(b / c)
+      n += (float)g * k;
+      parts += k > 1.f ? (float)g * k : 0.f;
+    }
+    const float rounds = ceilf(n * (1.f / RESIDENT));
+    const float whole = START + (float)c, even = START + work * __builtin_amdgcn_rcpf(n);
+    float cost = (rounds > 1.f ? fmaxf(whole, rounds * even) : whole) + (parts > 0.f ? MERGE : 0.f);
+    if (parts > (float)a.max_parts) cost = INFINITY;  // no room for its partials
+    const uint32_t best = wave_min((uint32_t)fminf(cost * 8.f, 60e6f) << 6 | lane);  // (of equals the fewest splits)
+    span = lane_value(c, best & 63);
+    // the reciprocal's division may be off for lengths beyond 2^16 blocks: whole numbers decide whether the partials have room
+    if (longest > 1 << 16) {
+      const int k = splits(mine);
+      if (wave_sum(k > 1 ? (float)groups * (float)k : 0.f) > (float)a.max_parts) span = longest;
+    }
   }
   __device__ inline int splits(const ChunkSeq& q) const { return (q.blocks() + span - 1) / span; }
-  // item x of all; of which a (sequence, tile, K/V head) counts its splits, or, MERGE, once if there are several
-  template <bool MERGE>
-  __device__ inline bool find(int x, ChunkWork& w) const {
+  // item x of all, of which a (sequence, tile, K/V head) counts its splits
+  __device__ inline bool find(int x, ChunkWork& w) {
     const int lane = threadIdx.x & 63;
-    int base = 0, parts = 0;
-    for (int s0 = 0; s0 < a.B; s0 += 64) {
-      const ChunkSeq q = chunk_seq(a, s0 + lane);
-      const int k = splits(q), g = q.tiles * a.n_kv_heads, n = MERGE ? (k > 1 ? g : 0) : g * k;
-      const int upto = base + wave_scan(n), pupto = parts + wave_scan(k > 1 ? g * k : 0);
+    if (!MANY && a.B == 1) {
+      w.seq = ChunkSeq{lane_value(mine.r0, 0), lane_value(mine.n, 0), lane_value(mine.L, 0), lane_value(mine.tiles, 0)};
+      w.s = w.part0 = w.merge0 = 0;
+      w.nth = x;
+      w.splits = splits(w.seq);
+      return x < w.seq.tiles * a.n_kv_heads * w.splits;
+    }
+    int base = 0, parts = 0, merges = 0;
+    for (int s0 = 0; s0 < (MANY ? a.B : 1); s0 += 64) {
+      if (MANY) mine = chunk_seq(a, s0 + lane), id = s0 + lane;
+      const int k = splits(mine), g = mine.tiles * a.n_kv_heads;
+      const int upto = base + wave_scan(g * k), pupto = parts + wave_scan(k > 1 ? g * k : 0), mupto = merges + wave_scan(k > 1 ? g : 0);
       const uint64_t here = __ballot(x < upto);
       if (here) {
         const int l = __builtin_ctzll(here);
-        w.seq = ChunkSeq{lane_value(q.r0, l), lane_value(q.n, l), lane_value(q.L, l), lane_value(q.tiles, l)};
-        w.s = s0 + l;
-        w.nth = x - (lane_value(upto, l) - lane_value(n, l));
+        w.seq = ChunkSeq{lane_value(mine.r0, l), lane_value(mine.n, l), lane_value(mine.L, l), lane_value(mine.tiles, l)};
+        w.s = lane_value(id, l);
         w.splits = lane_value(k, l);
-        w.part0 = lane_value(pupto, l) - (w.splits > 1 ? lane_value(g, l) * w.splits : 0);
+        const int gl = lane_value(g, l);
+        w.nth = x - (lane_value(upto, l) - gl * w.splits);
+        w.part0 = lane_value(pupto, l) - (w.splits > 1 ? gl * w.splits : 0);
+        w.merge0 = lane_value(mupto, l) - (w.splits > 1 ? gl : 0);
         return true;
       }
       base = lane_value(upto, 63);
       parts = lane_value(pupto, 63);
+      merges = lane_value(mupto, 63);
     }
     return false;
+  }
+  // tiles that are split
+  __device__ inline int merges() {
+    int sum = 0;
+    for (int s0 = 0; s0 < (MANY ? a.B : 1); s0 += 64) {
+      const ChunkSeq q = MANY ? chunk_seq(a, s0 + (threadIdx.x & 63)) : mine;
+      sum += lane_value(wave_scan(splits(q) > 1 ? q.tiles * a.n_kv_heads : 0), 63);
+    }
+    return sum;
   }
 };
 
@@ -142,7 +214,7 @@ struct ChunkLds {
   }
 };
 
-template <int DH>
+template <int DH, bool MANY>
 __global__ __launch_bounds__(CH_THREADS, 2) void chunk_attn_q8_kernel(ChunkArgs a) {
   using Lds = ChunkLds<DH>;
   constexpr int MT = DH / 32, STEPS = DH / 16, OW = MT * 16 * 64;
@@ -154,9 +226,13 @@ __global__ __launch_bounds__(CH_THREADS, 2) void chunk_attn_q8_kernel(ChunkArgs 
       const ChunkSeq q = chunk_seq(a, s);
       if (q.n <= 0) a.status[s] = q.n < 0;
     }
-  const ChunkPlan plan(a);
+  ChunkPlan<MANY> plan(a);
+  if (blockIdx.x == 0 && a.max_parts > 0) {
+    const int n = plan.merges();
+    if (tid == 0) a.merges[0] = min(n, CH_MAX_MERGES);
+  }
   ChunkWork w;
-  if (!plan.find<false>(blockIdx.x, w)) return;
+  if (!plan.find(blockIdx.x, w)) return;
   const ChunkSeq seq = w.seq;
   const int nq = seq.n * a.group, splits = w.splits;
   const int head = w.nth % a.n_kv_heads, sp = w.nth / a.n_kv_heads % splits, tile = seq.tiles - 1 - w.nth / a.n_kv_heads / splits;
@@ -219,16 +295,16 @@ __global__ __launch_bounds__(CH_THREADS, 2) void chunk_attn_q8_kernel(ChunkArgs 
         const float of_k = a.k_scale[plane + ids], of_v = a.v_scale[plane + ids];
         ksc = !there ? 1.f : ok ? of_k : NAN;  // a page that is not there makes its rows NaN
         vsc = there ? of_v : 1.f;
-        __builtin_amdgcn_s_waitcnt(0x0f70);  // vmcnt(0): the compiler would wait for these later, and for all that is asked for here
       }
       const int at = 2 * b + page_of - ids_from;
       const size_t page = (plane + (uint32_t)__builtin_amdgcn_readlane(ids, at)) * (32 * DH);
+#pragma unroll
+      for (int i = 0; i < UNITS; ++i) load_to_lds<false>((is_v(i) ? a.v_pool : a.k_pool) + page, piece * 16, to + i * 1024);
 #pragma unroll
       for (int i = 0; i < UNITS; ++i) {
         const float scale = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(is_v(i) ? vsc : ksc), at));
         scale0[i] = b & 1 ? scale0[i] : scale;
         scale1[i] = b & 1 ? scale : scale1[i];
-        load_to_lds<false>((is_v(i) ? a.v_pool : a.k_pool) + page, piece * 16, to + i * 1024);
       }
     } else {
       const int key0 = (b - cached) * CH_KEYS + wave * 8;
@@ -461,22 +537,22 @@ __global__ __launch_bounds__(CH_THREADS, 2) void chunk_attn_q8_kernel(ChunkArgs 
       // Each query's reference by itself: its result does not depend on those beside it.
       const float ref = top > m + SLACK ? top : m, alpha = __builtin_amdgcn_exp2f(m - ref);
       m = ref;
-      if (t > 0) values(last_values(t));
-      q8_rescale<MT>(o, alpha);
+      float p[16], sum = 0.f;
       {
 #pragma clang fp contract(off)
         // Product and difference rounded one by one.  Fused, as above, the rounding of the reference's own product would stay in
         // the exponent, the same for all keys: next to nothing up to 2^20, but anything far beyond (`far`).
-        float p[16], sum = 0.f;
 #pragma unroll
         for (int v = 0; v < 16; ++v) {
           const float x = s[v] * f;
           p[v] = __builtin_amdgcn_exp2f(x - m);
           sum += p[v];
         }
-        l = l * alpha + sum;
-        pack(p);
       }
+      if (t > 0) values(last_values(t));
+      l = l * alpha + sum;
+      pack(p);
+      if (__ballot(alpha != 1.f)) q8_rescale<MT>(o, alpha);
       far = __ballot(fabsf(m) > 1048576.f && m != NO_REFERENCE) != 0;
       if (t == tiles - 1) break;
       scores(next_keys(t));
@@ -504,7 +580,11 @@ __global__ __launch_bounds__(CH_THREADS, 2) void chunk_attn_q8_kernel(ChunkArgs 
     }
     if (any_odd) chunk_add_odd_values(a, seq, head, DH, q0, q1, first_partly_seen(row_first));
   } else {
-    const int part = w.part0 + w.nth;
+    const int part = w.part0 + w.nth, tiles_done = w.nth / a.n_kv_heads / splits, merge = w.merge0 + tiles_done * a.n_kv_heads + head;
+    if (sp == 0 && tid == 0 && merge < CH_MAX_MERGES) {
+      const bool room = w.part0 + (tiles_done + 1) * splits * a.n_kv_heads <= a.max_parts;
+      reinterpret_cast<ChunkMerge*>(a.merges + 8)[merge] = ChunkMerge{seq.r0, seq.n, tile, head, room ? splits : 0, part, a.n_kv_heads, 0};
+    }
     if (live_wave && part < a.max_parts) {  // (else more work than T rows can be: ranges that overlap)
       const size_t image = (size_t)part * CH_WAVES + wave;
       if (hh == 0) {
@@ -527,44 +607,68 @@ __global__ __launch_bounds__(CH_THREADS, 2) void chunk_attn_q8_kernel(ChunkArgs 
   }
 }
 
-// Merges the partials of 32 queries of a (sequence, tile, K/V head) in split order, 32 columns per wavefront.
+// Merges the partials of 32 queries of a (sequence, tile, K/V head) in split order, 32 columns per wavefront, every second
+// split from h on, four at a time with all their loads together; the two sums are joined through LDS.
 template <int DH>
-__global__ __launch_bounds__(64 * (DH / 32)) void chunk_merge_kernel(ChunkArgs a) {
-  constexpr int MT = DH / 32, OW = MT * 16 * 64;
-  const int tid = threadIdx.x, lane = tid & 63, n32 = lane & 31, hh = lane >> 5, mt = tid >> 6;
-  const ChunkPlan plan(a);
-  for (int x = blockIdx.x / CH_WAVES;; x += gridDim.x / CH_WAVES) {
-    const int wave = blockIdx.x % CH_WAVES;
-    ChunkWork w;
-    if (!plan.find<true>(x, w)) return;
-    const ChunkSeq seq = w.seq;
-    const int nq = seq.n * a.group, splits = w.splits, head = w.nth % a.n_kv_heads, rest = w.nth / a.n_kv_heads;
-    const int tile = seq.tiles - 1 - rest, q0 = tile * CH_QUERIES, qw = q0 + wave * 32, qi = qw + n32;
-    if (qw >= nq || w.part0 + (rest + 1) * splits * a.n_kv_heads > a.max_parts) continue;
-    float m = NO_REFERENCE, l = 0.f;
-    bool odd = false;
-    f32x4 o[4] = {};
-    for (int sp = 0; sp < splits; ++sp) {
-      const size_t image = (size_t)(w.part0 + (rest * splits + sp) * a.n_kv_heads + head) * CH_WAVES + wave;
-      const float pm = a.pm[image * 32 + n32], pl = a.pl[image * 32 + n32];
-      const float top = fmaxf(m, pm), keep = __builtin_amdgcn_exp2f(m - top), f = __builtin_amdgcn_exp2f(pm - top);
-      odd = odd || (__float_as_uint(pl) >> 31) != 0;
-      l = l * keep + fabsf(pl) * f;
-      m = top;
+__global__ __launch_bounds__(128 * (DH / 32)) void chunk_merge_kernel(ChunkArgs a) {
+  constexpr int MT = DH / 32, OW = MT * 16 * 64, BATCH = 4, H = 2;
+  __shared__ float sm_m[32], sm_l[32];
+  __shared__ f32x4 sm_o[4][64 * MT];
+  const int tid = threadIdx.x, lane = tid & 63, n32 = lane & 31, hh = lane >> 5, mt = (tid >> 6) % MT, h = tid / (64 * MT);
+  const int x = blockIdx.x / CH_WAVES, wave = blockIdx.x % CH_WAVES;
+  if (x >= a.merges[0]) return;
+  const ChunkMerge w = reinterpret_cast<const ChunkMerge*>(a.merges + 8)[x];
+  const int nq = w.n * a.group, q0 = w.tile * CH_QUERIES, qw = q0 + wave * 32, qi = qw + n32;
+  if (qw >= nq || w.splits == 0) return;
+  float m = NO_REFERENCE, l = 0.f;
+  bool odd = false;
+  f32x4 o[4] = {};
+  for (int s0 = h; s0 < w.splits; s0 += H * BATCH) {
+    float pm[BATCH], pl[BATCH];
+    f32x4 po[BATCH][4];
 #pragma unroll
-      for (int g = 0; g < 4; ++g)
-        o[g] = o[g] * keep + *reinterpret_cast<const f32x4*>(a.po + image * OW + (mt * 4 + g) * 256 + lane * 4) * f;
-    }
-    if (qi < nq) {
-      const float inv = 1.0f / l;
-      uint16_t* dst = a.out + ((size_t)(seq.r0 + qi / a.group) * a.n_kv_heads * a.group + head * a.group + qi % a.group) * DH + 32 * mt + 4 * hh;
+    for (int k = 0; k < BATCH; ++k) {
+      const size_t image = (size_t)(w.part + min(s0 + H * k, w.splits - 1) * w.step) * CH_WAVES + wave;
+      pm[k] = a.pm[image * 32 + n32];
+      pl[k] = a.pl[image * 32 + n32];
 #pragma unroll
-      for (int g = 0; g < 4; ++g)
-        *reinterpret_cast<u32x2*>(dst + 8 * g) = u32x2{pack2bf(o[g][0] * inv, o[g][1] * inv), pack2bf(o[g][2] * inv, o[g][3] * inv)};
+      for (int g = 0; g < 4; ++g) po[k][g] = *reinterpret_cast<const f32x4*>(a.po + image * OW + (mt * 4 + g) * 256 + lane * 4);
     }
-    if (__syncthreads_or(odd)) chunk_add_odd_values(a, seq, head, DH, qw, min(nq, qw + 32), first_partly_seen(q0 / a.group));
-    __syncthreads();
+    float top = m;
+#pragma unroll
+    for (int k = 0; k < BATCH; ++k) top = fmaxf(top, pm[k]);
+    const float keep = __builtin_amdgcn_exp2f(m - top);
+    m = top;
+    l *= keep;
+#pragma unroll
+    for (int g = 0; g < 4; ++g) o[g] *= keep;
+#pragma unroll
+    for (int k = 0; k < BATCH; ++k) {
+      if (s0 + H * k >= w.splits) break;
+      const float f = __builtin_amdgcn_exp2f(pm[k] - m);
+      odd = odd || (__float_as_uint(pl[k]) >> 31) != 0;
+      l += f * fabsf(pl[k]);
+#pragma unroll
+      for (int g = 0; g < 4; ++g) o[g] += po[k][g] * f;
+    }
   }
+  if (h > 0) {
+#pragma unroll
+    for (int g = 0; g < 4; ++g) sm_o[g][mt * 64 + lane] = o[g];
+    if (mt == 0 && hh == 0) sm_m[n32] = m, sm_l[n32] = l;
+  }
+  const bool any_odd = __syncthreads_or(odd);
+  if (h == 0 && qi < nq) {
+    const float top = fmaxf(m, sm_m[n32]), keep = __builtin_amdgcn_exp2f(m - top), f = __builtin_amdgcn_exp2f(sm_m[n32] - top);
+    const float inv = 1.0f / (l * keep + sm_l[n32] * f);
+    uint16_t* dst = a.out + ((size_t)(w.r0 + qi / a.group) * a.n_kv_heads * a.group + w.head * a.group + qi % a.group) * DH + 32 * mt + 4 * hh;
+#pragma unroll
+    for (int g = 0; g < 4; ++g) {
+      const f32x4 r = (o[g] * keep + sm_o[g][mt * 64 + lane] * f) * inv;
+      *reinterpret_cast<u32x2*>(dst + 8 * g) = u32x2{pack2bf(r[0], r[1]), pack2bf(r[2], r[3])};
+    }
+  }
+  if (any_odd) chunk_add_odd_values(a, ChunkSeq{w.r0, w.n, 0, 0}, w.head, DH, qw, min(nq, qw + 32), first_partly_seen(q0 / a.group));
 }
 
 // ------------------------------------------------------------------ launch
@@ -573,20 +677,21 @@ static int chunk_max_parts(int T, int max_prefix) {
   return most <= CH_LEAST ? 0 : CH_MAX_PARTS;
 }
 size_t attn_chunk_ws_floats(int B, int T, int group, int n_kv_heads, int head_dim, int max_prefix) {
-  return (size_t)chunk_max_parts(T, max_prefix) * CH_WAVES * (32 * head_dim + 64);
+  const size_t parts = (size_t)chunk_max_parts(T, max_prefix);
+  return parts == 0 ? 0 : parts * CH_WAVES * (32 * head_dim + 64) + 8 * (CH_MAX_MERGES + 1);
 }
 
-template <int DH>
+template <int DH, bool MANY>
 static int chunk_run(const ChunkArgs& a, hipStream_t st) {
   constexpr size_t lds = ChunkLds<DH>::BYTES;
   static DeviceOnce once;
-  allow_lds(once, chunk_attn_q8_kernel<DH>, lds);
+  allow_lds(once, chunk_attn_q8_kernel<DH, MANY>, lds);
   const long items = ((long)a.T * a.group / CH_QUERIES + a.B) * a.n_kv_heads;
   const int grid = (int)std::min(items + a.max_parts, 1l << 30);
-  chunk_attn_q8_kernel<DH><<<grid, CH_THREADS, lds, st>>>(a);
+  chunk_attn_q8_kernel<DH, MANY><<<grid, CH_THREADS, lds, st>>>(a);
   int rc = check_launch();
   if (rc != TRJ_OK || a.max_parts == 0) return rc;
-  chunk_merge_kernel<DH><<<CH_WAVES * (int)std::min(items, 128l), 64 * (DH / 32), 0, st>>>(a);
+  chunk_merge_kernel<DH><<<CH_WAVES * (int)std::min(items, (long)CH_MAX_MERGES), 128 * (DH / 32), 0, st>>>(a);
   return check_launch();
 }
 
@@ -600,8 +705,9 @@ int launch_attn_chunk_q8(const uint16_t* q, int q_stride, const void* k_pool, co
   float* const pm = ws + images * 32 * head_dim;
   const ChunkArgs a{q, k_rows, v_rows, (const uint8_t*)k_pool, (const uint8_t*)v_pool, k_scale, v_scale, node_off, block_table,
                     prefix_len, q_stride, row_stride, max_blocks, B, T, n_kv_heads, group, n_blocks, max_prefix, parts,
-                    scale * LOG2E, ws, pm, pm + images * 32, out, status};
-  return head_dim == 128 ? chunk_run<128>(a, st) : chunk_run<64>(a, st);
+                    scale * LOG2E, ws, pm, pm + images * 32, (int32_t*)(pm + images * 64), out, status};
+  if (B > 64) return head_dim == 128 ? chunk_run<128, true>(a, st) : chunk_run<64, true>(a, st);
+  return head_dim == 128 ? chunk_run<128, false>(a, st) : chunk_run<64, false>(a, st);
 }
 
 }  // namespace trj
