@@ -38,6 +38,10 @@ struct ChunkSeq {
   int r0, n, L, tiles;  // n < 0: refused, with nothing written; L < 0: refused, rows of zeros
   __device__ inline int cached() const { return (L + CH_KEYS - 1) / CH_KEYS; }
   __device__ inline int blocks() const { return n <= 0 ? 0 : L < 0 ? 1 : cached() + (n + CH_KEYS - 1) / CH_KEYS; }
+  // blocks of all tiles, about: own rows are seen up to a tile's
+  __device__ inline float work() const {
+    return n <= 0 || L < 0 ? (float)tiles : (float)tiles * ((float)cached() + 0.5f * (float)((n + CH_KEYS - 1) / CH_KEYS + 1));
+  }
 };
 __device__ inline ChunkSeq chunk_seq(const ChunkArgs& a, int s) {
   ChunkSeq q{0, 0, 0, 0};
@@ -59,10 +63,11 @@ struct ChunkMerge {
 };
 // The plan, the same on every wavefront of every workgroup: a split has `span` blocks at most, of one sequence evenly
 // many.  Up to 64 sequences (not MANY) 32 spans are weighed, one per lane, the longest sequence in 1 .. 32 splits:
-//   cost = rounds of workgroups * (START + blocks of one) + MERGE if anything is split
-// in times that a compute unit takes for a block of 256 queries (2.3 us); sequences come longest first, so that what starts
-// last is short.  Beyond 64 sequences neither is done: index order, and spans of an even share.
-constexpr float START = 4.5f, MERGE = 2.5f, RESIDENT = 256.f;  // one workgroup per compute unit at a time
+//   cost = rounds of workgroups * (START + blocks of one) + MERGE and PART for each of the parts if anything is split
+// in times that a compute unit takes for a block of 256 queries (2.3 us).  Sequences come longest first, so that what starts
+// last is short and rounds fill up: the middle between whole rounds of average items and no idle unit is taken.  Beyond 64 sequences
+// neither is done: index order, and spans of an even share.
+constexpr float START = 4.5f, MERGE = 2.5f, PART = 0.03f, RESIDENT = 256.f;  // one workgroup per compute unit at a time
 template <bool MANY>
 struct ChunkPlan {
   const ChunkArgs& a;
@@ -74,7 +79,7 @@ struct ChunkPlan {
     for (int s0 = 0; s0 < (MANY ? a.B : 1); s0 += 64) {
       mine = chunk_seq(a, s0 + lane);
       if (!MANY && a.B == 1) break;
-      work += wave_sum((float)mine.tiles * (float)mine.blocks());
+      work += wave_sum(mine.work());
     }
     work *= a.n_kv_heads;
     id = lane;
@@ -102,7 +107,7 @@ struct ChunkPlan {
     const int c = (longest + (lane & 31)) / ((lane & 31) + 1);
     const float each = __builtin_amdgcn_rcpf((float)c);
     float n = 0.f, parts = 0.f;
-    if (a.B == 1) work = (float)lane_value(groups, 0) * (float)longest;
+    if (a.B == 1) work = wave_sum(mine.work()) * a.n_kv_heads;  // (lanes behind the first have none)
     for (int t = 0; t < a.B; ++t) {
       const int b = lane_value(blocks, t), g = lane_value(groups, t);
       const float k = floorf(((float)(b + c) - 0.5f) * each);  // ceil(b / c)
@@ -111,7 +116,7 @@ struct ChunkPlan {
     }
     const float rounds = ceilf(n * (1.f / RESIDENT));
     const float whole = START + (float)c, even = START + work * __builtin_amdgcn_rcpf(n);
-    float cost = (rounds > 1.f ? fmaxf(whole, rounds * even) : whole) + (parts > 0.f ? MERGE : 0.f);
+    float cost = (rounds > 1.f ? fmaxf(whole, 0.5f * even * (rounds + n * (1.f / RESIDENT))) : whole) + (parts > 0.f ? MERGE + PART * parts : 0.f);
     if (parts > (float)a.max_parts) cost = INFINITY;  // no room for its partials
     const uint32_t best = wave_min((uint32_t)fminf(cost * 8.f, 60e6f) << 6 | lane);  // (of equals the fewest splits)
     span = lane_value(c, best & 63);
@@ -591,12 +596,14 @@ __global__ __launch_bounds__(CH_THREADS, 2) void chunk_attn_q8_kernel(ChunkArgs 
         a.pm[image * 32 + n32] = m;
         a.pl[image * 32 + n32] = any_odd ? -l : l;  // (a sum of weights is not negative)
       }
+      if (qw + n32 < nq) {
 #pragma unroll
-      for (int mt = 0; mt < MT; ++mt)
+        for (int mt = 0; mt < MT; ++mt)
 #pragma unroll
-        for (int g = 0; g < 4; ++g)
-          *reinterpret_cast<f32x4*>(a.po + image * OW + (mt * 4 + g) * 256 + lane * 4) =
-              f32x4{o[mt][4 * g], o[mt][4 * g + 1], o[mt][4 * g + 2], o[mt][4 * g + 3]};
+          for (int g = 0; g < 4; ++g)
+            *reinterpret_cast<f32x4*>(a.po + image * OW + (mt * 4 + g) * 256 + lane * 4) =
+                f32x4{o[mt][4 * g], o[mt][4 * g + 1], o[mt][4 * g + 2], o[mt][4 * g + 3]};
+      }
     }
   }
   if (judge) {
@@ -615,60 +622,64 @@ __global__ __launch_bounds__(128 * (DH / 32)) void chunk_merge_kernel(ChunkArgs 
   __shared__ float sm_m[32], sm_l[32];
   __shared__ f32x4 sm_o[4][64 * MT];
   const int tid = threadIdx.x, lane = tid & 63, n32 = lane & 31, hh = lane >> 5, mt = (tid >> 6) % MT, h = tid / (64 * MT);
-  const int x = blockIdx.x / CH_WAVES, wave = blockIdx.x % CH_WAVES;
-  if (x >= a.merges[0]) return;
-  const ChunkMerge w = reinterpret_cast<const ChunkMerge*>(a.merges + 8)[x];
-  const int nq = w.n * a.group, q0 = w.tile * CH_QUERIES, qw = q0 + wave * 32, qi = qw + n32;
-  if (qw >= nq || w.splits == 0) return;
-  float m = NO_REFERENCE, l = 0.f;
-  bool odd = false;
-  f32x4 o[4] = {};
-  for (int s0 = h; s0 < w.splits; s0 += H * BATCH) {
-    float pm[BATCH], pl[BATCH];
-    f32x4 po[BATCH][4];
+  const int all = a.merges[0] * CH_WAVES;
+  for (int u = blockIdx.x; u < all; u += gridDim.x) {
+    const int x = u / CH_WAVES, wave = u % CH_WAVES;
+    const ChunkMerge w = reinterpret_cast<const ChunkMerge*>(a.merges + 8)[x];
+    const int nq = w.n * a.group, q0 = w.tile * CH_QUERIES, qw = q0 + wave * 32, qi = qw + n32;
+    if (qw >= nq || w.splits == 0) continue;
+    float m = NO_REFERENCE, l = 0.f;
+    bool odd = false;
+    f32x4 o[4] = {};
+    for (int s0 = h; s0 < w.splits; s0 += H * BATCH) {
+      float pm[BATCH], pl[BATCH];
+      f32x4 po[BATCH][4];
 #pragma unroll
-    for (int k = 0; k < BATCH; ++k) {
-      const size_t image = (size_t)(w.part + min(s0 + H * k, w.splits - 1) * w.step) * CH_WAVES + wave;
-      pm[k] = a.pm[image * 32 + n32];
-      pl[k] = a.pl[image * 32 + n32];
+      for (int k = 0; k < BATCH; ++k) {
+        const size_t image = (size_t)(w.part + min(s0 + H * k, w.splits - 1) * w.step) * CH_WAVES + wave;
+        pm[k] = a.pm[image * 32 + n32];
+        pl[k] = a.pl[image * 32 + n32];
 #pragma unroll
-      for (int g = 0; g < 4; ++g) po[k][g] = *reinterpret_cast<const f32x4*>(a.po + image * OW + (mt * 4 + g) * 256 + lane * 4);
+        for (int g = 0; g < 4; ++g)
+          po[k][g] = qi < nq ? *reinterpret_cast<const f32x4*>(a.po + image * OW + (mt * 4 + g) * 256 + lane * 4) : f32x4{0, 0, 0, 0};
+      }
+      float top = m;
+#pragma unroll
+      for (int k = 0; k < BATCH; ++k) top = fmaxf(top, pm[k]);
+      const float keep = __builtin_amdgcn_exp2f(m - top);
+      m = top;
+      l *= keep;
+#pragma unroll
+      for (int g = 0; g < 4; ++g) o[g] *= keep;
+#pragma unroll
+      for (int k = 0; k < BATCH; ++k) {
+        if (s0 + H * k >= w.splits) break;
+        const float f = __builtin_amdgcn_exp2f(pm[k] - m);
+        odd = odd || (__float_as_uint(pl[k]) >> 31) != 0;
+        l += f * fabsf(pl[k]);
+#pragma unroll
+        for (int g = 0; g < 4; ++g) o[g] += po[k][g] * f;
+      }
     }
-    float top = m;
+    if (h > 0) {
 #pragma unroll
-    for (int k = 0; k < BATCH; ++k) top = fmaxf(top, pm[k]);
-    const float keep = __builtin_amdgcn_exp2f(m - top);
-    m = top;
-    l *= keep;
-#pragma unroll
-    for (int g = 0; g < 4; ++g) o[g] *= keep;
-#pragma unroll
-    for (int k = 0; k < BATCH; ++k) {
-      if (s0 + H * k >= w.splits) break;
-      const float f = __builtin_amdgcn_exp2f(pm[k] - m);
-      odd = odd || (__float_as_uint(pl[k]) >> 31) != 0;
-      l += f * fabsf(pl[k]);
-#pragma unroll
-      for (int g = 0; g < 4; ++g) o[g] += po[k][g] * f;
+      for (int g = 0; g < 4; ++g) sm_o[g][mt * 64 + lane] = o[g];
+      if (mt == 0 && hh == 0) sm_m[n32] = m, sm_l[n32] = l;
     }
-  }
-  if (h > 0) {
+    const bool any_odd = __syncthreads_or(odd);
+    if (h == 0 && qi < nq) {
+      const float top = fmaxf(m, sm_m[n32]), keep = __builtin_amdgcn_exp2f(m - top), f = __builtin_amdgcn_exp2f(sm_m[n32] - top);
+      const float inv = 1.0f / (l * keep + sm_l[n32] * f);
+      uint16_t* dst = a.out + ((size_t)(w.r0 + qi / a.group) * a.n_kv_heads * a.group + w.head * a.group + qi % a.group) * DH + 32 * mt + 4 * hh;
 #pragma unroll
-    for (int g = 0; g < 4; ++g) sm_o[g][mt * 64 + lane] = o[g];
-    if (mt == 0 && hh == 0) sm_m[n32] = m, sm_l[n32] = l;
-  }
-  const bool any_odd = __syncthreads_or(odd);
-  if (h == 0 && qi < nq) {
-    const float top = fmaxf(m, sm_m[n32]), keep = __builtin_amdgcn_exp2f(m - top), f = __builtin_amdgcn_exp2f(sm_m[n32] - top);
-    const float inv = 1.0f / (l * keep + sm_l[n32] * f);
-    uint16_t* dst = a.out + ((size_t)(w.r0 + qi / a.group) * a.n_kv_heads * a.group + w.head * a.group + qi % a.group) * DH + 32 * mt + 4 * hh;
-#pragma unroll
-    for (int g = 0; g < 4; ++g) {
-      const f32x4 r = (o[g] * keep + sm_o[g][mt * 64 + lane] * f) * inv;
-      *reinterpret_cast<u32x2*>(dst + 8 * g) = u32x2{pack2bf(r[0], r[1]), pack2bf(r[2], r[3])};
+      for (int g = 0; g < 4; ++g) {
+        const f32x4 r = (o[g] * keep + sm_o[g][mt * 64 + lane] * f) * inv;
+        *reinterpret_cast<u32x2*>(dst + 8 * g) = u32x2{pack2bf(r[0], r[1]), pack2bf(r[2], r[3])};
+      }
     }
+    if (any_odd) chunk_add_odd_values(a, ChunkSeq{w.r0, w.n, 0, 0}, w.head, DH, qw, min(nq, qw + 32), first_partly_seen(q0 / a.group));
+    __syncthreads();  // LDS is free again
   }
-  if (any_odd) chunk_add_odd_values(a, ChunkSeq{w.r0, w.n, 0, 0}, w.head, DH, qw, min(nq, qw + 32), first_partly_seen(q0 / a.group));
 }
 
 // ------------------------------------------------------------------ launch
@@ -691,7 +702,7 @@ static int chunk_run(const ChunkArgs& a, hipStream_t st) {
   chunk_attn_q8_kernel<DH, MANY><<<grid, CH_THREADS, lds, st>>>(a);
   int rc = check_launch();
   if (rc != TRJ_OK || a.max_parts == 0) return rc;
-  chunk_merge_kernel<DH><<<CH_WAVES * (int)std::min(items, (long)CH_MAX_MERGES), 128 * (DH / 32), 0, st>>>(a);
+  chunk_merge_kernel<DH><<<CH_WAVES * (int)std::min(items, 64l), 128 * (DH / 32), 0, st>>>(a);
   return check_launch();
 }
 
