@@ -493,8 +493,8 @@ __global__ __launch_bounds__(CH_THREADS, 2) void chunk_attn_q8_kernel(ChunkArgs 
 #pragma unroll
         for (int v = 0; v < 16; ++v) p[v] = fmaf(s[v], f, -m);
         const uint8_t *const k_from = next_keys(t), *const v_from = last_values(t);
-        // in this order: operands asked for AHEAD products before they are needed, exponentials beside the products
-        constexpr int AHEAD = 3, EXPS = 16 / STEPS;
+        // in this order: operands asked for a product before they are needed (2 to 4 took 1 to 4 % longer), exponentials beside the products
+        constexpr int AHEAD = 1, EXPS = 16 / STEPS;
         bf16x8 kop[STEPS], vop[STEPS];
         auto ask = [&](int j) {
           kop[j] = *reinterpret_cast<const bf16x8*>(k_from + j * Lds::K_STEP);
