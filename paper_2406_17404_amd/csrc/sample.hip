@@ -794,30 +794,32 @@ __global__ __launch_bounds__(SMP_THREADS) void sample_chunk_kernel(SampleArgs a,
   if (blockIdx.x == 0 && ch.row0 == 0) empty_sequences(a);
   Held<NV> row;
   row.load(a.x + (size_t)t * a.V + first, min(ch.size, a.V - first));
+  const size_t at = ch.at(t, c);
   bool first_row = false;
   const int s = sample_sequence(a, t, first_row);
-  if (s < 0) return;
-  const SampleRules r(a.rules + 4 * s);
-  if (first_row && c == 0 && tid == 0) a.status[s] = r.bad;
-  if (r.bad) return;
+  const SampleRules r(a.rules + 4 * max(s, 0));
+  if (s >= 0 && first_row && c == 0 && tid == 0) a.status[s] = r.bad;
+  if (s < 0 || r.bad) {
+    if (tid == 0) ch.n[at] = 0;  // nothing to weigh
+    return;
+  }
   const float mine = row.top(), top = block_max(mine, l.part);
-  const size_t at = ch.at(t, c);
   int n = -1;
-  if (!is_token(top)) {
+  if (!is_token(top) || r.t == 0.f) {
     n = 0;
-  } else if (r.short_by_k() && r.t > 0.f) {
+  } else if (r.short_by_k()) {
     const float bound = reached_by((int)r.top_k, mine, SampleScale(top, r.t), l);
     n = collect(row, fmaxf(bound, -3.4028235e38f), first, ch.data + at * SMP_BINS, SMP_CHUNK_LIST, l);
     if (n > SMP_CHUNK_LIST) n = -1;
   }
   if (tid == 0) ch.top[at] = top, ch.n[at] = n;
 }
-// largest logit of a row, and whether its chunks list all that top-k could keep
+// largest logit of a row, and whether its chunks list all that top-k could keep (or have no need to)
 struct ChunkedTop {
   float top;
   bool listed;
 };
-__device__ inline ChunkedTop chunked_top(const ChunkedRows& ch, int t, const SampleRules& r) {
+__device__ inline ChunkedTop chunked_top(const ChunkedRows& ch, int t) {
   float top = -INFINITY;
   bool listed = true;
   for (int c = threadIdx.x & 63; c < ch.chunks; c += 64) {
@@ -827,18 +829,15 @@ __device__ inline ChunkedTop chunked_top(const ChunkedRows& ch, int t, const Sam
   }
 #pragma unroll
   for (int d = 32; d > 0; d >>= 1) top = fmaxf(top, __shfl_xor(top, d));
-  return ChunkedTop{top, r.short_by_k() && __ballot(!listed) == 0};
+  return ChunkedTop{top, __ballot(!listed) == 0};
 }
 __global__ __launch_bounds__(SMP_THREADS) void sample_weigh_kernel(SampleArgs a, ChunkedRows ch) {
   __shared__ WeighLds l;
   const int tid = threadIdx.x, t = ch.row0 + blockIdx.x / ch.chunks, c = blockIdx.x % ch.chunks, first = c * ch.size;
+  const ChunkedTop x = chunked_top(ch, t);
+  if (x.listed) return;
   bool first_row = false;
-  const int s = sample_sequence(a, t, first_row);
-  if (s < 0) return;
-  const SampleRules r(a.rules + 4 * s);
-  if (r.bad || r.t == 0.f) return;
-  const ChunkedTop x = chunked_top(ch, t, r);
-  if (x.listed || !is_token(x.top)) return;
+  const SampleRules r(a.rules + 4 * sample_sequence(a, t, first_row));
   const SampleScale sc(x.top, r.t);
   uint64_t over = weigh_part(Pieces<2>{a.x + (size_t)t * a.V, first, min(first + ch.size, a.V)}, sc, r.least, l);
   if (r.least > 0) over = block_all64(over, l.part, Plus());
@@ -855,7 +854,7 @@ __global__ __launch_bounds__(SMP_THREADS) void sample_finish_kernel(SampleArgs a
   const SampleRules r(a.rules + 4 * s);
   const float u = a.uniform[t];
   if (r.bad) return;
-  const ChunkedTop x = chunked_top(ch, t, r);
+  const ChunkedTop x = chunked_top(ch, t);
   const float* const row = a.x + (size_t)t * a.V;
   if (!is_token(x.top) || r.t == 0.f) {
     uint64_t best = 0;
