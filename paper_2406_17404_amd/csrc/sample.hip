@@ -665,13 +665,14 @@ __device__ inline uint64_t weigh_part(const Pieces<2>& part, const SampleScale& 
   return over;
 }
 // A logit that at least k tokens of the workgroup reach, and few more: the lower end of the bin, of as many as threads over
-// the range that weighs anything, in which the k-th of the threads' largest ones lies.  -infinity where fewer threads hold tokens.
+// the range that weighs anything, in which the k-th of the threads' largest ones lies.  Where fewer threads hold tokens that
+// weigh anything, one that all of those reach: behind them top-k has nothing to choose.
 __device__ inline float reached_by(int k, float mine, const SampleScale& sc, ListLds& l) {
   constexpr float WIDE = (float)SMP_BINS / SMP_THREADS;
   const int tid = threadIdx.x;
   __syncthreads();
   l.count[tid] = 0;
-  if (tid == 0) l.bound_bin = -1;
+  if (tid == 0) l.bound_bin = SMP_THREADS - 1;
   __syncthreads();
   const int b = sc.bin(sc.seen(mine));
   if (b < SMP_BINS - 1) atomicAdd(&l.count[b / (SMP_BINS / SMP_THREADS)], 1u);
@@ -684,10 +685,9 @@ __device__ inline float reached_by(int k, float mine, const SampleScale& sc, Lis
   for (int w = 0; w < SMP_WAVES - 1; ++w) upto += w < (tid >> 6) ? (int)l.part.least[w] : 0;
   if (upto >= k && upto - c < k) l.bound_bin = tid;
   __syncthreads();
-  if (l.bound_bin < 0) return -INFINITY;
   // (a token's bin is off by less than 2^-20 of its place)
   const float below = 2.f * ((float)(l.bound_bin + 1) * WIDE) / sc.per_bin * 1.00001f;
-  return sc.infinite ? INFINITY : 2.f * sc.half_top - below - fabsf(sc.half_top) * 1e-6f;
+  return sc.infinite ? INFINITY : fmaxf(2.f * sc.half_top - below - fabsf(sc.half_top) * 1e-6f, -3.4028235e38f);
 }
 // Tokens from `bound` on to out[0 .. cap), in any order; their number
 template <int NV>
@@ -809,7 +809,7 @@ __global__ __launch_bounds__(SMP_THREADS) void sample_chunk_kernel(SampleArgs a,
     n = 0;
   } else if (r.short_by_k()) {
     const float bound = reached_by((int)r.top_k, mine, SampleScale(top, r.t), l);
-    n = collect(row, fmaxf(bound, -3.4028235e38f), first, ch.data + at * SMP_BINS, SMP_CHUNK_LIST, l);
+    n = collect(row, bound, first, ch.data + at * SMP_BINS, SMP_CHUNK_LIST, l);
     if (n > SMP_CHUNK_LIST) n = -1;
   }
   if (tid == 0) ch.top[at] = top, ch.n[at] = n;
@@ -930,8 +930,10 @@ struct SampleLaunch {
 static SampleLaunch sample_launch(int T, int V) {
   SampleLaunch p{0, 0, T};
   if (V <= SMP_ROW) return p;
-  const int least = (V + SMP_CHUNK - 1) / SMP_CHUNK, most = (V + 8 * SMP_THREADS - 1) / (8 * SMP_THREADS);
-  p.chunks = std::min(std::max(least, 512 / T), most);  // two workgroups per compute unit at a time
+  const int least = (V + SMP_CHUNK - 1) / SMP_CHUNK, most = (V + 16 * SMP_THREADS - 1) / (16 * SMP_THREADS);
+  // Two workgroups per compute unit at a time, but no fewer than 16 logits per thread: of one row of 128256, top-k 200, chunks of
+  // 8 per thread took 46 us, of 16 34 (their lists are put together by one workgroup); of 69 rows no difference.
+  p.chunks = std::min(std::max(least, 512 / T), most);
   p.size = ((V + p.chunks - 1) / p.chunks + 3) / 4 * 4;
   p.chunks = (V + p.size - 1) / p.size;
   p.rows = std::max(1, std::min(T, 4096 / p.chunks));
@@ -963,9 +965,7 @@ int launch_tree_sample(const float* x, const int32_t* node_off, int B, int T, in
   for (int row0 = 0; row0 < T; row0 += p.rows) {
     const ChunkedRows ch{row0, std::min(p.rows, T - row0), p.chunks, p.size, (float*)(data + all * (SMP_BINS + 1)),
                          (int32_t*)(data + all * (SMP_BINS + 1)) + all, data + all * SMP_BINS, data};
-    const int rc = p.size <= 8 * SMP_THREADS    ? sample_chunked<2>(a, ch, st)
-                   : p.size <= 32 * SMP_THREADS ? sample_chunked<8>(a, ch, st)
-                                                : sample_chunked<16>(a, ch, st);
+    const int rc = p.size <= 32 * SMP_THREADS ? sample_chunked<8>(a, ch, st) : sample_chunked<16>(a, ch, st);
     if (rc != TRJ_OK) return rc;
   }
   return TRJ_OK;

@@ -187,3 +187,77 @@ def test_two_streams_with_workspaces_of_their_own():
                 b.tree_sample(*a)
     torch.cuda.synchronize()
     assert all(np.array_equal(a[4].cpu().numpy(), w) for a, w in zip(args, want))
+
+
+@pytest.mark.parametrize("V", [2, 700, 32000, 32768, 32769, 100003])
+@pytest.mark.parametrize("t", [0.02, 1e-5])
+def test_fewer_tokens_that_weigh_anything_than_top_k_allows(V, t):
+    rng = np.random.default_rng(V)
+    rules = [(t, k, p, m) for k in (2, 50, 256) for p, m in ((1, 0), (0.6, 0), (1, 0.2), (0.9, 0.01))]
+    x = rng.normal(size=(len(rules), V))
+    x[::2] = np.round(x[::2] * 2)  # alike where few logits weigh anything
+    Call(x, [1] * len(rules), rules, rng.random(len(rules))).check()
+
+
+@pytest.mark.parametrize("V", [32768, 32769, 70001])
+def test_long_rows_without_tokens_and_infinities(V):
+    x = np.full((9, V), -INF)
+    x[1] = NAN
+    x[2, V - 1] = -5.0
+    x[3, [4, V - 2, V - 1]] = INF
+    x[3, 9] = 3e38
+    x[4] = np.where(np.arange(V) % 2, NAN, 1.0)
+    x[5] = np.where(np.arange(V) % 2, 3e38, -3e38)
+    x[6] = np.arange(V) * 1e-45
+    x[7, V // 2:] = np.linspace(-4, 4, V - V // 2)  # a half that a mask leaves nothing of
+    x[8, V // 3::4] = 2.0
+    for rules in RULES + [(1, 256, 1, 0), (1, 257, 1, 0), (1, 512, 0.9, 0), (1, V - 1, 1, 0), (1, V, 1, 0)]:
+        Call(x, [9], [rules], np.linspace(0, 0.999, 9)).check()
+
+
+def test_more_long_rows_than_a_workspace_holds_at_once():
+    # 2 chunks per row: rows beyond the 2048th go through the same room
+    rng = np.random.default_rng(8)
+    V, sizes = 33000, [1500, 0, 700, 1, 50]
+    rules = [(0.9, 40, 0.9, 0), (1, 0, 1, 0), (1, 0, 0.8, 0), (0, 0, 1, 0), (-1, 0, 1, 0)]
+    T = sum(sizes) + 2
+    x = torch.empty(T, V, device=DEV).normal_(generator=torch.Generator(DEV).manual_seed(8)).mul_(3)
+    u = rng.random(T).astype(np.float32)
+    off = offsets_of(sizes)
+    token, prob, status = ints(T), torch.full((T,), 9.0, device=DEV), ints(5)
+    ws = torch.full((b.tree_sample_workspace_bytes(5, T, V),), 255, dtype=torch.uint8, device=DEV)
+    b.tree_sample(x, i32(off), to_dev(np.array(rules, np.float32)), to_dev(u), token, prob, ws, status)
+    torch.cuda.synchronize()
+    token, prob = token.cpu().numpy(), prob.double().cpu().numpy()
+    assert list(status.cpu().numpy()) == [0, 0, 0, 0, 1]
+    for s, n in enumerate(sizes[:4]):
+        for t in range(off[s], off[s] + n, 97 if n > 100 else 1):
+            want, p = P.sample(x[t].cpu().numpy(), rules[s], u[t])
+            assert token[t] == want and abs(prob[t] - p) <= 2.0 ** -24 * p + V * 2.0 ** -38, (s, t)
+    assert (token[:off[4]] >= 0).all() and (token[off[4]:] == -7).all() and (prob[off[4]:] == 9.0).all()
+
+
+def test_logits_beyond_32_bits_of_offsets():
+    T, V = 140, 16777213  # 140 rows: the last ones start behind 2^31 logits
+    x = torch.full((T, V), -40.0, device=DEV)
+    rng = np.random.default_rng(9)
+    want = rng.integers(0, V, T)
+    x[torch.arange(T, device=DEV), torch.from_numpy(want).to(DEV)] = 1.0
+    ws = torch.empty(b.tree_sample_workspace_bytes(2, T, V), dtype=torch.uint8, device=DEV)
+    token, prob, status = ints(T), torch.full((T,), 9.0, device=DEV), ints(2)
+    rules = to_dev(np.array([(1, 40, 1, 0), (0.5, 0, 0.9, 0)], np.float32))
+    b.tree_sample(x, i32([0, 70, T]), rules, to_dev(rng.random(T).astype(np.float32)), token, prob, ws, status)
+    torch.cuda.synchronize()
+    assert list(status.cpu().numpy()) == [0, 0]
+    assert np.array_equal(token.cpu().numpy(), want) and (prob == 1.0).all()
+
+
+def test_probabilities_of_one_row_do_not_depend_on_its_neighbours():
+    # chunks of other sizes, another launch shape: the same tokens, the same bits
+    rng = np.random.default_rng(10)
+    x, u = (rng.normal(size=(300, 40001)) * 2).astype(np.float32), rng.random(300).astype(np.float32)
+    rules = [(0.9, 0, 0.95, 0)]
+    token, prob = Call(x, [300], rules, u).run()
+    for t in (0, 17, 299):
+        one, p = Call(x[t:t + 1], [1], rules, u[t:t + 1]).run()
+        assert one[0] == token[t] and p[0] == prob[t]
