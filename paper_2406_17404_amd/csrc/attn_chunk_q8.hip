@@ -79,11 +79,11 @@ struct ChunkPlan {
     for (int s0 = 0; s0 < (MANY ? a.B : 1); s0 += 64) {
       mine = chunk_seq(a, s0 + lane);
       if (!MANY && a.B == 1) break;
-      work += wave_sum(mine.work());
+      work += wave_sum(MANY ? (float)mine.tiles * (float)mine.blocks() : mine.work());
     }
     work *= a.n_kv_heads;
     id = lane;
-    if (MANY) {  // (a split sequence has at most twice its share of parts)
+    if (MANY) {  // (a sequence that is split has fewer than twice blocks / span splits: CH_MAX_PARTS in all at most)
       span = a.max_parts == 0 ? 1 << 30 : (int)fminf(fmaxf(ceilf(work * (1.0001f * 2 / CH_MAX_PARTS)), (float)CH_LEAST), 1e9f);
       return;
     }
@@ -150,6 +150,7 @@ struct ChunkPlan {
         w.splits = lane_value(k, l);
         const int gl = lane_value(g, l);
         w.nth = x - (lane_value(upto, l) - gl * w.splits);
+        if ((unsigned)w.nth >= (unsigned)(gl * w.splits)) return false;  // (sums beyond 2^31: ranges that overlap)
         w.part0 = lane_value(pupto, l) - (w.splits > 1 ? gl * w.splits : 0);
         w.merge0 = lane_value(mupto, l) - (w.splits > 1 ? gl : 0);
         return true;
@@ -608,7 +609,7 @@ __global__ __launch_bounds__(CH_THREADS, 2) void chunk_attn_q8_kernel(ChunkArgs 
   }
   if (judge) {
     bool bad = false;
-    for (int j = tid; j * 32 < seq.L; j += CH_THREADS) bad = bad || (unsigned)table[j] >= (unsigned)a.n_blocks;
+    for (int j = tid, pages = (seq.L + 31) >> 5; j < pages; j += CH_THREADS) bad = bad || (unsigned)table[j] >= (unsigned)a.n_blocks;
     bad = __syncthreads_or(bad);
     if (tid == 0) a.status[w.s] = bad;
   }

@@ -256,3 +256,117 @@ def test_two_streams_with_workspaces_of_their_own():
     torch.cuda.synchronize()
     for c, a in zip(calls, args):
         c.check(a[-2].float().cpu().numpy())
+
+
+@pytest.mark.parametrize("B,n,heads", [(65, 320, 4), (65, 1280, 1), (80, 300, 4), (70, 260, 5)])
+def test_many_prompts_at_once(B, n, heads):
+    # beyond 64 sequences, all of a length at which they are just split: every split has room for its partials
+    c = Call(np.random.default_rng(B + n), [0] * B, [n] * B, heads, 1, 64)
+    c.check()
+    assert not c.status.any()
+
+
+@pytest.mark.parametrize("seed", range(4))
+def test_many_sequences_of_any_lengths(seed):
+    rng = np.random.default_rng(900 + seed)
+    B, kv_heads, group = int(rng.integers(65, 200)), int(rng.integers(1, 3)), int(rng.integers(1, 6))
+    lens = rng.integers(0, 25, B) ** 2 * int(rng.integers(0, 2))
+    sizes = [int(x) for x in rng.integers(0, int(rng.choice([3, 60, 200])), B)]
+    sizes[B // 2] = 70
+    c = Call(rng, [int(x) for x in lens], sizes, kv_heads * group, kv_heads, 64, behind=2)
+    c.check()
+    assert not c.status.any()
+
+
+def test_an_unaligned_workspace():
+    c = Call(np.random.default_rng(15), [5000, 64], [3, 100], 4, 2, 64)
+    want, args = c.run(), c.device()
+    args[12] = torch.full((args[12].numel() + 13,), 255, dtype=torch.uint8, device=DEV)[13:]
+    b.chunk_attention_q8(*args)
+    torch.cuda.synchronize()
+    assert np.array_equal(args[13].float().cpu().numpy(), want)
+
+
+def pieces(c):
+    d = c.device()
+    return d[0], d[1:5], d[5:7], d[7:]
+
+
+def test_fractions_of_scales_do_not_count():
+    rng = np.random.default_rng(16)
+    c = Call(rng, [300, 45], [20, 7], 4, 2, 128)
+    want = c.run()
+    for w in "kv":
+        c.cache.scale[w] = (c.cache.scale[w] * rng.uniform(1, 1.999, c.cache.scale[w].shape)).astype(np.float32)
+    assert np.array_equal(c.run(), want)
+
+
+@pytest.mark.parametrize("dh,n_blocks", [(128, 800_000), (64, 1_500_000)])
+def test_pools_beyond_4_gib(dh, n_blocks):
+    c = Call(np.random.default_rng(dh), [700, 45], [20, 70], 4, 2, dh)
+    want = c.run()
+    q, pools, rows, rest = pieces(c)
+    shift = n_blocks - c.cache.n_blocks  # the same pages at the end of pools of 6.5 and 6.1 GB
+    big = [torch.empty((2, n_blocks) + t.shape[2:], dtype=t.dtype, device=DEV) for t in pools]
+    for x, y in zip(big, pools):
+        x[:, shift:] = y
+    assert big[0].numel() > 2 ** 32
+    rest[1] = torch.where(rest[1] >= 0, rest[1] + shift, rest[1])
+    b.chunk_attention_q8(q, *big, *rows, *rest)
+    torch.cuda.synchronize()
+    assert np.array_equal(rest[-2].float().cpu().numpy(), want) and not rest[-1].any()
+
+
+def test_rows_beyond_2_to_the_32_elements():
+    c = Call(np.random.default_rng(17), [50, 33, 100], [128, 100, 72], 4, 2, 64)
+    c.vr[299, 1, 3] = float("inf")
+    want = c.run()
+    q, pools, rows, rest = pieces(c)
+    wide = torch.empty(300, 1 << 24, dtype=torch.bfloat16, device=DEV)  # the longest stride, 10 GB
+    far, at = [], (1 << 24) - 1024
+    for x in (q, *rows):
+        n = x.shape[1] * 64
+        wide[:, at:at + n] = x.reshape(300, n)
+        far.append(wide[:, at:at + n].unflatten(1, (x.shape[1], 64)))
+        at += n
+    b.chunk_attention_q8(far[0], *pools, *far[1:], *rest)
+    torch.cuda.synchronize()
+    assert np.array_equal(rest[-2].float().cpu().numpy(), want) and np.isinf(want[299, 2:, 3]).all()
+
+
+@pytest.mark.parametrize("n", [1, 70])
+def test_the_longest_prefix(n):
+    # as long as positions go: few pages, named over and over
+    rng = np.random.default_rng(18)
+    L, n_blocks, dh = 2 ** 31 - 65 - n, 3, 64
+    pages = (L + 31) // 32
+    pool = {w: S.encode((rng.normal(size=(1, n_blocks, 32 * dh)) * 60).clip(-448, 448)) for w in "kv"}
+    scale = {w: np.full((1, n_blocks), 2.0 ** -6, np.float32) for w in "kv"}
+    q, kr, vr = (bf16(rng.normal(size=(n, 1, dh))) for _ in range(3))
+    table = (torch.arange(pages, device=DEV) % n_blocks).int()[None]
+    ws = torch.empty(b.chunk_attention_q8_workspace_bytes(1, n, 1, 1, dh, L), dtype=torch.uint8, device=DEV)
+    out, status = torch.full((n, 1, dh), 5.0, dtype=torch.bfloat16, device=DEV), ints(1)
+    b.chunk_attention_q8(q.to(DEV), *(torch.from_numpy(pool[w]).to(DEV) for w in "kv"),
+                         *(torch.from_numpy(scale[w]).to(DEV) for w in "kv"), kr.to(DEV), vr.to(DEV), i32([0, n]), table, i32([L]),
+                         L, dh ** -0.5, ws, out, status)
+    torch.cuda.synchronize()
+    assert status.tolist() == [0]
+    times = np.zeros((n_blocks, 32))
+    for p in range(n_blocks):
+        times[p] = len(range(p, pages, n_blocks))
+    if L % 32:
+        times[(pages - 1) % n_blocks, L % 32:] -= 1
+    keys, values = (S.page_values(pool[w][0], scale[w][0], w).reshape(-1, dh) for w in "kv")
+    # as for short ones, and 32-bit sums over a split's blocks, 2^25 / 32 of them at most: half a step of 2^-23 for each
+    # that the sum of weights adds, and for each product of 16 keys (four of a block) that the values' sums add
+    long_sum = 2.0 ** 20 * (2 * 2.0 ** -24 + 4 * 2.0 ** -23)
+    got = out.float().cpu().numpy()
+    for i in range(n):
+        f = q[i, 0].float().numpy().astype(np.float64)
+        k = np.concatenate([keys, kr[:i + 1, 0].float().numpy()])
+        v = np.concatenate([values, vr[:i + 1, 0].float().numpy()])
+        w = np.concatenate([times.ravel(), np.ones(i + 1)]) * np.exp(dh ** -0.5 * (k @ f))
+        w /= w.sum()
+        want, mean = w @ v, w @ np.abs(v)
+        tol = HALF * (np.abs(want) + mean) * (1 + HALF) + (long_sum + 2.0 ** -12) * mean
+        assert (np.abs(got[i, 0] - want) <= tol).all()
