@@ -24,7 +24,7 @@ struct ChunkArgs {
   const float *k_scale, *v_scale;
   const int32_t *node_off, *block_table, *prefix_len;
   int q_stride, row_stride, max_blocks, B, T, n_kv_heads, group, n_blocks, max_prefix;
-  int max_parts;
+  int max_parts, n_few;  // n_few rows of a sequence are 32 queries at most
   float scale_log2e;
   float *po, *pm, *pl;  // un-normalised partials: [part][wavefront] images of the accumulators, maxima and sums of 32 queries
   int32_t* merges;      // how many tiles there are to merge, then from word 8 on 8 words for each (ChunkMerge)
@@ -38,9 +38,12 @@ struct ChunkSeq {
   int r0, n, L, tiles;  // n < 0: refused, with nothing written; L < 0: refused, rows of zeros
   __device__ inline int cached() const { return (L + CH_KEYS - 1) / CH_KEYS; }
   __device__ inline int blocks() const { return n <= 0 ? 0 : L < 0 ? 1 : cached() + (n + CH_KEYS - 1) / CH_KEYS; }
-  // blocks of all tiles, about: own rows are seen up to a tile's
-  __device__ inline float work() const {
-    return n <= 0 || L < 0 ? (float)tiles : (float)tiles * ((float)cached() + 0.5f * (float)((n + CH_KEYS - 1) / CH_KEYS + 1));
+  // few queries (n_few rows at most), whose wavefronts each take pages of their own: a block costs a quarter of what it else does
+  __device__ inline int units(int n_few) const { return n <= n_few && L >= 0 ? (blocks() + 3) >> 2 : blocks(); }
+  // units of all tiles, about: own rows are seen up to a tile's
+  __device__ inline float work(int n_few) const {
+    return n <= n_few || L < 0 ? (float)(tiles * units(n_few))
+                               : (float)tiles * ((float)cached() + 0.5f * (float)((n + CH_KEYS - 1) / CH_KEYS + 1));
   }
 };
 __device__ inline ChunkSeq chunk_seq(const ChunkArgs& a, int s) {
@@ -79,7 +82,7 @@ struct ChunkPlan {
     for (int s0 = 0; s0 < (MANY ? a.B : 1); s0 += 64) {
       mine = chunk_seq(a, s0 + lane);
       if (!MANY && a.B == 1) break;
-      work += wave_sum(MANY ? (float)mine.tiles * (float)mine.blocks() : mine.work());
+      work += wave_sum(MANY ? (float)mine.tiles * (float)mine.units(a.n_few) : mine.work(a.n_few));
     }
     work *= a.n_kv_heads;
     id = lane;
@@ -88,7 +91,7 @@ struct ChunkPlan {
       return;
     }
     if (a.B > 1) {  // longest first
-      const int blocks = mine.blocks();
+      const int blocks = mine.units(a.n_few);
       int rank = 0;
       for (int t0 = 0; t0 < a.B; t0 += 8)  // (lanes behind the last sequence have no blocks)
 #pragma unroll
@@ -101,13 +104,13 @@ struct ChunkPlan {
       mine = ChunkSeq{to(mine.r0), to(mine.n), to(mine.L), to(mine.tiles)};
       id = to(lane);
     }
-    const int blocks = mine.blocks(), longest = max(lane_value(blocks, 0), 1), groups = mine.tiles * a.n_kv_heads;
+    const int blocks = mine.units(a.n_few), longest = max(lane_value(blocks, 0), 1), groups = mine.tiles * a.n_kv_heads;
     span = longest;
     if (a.max_parts == 0 || longest == 1) return;
     const int c = (longest + (lane & 31)) / ((lane & 31) + 1);
     const float each = __builtin_amdgcn_rcpf((float)c);
     float n = 0.f, parts = 0.f;
-    if (a.B == 1) work = wave_sum(mine.work()) * a.n_kv_heads;  // (lanes behind the first have none)
+    if (a.B == 1) work = wave_sum(mine.work(a.n_few)) * a.n_kv_heads;  // (lanes behind the first have none)
     for (int t = 0; t < a.B; ++t) {
       const int b = lane_value(blocks, t), g = lane_value(groups, t);
       const float k = floorf(((float)(b + c) - 0.5f) * each);  // ceil(b / c)
@@ -126,7 +129,7 @@ struct ChunkPlan {
       if (wave_sum(k > 1 ? (float)groups * (float)k : 0.f) > (float)a.max_parts) span = longest;
     }
   }
-  __device__ inline int splits(const ChunkSeq& q) const { return (q.blocks() + span - 1) / span; }
+  __device__ inline int splits(const ChunkSeq& q) const { return (q.units(a.n_few) + span - 1) / span; }
   // item x of all, of which a (sequence, tile, K/V head) counts its splits
   __device__ inline bool find(int x, ChunkWork& w) {
     const int lane = threadIdx.x & 63;
@@ -220,6 +223,225 @@ struct ChunkLds {
   }
 };
 
+// A sequence of 32 queries at most: every wavefront has them all and pages of its own, each CH_WAVES-th of the range, whose codes
+// come to slots of its own in LDS and go from there to the matrix units; the last wavefront takes the sequence's own rows first.
+// The wavefronts' sums are joined at the end.  In the other form seven wavefronts would only bring blocks for one.
+template <int DH>
+struct FewLds {
+  static constexpr int P = DH / 32, SLOTS = 256 / DH, SLOT = 2 * P * 1024;  // P KiB of codes of a page, K or V
+  static constexpr int IMAGE = DH / 32 * 16 * 64;                           // accumulators of a wavefront
+  static constexpr int BYTES = std::max(CH_WAVES * SLOTS * SLOT, CH_WAVES * (IMAGE + 2 * 32) * 4);
+};
+template <int DH>
+__device__ __forceinline__ bool chunk_few(const ChunkArgs& a, const ChunkWork& w, int head, int sp, int part, uint8_t* smem) {
+  using Lds = FewLds<DH>;
+  constexpr int MT = DH / 32, STEPS = DH / 16, OW = Lds::IMAGE, P = Lds::P, SLOTS = Lds::SLOTS, SLOT = Lds::SLOT;
+  const int tid = threadIdx.x, lane = tid & 63, n32 = lane & 31, hh = lane >> 5;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const ChunkSeq& seq = w.seq;
+  const int nq = seq.n * a.group, qi = min(n32, nq - 1), my_row = qi / a.group;
+  const int pages = (seq.L + 31) >> 5, all = pages + 1;
+  const int p0 = (int)((int64_t)all * sp / w.splits), p1 = (int)((int64_t)all * (sp + 1) / w.splits), pend = min(p1, pages);
+  const int mine = __builtin_amdgcn_readfirstlane(p0 + wave < pend ? (pend - p0 - wave + CH_WAVES - 1) / CH_WAVES : 0);
+  const int32_t* const table = a.block_table + (size_t)w.s * a.max_blocks;
+  const size_t plane = (size_t)head * a.n_blocks;
+  const float f = a.scale_log2e;
+  int ids = 0;  // of this wavefront's pages i, one per lane i % 64, and their scales
+  float ksc = 1.f, vsc = 1.f;
+  auto look_up = [&](int i0) {
+    const bool there = i0 + lane < mine;
+    const int id = there ? table[p0 + wave + (i0 + lane) * CH_WAVES] : 0;
+    const bool ok = (unsigned)id < (unsigned)a.n_blocks;
+    ids = ok ? id : 0;
+    const float of_k = a.k_scale[plane + ids];
+    ksc = ok ? of_k : NAN;  // a page that is not there makes its rows NaN
+    vsc = a.v_scale[plane + ids];
+  };
+  bf16x8 qreg[STEPS];
+  const uint16_t* qp = a.q + (size_t)(seq.r0 + my_row) * a.q_stride + (size_t)(head * a.group + qi % a.group) * DH + hh * 16;
+#pragma unroll
+  for (int j = 0; j < STEPS; ++j) qreg[j] = *reinterpret_cast<const bf16x8*>(qp + 32 * (j >> 1) + 8 * (j & 1));
+  f32x16 o[MT];
+#pragma unroll
+  for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+    for (int v = 0; v < 16; ++v) o[mt][v] = 0.f;
+  float m = NO_REFERENCE, l = 0.f;
+  u32x4 pk[2];
+  // weights of 32 keys from their scores; a higher reference by each query for itself
+  auto weigh = [&](const f32x16& s) {
+#pragma clang fp contract(off)
+    const float top = Softmax::largest(s, f), ref = top > m + SLACK ? top : m, alpha = __builtin_amdgcn_exp2f(m - ref);
+    m = ref;
+    float p[16], sum = 0.f;
+#pragma unroll
+    for (int v = 0; v < 16; ++v) {
+      const float x = s[v] * f;  // rounded by itself, as the reference was
+      p[v] = __builtin_amdgcn_exp2f(x - m);
+      sum += p[v];
+    }
+    l = l * alpha + sum;
+#pragma unroll
+    for (int kg = 0; kg < 2; ++kg)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) pk[kg][e] = pack2bf(p[8 * kg + 2 * e], p[8 * kg + 2 * e + 1]);
+    if (__ballot(alpha != 1.f)) q8_rescale<MT>(o, alpha);
+  };
+  look_up(0);
+  int odd = 0;
+  if (wave == CH_WAVES - 1 && p1 == all) {  // own rows
+    const size_t row = (size_t)a.row_stride, first = (size_t)seq.r0 * row + (size_t)head * DH;
+    bf16x8 k[STEPS];
+    const uint16_t* const kp = a.k_rows + first + min(n32, seq.n - 1) * row + hh * 16;
+#pragma unroll
+    for (int j = 0; j < STEPS; ++j) k[j] = *reinterpret_cast<const bf16x8*>(kp + 32 * (j >> 1) + 8 * (j & 1));
+    uint32_t v[MT][2][4];
+#pragma unroll
+    for (int kg = 0; kg < 2; ++kg)
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const uint16_t* const vp = a.v_rows + first + min(16 * kg + 8 * (e >> 2) + 4 * hh + (e & 3), seq.n - 1) * row + n32;
+#pragma unroll
+        for (int mt = 0; mt < MT; ++mt) {
+          uint32_t x = vp[32 * mt];
+          const bool is_odd = (x & 0x7f80u) == 0x7f80u;
+          odd |= (int)is_odd;
+          x = is_odd ? 0u : x;
+          v[mt][kg][e >> 1] = e & 1 ? v[mt][kg][e >> 1] | x << 16 : x;
+        }
+      }
+    f32x16 s;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) s[i] = 0.f;
+#pragma unroll
+    for (int j = 0; j < STEPS; ++j) s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k[j], qreg[j], s, 0, 0, 0);
+#pragma unroll
+    for (int i = 0; i < 16; ++i)
+      if (8 * (i >> 2) + (i & 3) + 4 * hh > my_row) s[i] = -INFINITY;
+    weigh(s);
+#pragma unroll
+    for (int kg = 0; kg < 2; ++kg)
+#pragma unroll
+      for (int mt = 0; mt < MT; ++mt)
+        o[mt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, u32x4{v[mt][kg][0], v[mt][kg][1], v[mt][kg][2], v[mt][kg][3]}),
+                                                        __builtin_bit_cast(bf16x8, pk[kg]), o[mt], 0, 0, 0);
+  }
+  const uint32_t slot0 = __builtin_amdgcn_readfirstlane((uint32_t)(size_t)(__attribute__((address_space(3))) uint8_t*)smem + wave * SLOTS * SLOT);
+  const uint8_t* const slot_r = smem + wave * SLOTS * SLOT + lane * 16;
+  auto ask = [&](int i, bool v) {
+    const size_t page = (plane + (uint32_t)__builtin_amdgcn_readlane(ids, i & 63)) * (32 * DH);
+    const uint32_t to = slot0 + i % SLOTS * SLOT + (v ? P * 1024 : 0);
+#pragma unroll
+    for (int j = 0; j < P; ++j) load_to_lds<false>((v ? a.v_pool : a.k_pool) + page + j * 1024, lane * 16, to + j * 1024);
+  };
+  // all but the newest n asked for have come
+  auto arrived = [&](int n) {
+    if (n >= 2 * SLOTS - 1) __builtin_amdgcn_s_waitcnt(P * (2 * SLOTS - 1) < 16 ? 0x0f70 + P * (2 * SLOTS - 1) : 0);
+    else if (n >= 2) __builtin_amdgcn_s_waitcnt(0x0f70 + 2 * P);
+    else if (n == 1) __builtin_amdgcn_s_waitcnt(0x0f70 + P);
+    else __builtin_amdgcn_s_waitcnt(0x0f70);
+    asm volatile("" ::: "memory");
+  };
+  float k_scales[SLOTS], v_scales[SLOTS];  // of the pages on their way
+  auto scales_of = [&](int i, int to) {
+    k_scales[to] = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(ksc), i & 63));
+    v_scales[to] = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(vsc), i & 63));
+  };
+#pragma unroll
+  for (int i = 0; i < SLOTS; ++i) {
+    scales_of(i, i);
+    if (i < mine) ask(i, false), ask(i, true);
+  }
+#pragma unroll 1
+  for (int i = 0; i < mine; ++i) {
+    const float k_of = k_scales[0], v_of = v_scales[0];
+#pragma unroll
+    for (int k = 0; k + 1 < SLOTS; ++k) k_scales[k] = k_scales[k + 1], v_scales[k] = v_scales[k + 1];
+    const uint8_t* const at = slot_r + i % SLOTS * SLOT;
+    const int behind = min(mine - 1 - i, SLOTS - 1), rest = seq.L - (p0 + wave + i * CH_WAVES) * 32;
+    arrived(2 * behind + 1);
+    u32x4 x[P];
+#pragma unroll
+    for (int j = 0; j < P; ++j) x[j] = *reinterpret_cast<const u32x4*>(at + j * 1024);
+    f32x16 s;
+#pragma unroll
+    for (int v = 0; v < 16; ++v) s[v] = 0.f;
+#pragma unroll
+    for (int j = 0; j < P; ++j) {
+      s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(operand(x[j][0], x[j][1], k_of), qreg[2 * j], s, 0, 0, 0);
+      s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(operand(x[j][2], x[j][3], k_of), qreg[2 * j + 1], s, 0, 0, 0);
+    }
+    if ((__float_as_uint(k_of) & 0x7fffffffu) > 0x7f800000u)
+#pragma unroll
+      for (int v = 0; v < 16; ++v) s[v] = NAN;
+    if (rest < 32)
+#pragma unroll
+      for (int v = 0; v < 16; ++v)
+        if (8 * (v >> 2) + (v & 3) + 4 * hh >= rest) s[v] = -INFINITY;
+    weigh(s);
+    arrived(2 * behind);
+#pragma unroll
+    for (int j = 0; j < P; ++j) x[j] = *reinterpret_cast<const u32x4*>(at + P * 1024 + j * 1024);
+    if (rest < 32)  // slots past the end may hold anything: their weights are 0, their values have to be numbers
+#pragma unroll
+      for (int j = 0; j < P; ++j)
+#pragma unroll
+        for (int d = 0; d < 4; ++d) {
+          const int keep = min(max(rest - 8 * d - 4 * hh, 0), 4);
+          x[j][d] &= keep == 4 ? 0xffffffffu : (1u << (8 * keep)) - 1u;
+        }
+#pragma unroll
+    for (int kg = 0; kg < 2; ++kg)
+#pragma unroll
+      for (int mt = 0; mt < MT; ++mt)
+        o[mt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(operand(x[mt][2 * kg], x[mt][2 * kg + 1], v_of), __builtin_bit_cast(bf16x8, pk[kg]), o[mt], 0, 0, 0);
+    if (i + SLOTS < mine) {
+      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // what came has been read
+      if (((i + SLOTS) & 63) == 0) look_up(i + SLOTS);
+      scales_of(i + SLOTS, SLOTS - 1);
+      ask(i + SLOTS, false);
+      ask(i + SLOTS, true);
+    }
+  }
+  // ---- the wavefronts' sums joined
+  l += __shfl_xor(l, 32);
+  const bool any_odd = __syncthreads_or(odd);
+  float* const sum_o = reinterpret_cast<float*>(smem);
+  float* const sum_m = sum_o + CH_WAVES * OW;
+  float* const sum_l = sum_m + CH_WAVES * 32;
+#pragma unroll
+  for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+    for (int g = 0; g < 4; ++g)
+      *reinterpret_cast<f32x4*>(sum_o + wave * OW + (mt * 4 + g) * 256 + lane * 4) = f32x4{o[mt][4 * g], o[mt][4 * g + 1], o[mt][4 * g + 2], o[mt][4 * g + 3]};
+  if (hh == 0) sum_m[wave * 32 + n32] = m, sum_l[wave * 32 + n32] = l;
+  __syncthreads();
+  float top = NO_REFERENCE, share[CH_WAVES], sum = 0.f;
+#pragma unroll
+  for (int k = 0; k < CH_WAVES; ++k) top = fmaxf(top, sum_m[k * 32 + n32]);
+#pragma unroll
+  for (int k = 0; k < CH_WAVES; ++k) share[k] = __builtin_amdgcn_exp2f(sum_m[k * 32 + n32] - top), sum += share[k] * sum_l[k * 32 + n32];
+  const size_t image = (size_t)part * CH_WAVES;
+  const bool split = w.splits > 1;
+  if (split && tid < 32 && part < a.max_parts) a.pm[image * 32 + n32] = top, a.pl[image * 32 + n32] = any_odd ? -sum : sum;
+  const float inv = split ? 1.f : 1.0f / sum;
+#pragma unroll
+  for (int c = 0; c < MT * 4 / CH_WAVES; ++c) {
+    const int u = c * CH_WAVES + wave;  // mt * 4 + g
+    f32x4 r = {0, 0, 0, 0};
+#pragma unroll
+    for (int k = 0; k < CH_WAVES; ++k) r += *reinterpret_cast<const f32x4*>(sum_o + k * OW + u * 256 + lane * 4) * share[k];
+    r *= inv;
+    if (n32 >= nq) continue;
+    if (!split)
+      *reinterpret_cast<u32x2*>(a.out + ((size_t)(seq.r0 + my_row) * a.n_kv_heads * a.group + head * a.group + qi % a.group) * DH + 32 * (u >> 2) + 8 * (u & 3) + 4 * hh) =
+          u32x2{pack2bf(r[0], r[1]), pack2bf(r[2], r[3])};
+    else if (part < a.max_parts)
+      *reinterpret_cast<f32x4*>(a.po + image * OW + u * 256 + lane * 4) = r;
+  }
+  return any_odd;
+}
+
 template <int DH, bool MANY>
 __global__ __launch_bounds__(CH_THREADS, 2) void chunk_attn_q8_kernel(ChunkArgs a) {
   using Lds = ChunkLds<DH>;
@@ -255,6 +477,26 @@ __global__ __launch_bounds__(CH_THREADS, 2) void chunk_attn_q8_kernel(ChunkArgs 
     return;
   }
   const int32_t* table = a.block_table + (size_t)w.s * a.max_blocks;
+  const int part = w.part0 + w.nth;
+  if (splits > 1) {
+    const int tiles_done = w.nth / a.n_kv_heads / splits, merge = w.merge0 + tiles_done * a.n_kv_heads + head;
+    if (sp == 0 && tid == 0 && merge < CH_MAX_MERGES) {
+      const bool room = w.part0 + (tiles_done + 1) * splits * a.n_kv_heads <= a.max_parts;  // (else ranges that overlap)
+      reinterpret_cast<ChunkMerge*>(a.merges + 8)[merge] = ChunkMerge{seq.r0, seq.n, tile, head, room ? splits : 0, part, a.n_kv_heads, 0};
+    }
+  }
+  auto verdict = [&]() {
+    bool bad = false;
+    for (int j = tid, pages = (seq.L + 31) >> 5; j < pages; j += CH_THREADS) bad = bad || (unsigned)table[j] >= (unsigned)a.n_blocks;
+    bad = __syncthreads_or(bad);
+    if (tid == 0) a.status[w.s] = bad;
+  };
+  if (seq.n <= a.n_few) {
+    const bool any_odd = chunk_few<DH>(a, w, head, sp, part, smem);
+    if (any_odd && splits == 1) chunk_add_odd_values(a, seq, head, DH, 0, nq, 0);
+    if (judge) verdict();
+    return;
+  }
   const int row_first = q0 / a.group, row_last = (q1 - 1) / a.group;
   const int cached = seq.cached(), blocks = cached + row_last / CH_KEYS + 1;  // of this tile
   const int b0 = __builtin_amdgcn_readfirstlane((int)((int64_t)blocks * sp / splits));
@@ -586,11 +828,6 @@ __global__ __launch_bounds__(CH_THREADS, 2) void chunk_attn_q8_kernel(ChunkArgs 
     }
     if (any_odd) chunk_add_odd_values(a, seq, head, DH, q0, q1, first_partly_seen(row_first));
   } else {
-    const int part = w.part0 + w.nth, tiles_done = w.nth / a.n_kv_heads / splits, merge = w.merge0 + tiles_done * a.n_kv_heads + head;
-    if (sp == 0 && tid == 0 && merge < CH_MAX_MERGES) {
-      const bool room = w.part0 + (tiles_done + 1) * splits * a.n_kv_heads <= a.max_parts;
-      reinterpret_cast<ChunkMerge*>(a.merges + 8)[merge] = ChunkMerge{seq.r0, seq.n, tile, head, room ? splits : 0, part, a.n_kv_heads, 0};
-    }
     if (live_wave && part < a.max_parts) {  // (else more work than T rows can be: ranges that overlap)
       const size_t image = (size_t)part * CH_WAVES + wave;
       if (hh == 0) {
@@ -607,12 +844,7 @@ __global__ __launch_bounds__(CH_THREADS, 2) void chunk_attn_q8_kernel(ChunkArgs 
       }
     }
   }
-  if (judge) {
-    bool bad = false;
-    for (int j = tid, pages = (seq.L + 31) >> 5; j < pages; j += CH_THREADS) bad = bad || (unsigned)table[j] >= (unsigned)a.n_blocks;
-    bad = __syncthreads_or(bad);
-    if (tid == 0) a.status[w.s] = bad;
-  }
+  if (judge) verdict();
 }
 
 // Merges the partials of 32 queries of a (sequence, tile, K/V head) in split order, 32 columns per wavefront, every second
@@ -695,7 +927,7 @@ size_t attn_chunk_ws_floats(int B, int T, int group, int n_kv_heads, int head_di
 
 template <int DH, bool MANY>
 static int chunk_run(const ChunkArgs& a, hipStream_t st) {
-  constexpr size_t lds = ChunkLds<DH>::BYTES;
+  constexpr size_t lds = std::max(ChunkLds<DH>::BYTES, FewLds<DH>::BYTES);
   static DeviceOnce once;
   allow_lds(once, chunk_attn_q8_kernel<DH, MANY>, lds);
   const long items = ((long)a.T * a.group / CH_QUERIES + a.B) * a.n_kv_heads;
@@ -717,7 +949,7 @@ int launch_attn_chunk_q8(const uint16_t* q, int q_stride, const void* k_pool, co
   float* const pm = ws + images * 32 * head_dim;
   const ChunkArgs a{q, k_rows, v_rows, (const uint8_t*)k_pool, (const uint8_t*)v_pool, k_scale, v_scale, node_off, block_table,
                     prefix_len, q_stride, row_stride, max_blocks, B, T, n_kv_heads, group, n_blocks, max_prefix, parts,
-                    scale * LOG2E, ws, pm, pm + images * 32, (int32_t*)(pm + images * 64), out, status};
+                    32 / group, scale * LOG2E, ws, pm, pm + images * 32, (int32_t*)(pm + images * 64), out, status};
   if (B > 64) return head_dim == 128 ? chunk_run<128, true>(a, st) : chunk_run<64, true>(a, st);
   return head_dim == 128 ? chunk_run<128, false>(a, st) : chunk_run<64, false>(a, st);
 }
