@@ -781,7 +781,7 @@ __global__ __launch_bounds__(SMP_THREADS, 4) void sample_row_kernel(SampleArgs a
 struct ChunkedRows {
   int row0, rows, chunks, size;  // of the launch; per row; logits, a multiple of 4
   float* top;                    // [rows][chunks]
-  int32_t* n;                    // tokens listed, -1: not all that top-k could keep
+  int32_t* n;                    // tokens listed, -1: not all that top-k or min-p could keep
   uint64_t *over, *data;         // weights that min-p allows; the list, or the weights per bin, [SMP_BINS]
   __device__ inline size_t at(int t, int c) const { return (size_t)(t - row0) * chunks + c; }
 };
@@ -807,14 +807,14 @@ __global__ __launch_bounds__(SMP_THREADS) void sample_chunk_kernel(SampleArgs a,
   int n = -1;
   if (!is_token(top) || r.t == 0.f) {
     n = 0;
-  } else if (r.short_by_k()) {
-    const float bound = reached_by((int)r.top_k, mine, SampleScale(top, r.t), l);
-    n = collect(row, bound, first, ch.data + at * SMP_BINS, SMP_CHUNK_LIST, l);
+  } else if (r.short_by_k() || r.short_by_min()) {
+    const float bound = r.short_by_k() ? reached_by((int)r.top_k, mine, SampleScale(top, r.t), l) : min_p_bound(r, top);
+    if (bound > -INFINITY) n = collect(row, bound, first, ch.data + at * SMP_BINS, SMP_CHUNK_LIST, l);
     if (n > SMP_CHUNK_LIST) n = -1;
   }
   if (tid == 0) ch.top[at] = top, ch.n[at] = n;
 }
-// largest logit of a row, and whether its chunks list all that top-k could keep (or have no need to)
+// largest logit of a row, and whether its chunks list all that top-k or min-p could keep (or have no need to)
 struct ChunkedTop {
   float top;
   bool listed;
@@ -871,7 +871,7 @@ __global__ __launch_bounds__(SMP_THREADS) void sample_finish_kernel(SampleArgs a
   }
   const SampleScale sc(x.top, r.t);
   if (x.listed) {
-    const int k = (int)r.top_k;
+    const int k = r.short_by_k() ? (int)r.top_k : 0;
     // entry e of all: chunk c's from upto[c] on
     uint32_t* const upto = l.few.bin;
     for (int c = tid; c <= SMP_BINS; c += SMP_THREADS) upto[c] = c < ch.chunks ? ch.n[ch.at(t, c)] : 0;
@@ -883,8 +883,8 @@ __global__ __launch_bounds__(SMP_THREADS) void sample_finish_kernel(SampleArgs a
         f(ch.data[ch.at(t, c) * SMP_BINS + (e - upto[c])]);
       }
     };
-    float bound = -INFINITY;
-    if (all > SMP_LIST) {
+    float bound = k > 0 ? -INFINITY : min_p_bound(r, x.top);
+    if (k > 0 && all > SMP_LIST) {
       uint64_t best = 0;
       entries([&](uint64_t key) { best = Larger()(best, key); });
       bound = reached_by(k, best == 0 ? -INFINITY : key_logit(best), sc, l);
@@ -898,7 +898,7 @@ __global__ __launch_bounds__(SMP_THREADS) void sample_finish_kernel(SampleArgs a
     __syncthreads();
     const int n = l.list_n;
     if (n <= SMP_LIST) {
-      finish_list(a, t, u, r, sc, l, n, min(n, k));
+      finish_list(a, t, u, r, sc, l, n, k > 0 ? min(n, k) : n);
       return;
     }
   }

@@ -261,3 +261,18 @@ def test_probabilities_of_one_row_do_not_depend_on_its_neighbours():
     for t in (0, 17, 299):
         one, p = Call(x[t:t + 1], [1], rules, u[t:t + 1]).run()
         assert one[0] == token[t] and p[0] == prob[t]
+
+
+@pytest.mark.parametrize("V", [32000, 50001, 128256])
+@pytest.mark.parametrize("m", [1e-11, 0.001, 0.05, 0.3, 1.0])
+def test_min_p_by_itself(V, m):
+    # few tokens above the border in every chunk, in one chunk only, more than lists hold, infinities
+    rng = np.random.default_rng(V)
+    x = rng.normal(size=(6, V)) * 3
+    x[1, :40] += 20
+    x[2] = np.round(rng.normal(size=V))
+    x[3] = -INF
+    x[3, [V - 1, 17]] = -8.0
+    x[4, [5, V - 3]] = INF
+    x[5, V // 2:] = 2.5
+    Call(x, [6], [(0.8, 0, 1, m)], rng.random(6)).check()
