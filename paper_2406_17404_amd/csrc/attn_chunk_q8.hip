@@ -65,12 +65,14 @@ struct ChunkMerge {
   int r0, n, tile, head, splits, part, step, pad;  // partial of split k: part + k * step
 };
 // The plan, the same on every wavefront of every workgroup: a split has `span` blocks at most, of one sequence evenly
-// many.  Up to 64 sequences (not MANY) 32 spans are weighed, one per lane, the longest sequence in 1 .. 32 splits:
-//   cost = rounds of workgroups * (START + blocks of one) + MERGE and PART for each of the parts if anything is split
+// many.  Up to 64 sequences (not MANY) 64 spans are weighed, one per lane, the longest sequence in 1 .. 32 splits, then 36 .. 160
+// (few heads and a long cache: 64 rows over 131072 positions, 8 heads on one, 147 us with 32 splits at most, 80 so):
+//   cost = rounds of workgroups * (START + units of one) + MERGE, PART for each of the parts and EACH for each of the longest's
+//          if anything is split
 // in times that a compute unit takes for a block of 256 queries (2.3 us).  Sequences come longest first, so that what starts
 // last is short and rounds fill up: the middle between whole rounds of average items and no idle unit is taken.  Beyond 64 sequences
 // neither is done: index order, and spans of an even share.
-constexpr float START = 4.5f, MERGE = 2.5f, PART = 0.03f, RESIDENT = 256.f;  // one workgroup per compute unit at a time
+constexpr float START = 4.5f, MERGE = 2.5f, PART = 0.03f, EACH = 0.1f, RESIDENT = 256.f;  // one workgroup per compute unit at a time
 template <bool MANY>
 struct ChunkPlan {
   const ChunkArgs& a;
@@ -107,7 +109,7 @@ struct ChunkPlan {
     const int blocks = mine.units(a.n_few), longest = max(lane_value(blocks, 0), 1), groups = mine.tiles * a.n_kv_heads;
     span = longest;
     if (a.max_parts == 0 || longest == 1) return;
-    const int c = (longest + (lane & 31)) / ((lane & 31) + 1);
+    const int most = lane < 32 ? lane + 1 : 32 + 4 * (lane - 31), c = (longest + most - 1) / most;
     const float each = __builtin_amdgcn_rcpf((float)c);
     float n = 0.f, parts = 0.f;
     if (a.B == 1) work = wave_sum(mine.work(a.n_few)) * a.n_kv_heads;  // (lanes behind the first have none)
@@ -119,7 +121,7 @@ struct ChunkPlan {
     }
     const float rounds = ceilf(n * (1.f / RESIDENT));
     const float whole = START + (float)c, even = START + work * __builtin_amdgcn_rcpf(n);
-    float cost = (rounds > 1.f ? fmaxf(whole, 0.5f * even * (rounds + n * (1.f / RESIDENT))) : whole) + (parts > 0.f ? MERGE + PART * parts : 0.f);
+    float cost = (rounds > 1.f ? fmaxf(whole, 0.5f * even * (rounds + n * (1.f / RESIDENT))) : whole) + (parts > 0.f ? MERGE + PART * parts + EACH * (float)most : 0.f);
     if (parts > (float)a.max_parts) cost = INFINITY;  // no room for its partials
     const uint32_t best = wave_min((uint32_t)fminf(cost * 8.f, 60e6f) << 6 | lane);  // (of equals the fewest splits)
     span = lane_value(c, best & 63);
