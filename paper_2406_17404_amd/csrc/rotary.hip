@@ -86,25 +86,27 @@ __device__ inline float2 turned(float x1, float x2, float2 cs) {
   return float2{x1 * cs.x - x2 * cs.y, x1 * cs.y + x2 * cs.x};
 }
 
-// ROWS rows per workgroup; WIDE: 16 bytes at a time, where pairs (or halves of them) come in such pieces
-template <class E, bool PAIRS, bool WIDE, int ROWS>
+// A workgroup per row.  Four rows per workgroup, a wavefront looking for the sequence of each, took 18.5 us instead of 16.4 for
+// 4096 rows of 40 heads of 128, 66.9 instead of 62.4 for 16384, and more for fewer (of 9 heads 10 % less for 16384).
+// WIDE: 16 bytes at a time, where pairs (or halves of them) come in such pieces.
+template <class E, bool PAIRS, bool WIDE>
 __global__ __launch_bounds__(ROT_THREADS) void rotary_kernel(RotaryArgs a) {
   constexpr int N = 16 / sizeof(E);
-  __shared__ float2 cs[ROWS][ROT_MAX_HALF];
-  __shared__ int position[ROWS];
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, t0 = blockIdx.x * ROWS;
+  __shared__ float2 cs[ROT_MAX_HALF];
+  __shared__ int position;
+  const int tid = threadIdx.x, t = blockIdx.x;
   if (blockIdx.x == 0)  // sequences without rows of their own
     for (int s = tid; s < a.B; s += ROT_THREADS) {
       const int r0 = a.node_off[s], r1 = a.node_off[s + 1];
       const bool bad = r0 < 0 || r1 < r0 || r1 > a.T;
       if (bad || r0 == r1) a.status[s] = bad;
     }
-  for (int r = wave; r < ROWS; r += ROT_THREADS / 64) {
-    const RotaryRow row = rotary_row(a, t0 + r);
+  if (tid < 64) {
+    const RotaryRow row = rotary_row(a, t);
     int at = -1;
     if (row.n > 0) {
       if (row.L >= 0) {
-        const int node = t0 + r - row.r0;
+        const int node = t - row.r0;
         if (a.parent) {
           const TreeParents p = load_parents(a.parent, row.r0, row.n);
           if (tree_valid(p, row.n)) {
@@ -119,60 +121,55 @@ __global__ __launch_bounds__(ROT_THREADS) void rotary_kernel(RotaryArgs a) {
           at = row.L + node;
         }
       }
-      if (t0 + r == row.r0 && lane == 0) a.status[row.s] = at < 0;
+      if (t == row.r0 && tid == 0) a.status[row.s] = at < 0;
     }
-    if (lane == 0) position[r] = at;
+    if (tid == 0) position = at;
   }
   __syncthreads();
-  for (int i = tid; i < ROWS * a.half; i += ROT_THREADS) {
-    const int r = i / a.half, j = i % a.half;
-    if (position[r] >= 0) cs[r][j] = cos_sin((double)position[r] * a.freqs[j], a.magnitude);
-  }
+  const int at = position;
+  if (at < 0) return;
+  for (int j = tid; j < a.half; j += ROT_THREADS) cs[j] = cos_sin((double)at * a.freqs[j], a.magnitude);
   __syncthreads();
   const int heads = a.n_heads + a.n_kv_heads, rot = 2 * a.half;
   // units of a head: what is turned, then what is copied
   const int turns = WIDE ? (PAIRS ? rot / N : a.half / N) : a.half;
   const int units = turns + (a.head_dim - rot) / (WIDE ? N : 1);
+  for (int i = tid; i < heads * units; i += ROT_THREADS) {
+    const int h = i / units, u = i % units;
+    const bool is_q = h < a.n_heads;
+    const int hk = is_q ? h : h - a.n_heads;
+    const E* src = (const E*)(is_q ? a.q : a.k) + (size_t)t * (is_q ? a.q_stride : a.k_stride) + (size_t)hk * a.head_dim;
+    E* dst = (E*)(is_q ? a.q_out : a.k_out) + (size_t)t * (is_q ? a.qo_stride : a.ko_stride) + (size_t)hk * a.head_dim;
+    if constexpr (WIDE) {
+      if (u >= turns) {
+        const int c = rot + (u - turns) * N;
+        *reinterpret_cast<u32x4*>(dst + c) = *reinterpret_cast<const u32x4*>(src + c);
+      } else if constexpr (PAIRS) {
+        Vec16<E> x = *reinterpret_cast<const Vec16<E>*>(src + u * N);
 #pragma unroll
-  for (int r = 0; r < ROWS; ++r) {
-    if (position[r] < 0) continue;
-    for (int i = tid; i < heads * units; i += ROT_THREADS) {
-      const int h = i / units, u = i % units;
-      const bool is_q = h < a.n_heads;
-      const int hk = is_q ? h : h - a.n_heads;
-      const E* src = (const E*)(is_q ? a.q : a.k) + (size_t)(t0 + r) * (is_q ? a.q_stride : a.k_stride) + (size_t)hk * a.head_dim;
-      E* dst = (E*)(is_q ? a.q_out : a.k_out) + (size_t)(t0 + r) * (is_q ? a.qo_stride : a.ko_stride) + (size_t)hk * a.head_dim;
-      if constexpr (WIDE) {
-        if (u >= turns) {
-          const int c = rot + (u - turns) * N;
-          *reinterpret_cast<u32x4*>(dst + c) = *reinterpret_cast<const u32x4*>(src + c);
-        } else if constexpr (PAIRS) {
-          Vec16<E> x = *reinterpret_cast<const Vec16<E>*>(src + u * N);
-#pragma unroll
-          for (int e = 0; e < N / 2; ++e) {
-            const float2 y = turned(to_float(x.v[2 * e]), to_float(x.v[2 * e + 1]), cs[r][u * (N / 2) + e]);
-            x.v[2 * e] = from_float<E>(y.x), x.v[2 * e + 1] = from_float<E>(y.y);
-          }
-          *reinterpret_cast<Vec16<E>*>(dst + u * N) = x;
-        } else {
-          Vec16<E> x1 = *reinterpret_cast<const Vec16<E>*>(src + u * N), x2 = *reinterpret_cast<const Vec16<E>*>(src + a.half + u * N);
-#pragma unroll
-          for (int e = 0; e < N; ++e) {
-            const float2 y = turned(to_float(x1.v[e]), to_float(x2.v[e]), cs[r][u * N + e]);
-            x1.v[e] = from_float<E>(y.x), x2.v[e] = from_float<E>(y.y);
-          }
-          *reinterpret_cast<Vec16<E>*>(dst + u * N) = x1;
-          *reinterpret_cast<Vec16<E>*>(dst + a.half + u * N) = x2;
+        for (int e = 0; e < N / 2; ++e) {
+          const float2 y = turned(to_float(x.v[2 * e]), to_float(x.v[2 * e + 1]), cs[u * (N / 2) + e]);
+          x.v[2 * e] = from_float<E>(y.x), x.v[2 * e + 1] = from_float<E>(y.y);
         }
+        *reinterpret_cast<Vec16<E>*>(dst + u * N) = x;
       } else {
-        if (u >= turns) {
-          const int c = rot + u - turns;
-          dst[c] = src[c];
-        } else {
-          const int c1 = PAIRS ? 2 * u : u, c2 = PAIRS ? 2 * u + 1 : u + a.half;
-          const float2 y = turned(to_float(src[c1]), to_float(src[c2]), cs[r][u]);
-          dst[c1] = from_float<E>(y.x), dst[c2] = from_float<E>(y.y);
+        Vec16<E> x1 = *reinterpret_cast<const Vec16<E>*>(src + u * N), x2 = *reinterpret_cast<const Vec16<E>*>(src + a.half + u * N);
+#pragma unroll
+        for (int e = 0; e < N; ++e) {
+          const float2 y = turned(to_float(x1.v[e]), to_float(x2.v[e]), cs[u * N + e]);
+          x1.v[e] = from_float<E>(y.x), x2.v[e] = from_float<E>(y.y);
         }
+        *reinterpret_cast<Vec16<E>*>(dst + u * N) = x1;
+        *reinterpret_cast<Vec16<E>*>(dst + a.half + u * N) = x2;
+      }
+    } else {
+      if (u >= turns) {
+        const int c = rot + u - turns;
+        dst[c] = src[c];
+      } else {
+        const int c1 = PAIRS ? 2 * u : u, c2 = PAIRS ? 2 * u + 1 : u + a.half;
+        const float2 y = turned(to_float(src[c1]), to_float(src[c2]), cs[u]);
+        dst[c1] = from_float<E>(y.x), dst[c2] = from_float<E>(y.y);
       }
     }
   }
@@ -180,10 +177,7 @@ __global__ __launch_bounds__(ROT_THREADS) void rotary_kernel(RotaryArgs a) {
 
 template <class E, bool PAIRS, bool WIDE>
 static int rotary_run(const RotaryArgs& a, hipStream_t st) {
-  const int rows = a.T >= 4096 ? 4 : 1;
-  const int grid = (a.T + rows - 1) / rows;
-  if (rows == 4) rotary_kernel<E, PAIRS, WIDE, 4><<<grid, ROT_THREADS, 0, st>>>(a);
-  else rotary_kernel<E, PAIRS, WIDE, 1><<<grid, ROT_THREADS, 0, st>>>(a);
+  rotary_kernel<E, PAIRS, WIDE><<<a.T, ROT_THREADS, 0, st>>>(a);
   return check_launch();
 }
 template <class E>
