@@ -419,7 +419,7 @@ int32_t tree_attention_q8_workspace_bytes(int32_t B, int32_t T, int32_t n_heads,
 /* tree_attention for one layer of the paged cache: row i of sequence s sees the
  * prefix_len[s] positions of the cache and the rows of its own ancestors and itself in k_rows,
  * v_rows (which the cache need not hold).  A sequence of one row is plain decoding, a chain of rows a
- * causal pass: a prompt goes in chains of at most TRJ_N_MAX rows, each appended before the next.  out: [T][n_heads][head_dim].  A key that a row does not see has no part in it
+ * causal pass: a prompt goes in chains of at most TRJ_N_MAX rows, each appended before the next, or whole through chunk_attention_q8.  out: [T][n_heads][head_dim].  A key that a row does not see has no part in it
  * whatever it holds, infinities and NaN included; a row that sees a value that is not finite
  * gets what the sums give.  max_prefix: host upper bound of prefix_len[s].  scale: positive, and a
  * finite fp32 number when multiplied by log2(e), else TRJ_ERR_BAD_SHAPE.

@@ -10,6 +10,17 @@
 //   O^T[dh, queries]  += V^T[dh, keys] * P^T[keys, queries]
 // Cached blocks (two pages) are converted on the way, codes times their power-of-two scale being bf16 numbers
 // exactly; the sequence's own rows are bf16 already and V is transposed.
+//
+// Bound by products for long chunks: 2048 rows after 16384 positions, 32 heads of 128, are 584 GFLOP in 640 to 680 us, 0.86 to
+// 0.91 PFLOP/s where a large library product reaches 1.19 to 1.33 on the same card.  The matrix units work 45 % of the
+// cycles, at a clock of 1.9 GHz under this load, LDS is active in 36 %, and a tile of 32 keys x 32 queries takes 152 vector
+// instructions beside its 16 products.  No part stands out: with one left out (675 us whole) the exponentials save 25 us, reading operands 56,
+// the conversion 75, conversion and loads 128.  Less per product would take more queries per wavefront, and two query tiles'
+// accumulators, weights and queries do not fit its 256 registers.
+// A whole prompt of 4096 rows, 32 heads on 8, takes 190 us (0.72), a third of it masked or partly seen tiles and start.
+// For short ones by the way to the first block and from the last: 12 us for an item of one block (plan 0.5, queries 0.8,
+// first codes 1.2, their conversion and barrier 1.4, two masked tiles 2.9, end 2.1; code that is not in the instruction cache yet
+// is in each), against 2.5 us per block of 256 queries, and by the merge's launch, 5 to 17 us with its traffic.
 #include <algorithm>
 #include <type_traits>
 
@@ -32,13 +43,15 @@ struct ChunkArgs {
   int32_t* status;
 };
 constexpr int CH_WAVES = 8, CH_THREADS = 64 * CH_WAVES, CH_QUERIES = 32 * CH_WAVES, CH_KEYS = 64;
-constexpr int CH_MAX_PARTS = 512, CH_MAX_MERGES = CH_MAX_PARTS / 2, CH_LEAST = 4;  // partials that a call may leave to the merge; blocks that a split has at least
+constexpr int CH_MAX_PARTS = 512, CH_MAX_MERGES = CH_MAX_PARTS / 2;  // partials that a call may leave to the merge
+// Calls in which no sequence can have more blocks have neither partials nor a merge; beyond 64 sequences a split's least span.
+constexpr int CH_LEAST = 4;
 
 struct ChunkSeq {
   int r0, n, L, tiles;  // n < 0: refused, with nothing written; L < 0: refused, rows of zeros
   __device__ inline int cached() const { return (L + CH_KEYS - 1) / CH_KEYS; }
   __device__ inline int blocks() const { return n <= 0 ? 0 : L < 0 ? 1 : cached() + (n + CH_KEYS - 1) / CH_KEYS; }
-  // few queries (n_few rows at most), whose wavefronts each take pages of their own: a block costs a quarter of what it else does
+  // blocks, of few queries (n_few rows at most) four to a unit
   __device__ inline int units(int n_few) const { return n <= n_few && L >= 0 ? (blocks() + 3) >> 2 : blocks(); }
   // units of all tiles, about: own rows are seen up to a tile's
   __device__ inline float work(int n_few) const {
@@ -64,14 +77,14 @@ struct ChunkWork {
 struct ChunkMerge {
   int r0, n, tile, head, splits, part, step, pad;  // partial of split k: part + k * step
 };
-// The plan, the same on every wavefront of every workgroup: a split has `span` blocks at most, of one sequence evenly
-// many.  Up to 64 sequences (not MANY) 64 spans are weighed, one per lane, the longest sequence in 1 .. 32 splits, then 36 .. 160
+// The plan, the same on every wavefront of every workgroup: a split has `span` units at most, of one sequence evenly many.
+// Up to 64 sequences (not MANY) 64 spans are weighed, one per lane, the longest sequence in 1 .. 32 splits, then 36 .. 160
 // (few heads and a long cache: 64 rows over 131072 positions, 8 heads on one, 147 us with 32 splits at most, 80 so):
-//   cost = rounds of workgroups * (START + units of one) + MERGE, PART for each of the parts and EACH for each of the longest's
-//          if anything is split
-// in times that a compute unit takes for a block of 256 queries (2.3 us).  Sequences come longest first, so that what starts
-// last is short and rounds fill up: the middle between whole rounds of average items and no idle unit is taken.  Beyond 64 sequences
-// neither is done: index order, and spans of an even share.
+//   cost = rounds of workgroups * (START + units of one), and if anything is split MERGE, PART for each of the parts and
+//          EACH for each split of the longest
+// A unit is what a compute unit takes for a block of 256 queries, 2.3 us, or for four of few queries (0.6 to 0.9 us each).
+// Sequences come longest first, so that what starts last is short and rounds fill up: the middle between whole rounds of
+// average items and no idle unit is taken.  Beyond 64 sequences neither is done: index order, and spans of an even share.
 constexpr float START = 4.5f, MERGE = 2.5f, PART = 0.03f, EACH = 0.1f, RESIDENT = 256.f;  // one workgroup per compute unit at a time
 template <bool MANY>
 struct ChunkPlan {
@@ -227,7 +240,9 @@ struct ChunkLds {
 
 // A sequence of 32 queries at most: every wavefront has them all and pages of its own, each CH_WAVES-th of the range, whose codes
 // come to slots of its own in LDS and go from there to the matrix units; the last wavefront takes the sequence's own rows first.
-// The wavefronts' sums are joined at the end.  In the other form seven wavefronts would only bring blocks for one.
+// The wavefronts' sums are joined at the end.  In the other form seven wavefronts would only bring blocks for one: 64 sequences of
+// a row over 2000 positions, 32 heads on 8, took 142 us so and take 79 here, one row over 131072, 64 heads on 8, 112 and 57
+// (268 MB, 4.7 TB/s).
 template <int DH>
 struct FewLds {
   static constexpr int P = DH / 32, SLOTS = 256 / DH, SLOT = 2 * P * 1024;  // P KiB of codes of a page, K or V

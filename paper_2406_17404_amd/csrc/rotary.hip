@@ -4,6 +4,10 @@
 //
 // Angle, reduction and the two polynomials are worked out in 64 bits, once per row and pair for all heads, and
 // rounded to 32 bits; products are 32-bit, each result is rounded once.
+//
+// Bound by memory for many rows: 4096 rows of 64 heads of 128 in bf16, 134 MB, take 29 us = 4.6 TB/s (a large copy moves 4.9).
+// For few by one chain of latencies, from the lengths over the tree to the position, its angles in 64 bits and the rows: 4.0 us
+// for a row, 4.3 for a tree of 69, in calls of 8.6 and 9.1.
 #include <algorithm>
 #include <cmath>
 
