@@ -370,3 +370,92 @@ def test_the_longest_prefix(n):
         want, mean = w @ v, w @ np.abs(v)
         tol = HALF * (np.abs(want) + mean) * (1 + HALF) + (long_sum + 2.0 ** -12) * mean
         assert (np.abs(got[i, 0] - want) <= tol).all()
+
+
+@pytest.mark.parametrize("value", [float("nan"), float("inf"), -float("inf")])
+@pytest.mark.parametrize("L,n,heads", [(9000, 7, 4), (9000, 16, 4), (0, 3, 4), (64, 5, 6), (9000, 100, 4)])
+def test_what_is_not_finite_in_split_sequences_and_short_ones(value, L, n, heads):
+    rng = np.random.default_rng(19)
+    c = Call(rng, [L], [n], heads, 2, 64)
+    clean = c.check()
+    j, g = n - 2, heads // 2
+    c.kr[j, 0, 3] = value
+    c.vr[j, 1, 5] = value
+    got = c.run()
+    assert np.array_equal(got[:j], clean[:j])
+    if value == value:
+        assert (got[j:, g:, 5] == value).all()
+    else:
+        assert np.isnan(got[j:, g:, 5]).all() and np.isnan(got[j:, :g]).all()
+    keep = [d for d in range(64) if d != 5]
+    assert np.array_equal(got[j:, g:][:, :, keep], clean[j:, g:][:, :, keep])
+
+
+@pytest.mark.parametrize("L,n", [(33, 40), (33, 1), (65, 200), (9001, 3), (9001, 90)])
+def test_unused_slots_of_the_last_page_may_hold_anything(L, n):
+    c = Call(np.random.default_rng(20), [L], [n], 2, 1, 128)
+    want = c.check()
+    last, used = c.cache.table[0, (L - 1) // 32], (L - 1) % 32 + 1
+    for code in (NAN_CODE, 255, 126):
+        for w in "kv":
+            page = c.cache.pool[w][:, :, last]
+            page[..., S.offsets(128, w)[used:]] = code
+            c.cache.pool[w][:, :, last] = page
+        assert np.array_equal(c.run(), want)
+
+
+@pytest.mark.parametrize("n", [3, 60])
+def test_pages_that_are_not_there(n):
+    c = Call(np.random.default_rng(21), [9000, 9000, 70], [n] * 3, 2, 1, 64)
+    c.cache.table[0, 200], c.cache.table[2, 0] = -1, c.cache.n_blocks
+    got = c.run()
+    assert list(c.status) == [1, 0, 1] and np.isnan(got[:n]).all() and np.isnan(got[2 * n:]).all()
+    c.check(got, skip=(0, 2))
+
+
+@pytest.mark.parametrize("n", [1, 10])
+def test_scores_far_from_zero_of_few_queries(n):
+    rng = np.random.default_rng(22)
+    c = Call(rng, [40], [n], 2, 1, 64, exps=(40, 41))
+    c.cache.scale["v"][:] = 1.0
+    c.q = (c.q.float() * 2.0 ** 70).bfloat16()
+    got = c.run()
+    keys = np.concatenate([c.cache.values("k", 0)[0], c.kr[:, 0].float().numpy()])
+    vals = np.concatenate([c.cache.values("v", 0)[0], c.vr[:, 0].float().numpy()])
+    for i in range(n):
+        for h in range(2):
+            v = vals[(keys[:40 + i + 1] @ c.q[i, h].float().numpy().astype(np.float64)).argmax()]
+            assert np.abs(got[i, h] - v).max() <= HALF * np.abs(v).max()
+    c = Call(rng, [40], [n], 1, 1, 64, scale=1e30)
+    c.q = -c.q.abs()
+    c.cache.pool["k"][:] &= 127  # every score below -1e30
+    c.kr = c.kr.abs()
+    assert np.isfinite(c.run()).all()
+
+
+@pytest.mark.parametrize("dh,n", [(64, 1), (128, 3), (64, 40)])
+def test_many_pages_of_one_workgroup(dh, n):
+    # so many heads that nothing is split: a wavefront looks pages up several times
+    rng = np.random.default_rng(23)
+    L, heads, n_blocks = 40000 - 5, 256, 40
+    pages = (L + 31) // 32
+    codes = {w: (rng.normal(size=(heads, n_blocks, 32 * dh)) * 60).clip(-448, 448) for w in "kv"}
+    pool = {w: S.encode(codes[w]) for w in "kv"}
+    scale = {w: (2.0 ** rng.integers(-8, -4, (heads, n_blocks))).astype(np.float32) for w in "kv"}
+    table = rng.integers(0, n_blocks, pages)
+    q, kr, vr = (bf16(rng.normal(size=(n, heads, dh))) for _ in range(3))
+    ws = torch.empty(b.chunk_attention_q8_workspace_bytes(1, n, heads, heads, dh, L), dtype=torch.uint8, device=DEV)
+    out, status = torch.full((n, heads, dh), 5.0, dtype=torch.bfloat16, device=DEV), ints(1)
+    b.chunk_attention_q8(q.to(DEV), *(torch.from_numpy(pool[w]).to(DEV) for w in "kv"),
+                         *(torch.from_numpy(scale[w]).to(DEV) for w in "kv"), kr.to(DEV), vr.to(DEV), i32([0, n]),
+                         i32(table[None]), i32([L]), L, dh ** -0.5, ws, out, status)
+    torch.cuda.synchronize()
+    assert status.tolist() == [0]
+    got = out.float().cpu().numpy()
+    for h in (0, 100, 255):
+        k, v = (S.page_values(pool[w][h], scale[w][h], w)[table].reshape(-1, dh)[:L] for w in "kv")
+        rows = [x[:, h:h + 1].float().numpy() for x in (q, kr, vr)]
+        want, mean = P.chunk_attention(rows[0], k[None], v[None], rows[1], rows[2], dh ** -0.5)
+        # 32-bit sums of up to 625 blocks in a row: half a step of 2^-23 for the weights', one for each product of the values'
+        tol = HALF * (np.abs(want) + mean) * (1 + HALF) + (625 * 2 * (2.0 ** -24 + 2 * 2.0 ** -23) + 2.0 ** -12) * mean
+        assert (np.abs(got[:, h:h + 1] - want) <= tol).all()
