@@ -7,11 +7,12 @@
 // Weights are whole numbers, so that sums do not depend on their order and every comparison with a border is exact.
 // As all three rules keep first parts, only the sum of what each keeps matters: of the smallest the target is a share.  No
 // row is sorted.  Two ways:
-//   the short list  where top-k (or min-p without top-p) leaves few tokens: of the 1024 threads' largest logits the k-th is
-//                   a bound that k tokens reach and few more; those are collected, put in order and weighed
+//   the short list  where top-k (or min-p without top-p) leaves few tokens: of the threads' largest logits the k-th is
+//                   a bound that k tokens reach and few more (of more than half the threads' number the k-th of all, by
+//                   counting); those are collected, put in order and weighed
 //   the histogram   of the weights over max x - x, which finds the bin in which a running sum (or count) crosses a
 //                   border; the tokens of that bin alone are put in order
-// A top-k of more than half the threads, and rows with thousands of tokens in a bin that a border crosses, take a third way, which
+// A top-k of more than SMP_SHORT, and rows with thousands of tokens in a bin that a border crosses, take a third way, which
 // reads the row from memory for every step: 62 us for one row of 32000 and top-k 2000, 190 for 1024 rows.
 //
 // Rows of up to 32768 logits stay in the registers of one workgroup, which reads them once: 1024 x 32000 take 34 us with top-k 50
@@ -27,7 +28,7 @@
 namespace trj {
 
 constexpr int SMP_ABREAST = 2;
-constexpr int SMP_THREADS = 512, SMP_WAVES = SMP_THREADS / 64, SMP_BINS = 2048, SMP_LIST = 2048;
+constexpr int SMP_THREADS = 512, SMP_WAVES = SMP_THREADS / 64, SMP_BINS = 2048, SMP_LIST = 2048, SMP_SHORT = SMP_LIST * 3 / 4;
 constexpr double SMP_UNIT = 274877906944.0;      // 2^38
 constexpr float SMP_RANGE = 27.1f;               // exp(-27.1) * 2^38 rounds to 0
 typedef float f32x4_row __attribute__((ext_vector_type(4), aligned(4)));  // rows of odd length start anywhere
@@ -62,7 +63,7 @@ struct SampleRules {
     bad = !(t >= 0.f && t < INFINITY) || top_k != top_k || top_p != top_p || m != m;
     least = m > 0.f ? (uint64_t)ceil((double)fminf(m, 1.f) * SMP_UNIT) : 0;
   }
-  __device__ inline bool short_by_k() const { return top_k >= 1.f && top_k <= SMP_THREADS / 2; }
+  __device__ inline bool short_by_k() const { return top_k >= 1.f && top_k <= SMP_SHORT; }
   __device__ inline bool short_by_min() const { return least > 0 && !(top_p < 1.f) && !(top_k >= 1.f); }
 };
 
@@ -198,6 +199,9 @@ struct ListLds {  // of what makes a list
     __syncthreads();
   }
 };
+struct ChunkLds : ListLds {
+  uint32_t counts[SMP_BINS + 1];
+};
 struct WeighLds {  // of what adds up weights
   uint64_t before[SMP_BINS + 1];
   Parts part;
@@ -211,7 +215,7 @@ struct SampleLds : ListLds {
     } few;
     Histogram zoom;
     struct { uint64_t key[SMP_LIST], w[SMP_LIST]; } list;
-    uint32_t counts[SMP_BINS + 1];
+    uint32_t counts[SMP_BINS + 1];  // (leaves few.bin as it is)
   };
   uint64_t found_upto, found_key, found_w;
   int found_bin[2];
@@ -697,6 +701,21 @@ __device__ inline float reached_by(int k, float mine, const SampleScale& sc, Lis
   const float below = 2.f * ((float)(l.bound_bin + 1) * WIDE) / sc.per_bin * 1.00001f;
   return sc.infinite ? INFINITY : fmaxf(2.f * sc.half_top - below - fabsf(sc.half_top) * 1e-6f, -3.4028235e38f);
 }
+// The same for a k beyond half the threads, of all tokens that `each` goes over: the lower end of the bin in which the k-th lies.
+template <class Lds, class Each>
+__device__ inline float reached_by_count(int k, const SampleScale& sc, Lds& l, Each each) {
+  __syncthreads();
+  for (int i = threadIdx.x; i <= SMP_BINS; i += SMP_THREADS) l.counts[i] = 0;
+  __syncthreads();
+  each([&](float v) {
+    const int b = sc.bin(sc.seen(v));
+    if (b < SMP_BINS - 1) atomicAdd(&l.counts[b], 1u);
+  });
+  const int all = (int)sum_bins(l.counts, l.part);
+  const int b = all < k ? SMP_BINS - 1 : crossing(l.counts, k - 1);
+  const float below = 2.f * (float)(b + 1) / sc.per_bin * 1.00001f;  // (as above)
+  return sc.infinite ? INFINITY : fmaxf(2.f * sc.half_top - below - fabsf(sc.half_top) * 1e-6f, -3.4028235e38f);
+}
 // Tokens from `bound` on to out[0 .. cap), in any order; their number
 template <int NV>
 __device__ inline int collect(const Held<NV>& x, float bound, int first_index, uint64_t* out, int cap, ListLds& l) {
@@ -769,7 +788,9 @@ __global__ __launch_bounds__(SMP_THREADS, 4) void sample_row_kernel(SampleArgs a
   // ---- the short list
   if (r.short_by_k() || r.short_by_min()) {
     const int k = r.short_by_k() ? (int)r.top_k : 0;
-    const float bound = k > 0 ? reached_by(k, mine, sc, l) : min_p_bound(r, top);
+    const float bound = k == 0                 ? min_p_bound(r, top)
+                        : k <= SMP_THREADS / 2 ? reached_by(k, mine, sc, l)
+                                               : reached_by_count(k, sc, l, [&](auto f) { row.each([&](float v, int) { f(v); }); });
     if (bound > -INFINITY) {
       const int n = collect(row, bound, 0, l.few.key, SMP_LIST, l);
       if (n <= SMP_LIST) {
@@ -793,11 +814,11 @@ struct ChunkedRows {
   uint64_t *over, *data;         // weights that min-p allows; the list, or the weights per bin, [SMP_BINS]
   __device__ inline size_t at(int t, int c) const { return (size_t)(t - row0) * chunks + c; }
 };
-constexpr int SMP_CHUNK_LIST = 1024;
+constexpr int SMP_CHUNK_LIST = SMP_BINS;  // as many as a chunk has room for
 
 template <int NV>
 __global__ __launch_bounds__(SMP_THREADS) void sample_chunk_kernel(SampleArgs a, ChunkedRows ch) {
-  __shared__ ListLds l;
+  __shared__ ChunkLds l;
   const int tid = threadIdx.x, t = ch.row0 + blockIdx.x / ch.chunks, c = blockIdx.x % ch.chunks, first = c * ch.size;
   if (blockIdx.x == 0 && ch.row0 == 0) empty_sequences(a);
   Held<NV> row;
@@ -816,7 +837,11 @@ __global__ __launch_bounds__(SMP_THREADS) void sample_chunk_kernel(SampleArgs a,
   if (!is_token(top) || r.t == 0.f) {
     n = 0;
   } else if (r.short_by_k() || r.short_by_min()) {
-    const float bound = r.short_by_k() ? reached_by((int)r.top_k, mine, SampleScale(top, r.t), l) : min_p_bound(r, top);
+    const int k = r.short_by_k() ? (int)r.top_k : 0;
+    const SampleScale sc(top, r.t);
+    const float bound = k == 0                 ? min_p_bound(r, top)
+                        : k <= SMP_THREADS / 2 ? reached_by(k, mine, sc, l)
+                                               : reached_by_count(k, sc, l, [&](auto f) { row.each([&](float v, int) { f(v); }); });
     if (bound > -INFINITY) n = collect(row, bound, first, ch.data + at * SMP_BINS, SMP_CHUNK_LIST, l);
     if (n > SMP_CHUNK_LIST) n = -1;
   }
@@ -892,7 +917,9 @@ __global__ __launch_bounds__(SMP_THREADS) void sample_finish_kernel(SampleArgs a
       }
     };
     float bound = k > 0 ? -INFINITY : min_p_bound(r, x.top);
-    if (k > 0 && all > SMP_LIST) {
+    if (k > SMP_THREADS / 2 && all > SMP_LIST) {  // (the counts lie before upto)
+      bound = reached_by_count(k, sc, l, [&](auto f) { entries([&](uint64_t key) { f(key_logit(key)); }); });
+    } else if (k > 0 && all > SMP_LIST) {
       uint64_t best = 0;
       entries([&](uint64_t key) { best = Larger()(best, key); });
       bound = reached_by(k, best == 0 ? -INFINITY : key_logit(best), sc, l);

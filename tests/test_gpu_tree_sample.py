@@ -276,3 +276,19 @@ def test_min_p_by_itself(V, m):
     x[4, [5, V - 3]] = INF
     x[5, V // 2:] = 2.5
     Call(x, [6], [(0.8, 0, 1, m)], rng.random(6)).check()
+
+
+@pytest.mark.parametrize("V", [300, 3000, 32000, 50001, 128256])
+@pytest.mark.parametrize("k", [255, 256, 257, 700, 1024, 1536, 1537])
+def test_long_short_lists(V, k):
+    rng = np.random.default_rng(V + k)
+    x = rng.normal(size=(7, V)) * 3
+    x[1, :min(V, 1200)] += 20  # all that count in one chunk
+    x[2] = np.round(rng.normal(size=V))
+    x[3] = -INF
+    x[3, [V - 1, 17]] = -8.0
+    x[4, [5, V - 3]] = INF
+    x[5, V // 2:] = 2.5
+    x[6, ::3] = NAN
+    for p, m in ((1, 0), (0.7, 0), (0.95, 0.001)):
+        Call(x, [7], [(0.8, k, p, m)], rng.random(7)).check()
