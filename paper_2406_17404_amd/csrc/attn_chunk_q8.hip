@@ -35,7 +35,7 @@ struct ChunkArgs {
   const float *k_scale, *v_scale;
   const int32_t *node_off, *block_table, *prefix_len;
   int q_stride, row_stride, max_blocks, B, T, n_kv_heads, group, n_blocks, max_prefix;
-  int max_parts, n_few;  // n_few rows of a sequence are 32 queries at most
+  int max_parts;
   float scale_log2e;
   float *po, *pm, *pl;  // un-normalised partials: [part][wavefront] images of the accumulators, maxima and sums of 32 queries
   int32_t* merges;      // how many tiles there are to merge, then from word 8 on 8 words for each (ChunkMerge)
@@ -49,24 +49,26 @@ constexpr int CH_LEAST = 4;
 
 struct ChunkSeq {
   int r0, n, L, tiles;  // n < 0: refused, with nothing written; L < 0: refused, rows of zeros
+  int few;              // 1: tiles of 32 queries, a wavefront per page (chunk_few), else of CH_QUERIES
   __device__ inline int cached() const { return (L + CH_KEYS - 1) / CH_KEYS; }
   __device__ inline int blocks() const { return n <= 0 ? 0 : L < 0 ? 1 : cached() + (n + CH_KEYS - 1) / CH_KEYS; }
-  // blocks, of few queries (n_few rows at most) four to a unit
-  __device__ inline int units(int n_few) const { return n <= n_few && L >= 0 ? (blocks() + 3) >> 2 : blocks(); }
+  // blocks, of few queries four to a unit
+  __device__ inline int units() const { return few ? (blocks() + 3) >> 2 : blocks(); }
   // units of all tiles, about: own rows are seen up to a tile's
-  __device__ inline float work(int n_few) const {
-    return n <= n_few || L < 0 ? (float)(tiles * units(n_few))
-                               : (float)tiles * ((float)cached() + 0.5f * (float)((n + CH_KEYS - 1) / CH_KEYS + 1));
+  __device__ inline float work() const {
+    return few || L < 0 ? (float)(tiles * units())
+                        : (float)tiles * ((float)cached() + 0.5f * (float)((n + CH_KEYS - 1) / CH_KEYS + 1));
   }
 };
 __device__ inline ChunkSeq chunk_seq(const ChunkArgs& a, int s) {
-  ChunkSeq q{0, 0, 0, 0};
+  ChunkSeq q{0, 0, 0, 0, 0};
   if (s >= a.B) return q;
   const int r0 = a.node_off[s], r1 = a.node_off[s + 1], L = a.prefix_len[s];
   q.r0 = r0;
   q.n = r0 < 0 || r1 < r0 || r1 > a.T ? -1 : r1 - r0;
   q.L = L >= 0 && L <= a.max_prefix && L <= (int64_t)q8_pages_at_most(a.max_blocks) * 32 ? L : -1;
   q.tiles = q.n <= 0 ? 0 : (q.n * a.group + CH_QUERIES - 1) / CH_QUERIES;
+  q.few = q.n > 0 && q.n * a.group <= 32 && q.L >= 0;
   return q;
 }
 
@@ -75,7 +77,7 @@ struct ChunkWork {
   int s, nth, splits, part0, merge0;  // first partial and first merge of the sequence
 };
 struct ChunkMerge {
-  int r0, n, tile, head, splits, part, step, pad;  // partial of split k: part + k * step
+  int r0, q0, q1, head, splits, part, step, pad;  // queries of the sequence; partial of split k: part + k * step
 };
 // The plan, the same on every wavefront of every workgroup: a split has `span` units at most, of one sequence evenly many.
 // Up to 64 sequences (not MANY) 64 spans are weighed, one per lane, the longest sequence in 1 .. 32 splits, then 36 .. 160
@@ -85,6 +87,7 @@ struct ChunkMerge {
 // A unit is what a compute unit takes for a block of 256 queries, 2.3 us, or for four of few queries (0.6 to 0.9 us each).
 // Sequences come longest first, so that what starts last is short and rounds fill up: the middle between whole rounds of
 // average items and no idle unit is taken.  Beyond 64 sequences neither is done: index order, and spans of an even share.
+constexpr int SHORT = 16;
 constexpr float START = 4.5f, MERGE = 2.5f, PART = 0.03f, EACH = 0.1f, RESIDENT = 256.f;  // one workgroup per compute unit at a time
 template <bool MANY>
 struct ChunkPlan {
@@ -96,8 +99,13 @@ struct ChunkPlan {
     float work = 0.f;
     for (int s0 = 0; s0 < (MANY ? a.B : 1); s0 += 64) {
       mine = chunk_seq(a, s0 + lane);
+      if (!MANY) {  // few workgroups even so: short sequences in tiles of 32 queries as well
+        const int tiles = mine.n <= 0 ? 0 : (mine.n * a.group + 31) >> 5;
+        if (wave_sum((float)tiles) * (float)a.n_kv_heads <= RESIDENT && mine.n > 0 && mine.L >= 0 && mine.blocks() <= SHORT)
+          mine.few = 1, mine.tiles = tiles;
+      }
       if (!MANY && a.B == 1) break;
-      work += wave_sum(MANY ? (float)mine.tiles * (float)mine.units(a.n_few) : mine.work(a.n_few));
+      work += wave_sum(MANY ? (float)mine.tiles * (float)mine.units() : mine.work());
     }
     work *= a.n_kv_heads;
     id = lane;
@@ -106,7 +114,7 @@ struct ChunkPlan {
       return;
     }
     if (a.B > 1) {  // longest first
-      const int blocks = mine.units(a.n_few);
+      const int blocks = mine.units();
       int rank = 0;
       for (int t0 = 0; t0 < a.B; t0 += 8)  // (lanes behind the last sequence have no blocks)
 #pragma unroll
@@ -116,16 +124,16 @@ struct ChunkPlan {
         }
       rank = lane < a.B ? rank : lane;
       auto to = [&](int v) { return __builtin_amdgcn_ds_permute(rank << 2, v); };
-      mine = ChunkSeq{to(mine.r0), to(mine.n), to(mine.L), to(mine.tiles)};
+      mine = ChunkSeq{to(mine.r0), to(mine.n), to(mine.L), to(mine.tiles), to(mine.few)};
       id = to(lane);
     }
-    const int blocks = mine.units(a.n_few), longest = max(lane_value(blocks, 0), 1), groups = mine.tiles * a.n_kv_heads;
+    const int blocks = mine.units(), longest = max(lane_value(blocks, 0), 1), groups = mine.tiles * a.n_kv_heads;
     span = longest;
     if (a.max_parts == 0 || longest == 1) return;
     const int most = lane < 32 ? lane + 1 : 32 + 4 * (lane - 31), c = (longest + most - 1) / most;
     const float each = __builtin_amdgcn_rcpf((float)c);
     float n = 0.f, parts = 0.f;
-    if (a.B == 1) work = wave_sum(mine.work(a.n_few)) * a.n_kv_heads;  // (lanes behind the first have none)
+    if (a.B == 1) work = wave_sum(mine.work()) * a.n_kv_heads;  // (lanes behind the first have none)
     for (int t = 0; t < a.B; ++t) {
       const int b = lane_value(blocks, t), g = lane_value(groups, t);
       const float k = floorf(((float)(b + c) - 0.5f) * each);  // ceil(b / c)
@@ -144,12 +152,12 @@ struct ChunkPlan {
       if (wave_sum(k > 1 ? (float)groups * (float)k : 0.f) > (float)a.max_parts) span = longest;
     }
   }
-  __device__ inline int splits(const ChunkSeq& q) const { return (q.units(a.n_few) + span - 1) / span; }
+  __device__ inline int splits(const ChunkSeq& q) const { return (q.units() + span - 1) / span; }
   // item x of all, of which a (sequence, tile, K/V head) counts its splits
   __device__ inline bool find(int x, ChunkWork& w) {
     const int lane = threadIdx.x & 63;
     if (!MANY && a.B == 1) {
-      w.seq = ChunkSeq{lane_value(mine.r0, 0), lane_value(mine.n, 0), lane_value(mine.L, 0), lane_value(mine.tiles, 0)};
+      w.seq = ChunkSeq{lane_value(mine.r0, 0), lane_value(mine.n, 0), lane_value(mine.L, 0), lane_value(mine.tiles, 0), lane_value(mine.few, 0)};
       w.s = w.part0 = w.merge0 = 0;
       w.nth = x;
       w.splits = splits(w.seq);
@@ -163,7 +171,7 @@ struct ChunkPlan {
       const uint64_t here = __ballot(x < upto);
       if (here) {
         const int l = __builtin_ctzll(here);
-        w.seq = ChunkSeq{lane_value(mine.r0, l), lane_value(mine.n, l), lane_value(mine.L, l), lane_value(mine.tiles, l)};
+        w.seq = ChunkSeq{lane_value(mine.r0, l), lane_value(mine.n, l), lane_value(mine.L, l), lane_value(mine.tiles, l), lane_value(mine.few, l)};
         w.s = lane_value(id, l);
         w.splits = lane_value(k, l);
         const int gl = lane_value(g, l);
@@ -193,7 +201,7 @@ struct ChunkPlan {
 // Infinities and NaN among V rows that some query of the tile does not see are left out of the products (times
 // the weight 0 they would be NaN) and added here, rarely, to the stored results of those who do see them: rows
 // from..row of the sequence.
-__device__ inline void chunk_add_odd_values(const ChunkArgs& a, const ChunkSeq& seq, int head, int dh, int q0, int q1, int from) {
+__device__ inline void chunk_add_odd_values(const ChunkArgs& a, int r0, int head, int dh, int q0, int q1, int from) {
   __builtin_amdgcn_s_waitcnt(0);  // the stores are in the L2
   __syncthreads();
 #pragma unroll 1
@@ -206,12 +214,12 @@ __device__ inline void chunk_add_odd_values(const ChunkArgs& a, const ChunkSeq& 
     for (int j = from; j <= row; ++j) {
 #pragma unroll
       for (int e = 0; e < 2; ++e) {
-        const uint16_t x = v[(size_t)(seq.r0 + j) * a.row_stride + e];
+        const uint16_t x = v[(size_t)(r0 + j) * a.row_stride + e];
         if ((x & 0x7f80) == 0x7f80) sum[e] += bf2f(x), odd = true;
       }
     }
     if (!odd) continue;
-    uint32_t* const at = reinterpret_cast<uint32_t*>(a.out + ((size_t)(seq.r0 + row) * a.n_kv_heads * a.group + head * a.group + q % a.group) * dh + c);
+    uint32_t* const at = reinterpret_cast<uint32_t*>(a.out + ((size_t)(r0 + row) * a.n_kv_heads * a.group + head * a.group + q % a.group) * dh + c);
     const uint32_t was = __hip_atomic_load(at, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
     *at = pack2bf(bf2f((uint16_t)was) + sum[0], bf2f((uint16_t)(was >> 16)) + sum[1]);
   }
@@ -238,8 +246,8 @@ struct ChunkLds {
   }
 };
 
-// A sequence of 32 queries at most: every wavefront has them all and pages of its own, each CH_WAVES-th of the range, whose codes
-// come to slots of its own in LDS and go from there to the matrix units; the last wavefront takes the sequence's own rows first.
+// A tile of 32 queries: every wavefront has them all and pages of its own, each CH_WAVES-th of the range, first of the
+// sequence's own rows, then of the cache, whose codes come to slots of its own in LDS and go from there to the matrix units.
 // The wavefronts' sums are joined at the end.  In the other form seven wavefronts would only bring blocks for one: 64 sequences of
 // a row over 2000 positions, 32 heads on 8, took 142 us so and take 79 here, one row over 131072, 64 heads on 8, 112 and 57
 // (268 MB, 4.7 TB/s).
@@ -250,14 +258,14 @@ struct FewLds {
   static constexpr int BYTES = std::max(CH_WAVES * SLOTS * SLOT, CH_WAVES * (IMAGE + 2 * 32) * 4);
 };
 template <int DH>
-__device__ __forceinline__ bool chunk_few(const ChunkArgs& a, const ChunkWork& w, int head, int sp, int part, uint8_t* smem) {
+__device__ __forceinline__ bool chunk_few(const ChunkArgs& a, const ChunkWork& w, int head, int sp, int part, int q0, int q1, uint8_t* smem) {
   using Lds = FewLds<DH>;
   constexpr int MT = DH / 32, STEPS = DH / 16, OW = Lds::IMAGE, P = Lds::P, SLOTS = Lds::SLOTS, SLOT = Lds::SLOT;
   const int tid = threadIdx.x, lane = tid & 63, n32 = lane & 31, hh = lane >> 5;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const ChunkSeq& seq = w.seq;
-  const int nq = seq.n * a.group, qi = min(n32, nq - 1), my_row = qi / a.group;
-  const int pages = (seq.L + 31) >> 5, all = pages + 1;
+  const int qi = min(q0 + n32, q1 - 1), my_row = qi / a.group;
+  const int pages = (seq.L + 31) >> 5, all = pages + (q1 - 1) / a.group / 32 + 1;  // the cache's, then own rows, 32 to a page
   const int p0 = (int)((int64_t)all * sp / w.splits), p1 = (int)((int64_t)all * (sp + 1) / w.splits), pend = min(p1, pages);
   const int mine = __builtin_amdgcn_readfirstlane(p0 + wave < pend ? (pend - p0 - wave + CH_WAVES - 1) / CH_WAVES : 0);
   const int32_t* const table = a.block_table + (size_t)w.s * a.max_blocks;
@@ -306,10 +314,13 @@ __device__ __forceinline__ bool chunk_few(const ChunkArgs& a, const ChunkWork& w
   };
   look_up(0);
   int odd = 0;
-  if (wave == CH_WAVES - 1 && p1 == all) {  // own rows
+  const int own0 = max(p0, pages), partly = first_partly_seen(q0 / a.group);
+#pragma unroll 1
+  for (int p = own0 + ((wave - (own0 - p0)) & (CH_WAVES - 1)); p < p1; p += CH_WAVES) {  // own rows
+    const int j0 = (p - pages) * 32;
     const size_t row = (size_t)a.row_stride, first = (size_t)seq.r0 * row + (size_t)head * DH;
     bf16x8 k[STEPS];
-    const uint16_t* const kp = a.k_rows + first + min(n32, seq.n - 1) * row + hh * 16;
+    const uint16_t* const kp = a.k_rows + first + min(j0 + n32, seq.n - 1) * row + hh * 16;
 #pragma unroll
     for (int j = 0; j < STEPS; ++j) k[j] = *reinterpret_cast<const bf16x8*>(kp + 32 * (j >> 1) + 8 * (j & 1));
     uint32_t v[MT][2][4];
@@ -317,11 +328,11 @@ __device__ __forceinline__ bool chunk_few(const ChunkArgs& a, const ChunkWork& w
     for (int kg = 0; kg < 2; ++kg)
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
-        const uint16_t* const vp = a.v_rows + first + min(16 * kg + 8 * (e >> 2) + 4 * hh + (e & 3), seq.n - 1) * row + n32;
+        const uint16_t* const vp = a.v_rows + first + min(j0 + 16 * kg + 8 * (e >> 2) + 4 * hh + (e & 3), seq.n - 1) * row + n32;
 #pragma unroll
         for (int mt = 0; mt < MT; ++mt) {
           uint32_t x = vp[32 * mt];
-          const bool is_odd = (x & 0x7f80u) == 0x7f80u;
+          const bool is_odd = j0 >= partly && (x & 0x7f80u) == 0x7f80u;
           odd |= (int)is_odd;
           x = is_odd ? 0u : x;
           v[mt][kg][e >> 1] = e & 1 ? v[mt][kg][e >> 1] | x << 16 : x;
@@ -334,7 +345,7 @@ __device__ __forceinline__ bool chunk_few(const ChunkArgs& a, const ChunkWork& w
     for (int j = 0; j < STEPS; ++j) s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k[j], qreg[j], s, 0, 0, 0);
 #pragma unroll
     for (int i = 0; i < 16; ++i)
-      if (8 * (i >> 2) + (i & 3) + 4 * hh > my_row) s[i] = -INFINITY;
+      if (j0 + 8 * (i >> 2) + (i & 3) + 4 * hh > my_row) s[i] = -INFINITY;
     weigh(s);
 #pragma unroll
     for (int kg = 0; kg < 2; ++kg)
@@ -449,7 +460,7 @@ __device__ __forceinline__ bool chunk_few(const ChunkArgs& a, const ChunkWork& w
 #pragma unroll
     for (int k = 0; k < CH_WAVES; ++k) r += *reinterpret_cast<const f32x4*>(sum_o + k * OW + u * 256 + lane * 4) * share[k];
     r *= inv;
-    if (n32 >= nq) continue;
+    if (q0 + n32 >= q1) continue;
     if (!split)
       *reinterpret_cast<u32x2*>(a.out + ((size_t)(seq.r0 + my_row) * a.n_kv_heads * a.group + head * a.group + qi % a.group) * DH + 32 * (u >> 2) + 8 * (u & 3) + 4 * hh) =
           u32x2{pack2bf(r[0], r[1]), pack2bf(r[2], r[3])};
@@ -482,7 +493,7 @@ __global__ __launch_bounds__(CH_THREADS, 2) void chunk_attn_q8_kernel(ChunkArgs 
   const int nq = seq.n * a.group, splits = w.splits;
   const int head = w.nth % a.n_kv_heads, sp = w.nth / a.n_kv_heads % splits, tile = seq.tiles - 1 - w.nth / a.n_kv_heads / splits;
   const int row_len = a.n_kv_heads * a.group * DH;
-  const int q0 = tile * CH_QUERIES, q1 = min(nq, q0 + CH_QUERIES);
+  const int q0 = tile * (seq.few ? 32 : CH_QUERIES), q1 = min(nq, q0 + (seq.few ? 32 : CH_QUERIES));
   const bool judge = head == 0 && sp == 0 && tile == 0;
   if (seq.L < 0) {
     const int width = DH / 4;
@@ -499,7 +510,7 @@ __global__ __launch_bounds__(CH_THREADS, 2) void chunk_attn_q8_kernel(ChunkArgs 
     const int tiles_done = w.nth / a.n_kv_heads / splits, merge = w.merge0 + tiles_done * a.n_kv_heads + head;
     if (sp == 0 && tid == 0 && merge < CH_MAX_MERGES) {
       const bool room = w.part0 + (tiles_done + 1) * splits * a.n_kv_heads <= a.max_parts;  // (else ranges that overlap)
-      reinterpret_cast<ChunkMerge*>(a.merges + 8)[merge] = ChunkMerge{seq.r0, seq.n, tile, head, room ? splits : 0, part, a.n_kv_heads, 0};
+      reinterpret_cast<ChunkMerge*>(a.merges + 8)[merge] = ChunkMerge{seq.r0, q0, q1, head, room ? splits : 0, part, a.n_kv_heads, 0};
     }
   }
   auto verdict = [&]() {
@@ -508,9 +519,9 @@ __global__ __launch_bounds__(CH_THREADS, 2) void chunk_attn_q8_kernel(ChunkArgs 
     bad = __syncthreads_or(bad);
     if (tid == 0) a.status[w.s] = bad;
   };
-  if (seq.n <= a.n_few) {
-    const bool any_odd = chunk_few<DH>(a, w, head, sp, part, smem);
-    if (any_odd && splits == 1) chunk_add_odd_values(a, seq, head, DH, 0, nq, 0);
+  if (seq.few) {
+    const bool any_odd = chunk_few<DH>(a, w, head, sp, part, q0, q1, smem);
+    if (any_odd && splits == 1) chunk_add_odd_values(a, seq.r0, head, DH, q0, q1, first_partly_seen(q0 / a.group));
     if (judge) verdict();
     return;
   }
@@ -843,7 +854,7 @@ __global__ __launch_bounds__(CH_THREADS, 2) void chunk_attn_q8_kernel(ChunkArgs 
           *reinterpret_cast<u32x2*>(dst + 32 * mt + 8 * g) = v;
         }
     }
-    if (any_odd) chunk_add_odd_values(a, seq, head, DH, q0, q1, first_partly_seen(row_first));
+    if (any_odd) chunk_add_odd_values(a, seq.r0, head, DH, q0, q1, first_partly_seen(row_first));
   } else {
     if (live_wave && part < a.max_parts) {  // (else more work than T rows can be: ranges that overlap)
       const size_t image = (size_t)part * CH_WAVES + wave;
@@ -876,8 +887,8 @@ __global__ __launch_bounds__(128 * (DH / 32)) void chunk_merge_kernel(ChunkArgs 
   for (int u = blockIdx.x; u < all; u += gridDim.x) {
     const int x = u / CH_WAVES, wave = u % CH_WAVES;
     const ChunkMerge w = reinterpret_cast<const ChunkMerge*>(a.merges + 8)[x];
-    const int nq = w.n * a.group, q0 = w.tile * CH_QUERIES, qw = q0 + wave * 32, qi = qw + n32;
-    if (qw >= nq || w.splits == 0) continue;
+    const int qw = w.q0 + wave * 32, qi = qw + n32;
+    if (qw >= w.q1 || w.splits == 0) continue;
     float m = NO_REFERENCE, l = 0.f;
     bool odd = false;
     f32x4 o[4] = {};
@@ -891,7 +902,7 @@ __global__ __launch_bounds__(128 * (DH / 32)) void chunk_merge_kernel(ChunkArgs 
         pl[k] = a.pl[image * 32 + n32];
 #pragma unroll
         for (int g = 0; g < 4; ++g)
-          po[k][g] = qi < nq ? *reinterpret_cast<const f32x4*>(a.po + image * OW + (mt * 4 + g) * 256 + lane * 4) : f32x4{0, 0, 0, 0};
+          po[k][g] = qi < w.q1 ? *reinterpret_cast<const f32x4*>(a.po + image * OW + (mt * 4 + g) * 256 + lane * 4) : f32x4{0, 0, 0, 0};
       }
       float top = m;
 #pragma unroll
@@ -917,7 +928,7 @@ __global__ __launch_bounds__(128 * (DH / 32)) void chunk_merge_kernel(ChunkArgs 
       if (mt == 0 && hh == 0) sm_m[n32] = m, sm_l[n32] = l;
     }
     const bool any_odd = __syncthreads_or(odd);
-    if (h == 0 && qi < nq) {
+    if (h == 0 && qi < w.q1) {
       const float top = fmaxf(m, sm_m[n32]), keep = __builtin_amdgcn_exp2f(m - top), f = __builtin_amdgcn_exp2f(sm_m[n32] - top);
       const float inv = 1.0f / (l * keep + sm_l[n32] * f);
       uint16_t* dst = a.out + ((size_t)(w.r0 + qi / a.group) * a.n_kv_heads * a.group + w.head * a.group + qi % a.group) * DH + 32 * mt + 4 * hh;
@@ -927,7 +938,7 @@ __global__ __launch_bounds__(128 * (DH / 32)) void chunk_merge_kernel(ChunkArgs 
         *reinterpret_cast<u32x2*>(dst + 8 * g) = u32x2{pack2bf(r[0], r[1]), pack2bf(r[2], r[3])};
       }
     }
-    if (any_odd) chunk_add_odd_values(a, ChunkSeq{w.r0, w.n, 0, 0}, w.head, DH, qw, min(nq, qw + 32), first_partly_seen(q0 / a.group));
+    if (any_odd) chunk_add_odd_values(a, w.r0, w.head, DH, qw, min(w.q1, qw + 32), first_partly_seen(w.q0 / a.group));
     __syncthreads();  // LDS is free again
   }
 }
@@ -948,7 +959,8 @@ static int chunk_run(const ChunkArgs& a, hipStream_t st) {
   static DeviceOnce once;
   allow_lds(once, chunk_attn_q8_kernel<DH, MANY>, lds);
   const long items = ((long)a.T * a.group / CH_QUERIES + a.B) * a.n_kv_heads;
-  const int grid = (int)std::min(items + a.max_parts, 1l << 30);
+  const long few = MANY ? 0 : std::min(((long)a.T * a.group / 32 + a.B) * a.n_kv_heads, (long)RESIDENT);  // of short sequences
+  const int grid = (int)std::min(items + few + a.max_parts, 1l << 30);
   chunk_attn_q8_kernel<DH, MANY><<<grid, CH_THREADS, lds, st>>>(a);
   int rc = check_launch();
   if (rc != TRJ_OK || a.max_parts == 0) return rc;
@@ -966,7 +978,7 @@ int launch_attn_chunk_q8(const uint16_t* q, int q_stride, const void* k_pool, co
   float* const pm = ws + images * 32 * head_dim;
   const ChunkArgs a{q, k_rows, v_rows, (const uint8_t*)k_pool, (const uint8_t*)v_pool, k_scale, v_scale, node_off, block_table,
                     prefix_len, q_stride, row_stride, max_blocks, B, T, n_kv_heads, group, n_blocks, max_prefix, parts,
-                    32 / group, scale * LOG2E, ws, pm, pm + images * 32, (int32_t*)(pm + images * 64), out, status};
+                    scale * LOG2E, ws, pm, pm + images * 32, (int32_t*)(pm + images * 64), out, status};
   if (B > 64) return head_dim == 128 ? chunk_run<128, true>(a, st) : chunk_run<64, true>(a, st);
   return head_dim == 128 ? chunk_run<128, false>(a, st) : chunk_run<64, false>(a, st);
 }

@@ -459,3 +459,44 @@ def test_many_pages_of_one_workgroup(dh, n):
         # 32-bit sums of up to 625 blocks in a row: half a step of 2^-23 for the weights', one for each product of the values'
         tol = HALF * (np.abs(want) + mean) * (1 + HALF) + (625 * 2 * (2.0 ** -24 + 2 * 2.0 ** -23) + 2.0 ** -12) * mean
         assert (np.abs(got[:, h:h + 1] - want) <= tol).all()
+
+
+@pytest.mark.parametrize("L,n", [(0, 33), (0, 64), (0, 65), (1, 33), (31, 40), (32, 64), (33, 63), (63, 33), (64, 64), (65, 50), (100, 96),
+                                 (257, 130)])
+def test_short_sequences_of_many_heads(L, n):
+    # more tiles of 32 queries than are taken one by one
+    c = Call(np.random.default_rng(7 * L + n), [L], [n], 140, 140, 64)
+    c.check()
+
+
+@pytest.mark.parametrize("heads,kv_heads,dh", [(2, 1, 64), (4, 2, 128), (3, 1, 128)])
+@pytest.mark.parametrize("L,n", [(0, 1100), (1, 1089), (33, 1025), (95, 1030), (1000, 17), (1023, 90), (1025, 33)])
+def test_sequences_just_beyond_short_ones(heads, kv_heads, dh, L, n):
+    Call(np.random.default_rng(L + n), [L], [n], heads, kv_heads, dh).check()
+
+
+@pytest.mark.parametrize("seed", range(4))
+def test_short_sequences_beside_long_ones(seed):
+    rng = np.random.default_rng(950 + seed)
+    kv_heads, group, dh = int(rng.integers(1, 4)), int(rng.choice([1, 4, 8])), int(rng.choice([64, 128]))
+    lens = [int(x) for x in rng.choice([0, 20, 300, 800, 1500, 3000], 6)]
+    sizes = [int(x) for x in rng.choice([1, 5, 33, 50, 90], 6)]
+    c = Call(rng, lens, sizes, kv_heads * group, kv_heads, dh, behind=1)
+    c.check()
+    assert not c.status.any()
+
+
+@pytest.mark.parametrize("value", [float("nan"), float("inf")])
+@pytest.mark.parametrize("j", [0, 40, 63, 64, 100, 149])
+def test_what_is_not_finite_in_a_short_prompt(value, j):
+    c = Call(np.random.default_rng(24), [30], [150], 4, 2, 64)
+    clean = c.check()
+    c.kr[j, 0, 3] = value
+    c.vr[j, 1, 5] = value
+    got = c.run()
+    assert np.array_equal(got[:j], clean[:j])
+    assert (np.isnan if value != value else np.isinf)(got[j:, 2:, 5]).all()
+    if value != value:
+        assert np.isnan(got[j:, :2]).all()
+    keep = [d for d in range(64) if d != 5]
+    assert np.array_equal(got[j:, 2:][:, :, keep], clean[j:, 2:][:, :, keep])
