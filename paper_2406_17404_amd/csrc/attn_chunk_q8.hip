@@ -47,6 +47,11 @@ constexpr int CH_MAX_PARTS = 512, CH_MAX_MERGES = CH_MAX_PARTS / 2;  // partials
 // Calls in which no sequence can have more blocks have neither partials nor a merge; beyond 64 sequences a split's least span.
 constexpr int CH_LEAST = 4;
 
+// Queries of a sequence that are taken 32 at a time, with a wavefront per page (chunk_few): a block takes such a workgroup 0.4 to
+// 0.9 us, one of the other form 1.5 with few wavefronts at work.  40 sequences of 8 rows over 2000 positions, 64 heads on 8: 82 us so,
+// 130 else; of 128 queries, 64 sequences of 30 rows over 4000, 32 on 8, 342 and 285.
+constexpr int CH_FEW = 64;
+
 struct ChunkSeq {
   int r0, n, L, tiles;  // n < 0: refused, with nothing written; L < 0: refused, rows of zeros
   int few;              // 1: tiles of 32 queries, a wavefront per page (chunk_few), else of CH_QUERIES
@@ -67,8 +72,8 @@ __device__ inline ChunkSeq chunk_seq(const ChunkArgs& a, int s) {
   q.r0 = r0;
   q.n = r0 < 0 || r1 < r0 || r1 > a.T ? -1 : r1 - r0;
   q.L = L >= 0 && L <= a.max_prefix && L <= (int64_t)q8_pages_at_most(a.max_blocks) * 32 ? L : -1;
-  q.tiles = q.n <= 0 ? 0 : (q.n * a.group + CH_QUERIES - 1) / CH_QUERIES;
-  q.few = q.n > 0 && q.n * a.group <= 32 && q.L >= 0;
+  q.few = q.n > 0 && q.n * a.group <= CH_FEW && q.L >= 0;
+  q.tiles = q.n <= 0 ? 0 : q.few ? (q.n * a.group + 31) >> 5 : (q.n * a.group + CH_QUERIES - 1) / CH_QUERIES;
   return q;
 }
 
@@ -87,7 +92,7 @@ struct ChunkMerge {
 // A unit is what a compute unit takes for a block of 256 queries, 2.3 us, or for four of few queries (0.6 to 0.9 us each).
 // Sequences come longest first, so that what starts last is short and rounds fill up: the middle between whole rounds of
 // average items and no idle unit is taken.  Beyond 64 sequences neither is done: index order, and spans of an even share.
-constexpr int SHORT = 16;
+constexpr int SHORT = 96;  // blocks
 constexpr float START = 4.5f, MERGE = 2.5f, PART = 0.03f, EACH = 0.1f, RESIDENT = 256.f;  // one workgroup per compute unit at a time
 template <bool MANY>
 struct ChunkPlan {
@@ -99,9 +104,12 @@ struct ChunkPlan {
     float work = 0.f;
     for (int s0 = 0; s0 < (MANY ? a.B : 1); s0 += 64) {
       mine = chunk_seq(a, s0 + lane);
-      if (!MANY) {  // few workgroups even so: short sequences in tiles of 32 queries as well
+      if (!MANY) {
+        // Where all tiles of 32 queries fit one round, short sequences (and longer ones of four tiles) come in such tiles: 40
+        // rows after 500 positions, 32 heads on 8, took 20 us in the other form and take 14, 100 after 3500 38 and 30, 128 after 8000,
+        // the border, 45 and 48, 16 after 130000 119 and 70.
         const int tiles = mine.n <= 0 ? 0 : (mine.n * a.group + 31) >> 5;
-        if (wave_sum((float)tiles) * (float)a.n_kv_heads <= RESIDENT && mine.n > 0 && mine.L >= 0 && mine.blocks() <= SHORT)
+        if (wave_sum((float)tiles) * (float)a.n_kv_heads <= RESIDENT && mine.n > 0 && mine.L >= 0 && (mine.blocks() <= SHORT || tiles <= 4))
           mine.few = 1, mine.tiles = tiles;
       }
       if (!MANY && a.B == 1) break;
@@ -958,9 +966,10 @@ static int chunk_run(const ChunkArgs& a, hipStream_t st) {
   constexpr size_t lds = std::max(ChunkLds<DH>::BYTES, FewLds<DH>::BYTES);
   static DeviceOnce once;
   allow_lds(once, chunk_attn_q8_kernel<DH, MANY>, lds);
-  const long items = ((long)a.T * a.group / CH_QUERIES + a.B) * a.n_kv_heads;
-  const long few = MANY ? 0 : std::min(((long)a.T * a.group / 32 + a.B) * a.n_kv_heads, (long)RESIDENT);  // of short sequences
-  const int grid = (int)std::min(items + few + a.max_parts, 1l << 30);
+  const long queries = (long)a.T * a.group, most = (queries / 32 + a.B) * a.n_kv_heads;
+  const long tiles = std::min(most, (queries / CH_QUERIES + CH_FEW / 32 * a.B) * a.n_kv_heads);
+  const long items = MANY ? tiles : std::min(most, tiles + (long)RESIDENT);  // with those of short sequences
+  const int grid = (int)std::min(items + a.max_parts, 1l << 30);
   chunk_attn_q8_kernel<DH, MANY><<<grid, CH_THREADS, lds, st>>>(a);
   int rc = check_launch();
   if (rc != TRJ_OK || a.max_parts == 0) return rc;

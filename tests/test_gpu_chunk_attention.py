@@ -500,3 +500,50 @@ def test_what_is_not_finite_in_a_short_prompt(value, j):
         assert np.isnan(got[j:, :2]).all()
     keep = [d for d in range(64) if d != 5]
     assert np.array_equal(got[j:, 2:][:, :, keep], clean[j:, 2:][:, :, keep])
+
+
+@pytest.mark.parametrize("L,n", [(0, 129), (0, 192), (0, 193), (1, 130), (31, 160), (33, 129), (63, 255), (64, 256), (65, 257), (100, 150),
+                                 (257, 130), (1000, 133)])
+def test_longer_sequences_of_many_heads(L, n):
+    # and more than 128 queries of a head
+    c = Call(np.random.default_rng(9 * L + n), [L], [n], 140, 140, 64, wide=8 * (n % 2))
+    c.check()
+
+
+@pytest.mark.parametrize("dh,heads", [(64, 140), (128, 70)])
+def test_packed_sequences_of_many_heads(dh, heads):
+    c = Call(np.random.default_rng(dh), [70, 0, 1000, 33], [150, 140, 1, 260], heads, heads // 2, dh, behind=2)
+    c.check()
+    assert not c.status.any()
+
+
+@pytest.mark.parametrize("value", [float("nan"), float("inf")])
+@pytest.mark.parametrize("j", [0, 63, 64, 100, 149])
+def test_what_is_not_finite_with_many_heads(value, j):
+    c = Call(np.random.default_rng(25), [30], [150], 140, 70, 64)
+    clean = c.check()
+    c.kr[j, 0, 3] = value
+    c.vr[j, 1, 5] = value
+    got = c.run()
+    assert np.array_equal(got[:j], clean[:j])
+    assert (np.isnan if value != value else np.isinf)(got[j:, 2:4, 5]).all()
+    if value != value:
+        assert np.isnan(got[j:, :2]).all()
+    keep = [d for d in range(64) if d != 5]
+    assert np.array_equal(got[j:, 2:][:, :, keep], clean[j:, 2:][:, :, keep])
+
+
+@pytest.mark.parametrize("n", [129, 200])
+def test_far_scores_and_unused_slots_with_many_heads(n):
+    c = Call(np.random.default_rng(26), [41], [n], 140, 140, 64)
+    want = c.check()
+    for w in "kv":
+        page = c.cache.pool[w][:, :, c.cache.table[0, 1]]
+        page[..., S.offsets(64, w)[9:]] = NAN_CODE
+        c.cache.pool[w][:, :, c.cache.table[0, 1]] = page
+    assert np.array_equal(c.run(), want)
+    c = Call(np.random.default_rng(27), [40], [n], 140, 140, 64, scale=1e30)
+    c.q = -c.q.abs()
+    c.cache.pool["k"][:] &= 127  # every score below -1e30
+    c.kr = c.kr.abs()
+    assert np.isfinite(c.run()).all()
