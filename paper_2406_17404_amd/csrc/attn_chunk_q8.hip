@@ -11,13 +11,13 @@
 // Cached blocks (two pages) are converted on the way, codes times their power-of-two scale being bf16 numbers
 // exactly; the sequence's own rows are bf16 already and V is transposed.
 //
-// Bound by products for long chunks: 2048 rows after 16384 positions, 32 heads of 128, are 584 GFLOP in 640 to 680 us, 0.86 to
+// Bound by products for long chunks: 2048 rows after 16384 positions, 32 heads of 128, are 584 GFLOP in 640 to 710 us, 0.82 to
 // 0.91 PFLOP/s where a large library product reaches 1.19 to 1.33 on the same card.  The matrix units work 45 % of the
 // cycles, at a clock of 1.9 GHz under this load, LDS is active in 36 %, and a tile of 32 keys x 32 queries takes 152 vector
 // instructions beside its 16 products.  No part stands out: with one left out (675 us whole) the exponentials save 25 us, reading operands 56,
 // the conversion 75, conversion and loads 128.  Less per product would take more queries per wavefront, and two query tiles'
 // accumulators, weights and queries do not fit its 256 registers.
-// A whole prompt of 4096 rows, 32 heads on 8, takes 190 us (0.72), a third of it masked or partly seen tiles and start.
+// A whole prompt of 4096 rows, 32 heads on 8, takes 190 to 200 us (0.7), a third of it masked or partly seen tiles and start.
 // For short ones by the way to the first block and from the last: 12 us for an item of one block (plan 0.5, queries 0.8,
 // first codes 1.2, their conversion and barrier 1.4, two masked tiles 2.9, end 2.1; code that is not in the instruction cache yet
 // is in each), against 2.5 us per block of 256 queries, and by the merge's launch, 5 to 17 us with its traffic.
