@@ -93,6 +93,7 @@ struct ChunkMerge {
 // Sequences come longest first, so that what starts last is short and rounds fill up: the middle between whole rounds of
 // average items and no idle unit is taken.  Beyond 64 sequences neither is done: index order, and spans of an even share.
 constexpr int SHORT = 96;  // blocks
+constexpr float FEW_TILES = 32.f;
 constexpr float START = 4.5f, MERGE = 2.5f, PART = 0.03f, EACH = 0.1f, RESIDENT = 256.f;  // one workgroup per compute unit at a time
 template <bool MANY>
 struct ChunkPlan {
@@ -105,11 +106,12 @@ struct ChunkPlan {
     for (int s0 = 0; s0 < (MANY ? a.B : 1); s0 += 64) {
       mine = chunk_seq(a, s0 + lane);
       if (!MANY) {
-        // Where all tiles of 32 queries fit one round, short sequences (and longer ones of four tiles) come in such tiles: 40
-        // rows after 500 positions, 32 heads on 8, took 20 us in the other form and take 14, 100 after 3500 38 and 30, 128 after 8000,
-        // the border, 45 and 48, 16 after 130000 119 and 70.
+        // Where all tiles of 32 queries fit one round, short sequences come in such tiles, and longer ones of four tiles, or of any
+        // number if they are few in all: 40 rows after 500 positions, 32 heads on 8, took 20 us in the other form and take 14, 100 after
+        // 3500 38 and 30, 128 after 8000, the border, 45 and 48; 16 after 130000 119 and 70; 64 after 30000, 8 heads on one, 47 and 32.
         const int tiles = mine.n <= 0 ? 0 : (mine.n * a.group + 31) >> 5;
-        if (wave_sum((float)tiles) * (float)a.n_kv_heads <= RESIDENT && mine.n > 0 && mine.L >= 0 && (mine.blocks() <= SHORT || tiles <= 4))
+        const float all = wave_sum((float)tiles) * (float)a.n_kv_heads;
+        if (all <= RESIDENT && mine.n > 0 && mine.L >= 0 && (mine.blocks() <= SHORT || tiles <= 4 || all <= FEW_TILES))
           mine.few = 1, mine.tiles = tiles;
       }
       if (!MANY && a.B == 1) break;

@@ -547,3 +547,26 @@ def test_far_scores_and_unused_slots_with_many_heads(n):
     c.cache.pool["k"][:] &= 127  # every score below -1e30
     c.kr = c.kr.abs()
     assert np.isfinite(c.run()).all()
+
+
+@pytest.mark.parametrize("heads,kv_heads,dh,n", [(16, 8, 64, 100), (16, 8, 128, 77), (40, 8, 64, 130), (24, 24, 64, 140)])
+@pytest.mark.parametrize("L", [9000, 6500 - 31, 12001])
+def test_long_sequences_of_several_heads(heads, kv_heads, dh, n, L):
+    # split, in tiles of 256 queries
+    c = Call(np.random.default_rng(L + n), [L], [n], heads, kv_heads, dh)
+    clean = c.check()
+    assert list(c.status) == [0]
+    last, used = c.cache.table[0, (L - 1) // 32], (L - 1) % 32 + 1
+    for w in "kv":
+        page = c.cache.pool[w][:, :, last]
+        page[..., S.offsets(dh, w)[used:]] = NAN_CODE
+        c.cache.pool[w][:, :, last] = page
+    assert np.array_equal(c.run(), clean)
+    j, g = n - 20, heads // kv_heads
+    c.kr[j, 0, 3] = c.vr[j, 1, 5] = float("nan")
+    got = c.run()
+    assert np.array_equal(got[:j], clean[:j]) and np.isnan(got[j:, :g]).all() and np.isnan(got[j:, g:2 * g, 5]).all()
+    keep = [d for d in range(dh) if d != 5]
+    assert np.array_equal(got[j:, g:][:, :, keep], clean[j:, g:][:, :, keep])
+    c.cache.table[0, 100] = -1
+    assert np.isnan(c.run()).all() and list(c.status) == [1]
