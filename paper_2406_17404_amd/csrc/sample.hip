@@ -736,8 +736,9 @@ __device__ inline void give_first(const SampleArgs& a, int t, uint64_t best) {
 }
 
 __device__ inline float min_p_bound(const SampleRules& r, float top) {
-  // a token below it weighs less than `least`, by far more than a weight's error
-  return (float)((double)top + log((double)r.least * 0.999 / SMP_UNIT) * r.t - fabs((double)top) * 1e-6);
+  // A weight is rounded to nearest: `least` from least - 0.5 of a unit on.  A token below the bound is less than that by a
+  // thousandth, far more than the errors of weights (2^-40 of them) and of the bound (2^-24 of its two terms).
+  return (float)((double)top + log(((double)r.least - 0.5) * 0.999 / SMP_UNIT) * r.t - fabs((double)top) * 1e-6);
 }
 
 // Everything from the row in memory, for the few rows that need it.

@@ -292,3 +292,21 @@ def test_long_short_lists(V, k):
     x[6, ::3] = NAN
     for p, m in ((1, 0), (0.7, 0), (0.95, 0.001)):
         Call(x, [7], [(0.8, k, p, m)], rng.random(7)).check()
+
+
+@pytest.mark.parametrize("V,least,n", [(32000, 1, 31998), (32000, 3, 8000), (32000, 275, 1500), (50001, 275, 1500), (50001, 3, 6000),
+                                       (128256, 1, 17000), (128256, 275, 1900)])
+@pytest.mark.parametrize("u", [0.5, 1 - 2.0 ** -24])
+def test_tiny_min_p_keeps_what_is_rounded_up_to_it(V, least, n, u):
+    # weights are rounded to nearest: least - 0.3 of a unit weighs `least` and is kept, least - 0.7 is not.  The kept ones
+    # together weigh more than 2^-24 of the first token, so that the largest number reaches them.
+    assert n * least > 2 ** 14
+    x = np.full((2, V), -INF, np.float32)
+    x[0, 0] = x[1, V - 1] = 0.0
+    rest = np.linspace(1, V - 2, n).astype(int)
+    x[:, rest] = np.log((least - 0.3) * 2.0 ** -38)
+    x[:, np.setdiff1d(np.arange(1, V - 1), rest)[:50]] = np.log((least - 0.7) * 2.0 ** -38)
+    c = Call(x, [2], [(1, 0, 1, least * 2.0 ** -38)], [u] * 2)
+    assert len(P.kept(c.x[0], c.rules[0])[0]) == n + 1
+    token, _ = c.check()
+    assert u < 0.6 or np.isin(token, rest).all()
