@@ -820,18 +820,28 @@ __global__ __launch_bounds__(CH_THREADS, 2) void chunk_attn_q8_kernel(ChunkArgs 
           if (8 * (v >> 2) + (v & 3) >= limit) s[v] = -INFINITY;
       }
       top = Softmax::largest(s, f);
-      // Each query's reference by itself: its result does not depend on those beside it.
+      // Each query's reference by itself, and its weights by one formula whatever the step: its result does not depend, in any bit,
+      // on those beside it, which decide which step a tile goes through.
       const float ref = top > m + SLACK ? top : m, alpha = __builtin_amdgcn_exp2f(m - ref);
       m = ref;
+      const bool is_far = fabsf(m) > 1048576.f && m != NO_REFERENCE;
+      far = __ballot(is_far) != 0;
       float p[16], sum = 0.f;
       {
 #pragma clang fp contract(off)
-        // Product and difference rounded one by one.  Fused, as above, the rounding of the reference's own product would stay in
-        // the exponent, the same for all keys: next to nothing up to 2^20, but anything far beyond (`far`).
+        // Fused as above, what the reference's own product was rounded by stays in the exponent: the same for all keys, so that it
+        // goes out with the sum, while it is small.  Far from zero it would overflow, and product and difference are rounded one by one.
+#pragma unroll
+        for (int v = 0; v < 16; ++v) p[v] = fmaf(s[v], f, -m);
+        if (far)
+#pragma unroll
+          for (int v = 0; v < 16; ++v) {
+            const float x = s[v] * f;
+            p[v] = is_far ? x - m : p[v];
+          }
 #pragma unroll
         for (int v = 0; v < 16; ++v) {
-          const float x = s[v] * f;
-          p[v] = __builtin_amdgcn_exp2f(x - m);
+          p[v] = __builtin_amdgcn_exp2f(p[v]);
           sum += p[v];
         }
       }
@@ -839,7 +849,6 @@ __global__ __launch_bounds__(CH_THREADS, 2) void chunk_attn_q8_kernel(ChunkArgs 
       l = l * alpha + sum;
       pack(p);
       if (__ballot(alpha != 1.f)) q8_rescale<MT>(o, alpha);
-      far = __ballot(fabsf(m) > 1048576.f && m != NO_REFERENCE) != 0;
       if (t == tiles - 1) break;
       scores(next_keys(t));
       top = Softmax::largest(s, f);
