@@ -348,6 +348,9 @@ def tr_verify_step_template(desc: ModelDesc, weights: Weights, k_pool, v_pool, k
 
 
 # ------------------------------------------------------------------ paged 8-bit cache
+_TOO_SMALL = "a buffer of 32-bit numbers is smaller than the sequences or rows of the call"
+
+
 def _rows(t: torch.Tensor):
     """Pointer, row stride and layer stride of rows [(layers,) T, heads, head_dim], which may be parts of
     wider rows."""
@@ -518,9 +521,11 @@ def tree_sample(logits, node_off, rules, uniform, token_out, prob_out, workspace
     T, V = logits.shape
     B = node_off.shape[0] - 1
     if logits.dtype != torch.float32 or rules.dtype != torch.float32 or uniform.dtype != torch.float32 or \
-            rules.shape != (B, 4) or uniform.numel() < T or token_out.numel() < T or \
+            rules.shape != (B, 4) or uniform.numel() < T or \
             (prob_out is not None and (prob_out.dtype != torch.float32 or prob_out.numel() < T)):
         raise ValueError("logits [T, V], rules [B, 4], uniform [T] and prob_out [T] are fp32")
+    if token_out.nbytes < 4 * T:
+        raise ValueError(_TOO_SMALL)
     _check("tree_sample", lib().tree_sample(
         _ptr(logits), _ptr(node_off), B, T, V, _ptr(rules), _ptr(uniform), _ptr(token_out), _ptr(prob_out),
         _ptr(workspace), workspace.numel() * workspace.element_size(), _ptr(status_dev), _stream()))
