@@ -475,9 +475,13 @@ def rotary_rows(q_rows, k_rows, parent, node_off, prefix_len, freqs, magnitude, 
         raise ValueError("rows and results are of the same type, rows and head_dim")
     if freqs.dtype != torch.float64:
         raise ValueError("freqs are numbers of 64 bits")
+    B = node_off.shape[0] - 1
+    if node_off.nbytes < 4 * (B + 1) or prefix_len.nbytes < 4 * B or status_dev.nbytes < 4 * B or \
+            (parent is not None and parent.nbytes < 4 * T):
+        raise ValueError(_TOO_SMALL)
     (qp, q_stride, _), (kp, k_stride, _), (qo, qo_stride, _), (ko, ko_stride, _) = map(_rows, (q_rows, k_rows, q_out, k_out))
     _check("rotary_rows", lib().rotary_rows(
-        qp, q_stride, kp, k_stride, _ptr(parent), _ptr(node_off), _ptr(prefix_len), node_off.shape[0] - 1, T, n_heads,
+        qp, q_stride, kp, k_stride, _ptr(parent), _ptr(node_off), _ptr(prefix_len), B, T, n_heads,
         n_kv_heads, head_dim, 2 * freqs.numel(), layout, _ptr(freqs), magnitude, dtype_code(q_rows.dtype), qo, qo_stride, ko,
         ko_stride, _ptr(status_dev), _stream()))
 
@@ -495,6 +499,9 @@ def chunk_attention_q8(q_rows, k_pool, v_pool, k_scale, v_scale, k_rows, v_rows,
     B, max_blocks = block_table.shape
     n_kv_heads, n_blocks = k_scale.shape
     T, n_heads, head_dim = q_rows.shape
+    if node_off.nbytes < 4 * (B + 1) or block_table.nbytes < 4 * B * max_blocks or prefix_len.nbytes < 4 * B or \
+            status_dev.nbytes < 4 * B:
+        raise ValueError(_TOO_SMALL)
     qp, q_stride, _ = _rows(q_rows)
     kp, stride, _ = _rows(k_rows)
     vp, v_stride, _ = _rows(v_rows)
@@ -524,7 +531,7 @@ def tree_sample(logits, node_off, rules, uniform, token_out, prob_out, workspace
             rules.shape != (B, 4) or uniform.numel() < T or \
             (prob_out is not None and (prob_out.dtype != torch.float32 or prob_out.numel() < T)):
         raise ValueError("logits [T, V], rules [B, 4], uniform [T] and prob_out [T] are fp32")
-    if token_out.nbytes < 4 * T:
+    if token_out.nbytes < 4 * T or node_off.nbytes < 4 * (B + 1) or status_dev.nbytes < 4 * B:
         raise ValueError(_TOO_SMALL)
     _check("tree_sample", lib().tree_sample(
         _ptr(logits), _ptr(node_off), B, T, V, _ptr(rules), _ptr(uniform), _ptr(token_out), _ptr(prob_out),
