@@ -378,6 +378,11 @@ def _check_pools(k_pool, v_pool, k_scale, v_scale, pages, head_dim):
 def kv_block_tables(block_table, held, prefix_len, node_off, T, free_list, free_count, held_out, free_count_out,
                     row_slot, status_dev):
     B, max_blocks = block_table.shape
+    if block_table.nbytes < 4 * B * max_blocks or held.nbytes < 4 * B or prefix_len.nbytes < 4 * B or \
+            node_off.nbytes < 4 * (B + 1) or free_list.nbytes < 4 * free_list.shape[0] or free_count.nbytes < 4 or \
+            held_out.nbytes < 4 * B or free_count_out.nbytes < 4 or status_dev.nbytes < 4 * B or \
+            (row_slot is not None and row_slot.nbytes < 4 * T):
+        raise ValueError(_TOO_SMALL)
     _check("kv_block_tables", lib().kv_block_tables(
         _ptr(block_table), max_blocks, _ptr(held), _ptr(prefix_len), _ptr(node_off), B, T, _ptr(free_list),
         free_list.shape[0], _ptr(free_count), _ptr(held_out), _ptr(free_count_out), _ptr(row_slot),
@@ -390,6 +395,10 @@ def kv_append_q8(k_pool, v_pool, k_scale, v_scale, k_rows, v_rows, path, accept_
     the last, rows [n_layers, T, n_kv_heads, head_dim]."""
     B, max_blocks = block_table.shape
     n_kv_heads, n_blocks = k_scale.shape[-2:]
+    if node_off.nbytes < 4 * (B + 1) or block_table.nbytes < 4 * B * max_blocks or prefix_len.nbytes < 4 * B or \
+            new_len.nbytes < 4 * B or status_dev.nbytes < 4 * B or \
+            (path is not None and (path.nbytes < 4 * B * N_MAX or accept_len is not None and accept_len.nbytes < 4 * B)):
+        raise ValueError(_TOO_SMALL)
     kp, stride, layer_stride = _rows(k_rows)
     vp, v_stride, v_layer_stride = _rows(v_rows)
     if k_rows.shape != v_rows.shape or (stride, layer_stride) != (v_stride, v_layer_stride) or k_rows.dtype != v_rows.dtype:
@@ -419,6 +428,9 @@ def tree_attention_q8(q_rows, k_pool, v_pool, k_scale, v_scale, k_rows, v_rows, 
     B, max_blocks = block_table.shape
     n_kv_heads, n_blocks = k_scale.shape
     T, n_heads, head_dim = q_rows.shape
+    if parent.nbytes < 4 * T or node_off.nbytes < 4 * (B + 1) or block_table.nbytes < 4 * B * max_blocks or \
+            prefix_len.nbytes < 4 * B or status_dev.nbytes < 4 * B:
+        raise ValueError(_TOO_SMALL)
     qp, q_stride, _ = _rows(q_rows)
     kp, stride, _ = _rows(k_rows)
     vp, v_stride, _ = _rows(v_rows)
@@ -449,11 +461,19 @@ def tree_logits(logits, tok, parent, node_off, ctx, ctx_off, gen_start, penaltie
         raise ValueError("logits and logits_out are fp32 of the same shape")
     if allowed is not None and allowed.nbytes < 4 * T * ((V + 31) // 32):
         raise ValueError("allowed has ceil(V / 32) words of 32 bits per row")
+    if parent.nbytes < 4 * T or node_off.nbytes < 4 * (B + 1) or status_dev.nbytes < 4 * B or \
+            (argmax_out is not None and argmax_out.nbytes < 4 * T) or (bias_off is not None and bias_off.nbytes < 4 * (B + 1)) or \
+            (penalties is not None and (
+                penalties.nbytes < 12 * B or tok is not None and tok.nbytes < 4 * T or
+                ctx is not None and (ctx_off is not None and ctx_off.nbytes < 4 * (B + 1) or
+                                     gen_start is not None and gen_start.nbytes < 4 * B))):
+        raise ValueError(_TOO_SMALL)
+    n_ctx = 0 if ctx is None else min(ctx.numel(), ctx.nbytes // 4)
+    n_bias = 0 if bias_val is None or bias_tok is None else min(bias_tok.numel(), bias_tok.nbytes // 4, bias_val.numel(),
+                                                                bias_val.nbytes // 4)
     _check("tree_logits", lib().tree_logits(
-        _ptr(logits), _ptr(tok), _ptr(parent), _ptr(node_off), B, T, V, _ptr(ctx), 0 if ctx is None else ctx.numel(),
-        _ptr(ctx_off), _ptr(gen_start),
-        _ptr(penalties), _ptr(bias_tok), _ptr(bias_val),
-        0 if bias_val is None else min(bias_tok.numel(), bias_val.numel()), _ptr(bias_off), _ptr(allowed), _ptr(logits_out),
+        _ptr(logits), _ptr(tok), _ptr(parent), _ptr(node_off), B, T, V, _ptr(ctx), n_ctx, _ptr(ctx_off), _ptr(gen_start),
+        _ptr(penalties), _ptr(bias_tok), _ptr(bias_val), n_bias, _ptr(bias_off), _ptr(allowed), _ptr(logits_out),
         _ptr(argmax_out), _ptr(workspace), workspace.numel() * workspace.element_size(), _ptr(status_dev), _stream()))
 
 
