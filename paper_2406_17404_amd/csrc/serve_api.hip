@@ -193,7 +193,7 @@ int32_t rotary_rows(const void* q_rows, int32_t q_stride, const void* k_rows, in
 static int check_chunk(int B, int T, int n_heads, int n_kv_heads, int head_dim, int max_prefix) {
   TRJ_TRY(check_serve_rows(B, T));
   if (n_heads < 1 || n_kv_heads < 1 || n_heads % n_kv_heads != 0 || n_heads > 65535 || (head_dim != 64 && head_dim != 128) ||
-      max_prefix < 0 || (int64_t)max_prefix + T > INT32_MAX - 64 || (int64_t)T * n_heads > 1 << 30)
+      max_prefix < 0 || (int64_t)max_prefix + T > INT32_MAX - 63 || (int64_t)T * n_heads > 1 << 30)  // (rounded up to 64 they stay int32)
     return TRJ_ERR_BAD_SHAPE;
   return TRJ_OK;
 }

@@ -570,3 +570,27 @@ def test_long_sequences_of_several_heads(heads, kv_heads, dh, n, L):
     assert np.array_equal(got[j:, g:][:, :, keep], clean[j:, g:][:, :, keep])
     c.cache.table[0, 100] = -1
     assert np.isnan(c.run()).all() and list(c.status) == [1]
+
+
+@pytest.mark.parametrize("n,heads,dh", [(1, 1, 64), (200, 8, 64), (1, 1, 128)])
+def test_the_last_position_of_the_longest_prefix(n, heads, dh):
+    # every page is the first but the last one, in which the last position outweighs all others: e^60 to 2^31
+    L = 2 ** 31 - 64 - n
+    pages, last = (L + 31) // 32, (L - 1) % 32
+    k, v = (np.zeros((1, 2, 32 * dh), np.uint8) for _ in "kv")
+    places = {w: S.offsets(dh, w) for w in "kv"}
+    k[0, 1, places["k"][last, 0]] = S.encode(np.array(60.0))
+    v[0, 0], v[0, 1] = S.encode(np.array(1.0)), NAN_CODE
+    v[0, 1, places["v"][:last]], v[0, 1, places["v"][last]] = S.encode(np.array(1.0)), S.encode(np.array(3.0))
+    table = torch.zeros((1, pages), dtype=torch.int32, device=DEV)
+    table[0, -1] = 1
+    scale = torch.ones(1, 2, device=DEV)
+    q = torch.zeros(n, heads, dh, dtype=torch.bfloat16, device=DEV)
+    q[..., 0] = 1.0
+    own = torch.zeros(n, 1, dh, dtype=torch.bfloat16, device=DEV)
+    ws = torch.empty(b.chunk_attention_q8_workspace_bytes(1, n, heads, 1, dh, L), dtype=torch.uint8, device=DEV)
+    out, status = torch.full((n, heads, dh), 5.0, dtype=torch.bfloat16, device=DEV), ints(1)
+    b.chunk_attention_q8(q, torch.from_numpy(k).to(DEV), torch.from_numpy(v).to(DEV), scale, scale, own, own, i32([0, n]), table,
+                         i32([L]), L, 1.0, ws, out, status)
+    torch.cuda.synchronize()
+    assert status.tolist() == [0] and (out.float() - 3).abs().max() <= 2 * HALF * 3

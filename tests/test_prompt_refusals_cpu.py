@@ -98,3 +98,14 @@ def test_binding_refuses_host_tensors_and_other_types():
         b.rotary_rows(x, x, None, i, i, f, 1.0, b.ROTARY_HALVES, x.float(), x, i)
     with pytest.raises(ValueError, match="fp32"):
         b.tree_sample(torch.zeros(3, 8, dtype=torch.bfloat16), i, i, i, i, None, i, i)
+
+
+@pytest.mark.parametrize("T", [1, 1000, 1 << 20])
+def test_chunk_attention_takes_what_the_header_says_it_takes(T):
+    n, most = ctypes.c_size_t(0), (1 << 31) - 64 - T
+    small = dict(T=T, ws_bytes=8)  # (so that no call is made)
+    assert call("chunk_attention_q8", list(ATTN), ATTN, most=most, **small) == WS
+    assert call("chunk_attention_q8", list(ATTN), ATTN, most=most + 1, **small) == SHAPE
+    sizes = b.lib().chunk_attention_q8_workspace_bytes
+    assert sizes(4, T, 32, 8, 128, most, ctypes.byref(n)) == 0 and n.value > 0
+    assert sizes(4, T, 32, 8, 128, most + 1, ctypes.byref(n)) == SHAPE
