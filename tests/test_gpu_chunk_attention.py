@@ -594,3 +594,27 @@ def test_the_last_position_of_the_longest_prefix(n, heads, dh):
                          i32([L]), L, 1.0, ws, out, status)
     torch.cuda.synchronize()
     assert status.tolist() == [0] and (out.float() - 3).abs().max() <= 2 * HALF * 3
+
+
+@pytest.mark.parametrize("B", [9, 16, 33, 64])
+@pytest.mark.parametrize("kind", ["any", "long and short", "alike", "many heads"])
+def test_up_to_64_sequences_come_longest_first(B, kind):
+    rng = np.random.default_rng(1000 + B + len(kind))
+    lens, sizes = [int(x) for x in rng.integers(0, 400, B)], [int(x) for x in rng.choice([1, 1, 2, 9, 40], B)]
+    heads, kv_heads = 4, 2
+    if kind == "long and short":  # what is split lies at either end and in the middle
+        for s in (0, B // 2, B - 1):
+            lens[s], sizes[s] = int(rng.integers(5000, 9000)), int(rng.choice([1, 70]))
+    elif kind == "alike":
+        lens, sizes = [700] * B, [3] * B
+    elif kind == "many heads":  # tiles of 256 queries
+        heads, kv_heads, lens = 32, 8, [x // 3 for x in lens]
+        sizes = [int(x) for x in rng.choice([1, 20, 70, 130], B)]
+    sizes[3] = 0
+    c = Call(rng, lens, sizes, heads, kv_heads, 64, behind=1)
+    bad = B // 3 + 1
+    c.cache.lens[bad] = -1
+    got = c.run()
+    assert list(c.status) == [int(s == bad and sizes[s] > 0) for s in range(B)]
+    assert (got[c.off[bad]:c.off[bad + 1]] == 0).all()
+    c.check(got, skip=(bad,))
