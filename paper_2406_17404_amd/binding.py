@@ -378,15 +378,14 @@ def _check_pools(k_pool, v_pool, k_scale, v_scale, pages, head_dim):
 def kv_block_tables(block_table, held, prefix_len, node_off, T, free_list, free_count, held_out, free_count_out,
                     row_slot, status_dev):
     B, max_blocks = block_table.shape
-    if block_table.nbytes < 4 * B * max_blocks or held.nbytes < 4 * B or prefix_len.nbytes < 4 * B or \
-            node_off.nbytes < 4 * (B + 1) or free_list.nbytes < 4 * free_list.shape[0] or free_count.nbytes < 4 or \
-            held_out.nbytes < 4 * B or free_count_out.nbytes < 4 or status_dev.nbytes < 4 * B or \
-            (row_slot is not None and row_slot.nbytes < 4 * T):
+    n_blocks, b4 = free_list.shape[0], 4 * B
+    if block_table.nbytes < b4 * max_blocks or held.nbytes < b4 or prefix_len.nbytes < b4 or node_off.nbytes < b4 + 4 or \
+            free_list.nbytes < 4 * n_blocks or free_count.nbytes < 4 or held_out.nbytes < b4 or free_count_out.nbytes < 4 or \
+            status_dev.nbytes < b4 or (row_slot is not None and row_slot.nbytes < 4 * T):
         raise ValueError(_TOO_SMALL)
     _check("kv_block_tables", lib().kv_block_tables(
-        _ptr(block_table), max_blocks, _ptr(held), _ptr(prefix_len), _ptr(node_off), B, T, _ptr(free_list),
-        free_list.shape[0], _ptr(free_count), _ptr(held_out), _ptr(free_count_out), _ptr(row_slot),
-        _ptr(status_dev), _stream()))
+        _ptr(block_table), max_blocks, _ptr(held), _ptr(prefix_len), _ptr(node_off), B, T, _ptr(free_list), n_blocks,
+        _ptr(free_count), _ptr(held_out), _ptr(free_count_out), _ptr(row_slot), _ptr(status_dev), _stream()))
 
 
 def kv_append_q8(k_pool, v_pool, k_scale, v_scale, k_rows, v_rows, path, accept_len, node_off, block_table,
