@@ -518,7 +518,8 @@ int32_t chunk_attention_q8_workspace_bytes(int32_t B, int32_t T, int32_t n_heads
 
 /* Causal attention of new rows over one layer of the paged cache: row i of sequence s sees the prefix_len[s]
  * positions of the cache and the rows 0 .. i of its own in k_rows, v_rows (which the cache need not hold).  A sequence has any
- * number of rows: chunks of prompts and sequences that decode one row go in one call.  Arguments and what is said of
+ * number of rows: chunks of prompts and sequences that decode one row go in one call.  (Batches of tens of sequences that all
+ * decode one row are up to a fifth faster in tree_attention_q8.)  Arguments and what is said of
  * values that are not finite as in tree_attention_q8.  At most 2^20 rows in all, T * n_heads at most 2^30, max_prefix + T at
  * most 2^31 - 64 (TRJ_ERR_BAD_SHAPE).
  * Rows of zeros and status 1: prefix_len[s] outside [0, max_prefix] or beyond max_blocks pages; nothing and status 1: rows

@@ -11,16 +11,22 @@
 // Cached blocks (two pages) are converted on the way, codes times their power-of-two scale being bf16 numbers
 // exactly; the sequence's own rows are bf16 already and V is transposed.
 //
-// Bound by products for long chunks: 2048 rows after 16384 positions, 32 heads of 128, are 584 GFLOP in 640 to 710 us, 0.82 to
-// 0.91 PFLOP/s where a large library product reaches 1.19 to 1.33 on the same card.  The matrix units work 45 % of the
-// cycles, at a clock of 1.9 GHz under this load, LDS is active in 36 %, and a tile of 32 keys x 32 queries takes 152 vector
-// instructions beside its 16 products.  No part stands out: with one left out (675 us whole) the exponentials save 25 us, reading operands 56,
-// the conversion 75, conversion and loads 128.  Less per product would take more queries per wavefront, and two query tiles'
-// accumulators, weights and queries do not fit its 256 registers.
-// A whole prompt of 4096 rows, 32 heads on 8, takes 190 to 200 us (0.7), a third of it masked or partly seen tiles and start.
+// The softmax's weights are rounded to bf16 for the second product, whose operands are 16 bits wide; their sum is not.  Beside the
+// result's own rounding, 1.7e-3 of it as a whole, that makes 2.1e-3 to 2.3e-3, as in tree_attention_q8.
+//
+// Bound by vector instructions and products for long chunks: 2048 rows after 16384 positions, 32 heads of 128, are 584 GFLOP in 605
+// to 700 us, 0.83 to 0.96 PFLOP/s where a large library product reaches 1.19 to 1.33.  A tile of 32 keys x 32 queries takes
+// 1220 cycles of a SIMD, of which its 16 products are 512 (42 %) and its 149 vector instructions by count some 750, 16 exponentials
+// at a quarter of the rate among them; the two wavefronts of a SIMD hardly overlap these.  Some 30 of the 149 are no part of the
+// method: moves where the steps' states meet, selects of scales, scalars read back from lanes.  LDS is active in 38 % of the cycles;
+// with the exponentials left out (675 us whole) 25 us are saved, reading operands 56, the conversion 75, conversion and loads
+// 128.  Less per product would take more queries per wavefront, and two query tiles' accumulators, weights and queries do not fit its
+// 256 registers.
+// A whole prompt of 4096 rows, 32 heads on 8, takes 165 to 190 us (0.72 to 0.84): 65 blocks for each compute unit, which are 150 us at
+// 2.3 us a block, and the start and end of two items; masked products are 1.5 % of those worked out.
 // For short ones by the way to the first block and from the last: 12 us for an item of one block (plan 0.5, queries 0.8,
 // first codes 1.2, their conversion and barrier 1.4, two masked tiles 2.9, end 2.1; code that is not in the instruction cache yet
-// is in each), against 2.5 us per block of 256 queries, and by the merge's launch, 5 to 17 us with its traffic.
+// is in each), and by the merge's launch, 4 to 17 us with its traffic.
 #include <algorithm>
 #include <type_traits>
 
@@ -48,7 +54,7 @@ constexpr int CH_MAX_PARTS = 512, CH_MAX_MERGES = CH_MAX_PARTS / 2;  // partials
 constexpr int CH_LEAST = 4;
 
 // Queries of a sequence that are taken 32 at a time, with a wavefront per page (chunk_few): a block takes such a workgroup 0.4 to
-// 0.9 us, one of the other form 1.5 with few wavefronts at work.  40 sequences of 8 rows over 2000 positions, 64 heads on 8: 82 us so,
+// 0.9 us, one of the other form 1.5 with few wavefronts at work.  40 sequences of 8 rows over 2000 positions, 64 heads on 8: 78 us so,
 // 130 else; of 128 queries, 64 sequences of 30 rows over 4000, 32 on 8, 342 and 285.
 constexpr int CH_FEW = 64;
 
@@ -86,7 +92,8 @@ struct ChunkMerge {
 };
 // The plan, the same on every wavefront of every workgroup: a split has `span` units at most, of one sequence evenly many.
 // Up to 64 sequences (not MANY) 64 spans are weighed, one per lane, the longest sequence in 1 .. 32 splits, then 36 .. 160
-// (few heads and a long cache: 64 rows over 131072 positions, 8 heads on one, 147 us with 32 splits at most, 80 so):
+// (few heads and a long cache: 64 rows over 131072 positions, 8 heads on one, 147 us with 32 splits at most, 80 so; 62 since they
+// come in tiles of 32):
 //   cost = rounds of workgroups * (START + units of one), and if anything is split MERGE, PART for each of the parts and
 //          EACH for each split of the longest
 // A unit is what a compute unit takes for a block of 256 queries, 2.3 us, or for four of few queries (0.6 to 0.9 us each).
@@ -107,8 +114,8 @@ struct ChunkPlan {
       mine = chunk_seq(a, s0 + lane);
       if (!MANY) {
         // Where all tiles of 32 queries fit one round, short sequences come in such tiles, and longer ones of four tiles, or of any
-        // number if they are few in all: 40 rows after 500 positions, 32 heads on 8, took 20 us in the other form and take 14, 100 after
-        // 3500 38 and 30, 128 after 8000, the border, 45 and 48; 16 after 130000 119 and 70; 64 after 30000, 8 heads on one, 47 and 32.
+        // number if they are few in all: 40 rows after 500 positions, 32 heads on 8, took 20 us in the other form and take 13, 100 after
+        // 3500 38 and 29, 128 after 8000, the border, 45 and 48; 16 after 130000 119 and 66; 64 after 30000, 8 heads on one, 47 and 31.
         const int tiles = mine.n <= 0 ? 0 : (mine.n * a.group + 31) >> 5;
         const float all = wave_sum((float)tiles) * (float)a.n_kv_heads;
         if (all <= RESIDENT && mine.n > 0 && mine.L >= 0 && (mine.blocks() <= SHORT || tiles <= 4 || all <= FEW_TILES))
@@ -259,8 +266,8 @@ struct ChunkLds {
 // A tile of 32 queries: every wavefront has them all and pages of its own, each CH_WAVES-th of the range, first of the
 // sequence's own rows, then of the cache, whose codes come to slots of its own in LDS and go from there to the matrix units.
 // The wavefronts' sums are joined at the end.  In the other form seven wavefronts would only bring blocks for one: 64 sequences of
-// a row over 2000 positions, 32 heads on 8, took 142 us so and take 79 here, one row over 131072, 64 heads on 8, 112 and 57
-// (268 MB, 4.7 TB/s).
+// a row over 2000 positions, 32 heads on 8, took 142 us so and take 80 here, one row over 131072, 64 heads on 8, 112 and 56
+// (268 MB, 4.8 TB/s).
 template <int DH>
 struct FewLds {
   static constexpr int P = DH / 32, SLOTS = 256 / DH, SLOT = 2 * P * 1024;  // P KiB of codes of a page, K or V

@@ -13,13 +13,15 @@
 //   the histogram   of the weights over max x - x, which finds the bin in which a running sum (or count) crosses a
 //                   border; the tokens of that bin alone are put in order
 // A top-k of more than SMP_SHORT, and rows with thousands of tokens in a bin that a border crosses, take a third way, which
-// reads the row from memory for every step: 62 us for one row of 32000 and top-k 2000, 190 for 1024 rows.
+// reads the row from memory for every step: 61 us for one row of 32000 and top-k 2000, 190 for 1024 rows.
 //
-// Rows of up to 32768 logits stay in the registers of one workgroup, which reads them once: 1024 x 32000 take 34 us with top-k 50
-// (131 MB, 3.9 TB/s; a large copy moves 4.9), 65 under mixed rules with half of the logits masked, 77 without any rule, where 33 million
-// weights are worked out in 64 bits and added up in LDS.  One row takes 9 to 11 us with a short list and 20 without: a chain of barriers.
-// Longer rows are cut, for few rows to fill the chip: 69 x 128256 take 24 us, 13.7 for the chunks (2.6 TB/s), 3.8 for a launch that
-// finds nothing to weigh and 10.3 for the lists of eight chunks put together; 57 without rules.
+// Rows of up to 32768 logits come to the registers of one workgroup.  Short lists and greedy rows are made from there, with one
+// read: 1024 x 32000 take 34 us with top-k 50 (131 MB, 3.9 TB/s; a large copy moves 4.9).  The histogram reads the row twice more, for
+// the weights and for the tokens of the bins that count: 75 us without any rule, where 33 million weights are worked out in 64 bits and
+// added up in LDS, 58 to 69 under mixed rules with half of the logits masked.  One row takes 10 to 13 us with a short list and 20
+// without: a chain of barriers.
+// Longer rows are cut, for few rows to fill the chip: 69 x 128256 take 24 to 29 us, 13.7 for the chunks (2.6 TB/s), 3.8 for a launch
+// that finds nothing to weigh and 10.1 for the lists of seven chunks put together; 59 without rules.
 #include <algorithm>
 
 #include "kernels.h"
